@@ -67,6 +67,11 @@ typedef enum nsd_status {
     NSD_ERR_HIP = 7          /* a HIP runtime error; see nsd_last_error() */
 } nsd_status;
 
+/* Types of the arrays that may be held in fewer bits (attention, router,
+ * optimizer): 32-bit floats, or bfloat16 (the upper half of one).  Whatever the
+ * type, sums, softmax statistics and updates are computed in 32 bits. */
+typedef enum nsd_dtype { NSD_F32 = 0, NSD_BF16 = 1 } nsd_dtype;
+
 /* Duplicate coordinates in a COO input: summed (the "+=" of a singleton
  * inserted inside a sum, Section 5.5) or rejected (the `unique` annotation of
  * the storage formats, Section 5.3). */
@@ -801,6 +806,73 @@ nsd_status nsd_batax_workspace_size(const nsd_csr *A, int64_t npairs, size_t *by
 nsd_status nsd_batax_jacobian(const nsd_csr *A, float beta, int64_t npairs, int32_t *jrowptr,
                               int32_t *jcolind, float *jval, int32_t *nnz_out, void *ws,
                               size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * AdamW: one step of gradient descent with decoupled weight decay over many
+ * tensors in one launch.  It takes the gradients that the calls above write,
+ * of dense operands and of values on stored keys alike:
+ *     g' = grad_scale g
+ *     m  = beta1 m + (1 - beta1) g',   v = beta2 v + (1 - beta2) g'^2
+ *     w  = w (1 - lr weight_decay)
+ *          - lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps)
+ *
+ * A tensor is a flat array of n < 2^31 - 4096 values, at any address that its
+ * type allows.  `param` (fp32 or bf16) and the states are updated in place;
+ * `grad` (fp32 or bf16) is read.  `master` (bf16 weights only, or NULL) is the
+ * weights in fp32: the step updates it and writes its nearest bf16 to `param`.
+ * Without it a bf16 weight is rounded to one of its neighbours at random.
+ *
+ * States are fp32 arrays, or (state_bits = 8) 8-bit floats over a fp32 scale for
+ * every NSD_ADAMW_BLOCK consecutive values of a tensor (m_scale and v_scale:
+ * ceil(n / NSD_ADAMW_BLOCK) each; the last block may be short): m as e4m3
+ * (4 exponent, 3 mantissa bits, no infinity), v as e5m2.  The scale is the
+ * block's largest magnitude over 448 or 57344 (0 where that is below 2^-126:
+ * the block is zero).  A value is rounded up or down at random with its mean
+ * kept (16 random bits), a v that is not zero at least to the smallest code.
+ * A NaN in a block stays one value's; an infinity makes its block NaN.
+ * The random bits are a function of the step, the tensor's place in the list
+ * and the value's place in the tensor: the same step on the same data gives
+ * the same bits.  All zero states are the start (codes 0, scales 0).
+ *
+ * nsd_adamw_plan_size    bytes of the plan's device table (host output).
+ * nsd_adamw_plan_build   writes the table from host records; the addresses in
+ *                        them are kept in the caller's table, so a plan serves
+ *                        for as long as its arrays stay where they are.
+ *                        Synchronous.
+ * nsd_adamw_step         one step.  Async: one launch.
+ */
+#define NSD_ADAMW_BLOCK 256
+typedef struct nsd_adamw_tensor {
+    int64_t n;
+    void *param;
+    float *master;             /* or NULL */
+    const void *grad;
+    void *m, *v;               /* fp32 [n], or one byte a value */
+    float *m_scale, *v_scale;  /* 8-bit states only */
+    int32_t param_dtype, grad_dtype; /* nsd_dtype */
+    float weight_decay;
+} nsd_adamw_tensor;
+
+typedef struct nsd_adamw_plan {
+    int32_t ntensors, nchunks, state_bits;
+    const void *table; /* device, nsd_adamw_plan_size bytes, 8-byte aligned */
+} nsd_adamw_plan;
+
+/* Hyperparameters (host).  The pointers are device scalars or NULL; given, they
+ * are read when the step runs, so that a captured graph follows them. */
+typedef struct nsd_adamw {
+    double lr, beta1, beta2, eps; /* 0 <= beta < 1, eps >= 1e-30 */
+    int32_t step;                 /* t >= 1 */
+    const int32_t *step_dev;      /* t instead of `step` (>= 1) */
+    const float *lr_dev;          /* instead of lr */
+    const float *grad_scale;      /* factor of every gradient (a clip); NULL: 1 */
+} nsd_adamw;
+
+nsd_status nsd_adamw_plan_size(int32_t ntensors, const nsd_adamw_tensor *tensors, size_t *bytes);
+nsd_status nsd_adamw_plan_build(int32_t ntensors, const nsd_adamw_tensor *tensors,
+                                int32_t state_bits, nsd_adamw_plan *plan, void *table,
+                                size_t table_bytes, void *stream);
+nsd_status nsd_adamw_step(const nsd_adamw_plan *plan, const nsd_adamw *h, void *stream);
 
 #ifdef __cplusplus
 }

@@ -97,6 +97,29 @@ class nsd_ttv_plan(C.Structure):
                 ("lperm", C.c_void_p), ("lpair", C.c_void_p), ("lplan", nsd_plan)]
 
 
+# nsd_dtype
+F32, BF16 = 0, 1
+ADAMW_BLOCK = 256  # values that share a scale in 8-bit optimizer states
+
+
+class nsd_adamw_tensor(C.Structure):
+    _fields_ = [("n", C.c_int64), ("param", C.c_void_p), ("master", C.c_void_p),
+                ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("param_dtype", C.c_int32),
+                ("grad_dtype", C.c_int32), ("weight_decay", C.c_float)]
+
+
+class nsd_adamw_plan(C.Structure):
+    _fields_ = [("ntensors", C.c_int32), ("nchunks", C.c_int32), ("state_bits", C.c_int32),
+                ("table", C.c_void_p)]
+
+
+class nsd_adamw(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double),
+                ("eps", C.c_double), ("step", C.c_int32), ("step_dev", C.c_void_p),
+                ("lr_dev", C.c_void_p), ("grad_scale", C.c_void_p)]
+
+
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"libnsd.so is not built ({LIB_PATH}); run "
                       "`python -m paper_2303_07030_amd.build` first")
@@ -182,6 +205,10 @@ _SIGS = {
     "nsd_batax_workspace_size": (C.c_int, [_CSR, C.c_int64, C.POINTER(_SZ)]),
     "nsd_batax_jacobian": (C.c_int, [_CSR, C.c_float, C.c_int64, _P, _P, _P, C.POINTER(_I), _P,
                                      _SZ, _P]),
+    "nsd_adamw_plan_size": (C.c_int, [_I, C.POINTER(nsd_adamw_tensor), C.POINTER(_SZ)]),
+    "nsd_adamw_plan_build": (C.c_int, [_I, C.POINTER(nsd_adamw_tensor), _I,
+                                       C.POINTER(nsd_adamw_plan), _P, _SZ, _P]),
+    "nsd_adamw_step": (C.c_int, [C.POINTER(nsd_adamw_plan), C.POINTER(nsd_adamw), _P]),
     "nsd_loss_cp": (C.c_int, [_COO3, _P, _P, _P, _I, C.c_float, _P, _P, _P, _P, _P, _P, _SZ,
                               _P]),
 }
@@ -618,3 +645,36 @@ def nsd_validate_coo(dims, nnz, coords, check_unique, ws, stream=None):
     _check(_lib.nsd_validate_coo(len(dims), C.cast(_host_i32(dims), _P), nnz, C.cast(ptrs, _P),
                                  int(bool(check_unique)), _p(ws), _nbytes(ws), _stream(stream)),
            "nsd_validate_coo")
+
+
+# -------------------------------------------------------------- learning
+
+def dtype_of(t) -> int:
+    """nsd_dtype of a tensor (an integer passes through)."""
+    if isinstance(t, int):
+        return t
+    try:
+        return {torch.float32: F32, torch.bfloat16: BF16}[t.dtype]
+    except KeyError:
+        raise ValueError(f"{t.dtype} is neither float32 nor bfloat16") from None
+
+
+def nsd_adamw_plan_size(tensors) -> int:
+    """tensors: a list of nsd_adamw_tensor."""
+    b = _SZ(0)
+    _check(_lib.nsd_adamw_plan_size(len(tensors), (nsd_adamw_tensor * len(tensors))(*tensors),
+                                    C.byref(b)), "nsd_adamw_plan_size")
+    return b.value
+
+
+def nsd_adamw_plan_build(tensors, state_bits, table, stream=None) -> nsd_adamw_plan:
+    plan = nsd_adamw_plan()
+    _check(_lib.nsd_adamw_plan_build(len(tensors), (nsd_adamw_tensor * len(tensors))(*tensors),
+                                     state_bits, C.byref(plan), _p(table), _nbytes(table),
+                                     _stream(stream)), "nsd_adamw_plan_build")
+    plan._keep = table
+    return plan
+
+
+def nsd_adamw_step(plan: nsd_adamw_plan, h: nsd_adamw, stream=None):
+    _check(_lib.nsd_adamw_step(C.byref(plan), C.byref(h), _stream(stream)), "nsd_adamw_step")
