@@ -808,6 +808,51 @@ nsd_status nsd_batax_jacobian(const nsd_csr *A, float beta, int64_t npairs, int3
                               size_t ws_bytes, void *stream);
 
 /* ---------------------------------------------------------------------------
+ * Router of a sparse mixture.  Token t chooses topk of the experts by its
+ * logits x_t; the gates are the values of a CSR of ntok rows and `experts`
+ * columns with topk entries a row (rowptr[t] = t topk), the S that nsd_spmm
+ * multiplies and whose gradient nsd_spmm_vjp gives:
+ *     p_te   = softmax over e of x_te
+ *     S_t    = the topk largest logits, ties to the lowest expert, written in
+ *              increasing order of the expert
+ *     gate   = p_te, or (normalize) p_te / sum over S_t of p
+ *     n_e    = tokens that chose e,  N = tokens routed
+ *     L      = weight E sum_e (n_e / sum n) (sum_t p_te / N)
+ * A logit of -infinity closes an expert to a token: chosen only for want of
+ * others, its gate is a stored 0 and it is not counted.  skip[t] != 0 (skip may
+ * be NULL) leaves a token out of everything: its row stores 0 at the experts 0
+ * to topk - 1.  A token with every expert closed is not routed either.  A NaN
+ * makes its token's gates NaN.  logits: [ntok] rows of E values (nsd_dtype),
+ * `ld` values from one to the next; up to 1024 experts.
+ *
+ * nsd_route      colind, gate: [ntok x topk].  counts (int32 [E + 1]: the n_e,
+ *                then N) and loss (fp64, as every loss) are both given, or
+ *                both NULL: then the gates alone are computed and ws is not
+ *                needed.
+ * nsd_route_vjp  the gradient with respect to the logits of seed L (through the
+ *                probabilities; the counts are constants) and of the gates,
+ *                given theirs: dgate [ntok x topk] or NULL; counts (as
+ *                nsd_route wrote them) or NULL.  dlogits: [ntok x E] of the
+ *                logits' type, row after row whatever their ld; not the logits.
+ * Async.
+ */
+typedef struct nsd_router {
+    int32_t experts, topk;
+    int32_t dtype;     /* nsd_dtype of the logits and their gradient */
+    int32_t normalize; /* gates of a token add up to 1 */
+    int64_t ld;        /* of the logits, >= experts */
+} nsd_router;
+
+nsd_status nsd_route_workspace_size(int32_t ntok, const nsd_router *s, size_t *bytes);
+nsd_status nsd_route(int32_t ntok, const nsd_router *s, const void *logits, const uint8_t *skip,
+                     float weight, int32_t *colind, float *gate, int32_t *counts, double *loss,
+                     void *ws, size_t ws_bytes, void *stream);
+nsd_status nsd_route_vjp(int32_t ntok, const nsd_router *s, const void *logits,
+                         const uint8_t *skip, const int32_t *colind, const float *gate,
+                         const int32_t *counts, float weight, float seed, const float *dgate,
+                         void *dlogits, void *stream);
+
+/* ---------------------------------------------------------------------------
  * AdamW: one step of gradient descent with decoupled weight decay over many
  * tensors in one launch.  It takes the gradients that the calls above write,
  * of dense operands and of values on stored keys alike:

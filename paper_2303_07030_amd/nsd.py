@@ -102,6 +102,11 @@ F32, BF16 = 0, 1
 ADAMW_BLOCK = 256  # values that share a scale in 8-bit optimizer states
 
 
+class nsd_router(C.Structure):
+    _fields_ = [("experts", C.c_int32), ("topk", C.c_int32), ("dtype", C.c_int32),
+                ("normalize", C.c_int32), ("ld", C.c_int64)]
+
+
 class nsd_adamw_tensor(C.Structure):
     _fields_ = [("n", C.c_int64), ("param", C.c_void_p), ("master", C.c_void_p),
                 ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
@@ -205,6 +210,11 @@ _SIGS = {
     "nsd_batax_workspace_size": (C.c_int, [_CSR, C.c_int64, C.POINTER(_SZ)]),
     "nsd_batax_jacobian": (C.c_int, [_CSR, C.c_float, C.c_int64, _P, _P, _P, C.POINTER(_I), _P,
                                      _SZ, _P]),
+    "nsd_route_workspace_size": (C.c_int, [_I, C.POINTER(nsd_router), C.POINTER(_SZ)]),
+    "nsd_route": (C.c_int, [_I, C.POINTER(nsd_router), _P, _P, C.c_float, _P, _P, _P, _P, _P, _SZ,
+                            _P]),
+    "nsd_route_vjp": (C.c_int, [_I, C.POINTER(nsd_router), _P, _P, _P, _P, _P, C.c_float,
+                                C.c_float, _P, _P, _P]),
     "nsd_adamw_plan_size": (C.c_int, [_I, C.POINTER(nsd_adamw_tensor), C.POINTER(_SZ)]),
     "nsd_adamw_plan_build": (C.c_int, [_I, C.POINTER(nsd_adamw_tensor), _I,
                                        C.POINTER(nsd_adamw_plan), _P, _SZ, _P]),
@@ -657,6 +667,40 @@ def dtype_of(t) -> int:
         return {torch.float32: F32, torch.bfloat16: BF16}[t.dtype]
     except KeyError:
         raise ValueError(f"{t.dtype} is neither float32 nor bfloat16") from None
+
+
+def router_desc(experts, topk, logits, normalize=True, ld=None) -> nsd_router:
+    """logits: a tensor of rows of `experts` values (its type and row distance
+    are taken), or an nsd_dtype (then ld, default experts)."""
+    if isinstance(logits, torch.Tensor):
+        if logits.dim() != 2 or logits.shape[1] != experts or \
+                (experts > 1 and logits.numel() and logits.stride(1) != 1):
+            raise ValueError(f"logits {tuple(logits.shape)} are not rows of {experts} values")
+        if ld is None:
+            ld = logits.stride(0) if logits.shape[0] > 1 else experts
+    return nsd_router(experts, topk, dtype_of(logits), int(bool(normalize)),
+                      experts if ld is None else ld)
+
+
+def nsd_route_workspace_size(ntok: int, s: nsd_router) -> int:
+    b = _SZ(0)
+    _check(_lib.nsd_route_workspace_size(ntok, C.byref(s), C.byref(b)),
+           "nsd_route_workspace_size")
+    return b.value
+
+
+def nsd_route(ntok, s: nsd_router, logits, skip, weight, colind, gate, counts, loss, ws,
+              stream=None):
+    _check(_lib.nsd_route(ntok, C.byref(s), _p(logits), _p(skip), weight, _p(colind), _p(gate),
+                          _p(counts), _p(loss), _p(ws), _nbytes(ws), _stream(stream)),
+           "nsd_route")
+
+
+def nsd_route_vjp(ntok, s: nsd_router, logits, skip, colind, gate, counts, weight, seed, dgate,
+                  dlogits, stream=None):
+    _check(_lib.nsd_route_vjp(ntok, C.byref(s), _p(logits), _p(skip), _p(colind), _p(gate),
+                              _p(counts), weight, seed, _p(dgate), _p(dlogits),
+                              _stream(stream)), "nsd_route_vjp")
 
 
 def nsd_adamw_plan_size(tensors) -> int:
