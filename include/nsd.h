@@ -808,6 +808,70 @@ nsd_status nsd_batax_jacobian(const nsd_csr *A, float beta, int64_t npairs, int3
                               size_t ws_bytes, void *stream);
 
 /* ---------------------------------------------------------------------------
+ * Differential attention over the stored keys of a CSR mask A (rows: queries,
+ * columns: keys).  Every head has two query and two key halves of width d, one
+ * value of width dv, and a learned weight lambda_h:
+ *     s^m_p = scale <q^m_i, k^m_j> + bias_p        p = (i, j) stored, m = 1, 2
+ *     a^m   = softmax of s^m over the stored keys of row i
+ *     O_i   = sum_p (a^1_p - lambda_h a^2_p) v_j
+ * Q: [nrows][heads][2][d], K: [ncols][kv_heads][2][d], V: [ncols][kv_heads][dv],
+ * O: [nrows][heads][dv], all of one nsd_dtype, with ldq, ldk, ldv, ldo values
+ * from one row to the next, so that they may be parts of wider rows.  Head h
+ * reads key head h / (heads / kv_heads).  d <= 128, dv <= 256, heads <= 4096;
+ * any d and dv, any alignment.  A's values are not read.
+ * bias: [nnz] in A's storage order, for every head, or NULL.  A bias of
+ * -infinity masks its key: nothing of that key is used, finite or not.  A row
+ * without keys, or with every key masked, has O = 0 and no gradient.
+ *
+ * nsd_attn_item_len        the item length of A's plan (nsd_plan_build) that
+ *                          suits these calls; any plan serves.
+ * nsd_attn_diff            O and, when stat is not NULL, what the gradient
+ *                          needs: [nrows][heads][4] floats, either map's
+ *                          maximum and sum.
+ * nsd_attn_diff_vjp        gradients of Q, K, V (type and row distances of
+ *                          their tensors: ldq, ldk, ldv), lambda [heads] and, when
+ *                          dbias is not NULL, bias [nnz] (0 where masked), for
+ *                          the upstream dO (ldo) and nsd_attn_diff's stat on
+ *                          the same inputs.  Gradients of a key head add up its
+ *                          query heads'.
+ * nsd_attn_diff_workspace_size  bytes for both; At NULL: for nsd_attn_diff.
+ * nsd_attn_diff_decode     O for a few rows over long lists of keys: rowptr
+ *                          [nrows + 1] and colind need no plan, and may change
+ *                          from call to call (or from replay to replay of a
+ *                          graph) as a sequence's cache slots do.  Keys of a row
+ *                          may come in any order; colind NULL (no keys at all):
+ *                          every row is empty.  max_len (host): rows are
+ *                          split for up to so many entries; a longer one is
+ *                          right, and slower.
+ * Async.
+ */
+typedef struct nsd_attn {
+    int32_t heads, kv_heads; /* heads is a multiple of kv_heads */
+    int32_t d, dv;
+    int32_t dtype;
+    float scale;
+    int64_t ldq, ldk, ldv, ldo;
+} nsd_attn;
+
+nsd_status nsd_attn_item_len(int32_t nnz, const nsd_attn *s, int32_t *item_len);
+nsd_status nsd_attn_diff_workspace_size(const nsd_csr *A, const nsd_csc *At, const nsd_attn *s,
+                                        size_t *bytes);
+nsd_status nsd_attn_diff(const nsd_csr *A, const nsd_attn *s, const void *Q, const void *K,
+                         const void *V, const float *lambda, const float *bias, void *O,
+                         float *stat, void *ws, size_t ws_bytes, void *stream);
+nsd_status nsd_attn_diff_vjp(const nsd_csr *A, const nsd_csc *At, const nsd_attn *s, const void *Q,
+                             const void *K, const void *V, const float *lambda, const float *bias,
+                             const float *stat, const void *dO, void *dQ, void *dK, void *dV,
+                             float *dlambda, float *dbias, void *ws, size_t ws_bytes,
+                             void *stream);
+nsd_status nsd_attn_diff_decode_workspace_size(int32_t nrows, int32_t max_len, const nsd_attn *s,
+                                               size_t *bytes);
+nsd_status nsd_attn_diff_decode(int32_t nrows, const int32_t *rowptr, const int32_t *colind,
+                                int32_t max_len, const nsd_attn *s, const void *Q, const void *K,
+                                const void *V, const float *lambda, const float *bias, void *O,
+                                void *ws, size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------
  * Router of a sparse mixture.  Token t chooses topk of the experts by its
  * logits x_t; the gates are the values of a CSR of ntok rows and `experts`
  * columns with topk entries a row (rowptr[t] = t topk), the S that nsd_spmm

@@ -20,7 +20,7 @@ static nsd_status check_plan(const nsd_plan &pl, int32_t nnz, const char *what) 
     return NSD_OK;
 }
 
-static nsd_status check_csr(const nsd_csr *A, bool need_val, bool need_plan) {
+nsd_status check_csr(const nsd_csr *A, bool need_val, bool need_plan) {
     NSD_REQUIRE(A != nullptr, "CSR descriptor is NULL");
     NSD_REQUIRE(A->nrows >= 0 && A->ncols >= 0 && A->nnz >= 0, "negative CSR size");
     NSD_REQUIRE(A->rowptr != nullptr, "CSR rowptr is NULL");
@@ -33,7 +33,7 @@ static nsd_status check_csr(const nsd_csr *A, bool need_val, bool need_plan) {
     return NSD_OK;
 }
 
-static nsd_status check_csc(const nsd_csc *At, const nsd_csr *A) {
+nsd_status check_csc(const nsd_csc *At, const nsd_csr *A) {
     NSD_REQUIRE(At != nullptr, "CSC descriptor is NULL");
     NSD_REQUIRE(At->nrows == A->nrows && At->ncols == A->ncols && At->nnz == A->nnz,
                 "CSC shape (%d x %d, %d) differs from CSR (%d x %d, %d)", At->nrows, At->ncols,

@@ -249,6 +249,11 @@ inline WidthPlan narrow_plan(int k, bool whole, int scalar = kScalarWidth) {
 
 // ------------------------------------------- shared internal operations
 
+// Host checks of a matrix descriptor (its plan too when asked) and of the CSC
+// of the same matrix.
+nsd_status check_csr(const nsd_csr *A, bool need_val, bool need_plan);
+nsd_status check_csc(const nsd_csc *At, const nsd_csr *A);
+
 // Device-wide exclusive prefix sum of n int32 (in and out may alias).
 // The total goes to *total_dev when it is not NULL.
 size_t scan_ws_bytes(int64_t n);

@@ -102,6 +102,12 @@ F32, BF16 = 0, 1
 ADAMW_BLOCK = 256  # values that share a scale in 8-bit optimizer states
 
 
+class nsd_attn(C.Structure):
+    _fields_ = [("heads", C.c_int32), ("kv_heads", C.c_int32), ("d", C.c_int32),
+                ("dv", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float),
+                ("ldq", C.c_int64), ("ldk", C.c_int64), ("ldv", C.c_int64), ("ldo", C.c_int64)]
+
+
 class nsd_router(C.Structure):
     _fields_ = [("experts", C.c_int32), ("topk", C.c_int32), ("dtype", C.c_int32),
                 ("normalize", C.c_int32), ("ld", C.c_int64)]
@@ -210,6 +216,17 @@ _SIGS = {
     "nsd_batax_workspace_size": (C.c_int, [_CSR, C.c_int64, C.POINTER(_SZ)]),
     "nsd_batax_jacobian": (C.c_int, [_CSR, C.c_float, C.c_int64, _P, _P, _P, C.POINTER(_I), _P,
                                      _SZ, _P]),
+    "nsd_attn_item_len": (C.c_int, [_I, C.POINTER(nsd_attn), C.POINTER(_I)]),
+    "nsd_attn_diff_workspace_size": (C.c_int, [_CSR, _CSC, C.POINTER(nsd_attn),
+                                               C.POINTER(_SZ)]),
+    "nsd_attn_diff": (C.c_int, [_CSR, C.POINTER(nsd_attn), _P, _P, _P, _P, _P, _P, _P, _P, _SZ,
+                                _P]),
+    "nsd_attn_diff_vjp": (C.c_int, [_CSR, _CSC, C.POINTER(nsd_attn), _P, _P, _P, _P, _P, _P, _P,
+                                    _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "nsd_attn_diff_decode_workspace_size": (C.c_int, [_I, _I, C.POINTER(nsd_attn),
+                                                      C.POINTER(_SZ)]),
+    "nsd_attn_diff_decode": (C.c_int, [_I, _P, _P, _I, C.POINTER(nsd_attn), _P, _P, _P, _P, _P,
+                                       _P, _P, _SZ, _P]),
     "nsd_route_workspace_size": (C.c_int, [_I, C.POINTER(nsd_router), C.POINTER(_SZ)]),
     "nsd_route": (C.c_int, [_I, C.POINTER(nsd_router), _P, _P, C.c_float, _P, _P, _P, _P, _P, _SZ,
                             _P]),
@@ -667,6 +684,63 @@ def dtype_of(t) -> int:
         return {torch.float32: F32, torch.bfloat16: BF16}[t.dtype]
     except KeyError:
         raise ValueError(f"{t.dtype} is neither float32 nor bfloat16") from None
+
+
+def attn_desc(heads, kv_heads, d, dv, q, k, v, o, scale) -> nsd_attn:
+    """The shape of an attention over q [nrows, heads * 2 * d], k [ncols,
+    kv_heads * 2 * d], v [ncols, kv_heads * dv] and o [nrows, heads * dv]: their
+    type and row distances are taken."""
+    lds = []
+    for t, width, name in ((q, heads * 2 * d, "q"), (k, kv_heads * 2 * d, "k"),
+                           (v, kv_heads * dv, "v"), (o, heads * dv, "o")):
+        if t.dim() != 2 or t.shape[1] != width or t.dtype != q.dtype or \
+                (width > 1 and t.numel() and t.stride(1) != 1):
+            raise ValueError(f"{name}: {tuple(t.shape)} of {t.dtype} are not rows of {width} "
+                             f"values of {q.dtype}")
+        lds.append(t.stride(0) if t.shape[0] > 1 else width)
+    return nsd_attn(heads, kv_heads, d, dv, dtype_of(q), scale, *lds)
+
+
+def nsd_attn_item_len(nnz: int, s: nsd_attn) -> int:
+    L = _I(0)
+    _check(_lib.nsd_attn_item_len(nnz, C.byref(s), C.byref(L)), "nsd_attn_item_len")
+    return L.value
+
+
+def nsd_attn_diff_workspace_size(A: nsd_csr, At, s: nsd_attn) -> int:
+    b = _SZ(0)
+    _check(_lib.nsd_attn_diff_workspace_size(C.byref(A), None if At is None else C.byref(At),
+                                             C.byref(s), C.byref(b)),
+           "nsd_attn_diff_workspace_size")
+    return b.value
+
+
+def nsd_attn_diff(A: nsd_csr, s: nsd_attn, Q, K, V, lam, bias, O, stat, ws, stream=None):
+    _check(_lib.nsd_attn_diff(C.byref(A), C.byref(s), _p(Q), _p(K), _p(V), _p(lam), _p(bias),
+                              _p(O), _p(stat), _p(ws), _nbytes(ws), _stream(stream)),
+           "nsd_attn_diff")
+
+
+def nsd_attn_diff_vjp(A: nsd_csr, At: nsd_csc, s: nsd_attn, Q, K, V, lam, bias, stat, dO, dQ, dK,
+                      dV, dlam, dbias, ws, stream=None):
+    _check(_lib.nsd_attn_diff_vjp(C.byref(A), C.byref(At), C.byref(s), _p(Q), _p(K), _p(V),
+                                  _p(lam), _p(bias), _p(stat), _p(dO), _p(dQ), _p(dK), _p(dV),
+                                  _p(dlam), _p(dbias), _p(ws), _nbytes(ws), _stream(stream)),
+           "nsd_attn_diff_vjp")
+
+
+def nsd_attn_diff_decode_workspace_size(nrows: int, max_len: int, s: nsd_attn) -> int:
+    b = _SZ(0)
+    _check(_lib.nsd_attn_diff_decode_workspace_size(nrows, max_len, C.byref(s), C.byref(b)),
+           "nsd_attn_diff_decode_workspace_size")
+    return b.value
+
+
+def nsd_attn_diff_decode(nrows, rowptr, colind, max_len, s: nsd_attn, Q, K, V, lam, bias, O, ws,
+                         stream=None):
+    _check(_lib.nsd_attn_diff_decode(nrows, _p(rowptr), _p(colind), max_len, C.byref(s), _p(Q),
+                                     _p(K), _p(V), _p(lam), _p(bias), _p(O), _p(ws), _nbytes(ws),
+                                     _stream(stream)), "nsd_attn_diff_decode")
 
 
 def router_desc(experts, topk, logits, normalize=True, ld=None) -> nsd_router:
