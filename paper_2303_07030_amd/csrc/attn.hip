@@ -26,21 +26,17 @@
 // a t k - D sum a k)), so that it needs no D beforehand; the pass over columns
 // (the CSC) is then a plain weighted gather of q and dO, without a dot product
 // or an atomic.
-#include <algorithm>
-#include <type_traits>
-
-#include "nsd_internal.hpp"
+#include "attn.hpp"
+#include "attn_mfma.hpp"
 
 namespace nsd {
 
+using namespace attn;
+
 namespace {
 
-constexpr int kAttnThreads = 256;
-constexpr int kAttnWaves = kAttnThreads / kWave;
 constexpr int kDeep = 4;       // entries in flight per lane
-constexpr int kMaxD = 128, kMaxDv = 256;
 constexpr int kMinSplit = 64;  // entries of a decode split
-constexpr float kLog2e = 1.44269504088896340736f;
 
 // ------------------------------------------------------------ values
 
@@ -67,38 +63,7 @@ struct Raw {
     }
 };
 
-template <class T, int V>
-__device__ __forceinline__ void store_values(T *p, const float (&x)[V]) {
-    T t[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-        if constexpr (sizeof(T) == 4) {
-            t[e] = x[e];
-        } else {
-            const __bf16 r = static_cast<__bf16>(x[e]);
-            t[e] = __builtin_bit_cast(uint16_t, r);
-        }
-    }
-    __builtin_memcpy(p, t, sizeof t);
-}
-
-template <class T>
-__device__ __forceinline__ T narrow(float x) {
-    T t[1];
-    const float y[1] = {x};
-    store_values<T, 1>(t, y);
-    return t[0];
-}
-
 // ------------------------------------------------------------ shapes
-
-struct Shape {
-    int32_t H, Hk, grp, d, dv;
-    int64_t ldq, ldk, ldv, ldo;
-    float scale;
-    int32_t hps_log2;  // heads per slot (of queries; of keys in the column pass)
-    int32_t nhb;       // groups of them
-};
 
 // How a wave's lanes are split: g within a head's G lanes, the head, the entry.
 template <int G>
@@ -158,37 +123,7 @@ __device__ __forceinline__ float other_half(float x) {
     return lane_xor<G / 2>(x);
 }
 
-__device__ __forceinline__ float exp_diff(float s, float m) {
-    return __builtin_amdgcn_exp2f((s - m) * kLog2e);
-}
-__device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.f : m; }
-
-// The blocks of one XCD take neighbouring work.
-__device__ __forceinline__ int64_t near_block(int b, int nb) {
-    const int x = b % 8;
-    int start = 0;
-    for (int y = 0; y < x; ++y) start += (nb - y + 7) / 8;
-    return start + b / 8;
-}
-
 // ------------------------------------------------------------ forward
-
-struct FwdArgs {
-    Shape s;
-    const void *Q, *K, *V;
-    const float *lambda, *bias;
-    void *O;
-    float *stat;  // [rows][H][4]: maximum and sum of either map, or NULL
-    float *part;  // [partial][H][4 + 2 dv]
-    const int32_t *rowptr, *rowidx, *colind;
-    // plan
-    nsd_plan plan;
-    int32_t nrows;
-    // decode: splits of a row, entries of one
-    int32_t nsplit, per;
-    int64_t nmain;  // blocks that walk entries
-    int32_t all_empty;
-};
 
 // The entries that this lane takes of a batch, and the number of a key it may
 // read instead of one that is not there.
@@ -363,22 +298,6 @@ struct FwdLane {
     }
 };
 
-// Rows without entries: the empty sums.  One wave a row.
-template <class T>
-__device__ __forceinline__ void empty_row(const FwdArgs &a, int64_t row) {
-    const int lane = threadIdx.x % kWave;
-    T *o = static_cast<T *>(a.O) + row * a.s.ldo;
-    for (int c = lane; c < a.s.H * a.s.dv; c += kWave) o[c] = T(0);
-    if (a.stat)
-        for (int c = lane; c < a.s.H * 4; c += kWave) a.stat[row * a.s.H * 4 + c] = 0.f;
-}
-
-// The n-th row without entries, or -1.
-__device__ __forceinline__ int64_t nth_empty(const nsd_plan &plan, int nseg, int all, int64_t n) {
-    if (all) return n < nseg ? n : -1;
-    return n < plan.nempty ? plan.empty_seg[n] : -1;
-}
-
 template <class T, int VK, int VV, int G, bool EXACT, bool DECODE>
 __global__ __launch_bounds__(kAttnThreads) void attn_fwd_kernel(FwdArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -445,21 +364,6 @@ struct JoinArgs {
     nsd_plan plan;
     int32_t nsplit;  // decode (> 0)
 };
-
-// (row, first partial, partials) of the i-th long segment or decode row.
-__device__ __forceinline__ void long_segment(const nsd_plan &plan, const int32_t *ptr, int nsplit,
-                                             int64_t i, int64_t &row, int64_t &first,
-                                             int64_t &n) {
-    if (nsplit > 0) {
-        row = i;
-        first = i * nsplit;
-        n = nsplit;
-    } else {
-        row = plan.long_seg[i];
-        first = plan.chunk_ord[plan.long_first[i]];
-        n = ((int64_t)ptr[row + 1] - ptr[row] + plan.item_len - 1) / plan.item_len;
-    }
-}
 
 __device__ __forceinline__ float block_max(float v, float *sh) {
     for (int b = 1; b < kWave; b <<= 1) v = fmaxf(v, __shfl_xor(v, b));
@@ -539,21 +443,6 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(JoinArgs a) {
 }
 
 // ------------------------------------------------------------ backward, rows
-
-struct BwdArgs {
-    Shape s;
-    const void *Q, *K, *V, *dO;
-    const float *lambda, *bias, *stat;
-    void *dQ, *dK, *dV;
-    float *coef;  // [nnz][H][3]: a^1, a^2, t
-    float *D;     // [rows][H][2]
-    float *part;  // rows: [partial][H][2 + 4 d]; columns: [partial][Hk][2 d + dv]
-    const int32_t *ptr, *idx, *other, *perm;
-    nsd_plan plan;
-    int32_t nseg;
-    int64_t nmain;
-    int32_t all_empty;
-};
 
 template <class T, int VK, int VV, int G>
 struct RowLane {
@@ -912,6 +801,18 @@ __global__ __launch_bounds__(kAttnThreads) void attn_bias_kernel(int64_t nnz, in
     }
 }
 
+// The same from the matrix cores' coefficients, (ds^1, -, ds^2, -) by head.
+__global__ __launch_bounds__(kAttnThreads) void attn_bias_sum_kernel(int64_t nnz, int H,
+                                                                     const float *coef,
+                                                                     float *dbias) {
+    const int64_t step = (int64_t)gridDim.x * kAttnThreads;
+    for (int64_t e = (int64_t)blockIdx.x * kAttnThreads + threadIdx.x; e < nnz; e += step) {
+        float s = 0.f;
+        for (int h = 0; h < H; ++h) s += coef[(e * H + h) * 4] + coef[(e * H + h) * 4 + 2];
+        dbias[e] = s;
+    }
+}
+
 // dlambda = -sum over rows of D^2: each block adds a range of rows head by head
 // (fp64), the last launch adds the blocks.
 constexpr int kLambdaBlocks = 256;
@@ -1048,31 +949,49 @@ nsd_status check_attn(const nsd_attn *s) {
 }
 
 struct AttnWs {
-    float *part_row, *part_col, *coef, *D;
+    float *part_row, *part_col, *part_D, *coef, *D;
     double *lambda;
 };
 size_t carve_attn(void *ws, const nsd_csr *A, const nsd_csc *At, const nsd_attn *s, AttnWs *w) {
     Carver c(ws);
-    const size_t row = std::max(4 + 2 * s->dv, At ? 2 + 4 * s->d : 0);
-    w->part_row = c.take<float>((size_t)A->plan.nchunks * s->heads * row);
+    const bool cores = cores_pay(s);
+    const size_t chunk_heads = (size_t)A->plan.nchunks * s->heads;
+    const size_t row = std::max(4 + 2 * s->dv, !At ? 0 : cores ? 2 * s->d : 2 + 4 * s->d);
+    w->part_row = c.take<float>(chunk_heads * row);
     if (At) {
         w->part_col = c.take<float>((size_t)At->plan.nchunks * s->kv_heads * (2 * s->d + s->dv));
-        w->coef = c.take<float>((size_t)A->nnz * s->heads * 3);
+        w->part_D = c.take<float>(cores ? chunk_heads * 2 : 0);
+        w->coef = c.take<float>((size_t)A->nnz * s->heads * (cores ? 4 : 3));
         w->D = c.take<float>((size_t)A->nrows * s->heads * 2);
         w->lambda = c.take<double>((size_t)kLambdaBlocks * s->heads);
     }
     return c.bytes();
 }
 
-// Blocks of a pass: four waves' units each, then four empty segments each.
-nsd_status pass_blocks(const nsd_plan &plan, int32_t nnz, int32_t nseg, const Shape &s,
+// Blocks of a pass (`units`: one item for four waves each), then four empty
+// segments each.
+nsd_status pass_blocks(const nsd_plan &plan, int32_t nnz, int32_t nseg, int heads, int64_t units,
                        int64_t *nmain, int64_t *nblocks) {
-    *nmain = nnz == 0 ? 0 : ceil_div((int64_t)plan.nitems * s.nhb, kAttnWaves);
+    *nmain = nnz == 0 ? 0 : units;
     *nblocks = *nmain + ceil_div(nnz == 0 ? nseg : plan.nempty, kAttnWaves);
-    const int64_t joins = nnz == 0 ? 0 : (int64_t)plan.nlong * s.H;
+    const int64_t joins = nnz == 0 ? 0 : (int64_t)plan.nlong * heads;
     if (std::max(*nblocks, joins) > INT32_MAX)
         return fail(NSD_ERR_TOO_LARGE, "%lld blocks", (long long)std::max(*nblocks, joins));
     return NSD_OK;
+}
+int64_t pass_units(bool cores, int64_t items, const Shape &shape, const Slab &slab) {
+    return cores ? mfma_blocks(items, slab) : ceil_div(items * shape.nhb, kAttnWaves);
+}
+
+template <bool DECODE>
+void launch_forward(bool cores, const nsd_attn *s, const FwdArgs &a, const Slab &slab, int64_t nb,
+                    hipStream_t st) {
+    if (cores)
+        return mfma_forward(a, DECODE ? one_row(slab) : slab, nb, DECODE, st);
+    with_shape(s, [&](auto T, auto VK, auto VV, auto G, auto EX) {
+        attn_fwd_kernel<decltype(T), VK(), VV(), G(), EX(), DECODE>
+            <<<(unsigned)nb, kAttnThreads, 0, st>>>(a);
+    });
 }
 
 nsd_status check_chunks(const nsd_plan &pl, int32_t nnz) {
@@ -1092,9 +1011,10 @@ nsd_status nsd_attn_item_len(int32_t nnz, const nsd_attn *s, int32_t *item_len) 
     NSD_REQUIRE(item_len != nullptr, "item_len is NULL");
     NSD_REQUIRE(nnz >= 0, "negative nnz");
     NSD_TRY(check_attn(s));
-    // 16 waves a SIMD of every head group's items
-    const int64_t units = (int64_t)nnz * make_shape(s, s->heads).nhb;
-    *item_len = (int32_t)std::min<int64_t>(256, std::max<int64_t>(32, units / 16384));
+    // eight waves a SIMD of every head group's items
+    const int64_t units =
+        (int64_t)nnz * (cores_pay(s) ? make_slab(s).nslab : make_shape(s, s->heads).nhb);
+    *item_len = (int32_t)std::min<int64_t>(2048, std::max<int64_t>(32, units / 8192));
     return NSD_OK;
 }
 
@@ -1139,12 +1059,12 @@ nsd_status nsd_attn_diff(const nsd_csr *A, const nsd_attn *s, const void *Q, con
     a.nrows = A->nrows;
     a.all_empty = A->nnz == 0;
     int64_t nb;
-    NSD_TRY(pass_blocks(A->plan, A->nnz, A->nrows, a.s, &a.nmain, &nb));
+    const Slab slab = make_slab(s);
+    const bool cores = cores_pay(s);
+    NSD_TRY(pass_blocks(A->plan, A->nnz, A->nrows, s->heads,
+                        pass_units(cores, A->plan.nitems, a.s, slab), &a.nmain, &nb));
     const hipStream_t st = as_stream(stream);
-    with_shape(s, [&](auto T, auto VK, auto VV, auto G, auto EX) {
-        attn_fwd_kernel<decltype(T), VK(), VV(), G(), EX(), false>
-            <<<(unsigned)nb, kAttnThreads, 0, st>>>(a);
-    });
+    launch_forward<false>(cores, s, a, slab, nb, st);
     NSD_TRY(check_launch("attn_fwd_kernel"));
     if (A->nnz > 0 && A->plan.nlong > 0) {
         JoinArgs j = {a.s, a.part, lambda, O, stat, A->rowptr, A->plan, 0};
@@ -1205,28 +1125,40 @@ nsd_status nsd_attn_diff_vjp(const nsd_csr *A, const nsd_csc *At, const nsd_attn
     c.nseg = A->ncols;
     r.all_empty = c.all_empty = A->nnz == 0;
     int64_t nr, nc;
-    NSD_TRY(pass_blocks(A->plan, A->nnz, A->nrows, r.s, &r.nmain, &nr));
-    NSD_TRY(pass_blocks(At->plan, A->nnz, A->ncols, c.s, &c.nmain, &nc));
+    const Slab slab = make_slab(s), cslab = column_slab(slab);
+    const bool cores = cores_pay(s);
+    NSD_TRY(pass_blocks(A->plan, A->nnz, A->nrows, s->heads,
+                        pass_units(cores, A->plan.nitems, r.s, slab), &r.nmain, &nr));
+    NSD_TRY(pass_blocks(At->plan, A->nnz, A->ncols, s->kv_heads,
+                        pass_units(cores, At->plan.nitems, c.s, cslab), &c.nmain, &nc));
     const bool bf16 = s->dtype == NSD_BF16;
-    if (nr > 0) {
-        with_shape(s, [&](auto T, auto VK, auto VV, auto G, auto) {
-            attn_row_kernel<decltype(T), VK(), VV(), G()>
-                <<<(unsigned)nr, kAttnThreads, 0, st>>>(r);
-        });
-        NSD_TRY(check_launch("attn_row_kernel"));
-    }
-    if (A->nnz > 0 && A->plan.nlong > 0) {
-        const unsigned n = (unsigned)A->plan.nlong * s->heads;
-        if (bf16) attn_row_join_kernel<uint16_t><<<n, kAttnThreads, 0, st>>>(r);
-        else attn_row_join_kernel<float><<<n, kAttnThreads, 0, st>>>(r);
-        NSD_TRY(check_launch("attn_row_join_kernel"));
-    }
-    if (nc > 0) {
-        with_shape(s, [&](auto T, auto VK, auto VV, auto G, auto) {
-            attn_col_kernel<decltype(T), VK(), VV(), G()>
-                <<<(unsigned)nc, kAttnThreads, 0, st>>>(c);
-        });
-        NSD_TRY(check_launch("attn_col_kernel"));
+    const bool long_rows = A->nnz > 0 && A->plan.nlong > 0;
+    if (cores) {
+        r.part_D = w.part_D;
+        if (nr > 0) mfma_rows(r, slab, nr, st);
+        if (nc > 0) mfma_columns(c, cslab, nc, st);
+        NSD_TRY(check_launch("mfma_row_kernel"));
+    } else {
+        if (nr > 0) {
+            with_shape(s, [&](auto T, auto VK, auto VV, auto G, auto) {
+                attn_row_kernel<decltype(T), VK(), VV(), G()>
+                    <<<(unsigned)nr, kAttnThreads, 0, st>>>(r);
+            });
+            NSD_TRY(check_launch("attn_row_kernel"));
+        }
+        if (long_rows) {
+            const unsigned n = (unsigned)A->plan.nlong * s->heads;
+            if (bf16) attn_row_join_kernel<uint16_t><<<n, kAttnThreads, 0, st>>>(r);
+            else attn_row_join_kernel<float><<<n, kAttnThreads, 0, st>>>(r);
+            NSD_TRY(check_launch("attn_row_join_kernel"));
+        }
+        if (nc > 0) {
+            with_shape(s, [&](auto T, auto VK, auto VV, auto G, auto) {
+                attn_col_kernel<decltype(T), VK(), VV(), G()>
+                    <<<(unsigned)nc, kAttnThreads, 0, st>>>(c);
+            });
+            NSD_TRY(check_launch("attn_col_kernel"));
+        }
     }
     if (A->nnz > 0 && At->plan.nlong > 0) {
         const unsigned n = (unsigned)At->plan.nlong * s->kv_heads;
@@ -1236,8 +1168,12 @@ nsd_status nsd_attn_diff_vjp(const nsd_csr *A, const nsd_csc *At, const nsd_attn
     }
     if (dbias && A->nnz > 0) {
         const int64_t nb = std::min<int64_t>(ceil_div(A->nnz, kAttnThreads), 8192);
-        attn_bias_kernel<<<(unsigned)nb, kAttnThreads, 0, st>>>(A->nnz, s->heads, A->rowidx,
-                                                                w.coef, w.D, lambda, dbias);
+        if (cores)
+            attn_bias_sum_kernel<<<(unsigned)nb, kAttnThreads, 0, st>>>(A->nnz, s->heads, w.coef,
+                                                                        dbias);
+        else
+            attn_bias_kernel<<<(unsigned)nb, kAttnThreads, 0, st>>>(
+                A->nnz, s->heads, A->rowidx, w.coef, w.D, lambda, dbias);
         NSD_TRY(check_launch("attn_bias_kernel"));
     }
     const int nl = (int)std::min<int64_t>(std::max<int64_t>(ceil_div(A->nrows, 16), 1),
@@ -1249,12 +1185,13 @@ nsd_status nsd_attn_diff_vjp(const nsd_csr *A, const nsd_csc *At, const nsd_attn
 
 // Splits of a decode call's rows: enough for four waves a SIMD, of at least
 // kMinSplit entries.
-static void decode_splits(int32_t nrows, int32_t max_len, const Shape &s, int32_t *nsplit,
+static void decode_splits(int32_t nrows, int32_t max_len, const nsd_attn *s, int32_t *nsplit,
                           int32_t *per) {
-    const int64_t units = std::max<int64_t>((int64_t)nrows * s.nhb, 1);
+    const int64_t heads = cores_pay(s) ? make_slab(s).nslab : make_shape(s, s->heads).nhb;
+    const int64_t units = std::max<int64_t>(nrows * heads, 1);
     int64_t n = std::min<int64_t>(ceil_div(4096, units), ceil_div(max_len, kMinSplit));
     n = std::max<int64_t>(n, 1);
-    *per = (int32_t)std::max<int64_t>(ceil_div(max_len, n), 1);
+    *per = (int32_t)std::max<int64_t>(ceil_div(ceil_div(max_len, n), 32) * 32, 32);
     *nsplit = (int32_t)std::max<int64_t>(ceil_div(max_len, *per), 1);
 }
 
@@ -1264,7 +1201,7 @@ nsd_status nsd_attn_diff_decode_workspace_size(int32_t nrows, int32_t max_len, c
     NSD_REQUIRE(nrows >= 0 && max_len >= 0, "negative size");
     NSD_TRY(check_attn(s));
     int32_t nsplit, per;
-    decode_splits(nrows, max_len, make_shape(s, s->heads), &nsplit, &per);
+    decode_splits(nrows, max_len, s, &nsplit, &per);
     *bytes = nsplit == 1 ? 0
                          : (size_t)nrows * nsplit * s->heads * (4 + 2 * s->dv) * sizeof(float);
     return NSD_OK;
@@ -1293,18 +1230,19 @@ nsd_status nsd_attn_diff_decode(int32_t nrows, const int32_t *rowptr, const int3
     a.rowptr = rowptr;
     a.colind = colind;
     a.nrows = nrows;
-    decode_splits(nrows, max_len, a.s, &a.nsplit, &a.per);
-    a.nmain = ceil_div((int64_t)nrows * a.nsplit * a.s.nhb, kAttnWaves);
-    if (a.nmain > INT32_MAX) return fail(NSD_ERR_TOO_LARGE, "%lld blocks", (long long)a.nmain);
+    decode_splits(nrows, max_len, s, &a.nsplit, &a.per);
+    const Slab slab = make_slab(s);
+    const bool cores = cores_pay(s);
+    a.nmain = pass_units(cores, (int64_t)nrows * a.nsplit, a.s, slab);
+    const int64_t joins = a.nsplit > 1 ? (int64_t)nrows * s->heads : 0;
+    if (std::max(a.nmain, joins) > INT32_MAX)
+        return fail(NSD_ERR_TOO_LARGE, "%lld blocks", (long long)std::max(a.nmain, joins));
     const hipStream_t st = as_stream(stream);
-    with_shape(s, [&](auto T, auto VK, auto VV, auto G, auto EX) {
-        attn_fwd_kernel<decltype(T), VK(), VV(), G(), EX(), true>
-            <<<(unsigned)a.nmain, kAttnThreads, 0, st>>>(a);
-    });
+    launch_forward<true>(cores, s, a, slab, a.nmain, st);
     NSD_TRY(check_launch("attn_fwd_kernel"));
     if (a.nsplit > 1) {
         JoinArgs j = {a.s, a.part, lambda, O, nullptr, rowptr, nsd_plan{}, a.nsplit};
-        const unsigned n = (unsigned)nrows * s->heads;
+        const unsigned n = (unsigned)joins;
         if (s->dtype == NSD_BF16) attn_join_kernel<uint16_t><<<n, kAttnThreads, 0, st>>>(j);
         else attn_join_kernel<float><<<n, kAttnThreads, 0, st>>>(j);
         return check_launch("attn_join_kernel");

@@ -87,7 +87,7 @@ def test_bad_arguments_are_refused():
 
 def test_item_lengths():
     lens = [nsd.nsd_attn_item_len(n, shape()) for n in (0, 1, 10 ** 4, 10 ** 6, 10 ** 8)]
-    assert lens == sorted(lens) and lens[0] >= 1 and lens[-1] <= 256
+    assert lens == sorted(lens) and lens[0] >= 1 and lens[-1] <= 2048
 
 
 # --------------------------------------------- definition in 64 bits (numpy)
@@ -303,6 +303,78 @@ def test_heads(H, Hk, d, dv, dtype):
     bias[pat[0] == 5] = -np.inf
     c, T = make(rng, nq, nk, H, Hk, d, dv, dtype, pat, bias)
     check(c, T, run(c, T, item_len=8))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("H, Hk, d, dv", [(3, 3, 32, 64), (5, 5, 16, 32), (7, 7, 8, 16),
+                                          (6, 3, 24, 40), (9, 3, 32, 64), (10, 5, 16, 16),
+                                          (22, 11, 8, 8), (18, 2, 64, 128), (11, 1, 128, 256)])
+@pytest.mark.parametrize("density", [0.1, 0.9])
+def test_heads_that_do_not_fill_a_share(H, Hk, d, dv, density, dtype):
+    """Head counts that no number of heads taken together divides."""
+    rng = np.random.default_rng(H * 10 + d)
+    pat = pattern(rng, 75, 80, density, True, True)
+    c, T = make(rng, 75, 80, H, Hk, d, dv, dtype, pat)
+    check(c, T, run(c, T, item_len=300))
+
+
+def window(n, w, glob, step=1):
+    """Row i stores its last w columns (every step-th) and the first glob."""
+    i, j = np.mgrid[:n, :n]
+    return np.nonzero((j <= i) & (((i - j < w * step) & ((i - j) % step == 0)) | (j < glob)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("H, Hk, d, dv", [(8, 8, 16, 32), (8, 4, 64, 128), (2, 2, 32, 64),
+                                          (4, 1, 37, 20), (1, 1, 128, 256), (16, 2, 8, 8)])
+@pytest.mark.parametrize("n, w, glob, step", [(300, 64, 0, 1), (300, 40, 3, 1), (260, 35, 0, 3),
+                                              (200, 200, 0, 1), (150, 33, 17, 2)])
+def test_rows_that_share_columns(n, w, glob, step, H, Hk, d, dv, dtype):
+    rng = np.random.default_rng(n + w)
+    pat = window(n, w, glob, step)
+    c, T = make(rng, n, n, H, Hk, d, dv, dtype, pat)
+    for item_len in (64, 2000):
+        check(c, T, run(c, T, item_len=item_len))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("H, Hk, d, dv", [(8, 8, 16, 32), (8, 4, 64, 128), (2, 1, 32, 64)])
+def test_what_is_not_finite_stays_with_the_rows_and_heads_that_use_it(H, Hk, d, dv, dtype):
+    """A key and a value that are not finite, each in one head: other rows and other
+    heads are as without them."""
+    rng = np.random.default_rng(21)
+    n = 120
+    pat = window(n, 40, 2)
+    c, T = make(rng, n, n, H, Hk, d, dv, dtype, pat)
+    clean = run(c, T, item_len=500)
+    grp = H // Hk
+    bad = torch.zeros(n, H, dtype=torch.bool, device="cuda")  # (query, head) that may differ
+    user = np.zeros((n, n), bool)
+    user[pat] = True
+    user = torch.from_numpy(user).cuda()
+    k, v = T["k"].clone(), T["v"].clone()
+    k.view(n, Hk, 2 * d)[50, 0, 1] = math.nan
+    v.view(n, Hk, dv)[70, Hk - 1, 2] = math.inf
+    k.view(n, Hk, 2 * d)[90, Hk - 1, d + 1] = -math.inf
+    bad[:, :grp] |= user[:, 50, None]
+    bad[:, H - grp:] |= (user[:, 70] | user[:, 90])[:, None]
+    out = run(c, dict(T, k=k, v=v), item_len=500)
+    for x, width in (("o", dv), ("dq", 2 * d)):
+        a, b = (t[x].view(n, H, width)[~bad].float() for t in (clean, out))
+        # the same weights; walked apart, they are added in another order
+        assert bool(torch.isfinite(b).all()), x
+        assert float((a - b).abs().max()) <= 2.0 ** -7 * float(a.abs().max()), x
+    hit = user[:, 50]
+    assert bool(out["o"].view(n, H, dv)[hit, 0].isnan().all())
+    # keys whose every user is clean have clean gradients
+    badk = (bad.view(n, Hk, grp).any(2).float().t() @ user.float()).t() > 0  # [key, key head]
+    for x, width in (("dk", 2 * d), ("dv", dv)):
+        a, b = (t[x].view(n, Hk, width)[~badk].float() for t in (clean, out))
+        assert bool(torch.isfinite(b).all()), x
+        assert float((a - b).abs().max()) <= 2.0 ** -7 * float(a.abs().max()), x
 
 
 @pytest.mark.gpu
