@@ -1011,10 +1011,14 @@ nsd_status nsd_attn_item_len(int32_t nnz, const nsd_attn *s, int32_t *item_len) 
     NSD_REQUIRE(item_len != nullptr, "item_len is NULL");
     NSD_REQUIRE(nnz >= 0, "negative nnz");
     NSD_TRY(check_attn(s));
-    // eight waves a SIMD of every head group's items
-    const int64_t units =
-        (int64_t)nnz * (cores_pay(s) ? make_slab(s).nslab : make_shape(s, s->heads).nhb);
-    *item_len = (int32_t)std::min<int64_t>(2048, std::max<int64_t>(32, units / 8192));
+    // The vector form: 16 waves a SIMD of every head group's items, as long as the
+    // other passes' at most (1M entries, 4 heads of 8: 472 us a training step at up
+    // to 256, 509 at up to 2048).  On the matrix cores: eight, whose rows can share
+    // tiles only within an item (a window of 256: 1.93 ms at 256, 1.25 at 1088).
+    const bool cores = cores_pay(s);
+    const int64_t units = (int64_t)nnz * (cores ? make_slab(s).nslab : make_shape(s, s->heads).nhb);
+    *item_len = (int32_t)(cores ? std::min<int64_t>(2048, std::max<int64_t>(32, units / 8192))
+                                : std::min<int64_t>(256, std::max<int64_t>(32, units / 16384)));
     return NSD_OK;
 }
 
