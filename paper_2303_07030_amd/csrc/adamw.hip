@@ -173,30 +173,65 @@ __device__ __forceinline__ float block_scale(const float (&x)[kPer], float inv_t
 
 // y >= 0 to a code of MANT mantissa bits, smallest normal 2^LOW, largest code
 // MAX: the bits that the code drops carry into those it keeps by 16 random ones
-// (and half a unit of those).  Below the smallest normal codes are 2^(LOW -
-// MANT) apart.  NaN becomes the format's.
+// (and half a unit of those).  Below the smallest normal, codes are 2^(LOW -
+// MANT) apart (a second moment's at least the first, where it is not zero), and
+// NaN becomes the format's: all so rare (a ten-thousandth of a normal
+// distribution's m) that a wave takes them apart (200M weights 476 -> 406 us:
+// the step is bound by its instructions).
 template <int MANT, int LOW, uint32_t MAX>
-__device__ __forceinline__ uint32_t encode(float y, uint32_t rnd) {
+__device__ __forceinline__ void encode(const float (&y)[kPer], const uint32_t (&rnd)[kPer],
+                                       uint32_t (&code)[kPer]) {
     constexpr int DROP = 23 - MANT;
-    const uint32_t t = __float_as_uint(y) + ((rnd << (DROP - 16)) | (1u << (DROP - 17)));
-    uint32_t code = (t >> DROP) - ((126 + LOW) << MANT);
-    const float frac = ((float)rnd + 0.5f) * 0x1p-16f;
-    constexpr float kSub = MANT == 3 ? 512.f : 65536.f;
-    const uint32_t small = (uint32_t)(int)floorf(add_r(y * kSub, frac));
     constexpr float kLow = MANT == 3 ? 0x1p-6f : 0x1p-14f;
-    code = y < kLow ? small : code;
-    code = code < MAX ? code : MAX;
-    return y == y ? code : 0x7Fu;
+    bool rare = false;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+        const uint32_t carry = (rnd[e] << (DROP - 16)) | (1u << (DROP - 17));
+        const uint32_t t = __float_as_uint(y[e]) + carry - ((uint32_t)(126 + LOW) << 23);
+        code[e] = min(t >> DROP, MAX);
+        rare |= !(y[e] >= kLow);
+    }
+    if (!__any(rare)) return;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+        const float frac = ((float)rnd[e] + 0.5f) * 0x1p-16f;
+        constexpr float kSub = MANT == 3 ? 512.f : 65536.f;
+        const uint32_t small = (uint32_t)(int)floorf(add_r(y[e] * kSub, frac));
+        code[e] = y[e] < kLow ? min(small, MAX) : code[e];
+        if (MANT == 2) code[e] = y[e] > 0.f ? max(code[e], 1u) : code[e];
+        code[e] = y[e] == y[e] ? code[e] : 0x7Fu;
+    }
 }
 
-__device__ __forceinline__ uint32_t encode_m(float x, float inv, uint32_t rnd) {
-    const uint32_t sign = (__float_as_uint(x) >> 24) & 0x80u;
-    return encode<3, -6, 0x7Eu>(mul_r(fabsf(x), inv), rnd) | sign;
+// Four values' codes, the first in the lowest byte.
+__device__ __forceinline__ uint32_t encode_m(const float (&x)[kPer], float inv,
+                                             const uint32_t (&rnd)[kPer]) {
+    float y[kPer];
+    uint32_t r[kPer], c[kPer], out = 0;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+        y[e] = mul_r(fabsf(x[e]), inv);
+        r[e] = rnd[e] & 0xFFFFu;
+    }
+    encode<3, -6, 0x7Eu>(y, r, c);
+#pragma unroll
+    for (int e = 0; e < kPer; ++e)
+        out |= (c[e] | (__float_as_uint(x[e]) >> 24 & 0x80u)) << (8 * e);
+    return out;
 }
-__device__ __forceinline__ uint32_t encode_v(float x, float inv, uint32_t rnd) {
-    const float y = mul_r(x, inv);
-    const uint32_t c = encode<2, -14, 0x7Bu>(y, rnd);
-    return y > 0.f && c == 0 ? 1u : c;
+__device__ __forceinline__ uint32_t encode_v(const float (&x)[kPer], float inv,
+                                             const uint32_t (&rnd)[kPer]) {
+    float y[kPer];
+    uint32_t r[kPer], c[kPer], out = 0;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+        y[e] = mul_r(x[e], inv);
+        r[e] = rnd[e] >> 16;
+    }
+    encode<2, -14, 0x7Bu>(y, r, c);
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) out |= c[e] << (8 * e);
+    return out;
 }
 
 __device__ __forceinline__ void decode_m(uint32_t c, float (&x)[kPer]) {
@@ -262,14 +297,8 @@ __device__ __forceinline__ void adam_block(const AdamTensor &t, const AdamScalar
         float im, iv;
         sm = block_scale(m, 1.f / 448.f, im);
         sv = block_scale(v, 1.f / 57344.f, iv);
-        uint32_t cm = 0, cv = 0;
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) {
-            cm |= encode_m(m[e], im, rnd[e] & 0xFFFFu) << (8 * e);
-            cv |= encode_v(v[e], iv, rnd[e] >> 16) << (8 * e);
-        }
-        store_codes<FULL>(t.m, i, left, cm);
-        store_codes<FULL>(t.v, i, left, cv);
+        store_codes<FULL>(t.m, i, left, encode_m(m, im, rnd));
+        store_codes<FULL>(t.v, i, left, encode_v(v, iv, rnd));
         if (threadIdx.x % kWave == 0) {
             global<float>(t.m_scale)[blk] = sm;
             global<float>(t.v_scale)[blk] = sv;
