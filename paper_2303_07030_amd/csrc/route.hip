@@ -150,26 +150,60 @@ struct RouteArgs {
     double *loss;
 };
 
-// One row's gates: the k largest, written in increasing expert order.  `sel`
-// gets a bit for every one of this lane's experts that was chosen.
+// Descending order of 8 or 16 keys by merging sorted halves (odd and even
+// places apart).
+template <int LO, int N, int STEP, int NE, class K>
+__device__ __forceinline__ void merge_keys(K (&key)[NE]) {
+    auto order = [&](int i, int j) {
+        const K a = key[i], b = key[j];
+        key[i] = a > b ? a : b;
+        key[j] = a > b ? b : a;
+    };
+    if constexpr (2 * STEP < N) {
+        merge_keys<LO, N, 2 * STEP>(key);
+        merge_keys<LO + STEP, N, 2 * STEP>(key);
+#pragma unroll
+        for (int i = LO + STEP; i + STEP < LO + N; i += 2 * STEP) order(i, i + STEP);
+    } else {
+        order(LO, LO + STEP);
+    }
+}
+template <int LO, int N, int NE, class K>
+__device__ __forceinline__ void sort_keys(K (&key)[NE]) {
+    if constexpr (N > 1) {
+        sort_keys<LO, N / 2>(key);
+        sort_keys<LO + N / 2, N / 2>(key);
+        merge_keys<LO, N, 1>(key);
+    }
+}
+
+// The k largest of a row: a bit for every one of this lane's experts that was
+// chosen.  Each lane sorts its keys once; a round is then a maximum over the
+// lanes' first keys and a step of the winner's list (without the sort, a round
+// looks through all of a lane's keys).
+// The last round's key tells who was chosen.
 template <class T, int G, int NE>
-__device__ __forceinline__ uint32_t choose(const RouteArgs &a, const float (&x)[NE], int e0) {
-    Key<T> key[NE];
+__device__ __forceinline__ uint32_t choose(int E, int k, const float (&x)[NE], int e0) {
+    Key<T> key[NE], list[NE];
 #pragma unroll
-    for (int n = 0; n < NE; ++n) key[n] = e0 + n < a.E ? make_key<T>(x[n], e0 + n) : Key<T>(0);
-    uint32_t sel = 0;
-    for (int j = 0; j < a.k; ++j) {
-        Key<T> m = key[0];
-#pragma unroll
-        for (int n = 1; n < NE; ++n) m = key[n] > m ? key[n] : m;
-        m = slot_max<G>(m);
+    for (int n = 0; n < NE; ++n) {
+        const Key<T> held = make_key<T>(x[n], e0 + n);
+        list[n] = key[n] = e0 + n < E ? held : Key<T>(0);
+    }
+    sort_keys<0, NE>(list);
+    Key<T> m = 0;
+    for (int j = 0; j < k; ++j) {
+        m = slot_max<G>(list[0]);
+        const bool won = list[0] == m;
 #pragma unroll
         for (int n = 0; n < NE; ++n) {
-            const bool won = key[n] == m;
-            sel |= won ? 1u << n : 0u;
-            key[n] = won ? Key<T>(0) : key[n];
+            const Key<T> keep = list[n], next = n + 1 < NE ? list[n + 1] : Key<T>(0);
+            list[n] = won ? next : keep;
         }
     }
+    uint32_t sel = 0;
+#pragma unroll
+    for (int n = 0; n < NE; ++n) sel |= key[n] >= m && key[n] != 0 ? 1u << n : 0u;
     return sel;
 }
 
@@ -182,9 +216,23 @@ __device__ __forceinline__ void route_total(const RouteArgs &a, int nb) {
     double p = 0.0;
     int32_t n = 0;
     if (q < per) {
-        for (int b = q; b < nb; b += per) {
-            p += a.part_p[(int64_t)b * a.E + e];
-            n += a.part_n[(int64_t)b * (a.E + 1) + e];
+        // eight blocks' partials in flight
+        constexpr int F = 8;
+        for (int b0 = q; b0 < nb; b0 += F * per) {
+            double x[F];
+            int32_t y[F];
+#pragma unroll
+            for (int i = 0; i < F; ++i) {
+                const int b = min(b0 + i * per, nb - 1);
+                x[i] = a.part_p[(int64_t)b * a.E + e];
+                y[i] = a.part_n[(int64_t)b * (a.E + 1) + e];
+            }
+#pragma unroll
+            for (int i = 0; i < F; ++i) {
+                const bool in = b0 + i * per < nb;
+                p += in ? x[i] : 0.0;
+                n += in ? y[i] : 0;
+            }
         }
     }
     sh_p[t] = p;
@@ -253,7 +301,7 @@ __global__ __launch_bounds__(STATS ? stat_threads(NE) : kPlainThreads) void rout
         load_row<T, NE>(static_cast<const T *>(a.x) + t * a.ld, e0, a.E, x);
         const bool on = !(a.skip && a.skip[t]);
         const float inv = softmax_row<G, NE>(x, e);
-        uint32_t sel = choose<T, G, NE>(a, x, e0);
+        uint32_t sel = choose<T, G, NE>(a.E, a.k, x, e0);
         uint32_t open = 0;  // experts that are available
 #pragma unroll
         for (int n = 0; n < NE; ++n) open |= x[n] == -INFINITY ? 0u : 1u << n;
@@ -267,10 +315,11 @@ __global__ __launch_bounds__(STATS ? stat_threads(NE) : kPlainThreads) void rout
         }
         if constexpr (STATS) {
             const bool use = mine && on;
+            const uint32_t counted = use ? sel & open : 0u;
 #pragma unroll
             for (int n = 0; n < NE; ++n) {
                 ps[n] += use ? (double)(e[n] * inv) : 0.0;
-                cnt[n] += use ? (int)((sel & open) >> n & 1) : 0;
+                cnt[n] += (int)(counted >> n & 1);
             }
             const int any = (int)slot_max<G>(open);
             rows += use && any ? 1 : 0;
@@ -342,6 +391,13 @@ __global__ __launch_bounds__(kRouteThreads) void route_total_kernel(RouteArgs a,
     route_total(a, nb);
 }
 
+// Orders a wave's LDS accesses (the hardware takes them in order: this is for the
+// compiler).
+__device__ __forceinline__ void wave_fence() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 struct VjpArgs {
     int32_t T, E, k, norm;
     int64_t ld;
@@ -387,24 +443,30 @@ __global__ __launch_bounds__(kPlainThreads) void route_vjp_kernel(VjpArgs a) {
 #pragma unroll
         for (int n = 0; n < NE; ++n) b[n] = 0.f;
         if (a.dgate) {
+            // the row's entries, one a lane (all of them where k <= G)
+            const int64_t o = t * a.k;
+            const int j0 = min(g, a.k - 1);
+            const int c0 = a.col[o + j0];
+            const float dg0 = a.dgate[o + j0], ga0 = a.norm ? a.gate[o + j0] : 0.f;
             float dot = 0.f;
             if (a.norm) {
-                for (int j = g; j < a.k; j += G) dot += a.gate[t * a.k + j] * a.dgate[t * a.k + j];
+                dot = g < a.k ? ga0 * dg0 : 0.f;
+                for (int j = g + G; j < a.k; j += G) dot += a.gate[o + j] * a.dgate[o + j];
                 dot = slot_sum<G>(dot);
             }
 #pragma unroll
             for (int n = 0; n < NE; ++n) mine[e0 + n] = 0.f;
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-            for (int j = g; j < a.k; j += G) {
-                const int c = a.col[t * a.k + j];
-                const float dg = a.dgate[t * a.k + j];
-                if ((unsigned)c < (unsigned)a.E)
-                    mine[c] = a.norm ? a.gate[t * a.k + j] * (dg - dot) : dg;
-            }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            wave_fence();
+            auto put = [&](int c, float ga, float dg) {
+                if ((unsigned)c < (unsigned)a.E) mine[c] = a.norm ? ga * (dg - dot) : dg;
+            };
+            if (g < a.k) put(c0, ga0, dg0);
+            for (int j = g + G; j < a.k; j += G)
+                put(a.col[o + j], a.norm ? a.gate[o + j] : 0.f, a.dgate[o + j]);
+            wave_fence();
 #pragma unroll
             for (int n = 0; n < NE; ++n) b[n] = mine[e0 + n];
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            wave_fence();
         }
         const float inv = softmax_row<G, NE>(x, e);
         float dot = 0.f;
