@@ -36,22 +36,27 @@ constexpr int kMaxRouteBlocks = 256;  // one a CU; each leaves a partial sum
 template <class T>
 using Key = std::conditional_t<sizeof(T) == 2, uint32_t, uint64_t>;
 
+// The value of the partner in a butterfly step of span M.  Written so that the
+// exchange becomes an operand of the instruction that uses it (every lane has a
+// partner, so what the bounds rule gives the others does not matter).
 template <int M>
-__device__ __forceinline__ uint32_t lane_xor_u(uint32_t v) {
-    return __float_as_uint(lane_xor<M>(__uint_as_float(v)));
+__device__ __forceinline__ uint32_t partner(uint32_t v) {
+    constexpr int kControl = M == 1 ? 0xB1 : M == 2 ? 0x4E : M == 4 ? 0x141 : 0x140;
+    if constexpr (M <= 8) return __builtin_amdgcn_update_dpp(0, (int)v, kControl, 0xF, 0xF, true);
+    else return __float_as_uint(lane_xor<M>(__uint_as_float(v)));
 }
 template <int M>
-__device__ __forceinline__ uint64_t lane_xor_u(uint64_t v) {
-    return (uint64_t)lane_xor_u<M>((uint32_t)(v >> 32)) << 32 | lane_xor_u<M>((uint32_t)v);
+__device__ __forceinline__ uint64_t partner(uint64_t v) {
+    return (uint64_t)partner<M>((uint32_t)(v >> 32)) << 32 | partner<M>((uint32_t)v);
 }
 // Reductions over a slot of G lanes, the result in every lane.
 template <int G, int M = 1, class V, class Op>
 __device__ __forceinline__ V slot_reduce(V v, Op op) {
     if constexpr (M < G) {
         V o;
-        if constexpr (std::is_same_v<V, float>) o = lane_xor<M>(v);
-        else if constexpr (std::is_same_v<V, int>) o = (int)lane_xor_u<M>((uint32_t)v);
-        else o = lane_xor_u<M>(v);
+        if constexpr (std::is_same_v<V, float>)
+            o = __uint_as_float(partner<M>(__float_as_uint(v)));
+        else o = partner<M>(v);
         return slot_reduce<G, 2 * M>(op(v, o), op);
     } else {
         return v;
