@@ -284,8 +284,20 @@ __device__ __forceinline__ void adam_block(const AdamTensor &t, const AdamScalar
         }
         m[e] = add_r(mul_r(m[e], a.b1), mul_r(gr, a.c1));
         v[e] = add_r(mul_r(v[e], a.b2), mul_r(mul_r(gr, a.c2), gr));
-        // the root and the quotient to one unit in the last place
-        const float den = __builtin_amdgcn_sqrtf(v[e]) * s.root + a.eps;
+    }
+    // the root and the quotient to one unit in the last place; the hardware's root
+    // takes normal numbers, smaller ones are scaled
+    float sq[kPer];
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) sq[e] = __builtin_amdgcn_sqrtf(v[e]);
+    if (__any(fminf(fminf(v[0], v[1]), fminf(v[2], v[3])) < 0x1p-126f)) {
+#pragma unroll
+        for (int e = 0; e < kPer; ++e)
+            if (v[e] < 0x1p-126f) sq[e] = __builtin_amdgcn_sqrtf(v[e] * 0x1p32f) * 0x1p-16f;
+    }
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+        const float den = sq[e] * s.root + a.eps;
         w[e] = w[e] * keep - s.rate * (m[e] * __builtin_amdgcn_rcpf(den));
     }
     uint32_t rnd[kPer];

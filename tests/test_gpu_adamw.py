@@ -334,3 +334,23 @@ def test_an_optimizer_refuses_what_does_not_fit():
         AdamW([p], [g], masters=[torch.ones(10, device="cuda")])
     AdamW([], []).step()
     assert ctypes.sizeof(nsd.nsd_adamw_tensor) == 80
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("weights", ["f32", "copy"])
+def test_second_moments_below_the_normal_numbers(weights):
+    """Gradients of 1e-20: v is denormal, its root is not, and eps is smaller."""
+    from paper_2303_07030_amd.optim import AdamW
+    rng = np.random.default_rng(9)
+    n, lr, b1, b2, eps = 1027, 1e-2, 0.9, 0.98, 1e-30
+    g = (10.0 ** rng.uniform(-20, -18, n)).astype(np.float32)
+    p = gpu(np.ones(n), torch.float32 if weights == "f32" else torch.bfloat16)
+    opt = AdamW([p], [gpu(g)], lr=lr, beta1=b1, beta2=b2, eps=eps, weight_decay=0.0,
+                masters=True if weights == "copy" else None)
+    opt.step()
+    got = as64(opt.masters[0] if weights == "copy" else p)
+    # of the first step m / sqrt(v) is 1; v is a multiple u of 2^-149, rounded three
+    # times, of which the root keeps half; the weight's own rounding
+    u = (1 - b2) * g.astype(np.float64) ** 2 / 2.0 ** -149
+    tol = lr * (1.5 / (u - 1.5) + 16 * EPS32) + 2 * EPS32
+    assert np.all(np.abs(got - (1.0 - lr)) <= tol)
