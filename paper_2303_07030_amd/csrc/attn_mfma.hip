@@ -341,11 +341,11 @@ struct Walk {
     __device__ __forceinline__ void fetch_group(int at) {
         const int l = threadIdx.x % 8;
         nrow0 = segidx[at];
-        const int row = nrow0 + l;
-        const bool one = l < R && row < nseg;
-        nlo = one ? max(segptr[row], at) : b0;
-        nhi = one ? max(min(segptr[row + 1], b0), nlo) : b0;
-        nend = min(segptr[min(nrow0 + R, nseg)], b0);
+        const int rows = min(R, nseg - nrow0);
+        const bool one = l < rows;
+        nlo = one ? max(segptr[nrow0 + l], at) : b0;
+        nhi = one ? max(min(segptr[nrow0 + l + 1], b0), nlo) : b0;
+        nend = min(segptr[nrow0 + rows], b0);
     }
     __device__ __forceinline__ void enter(int at) {
         row0 = nrow0;
@@ -362,7 +362,7 @@ struct Walk {
     __device__ __forceinline__ void load() {
         const int lane = threadIdx.x % kWave;
         if (!shared) {
-            const int e = min(p + lane % 32, b0 - 1);
+            const int e = p + min(lane % 32, b0 - 1 - p);
             c[0] = idx[e];
             b = bias ? bias[e] : 0.f;
             return;
@@ -371,8 +371,8 @@ struct Walk {
 #pragma unroll
         for (int r = 0; r < 8; r += 2) {
             if (r >= R) break;
-            const int row = r + lane / 32, e = from_lane(cur, row) + lane % 32;
-            c[r / 2] = e < from_lane(hi, row) ? idx[e] : INT32_MAX;
+            const int row = r + lane / 32, e = from_lane(cur, row);
+            c[r / 2] = lane % 32 < from_lane(hi, row) - e ? idx[e + lane % 32] : INT32_MAX;
         }
     }
 
@@ -385,12 +385,12 @@ struct Walk {
         if (!shared) {
             t.idx = c[0];
             t.bias = b;
-            t.used = (uint32_t)__ballot(p + lane % 32 < end && b != -INFINITY);
+            t.used = (uint32_t)__ballot(lane % 32 < end - p && b != -INFINITY);
             const int olo = from_lane(lo, sub), ohi = from_lane(hi, sub);
             t.bits = low_bits(min(max(ohi - p, 0), 32)) & ~low_bits(min(max(olo - p, 0), 32));
             t.start = max(olo, p);
-            p += 32;
-            t.last = p >= end;
+            t.last = end - p <= 32;
+            p = t.last ? end : p + 32;
         } else {
             const int lowest = __builtin_amdgcn_readfirstlane(min_8(first));
             int mine = 0;  // keys of row row0 + l
@@ -452,11 +452,11 @@ __device__ __forceinline__ void for_rows(const int32_t *segidx, const int32_t *s
 // One row's entries from p on, for a walk of that row alone: `own` lanes use them.
 __device__ __forceinline__ Tile alone(const int32_t *idx, const float *bias, int p, int end,
                                       bool own) {
-    const int l = threadIdx.x % 32, e = min(p + l, end - 1);
+    const int l = threadIdx.x % 32, e = p + min(l, end - 1 - p);
     Tile t = {};
     t.idx = idx[e];
     t.bias = bias ? bias[e] : 0.f;
-    t.used = (uint32_t)__ballot(p + l < end && t.bias != -INFINITY);
+    t.used = (uint32_t)__ballot(l < end - p && t.bias != -INFINITY);
     t.bits = own ? low_bits(min(end - p, 32)) : 0u;
     t.start = p;
     return t;
@@ -686,7 +686,7 @@ struct Fwd {
         const Tile c = row_tile(row, p, end);
         load_query(row);
         reset();
-        for (; p < end; p += 32) {
+        for (; p < end; p += min(32, end - p)) {
             const Tile t = alone(a.colind, a.bias, p, end, geo.sub == 0);
             if (t.used == 0) continue;
             const int idx = stand_in(t.idx, t.used);
@@ -811,7 +811,7 @@ __global__ __launch_bounds__(kAttnThreads, waves(NC, NV)) void mfma_fwd_kernel(F
         walk.begin(a.plan.item_ptr[u.item], a.plan.item_ptr[u.item + 1]);
     }
     Tile c = walk.make(), n = c;
-    f.load_query(c.row0 + f.geo.sub);
+    f.load_query((int64_t)c.row0 + f.geo.sub);
     int idx = stand_in(c.idx, c.used);
     f.load_keys(idx, c.used >> 16 != 0);
     f.load_values(idx, c.used >> 16 != 0);
@@ -824,7 +824,7 @@ __global__ __launch_bounds__(kAttnThreads, waves(NC, NV)) void mfma_fwd_kernel(F
         if (more) {
             idx = stand_in(n.idx, n.used);
             f.load_keys(idx, n.used >> 16 != 0);
-            if (c.last) f.load_query(n.row0 + f.geo.sub);
+            if (c.last) f.load_query((int64_t)n.row0 + f.geo.sub);
         }
         if (c.used) f.absorb(s0, s1, c);
         if (more) f.load_values(idx, n.used >> 16 != 0);
@@ -949,7 +949,7 @@ struct Rows {
     __device__ __forceinline__ void walk_apart(int row, int p, int end, float *out) {
         load_operands(row);
         begin(row);
-        for (; p < end; p += 32) {
+        for (; p < end; p += min(32, end - p)) {
             const Tile t = alone(a.other, a.bias, p, end, geo.sub == 0);
             if (t.used == 0) continue;
             load_keys(stand_in(t.idx, t.used), true);
@@ -1020,7 +1020,7 @@ struct RowSums {
     __device__ __forceinline__ void walk_apart(int row, int p, int end, int at) {
         const Tile c = row_tile(row, p, end);
         clear(acc);
-        for (; p < end; p += 32) {
+        for (; p < end; p += min(32, end - p)) {
             const Tile t = alone(a.other, a.bias, p, end, geo.sub == 0);
             if (t.used == 0) continue;
             float y[8][2], ds[8];
@@ -1088,8 +1088,8 @@ __global__ __launch_bounds__(kAttnThreads, waves(NC, NV)) void mfma_weight_kerne
     Walk walk(a.other, a.idx, a.ptr, a.bias, a.nseg, 8 >> b.lrh, f.geo.sub, a.bias == nullptr);
     walk.begin(a.plan.item_ptr[u.item], a.plan.item_ptr[u.item + 1]);
     Tile c = walk.make(), n = c;
-    f.load_operands(c.row0 + f.geo.sub);
-    f.begin(c.row0 + f.geo.sub);
+    f.load_operands((int64_t)c.row0 + f.geo.sub);
+    f.begin((int64_t)c.row0 + f.geo.sub);
     int idx = stand_in(c.idx, c.used);
     f.load_keys(idx, c.used >> 16 != 0);
     float *out = chunk >= 0 ? a.part_D : a.D;
@@ -1101,17 +1101,17 @@ __global__ __launch_bounds__(kAttnThreads, waves(NC, NV)) void mfma_weight_kerne
         if (more) {
             idx = stand_in(n.idx, n.used);
             f.load_keys(idx, n.used >> 16 != 0);
-            if (c.last) f.load_operands(n.row0 + f.geo.sub);
+            if (c.last) f.load_operands((int64_t)n.row0 + f.geo.sub);
         }
         if (c.used) f.absorb(s, t, c);
         if (c.last) {
             bad |= __any(f.D != f.D);
-            const int64_t at = chunk >= 0 ? chunk : c.row0 + f.geo.sub;
+            const int64_t at = chunk >= 0 ? chunk : (int64_t)c.row0 + f.geo.sub;
             const bool has = c.has(f.geo.sub);
             const float sum = over_groups_sum(f.D);
             if (f.geo.g == 0 && f.geo.used && has)
                 out[(at * a.s.H + f.geo.hx) * 2 + f.geo.map] = sum;
-            if (more) f.begin(n.row0 + f.geo.sub);
+            if (more) f.begin((int64_t)n.row0 + f.geo.sub);
         }
         if (!more) break;
         c = n;
@@ -1137,7 +1137,7 @@ __global__ __launch_bounds__(kAttnThreads, NK == 1 ? 2 : 1) void mfma_row_kernel
     Walk walk(a.other, a.idx, a.ptr, a.bias, a.nseg, 8 >> b.lrh, geo.sub, a.bias == nullptr);
     walk.begin(a.plan.item_ptr[u.item], a.plan.item_ptr[u.item + 1]);
     Tile c = walk.make(), n = c;
-    float D = sums.row_D(c.row0 + geo.sub), nD = D, y[8][2], ny[8][2];
+    float D = sums.row_D((int64_t)c.row0 + geo.sub), nD = D, y[8][2], ny[8][2];
     sums.load_pairs(c, y);
     sums.load_keys(stand_in(c.idx, c.used), c.used >> 16 != 0);
     clear(sums.acc);
@@ -1146,7 +1146,7 @@ __global__ __launch_bounds__(kAttnThreads, NK == 1 ? 2 : 1) void mfma_row_kernel
     while (true) {
         if (more) {
             sums.load_pairs(n, ny);
-            if (c.last) nD = sums.row_D(n.row0 + geo.sub);
+            if (c.last) nD = sums.row_D((int64_t)n.row0 + geo.sub);
         }
         float ds[8];
         sums.last_pairs(c, D, lambda, y, ds);
@@ -1277,9 +1277,9 @@ struct ColSums {
     __device__ __forceinline__ void walk_apart(int col, int p, int end, int at) {
         const Tile c = row_tile(col, p, end);
         reset();
-        for (; p < end; p += 32) {
+        for (; p < end; p += min(32, end - p)) {
             Tile t = alone(a.other, nullptr, p, end, sub() == 0);
-            const int64_t pos32 = a.perm[min(p + (int)(threadIdx.x % 32), end - 1)];
+            const int64_t pos32 = a.perm[p + min((int)(threadIdx.x % 32), end - 1 - p)];
             const float live = a.coef[(pos32 * a.s.H + kv0 * a.s.grp) * 4 + 3];
             t.used &= (uint32_t)__ballot(live != 0.f);
             if (t.used == 0) continue;
@@ -1433,11 +1433,7 @@ void with_cols(const Slab &b, F f) {
 // rows are half empty and the backward passes' coefficients as many as the heads:
 // 8 heads, d = 16, 60 a row 663 / 628 and 1569 / 2022, 3 heads, d = 32 502 / 661
 // and 1261 / 2108, so the vector form.
-#ifdef NSD_ATTN_CORES
-bool cores_pay(const nsd_attn *s) { return fits_cores(s) && NSD_ATTN_CORES; }
-#else
 bool cores_pay(const nsd_attn *s) { return fits_cores(s) && s->heads >= 2 * s->kv_heads; }
-#endif
 
 Slab make_slab(const nsd_attn *s) {
     const int grp = s->heads / s->kv_heads;
