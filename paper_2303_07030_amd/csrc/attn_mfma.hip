@@ -31,9 +31,9 @@
 // with the products taken half by half of one head, everything else masked.
 //
 // Bound by HBM where a cache is read once (sixteen tokens over 24K keys each, 4 key
-// heads of d = 64: 194 us, 4.3 TB/s of rows in random order), by instructions where
-// rows share keys (a training step of 8192 rows, a window of 256 and 16 keys more, 8
-// heads over 4: 1.25 ms).
+// heads of d = 64: 194 us, 4.3 TB/s of rows in random order), by
+// issue and latency at two waves a SIMD where rows share keys (a training step of
+// 8192 rows, a window of 256 and 16 keys more, 8 heads over 4: 1.25 ms).
 #include "attn.hpp"
 #include "attn_mfma.hpp"
 
