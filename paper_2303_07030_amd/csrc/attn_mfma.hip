@@ -22,9 +22,11 @@
 //
 // Rows of the product are ordered so that lane group g ends with both maps of
 // heads 2 g and 2 g + 1: the difference needs no exchange.  Weights go into the
-// products as two bfloat16 numbers, the nearest and what it leaves: 16 bits of
-// each, so that rounding the weights does not add to rounding the output (one
-// bfloat16 alone leaves 2^-9 of the sum of absolute terms).
+// products as three bfloat16 numbers, each the nearest to what those before leave:
+// the 24 bits of a 32-bit float.  The output is a difference of two maps that may
+// nearly cancel, and the row sums of a gradient's weights cancel always; with two
+// numbers (16 bits) what is left of such sums is wrong by up to 2^-17 of their
+// terms, more than the output's own rounding.
 //
 // Zeros in Q^T meet other heads' keys: a key that is not finite there would make
 // 0 times infinity.  A row whose sums come out NaN is therefore walked again
@@ -57,17 +59,24 @@ __device__ __forceinline__ u32x4 load16(const bf16_t *p) {
     return r;
 }
 
-// Eight weights as the nearest bfloat16 and the nearest of the rest.
-__device__ __forceinline__ void split_weights(const float (&p)[8], u32x4 &hi, u32x4 &lo) {
-    bf16x8 h, l;
+// Eight weights as sums of three bfloat16 numbers.
+struct Weights {
+    u32x4 part[3];
+    __device__ __forceinline__ explicit Weights(const float (&p)[8]) {
+        bf16x8 h[3];
 #pragma unroll
-    for (int t = 0; t < 8; ++t) {
-        h[t] = static_cast<__bf16>(p[t]);
-        l[t] = static_cast<__bf16>(p[t] - static_cast<float>(h[t]));
+        for (int t = 0; t < 8; ++t) {
+            float left = p[t];
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+                h[i][t] = static_cast<__bf16>(left);
+                left -= static_cast<float>(h[i][t]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 3; ++i) part[i] = __builtin_bit_cast(u32x4, h[i]);
     }
-    hi = __builtin_bit_cast(u32x4, h);
-    lo = __builtin_bit_cast(u32x4, l);
-}
+};
 
 // Column j of 8 rows of 8 columns, as a product's operand.
 __device__ __forceinline__ u32x4 column(const u32x4 (&v)[8], int j) {
@@ -520,17 +529,17 @@ struct SumCols {
     }
 };
 
-// acc += (hi + lo) rows.
+// acc += w rows.
 template <int NV>
-__device__ __forceinline__ void weigh(const u32x4 (&x)[NV][8], u32x4 hi, u32x4 lo,
+__device__ __forceinline__ void weigh(const u32x4 (&x)[NV][8], const Weights &w,
                                       f32x4v (&acc)[NV][8]) {
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const u32x4 b = column(x[v], j);
-            acc[v][j] = mma(hi, b, acc[v][j]);
-            acc[v][j] = mma(lo, b, acc[v][j]);
+#pragma unroll
+            for (int i = 0; i < 3; ++i) acc[v][j] = mma(w.part[i], b, acc[v][j]);
             // the paired columns are made one at a time: made all at once they
             // take as many registers again as the rows
             __builtin_amdgcn_sched_barrier(0);
@@ -674,9 +683,7 @@ struct Fwd {
             w[t] = exp_diff(s[t], ms);
             l += w[t];
         }
-        u32x4 hi, lo;
-        split_weights(w, hi, lo);
-        weigh(x, hi, lo, acc);
+        weigh(x, Weights(w), acc);
     }
 
     // Whether a sum is not finite: a row's own doing, or another's or another
@@ -1017,9 +1024,7 @@ struct RowSums {
         }
     }
     __device__ __forceinline__ void absorb(const float (&ds)[8]) {
-        u32x4 hi, lo;
-        split_weights(ds, hi, lo);
-        weigh(x, hi, lo, acc);
+        weigh(x, Weights(ds), acc);
     }
     // The entries [p, end) of a row again, by itself, from the last pairs.
     __device__ __forceinline__ void walk_apart(int row, int p, int end, int at) {
@@ -1298,10 +1303,9 @@ struct ColSums {
                 load_o(idx, true, gi);
                 drop_unused(qx, g, t.used);
                 drop_unused(ox, g, t.used);
-                u32x4 hi, lo;
-                split_weights(w, hi, lo);
-                weigh(qx, hi, lo, dk);
-                weigh(ox, hi, lo, dv);
+                const Weights parts(w);
+                weigh(qx, parts, dk);
+                weigh(ox, parts, dv);
             }
         }
         finish(c, at);
@@ -1370,8 +1374,7 @@ __global__ __launch_bounds__(kAttnThreads, NK * NV == 1 ? 2 : 1) void mfma_col_k
     bool more = !walk.done, bad = false;
     if (more) n = walk.make();
     while (true) {
-        u32x4 hi, lo;
-        split_weights(w, hi, lo);
+        const Weights parts(w);
         const bool turn = gi + 1 == grp;  // to the next tile
         const int ngi = turn ? 0 : gi + 1;
         const bool go = !turn || more;
@@ -1381,9 +1384,9 @@ __global__ __launch_bounds__(kAttnThreads, NK * NV == 1 ? 2 : 1) void mfma_col_k
         }
         const bool two = (turn ? n.used : c.used) >> 16 != 0;
         const int at = turn ? nidx : idx;
-        weigh(f.qx, hi, lo, f.dk);
+        weigh(f.qx, parts, f.dk);
         if (go) f.load_q(at, two, ngi);
-        weigh(f.ox, hi, lo, f.dv);
+        weigh(f.ox, parts, f.dv);
         if (go) f.load_o(at, two, ngi);
         if (go) {
             if (turn) f.load_weights(n, npos, 0, w);

@@ -608,3 +608,160 @@ def test_decode_follows_its_lists_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         check(dict(c, row=row, col=slots), T, dict(o=o), backward=False)
+
+
+# ------------------------------------------- weights keep the bits of 32-bit floats
+
+def two_parts(x):
+    """x as two bfloat16 numbers, the nearest and the nearest to what it leaves."""
+    x = torch.from_numpy(np.asarray(x, np.float32))
+    h = x.bfloat16().float()
+    return (h.double() + (x - h).bfloat16().double()).numpy()
+
+
+def alike(x, heads):
+    """The same columns for every head."""
+    return np.tile(x, (1, heads))
+
+
+CANCELLING = [(4, 2, 64, 128), (2, 1, 16, 24), (16, 2, 16, 16), (8, 1, 64, 136), (2, 2, 16, 24)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("lam", [0.0, -1.0])
+@pytest.mark.parametrize("form", ["rows", "decode"])
+@pytest.mark.parametrize("H, Hk, d, dv", CANCELLING)
+def test_sums_of_values_that_cancel(H, Hk, d, dv, form, lam, dtype):
+    """Four keys of weights e, 1, 1, 1 and values 1, -h, -l, 0, where h + l is what two
+    bfloat16 numbers hold of e: of the sum only the bits below theirs are left.
+    Scores, and all sums of products, are exact, so that the only errors are e's
+    (the exponent's two roundings, of |x| < 1, and the exponential's unit in the
+    last place: 4 EPS32) and the output's."""
+    x = np.arange(40, 45, 2.0 ** -5) / 8.0           # e in [0.53, 0.54] at -x / 8
+    fine = 5.0 + x / 64.0
+    e = np.exp(-fine[:, None] / 8.0 - np.arange(64) * 2.0 ** -14)  # the finer column's part
+    left = np.abs(e.astype(np.float32) - two_parts(e.astype(np.float32)))
+    i, j = np.unravel_index(left.argmax(), left.shape)
+    coarse = float(torch.tensor(fine[i]).bfloat16())
+    rest = fine[i] - coarse + j * 2.0 ** -11          # both exact in bfloat16 or not used
+    rest = float(torch.tensor(rest).bfloat16())
+    scale = 1.0 / math.sqrt(d)
+    e = math.exp(-(coarse + rest) / 8.0)
+    whole = float(two_parts(e))
+    h = float(torch.tensor(e).bfloat16())
+    k = np.zeros((4, 2, d))
+    k[0, :, 1], k[0, :, 3] = -coarse / 8.0 / scale, -rest / 8.0 / scale
+    q = np.zeros((1, 2, d))
+    q[..., 1] = q[..., 3] = 1.0
+    v = np.zeros((4, dv))
+    v[:3, ::3] = np.array([1.0, -h, -(whole - h)])[:, None]
+    v[:3, 1::3] = -v[:3, :1] / 4.0
+    rng = np.random.default_rng(0)
+    c, T = make(rng, 1, 4, H, Hk, d, dv, dtype, (np.zeros(4, int), np.arange(4)))
+    for name, x, heads in (("q", q.reshape(1, -1), H), ("k", k.reshape(4, -1), Hk), ("v", v, Hk)):
+        T[name].copy_(torch.from_numpy(alike(x, heads)))
+        assert np.array_equal(as64(T[name]), alike(x, heads)), "inputs are not exact"
+    T["lam"].fill_(lam)
+    w = np.array([e, 1.0, 1.0, 1.0]) / (3.0 + e)
+    want = alike(((1.0 - lam) * w[None] @ v), H)
+    bound = (1.0 - lam) * 4 * EPS32 * alike(w[0] * np.abs(v[:1]), H)
+    assert np.all((1.0 - lam) * abs(e - whole) / (3.0 + e) * np.abs(v[0, :2]) > 8 * bound[0, :2])
+    got = (run(c, T, item_len=32, backward=False) if form == "rows"
+           else decode(c, T, np.array([0, 4]), np.arange(4), 4))["o"]
+    assert np.all(np.abs(as64(got) - want) <= bound + 2.0 ** -8 * np.abs(want))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("H, Hk, d, dv", CANCELLING)
+def test_gradients_of_queries_that_cancel(H, Hk, d, dv, dtype):
+    """A row's score gradients add up to nothing, and so does dq in a column where all
+    its keys are 1 (its query is 0 there).  Rows of three keys, searched for what
+    two bfloat16 numbers would leave of each.  Errors: a weight's (the score's and
+    the exponent's roundings 3, the exponential 2, the sum over the row 3, the
+    quotient 4 and the product 1: 13 EPS32), of a D of three such terms 16, t - D
+    and its product 2."""
+    rng = np.random.default_rng(3)
+    n, scale = 24, 1.0 / math.sqrt(d)
+    s = rng.integers(-96, 97, (20_000, 3)) / 32.0
+    t = rng.integers(-96, 97, (20_000, 3)) / 32.0
+    a = np.exp(s * scale)
+    a /= a.sum(1, keepdims=True)
+    D = (a * t).sum(1, keepdims=True)
+    ds = a * (t - D)
+    mag = (a * (np.abs(t) + np.abs(D))).sum(1)
+    off = np.abs((two_parts(ds) - ds).sum(1))
+    best = np.argsort(off / mag)[-n:]
+    bound = 20 * EPS32 * mag[best]
+    assert np.all(off[best] > 2.0 * bound)
+    row, col = np.repeat(np.arange(n), 3), np.arange(3 * n)
+    c, T = make(rng, n, 3 * n, H, Hk, d, dv, dtype, (row, col))
+    q, k = np.zeros((n, 2, d)), np.zeros((3 * n, 2, d))
+    q[..., 2] = 1.0
+    k[..., 2] = s[best].reshape(-1, 1)
+    k[..., 5] = 1.0
+    v, go = np.zeros((3 * n, dv)), np.zeros((n, dv))
+    v[:, 7], go[:, 7] = t[best].reshape(-1), 1.0
+    for name, x, heads in (("q", q.reshape(n, -1), H), ("k", k.reshape(3 * n, -1), Hk),
+                           ("v", v, Hk), ("go", go, H)):
+        T[name].copy_(torch.from_numpy(alike(x, heads)))
+        assert np.array_equal(as64(T[name]), alike(x, heads)), "inputs are not exact"
+    T["lam"].fill_(-1.0)
+    out = as64(run(c, T, item_len=32)["dq"]).reshape(n, H, 2, d)
+    assert np.all(np.abs(out[..., 5]) <= scale * bound[:, None, None] * (1 + 2.0 ** -8))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("H, Hk, d, dv", CANCELLING)
+def test_gradients_of_keys_and_values_that_cancel(H, Hk, d, dv, dtype):
+    """Two rows with the same keys, the upstream gradient of one three times the
+    other's: with queries 3 and -1 in a column where the keys are 0 their parts of
+    dk cancel.  Rows of three keys of one score have the weight 1/3 to the last
+    bit, which 3 and a row of one key's -1 cancel in dv."""
+    rng = np.random.default_rng(5)
+    n, scale = 24, 1.0 / math.sqrt(d)
+    s = rng.integers(-96, 97, (20_000, 2)) / 32.0
+    t = rng.integers(-96, 97, (20_000, 2)) / 32.0
+    a = np.exp(s * scale)
+    a /= a.sum(1, keepdims=True)
+    D = (a * t).sum(1, keepdims=True)
+    ds = a * (t - D)
+    mag = a * (np.abs(t) + np.abs(D))
+    off = np.abs(3 * two_parts(ds) - two_parts(3 * ds))
+    # each row's weights 12, D 14 and the rest 2 roundings, as for queries; of both
+    pick = np.argsort((off / mag).min(1))[-n:]
+    bound = 2 * 18 * EPS32 * 3 * mag[pick]
+    assert np.all(off[pick] > 1.5 * bound)
+    third = np.float32(1.0) / np.float32(3.0)
+    assert abs(3.0 * float(two_parts(third)) - 1.0) >= 8 * 8 * EPS32
+
+    # rows 2 i, 2 i + 1: the pair on keys 2 i, 2 i + 1; the last two rows: dv's, with
+    # key 2 n of its own
+    nq, nk = 2 * n + 2, 2 * n + 3
+    row = np.concatenate([np.repeat(np.arange(2 * n), 2), [2 * n] * 3, [2 * n + 1]])
+    col = np.concatenate([np.ravel([[2 * i, 2 * i + 1] * 2 for i in range(n)]),
+                          2 * n + np.arange(3), [2 * n]]).astype(int)
+    c, T = make(rng, nq, nk, H, Hk, d, dv, dtype, (row, col))
+    q, k = np.zeros((nq, 2, d)), np.zeros((nk, 2, d))
+    v, go = np.zeros((nk, dv)), np.zeros((nq, dv))
+    q[: 2 * n, :, 2] = 1.0
+    q[0:2 * n:2, :, 5], q[1:2 * n:2, :, 5] = 3.0, -1.0
+    k[: 2 * n, :, 2] = s[pick].reshape(-1, 1)
+    v[: 2 * n, 7] = t[pick].reshape(-1)
+    go[0:2 * n:2, 7], go[1:2 * n:2, 7] = 1.0, 3.0
+    go[2 * n, 3], go[2 * n + 1, 3] = 3.0, -1.0
+    for name, x, heads in (("q", q.reshape(nq, -1), H), ("k", k.reshape(nk, -1), Hk),
+                           ("v", v, Hk), ("go", go, H)):
+        T[name].copy_(torch.from_numpy(alike(x, heads)))
+        assert np.array_equal(as64(T[name]), alike(x, heads)), "inputs are not exact"
+    T["lam"].fill_(0.0)
+    out = run(c, T, item_len=32)
+    dk = as64(out["dk"]).reshape(nk, Hk, 2, d)
+    grp = H // Hk
+    assert np.all(np.abs(dk[: 2 * n, :, 0, 5])
+                  <= grp * scale * bound.reshape(-1, 1) * (1 + 2.0 ** -8))
+    # 1 / 3 to 4 EPS32, its product with 3 and the sum: 8 EPS32 of the magnitude 1 each
+    dv_ = as64(out["dv"]).reshape(nk, Hk, dv)[2 * n, :, 3]
+    assert np.all(np.abs(dv_) <= grp * 8 * EPS32 * (1 + 2.0 ** -8))
