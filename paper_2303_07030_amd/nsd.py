@@ -701,6 +701,32 @@ def attn_desc(heads, kv_heads, d, dv, q, k, v, o, scale) -> nsd_attn:
     return nsd_attn(heads, kv_heads, d, dv, dtype_of(q), scale, *lds)
 
 
+def _dense(t, name, n, dtype):
+    """A tensor that a call reads or writes as `n` consecutive values (a raw
+    address and None pass through)."""
+    if isinstance(t, torch.Tensor) and (t.dtype != dtype or t.numel() < n
+                                        or not t.is_contiguous()):
+        raise ValueError(f"{name}: {tuple(t.shape)} of {t.dtype}, strides {t.stride()}, are not "
+                         f"{n} consecutive values of {dtype}")
+
+
+def _rows(t, name, n, width, ld, dtype):
+    """A tensor that a call takes as `n` rows of `width` values, `ld` from one to
+    the next: one of another distance would be read, or written, past its end."""
+    if not isinstance(t, torch.Tensor):
+        return
+    if n > 1 and ld != width:  # rows with something between them
+        fits = (t.dim() == 2 and t.shape[0] >= n and t.shape[1] >= width and t.stride(0) == ld
+                and (width == 1 or t.stride(1) == 1))
+    else:
+        fits = t.numel() >= n * width and t.is_contiguous()
+        fits = fits or (t.dim() == 2 and n == 1 and t.shape[1] >= width and
+                        (width == 1 or t.stride(1) == 1))
+    if not fits or t.dtype != dtype:
+        raise ValueError(f"{name}: {tuple(t.shape)} of {t.dtype}, strides {t.stride()}, are not "
+                         f"{n} rows of {width} values of {dtype}, {ld} from one to the next")
+
+
 def nsd_attn_item_len(nnz: int, s: nsd_attn) -> int:
     L = _I(0)
     _check(_lib.nsd_attn_item_len(nnz, C.byref(s), C.byref(L)), "nsd_attn_item_len")
@@ -723,6 +749,15 @@ def nsd_attn_diff(A: nsd_csr, s: nsd_attn, Q, K, V, lam, bias, O, stat, ws, stre
 
 def nsd_attn_diff_vjp(A: nsd_csr, At: nsd_csc, s: nsd_attn, Q, K, V, lam, bias, stat, dO, dQ, dK,
                       dV, dlam, dbias, ws, stream=None):
+    """dO, dQ, dK, dV: rows as O, Q, K, V of `s` have them (attn_desc)."""
+    T = torch.bfloat16 if s.dtype == BF16 else torch.float32
+    _rows(dO, "dO", A.nrows, s.heads * s.dv, s.ldo, T)
+    _rows(dQ, "dQ", A.nrows, s.heads * 2 * s.d, s.ldq, T)
+    _rows(dK, "dK", A.ncols, s.kv_heads * 2 * s.d, s.ldk, T)
+    _rows(dV, "dV", A.ncols, s.kv_heads * s.dv, s.ldv, T)
+    _dense(stat, "stat", A.nrows * s.heads * 4, torch.float32)
+    _dense(dlam, "dlam", s.heads, torch.float32)
+    _dense(dbias, "dbias", A.nnz, torch.float32)
     _check(_lib.nsd_attn_diff_vjp(C.byref(A), C.byref(At), C.byref(s), _p(Q), _p(K), _p(V),
                                   _p(lam), _p(bias), _p(stat), _p(dO), _p(dQ), _p(dK), _p(dV),
                                   _p(dlam), _p(dbias), _p(ws), _nbytes(ws), _stream(stream)),

@@ -85,6 +85,34 @@ def test_bad_arguments_are_refused():
                       torch.zeros(3, 32), torch.zeros(3, 64), 1.0)
 
 
+def test_rows_of_another_distance_are_refused():
+    """Queries, keys and values from one projection: their gradients have the same
+    row distances, which tensors of their own do not."""
+    n, w = 4, (64, 32, 32)
+    q, k, v = torch.zeros(n, 128).split(w, 1)
+    packed = torch.zeros(n, 128).split(w, 1)
+    o, lam, stat = torch.zeros(n, 64), torch.zeros(4), torch.zeros(n, 4, 4)
+    s = nsd.attn_desc(4, 2, 8, 16, q, k, v, o, 1.0)
+    good = dict(Q=q, K=k, V=v, lam=lam, bias=None, stat=stat, dO=o, dQ=packed[0], dK=packed[1],
+                dV=packed[2], dlam=lam, dbias=torch.zeros(3))
+
+    def vjp(**change):
+        nsd.nsd_attn_diff_vjp(csr(), csc(), s, *{**good, **change}.values(), None)
+
+    with pytest.raises(nsd.NsdError) as e:  # everything fits but the workspace
+        vjp()
+    assert e.value.status == nsd.NSD_ERR_WORKSPACE
+    for name, t in dict(dQ=torch.empty_like(q), dK=torch.zeros(n, 32), dV=torch.zeros(n, 32),
+                        dO=packed[0], dlam=lam.double(), stat=stat[:3],
+                        dbias=torch.zeros(2)).items():
+        with pytest.raises(ValueError, match=name):
+            vjp(**{name: t})
+    for name, t in dict(dQ=packed[0][:3], dK=packed[1].double(), dV=packed[2].t(),
+                        dbias=torch.zeros(6)[::2]).items():
+        with pytest.raises(ValueError, match=name):
+            vjp(**{name: t})
+
+
 def test_item_lengths():
     lens = [nsd.nsd_attn_item_len(n, shape()) for n in (0, 1, 10 ** 4, 10 ** 6, 10 ** 8)]
     assert lens == sorted(lens) and lens[0] >= 1 and lens[-1] <= 2048
