@@ -413,8 +413,10 @@ struct Walk {
 #pragma unroll
                 for (int r = 0; r < 8; r += 2) {
                     if (r >= R) break;
-                    const uint32_t k = (uint32_t)(c[r / 2] - lowest);
-                    const int v = or_lanes(k < 32u ? (int)(1u << k) : 0, 32);
+                    // past the row's end c is INT32_MAX, which no column is
+                    const uint32_t k = (uint32_t)c[r / 2] - (uint32_t)lowest;
+                    const bool near = k < 32u && c[r / 2] != INT32_MAX;
+                    const int v = or_lanes(near ? (int)(1u << k) : 0, 32);
                     const int x = from_lane(v, l % 2 * 32);
                     mine = l / 2 == r / 2 ? x : mine;
                 }
@@ -424,7 +426,7 @@ struct Walk {
                             __builtin_amdgcn_readfirstlane(left);
                 tries += !share;
             }
-            t.idx = lowest + lane % 32;
+            t.idx = (int)((uint32_t)lowest + lane % 32);  // past the last column: not used
             if (!share) {
                 const int row =
                     __builtin_ctz((uint32_t)__ballot(cur < hi) & 0xFFu);  // the first with any left

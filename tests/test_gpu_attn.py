@@ -613,6 +613,34 @@ def test_decode_in_a_cache_beyond_32_bit_offsets():
 
 
 @pytest.mark.gpu
+def test_rows_that_share_the_last_columns_there_can_be():
+    """2^31 - 1 keys, rows of the last of them: what stands for no column is the
+    number after the last."""
+    H, Hk, d, dv, nk, n, w = 2, 1, 8, 8, 2 ** 31 - 1, 30, 60
+    if torch.cuda.mem_get_info()[0] < 110 << 30:
+        pytest.skip("needs 110 GB of free memory")
+    rng = np.random.default_rng(14)
+    last = w + n - 1
+    i, j = np.mgrid[:n, :last]
+    pat = np.nonzero((j >= i) & (j < i + w))  # the last row: the last w columns
+    c, T = make(rng, n, last, H, Hk, d, dv, torch.bfloat16, pat)
+    k, v = (torch.empty(nk, width, dtype=torch.bfloat16, device="cuda") for width in (2 * d, dv))
+    k[-last:], v[-last:] = T["k"], T["v"]
+    far = dict(c, col=c["col"].astype(np.int64) + nk - last)
+    check(c, T, run(c, T, item_len=4000, backward=False), backward=False)
+    A = operand(far, n, nk, 4000, csc=False)
+    o = torch.full_like(T["go"], math.nan)
+    s = nsd.attn_desc(H, Hk, d, dv, T["q"], k, v, o, 1 / math.sqrt(d))
+    ws = torch.empty(max(nsd.nsd_attn_diff_workspace_size(A.desc, None, s), 256),
+                     dtype=torch.uint8, device="cuda")
+    nsd.nsd_attn_diff(A.desc, s, T["q"], k, v, T["lam"], None, o, None, ws)
+    torch.cuda.synchronize()
+    check(c, T, dict(o=o), backward=False)
+    del k, v
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.gpu
 def test_decode_follows_its_lists_in_a_graph():
     rng = np.random.default_rng(13)
     H, Hk, d, dv, nk, most = 4, 2, 32, 64, 600, 300
