@@ -402,7 +402,8 @@ nsd_status check_tensors(int32_t n, const nsd_adamw_tensor *ts, int32_t state_bi
                     "tensor %d: 8-bit states without scales", i);
         *chunks += ceil_div(t.n, kChunk);
     }
-    if (*chunks > INT32_MAX) return fail(NSD_ERR_TOO_LARGE, "%lld chunks", (long long)*chunks);
+    // a launch's threads are counted in 32 bits
+    if (*chunks > UINT32_MAX / kAdamThreads) return fail(NSD_ERR_TOO_LARGE, "%lld chunks", (long long)*chunks);
     return NSD_OK;
 }
 

@@ -306,9 +306,8 @@ template <class T, int VK, int VV, int G, bool EXACT, bool DECODE>
 __global__ __launch_bounds__(kAttnThreads) void attn_fwd_kernel(FwdArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     if (!DECODE && (int64_t)blockIdx.x >= a.nmain) {
-        const int64_t n = ((int64_t)blockIdx.x - a.nmain) * kAttnWaves + wave;
-        const int64_t row = nth_empty(a.plan, a.nrows, a.all_empty, n);
-        if (row >= 0) empty_row<T>(a, row);
+        for_empty(a.plan, a.nrows, a.all_empty, a.nmain,
+                  [&](int64_t row) { empty_row<T>(a, row); });
         return;
     }
     const int64_t unit = near_block(blockIdx.x, (int)a.nmain) * kAttnWaves + wave;
@@ -587,13 +586,7 @@ template <class T, int VK, int VV, int G>
 __global__ __launch_bounds__(kAttnThreads) void attn_row_kernel(BwdArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     if ((int64_t)blockIdx.x >= a.nmain) {
-        const int64_t n = ((int64_t)blockIdx.x - a.nmain) * kAttnWaves + wave;
-        const int64_t row = nth_empty(a.plan, a.nseg, a.all_empty, n);
-        if (row < 0) return;
-        const int lane = threadIdx.x % kWave;
-        T *o = static_cast<T *>(a.dQ) + row * a.s.ldq;
-        for (int c = lane; c < a.s.H * 2 * a.s.d; c += kWave) o[c] = T(0);
-        for (int c = lane; c < a.s.H * 2; c += kWave) a.D[row * a.s.H * 2 + c] = 0.f;
+        for_empty(a.plan, a.nseg, a.all_empty, a.nmain, [&](int64_t row) { empty_row<T>(a, row); });
         return;
     }
     const int64_t unit = near_block(blockIdx.x, (int)a.nmain) * kAttnWaves + wave;
@@ -734,12 +727,8 @@ __global__ __launch_bounds__(kAttnThreads) void attn_col_kernel(BwdArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     T *dK = static_cast<T *>(a.dK), *dV = static_cast<T *>(a.dV);
     if ((int64_t)blockIdx.x >= a.nmain) {
-        const int64_t n = ((int64_t)blockIdx.x - a.nmain) * kAttnWaves + wave;
-        const int64_t col = nth_empty(a.plan, a.nseg, a.all_empty, n);
-        if (col < 0) return;
-        const int lane = threadIdx.x % kWave;
-        for (int c = lane; c < a.s.Hk * 2 * a.s.d; c += kWave) dK[col * a.s.ldk + c] = T(0);
-        for (int c = lane; c < a.s.Hk * a.s.dv; c += kWave) dV[col * a.s.ldv + c] = T(0);
+        for_empty(a.plan, a.nseg, a.all_empty, a.nmain,
+                  [&](int64_t col) { empty_column<T>(a, col); });
         return;
     }
     const int64_t unit = near_block(blockIdx.x, (int)a.nmain) * kAttnWaves + wave;
@@ -972,14 +961,16 @@ size_t carve_attn(void *ws, const nsd_csr *A, const nsd_csc *At, const nsd_attn 
     return c.bytes();
 }
 
-// Blocks of a pass (`units`: one item for four waves each), then four empty
-// segments each.
+// Blocks of a pass: `units` (one item for four waves each), then those that walk
+// the empty segments, four at a time.
+constexpr int64_t kEmptyBlocks = 1 << 20;
 nsd_status pass_blocks(const nsd_plan &plan, int32_t nnz, int32_t nseg, int heads, int64_t units,
                        int64_t *nmain, int64_t *nblocks) {
     *nmain = nnz == 0 ? 0 : units;
-    *nblocks = *nmain + ceil_div(nnz == 0 ? nseg : plan.nempty, kAttnWaves);
+    *nblocks = *nmain + std::min(ceil_div(nnz == 0 ? nseg : plan.nempty, kAttnWaves),
+                                 kEmptyBlocks);
     const int64_t joins = nnz == 0 ? 0 : (int64_t)plan.nlong * heads;
-    if (std::max(*nblocks, joins) > INT32_MAX)
+    if (std::max(*nblocks, joins) > kMaxBlocks)
         return fail(NSD_ERR_TOO_LARGE, "%lld blocks", (long long)std::max(*nblocks, joins));
     return NSD_OK;
 }
@@ -1243,7 +1234,7 @@ nsd_status nsd_attn_diff_decode(int32_t nrows, const int32_t *rowptr, const int3
     const bool cores = cores_pay(s);
     a.nmain = pass_units(cores, (int64_t)nrows * a.nsplit, a.s, slab);
     const int64_t joins = a.nsplit > 1 ? (int64_t)nrows * s->heads : 0;
-    if (std::max(a.nmain, joins) > INT32_MAX)
+    if (std::max(a.nmain, joins) > kMaxBlocks)
         return fail(NSD_ERR_TOO_LARGE, "%lld blocks", (long long)std::max(a.nmain, joins));
     const hipStream_t st = as_stream(stream);
     launch_forward<true>(cores, s, a, slab, a.nmain, st);

@@ -12,6 +12,8 @@ namespace attn {
 
 constexpr int kAttnThreads = 256;
 constexpr int kAttnWaves = kAttnThreads / kWave;
+// Blocks of one launch: a grid's threads are counted in 32 bits.
+constexpr int64_t kMaxBlocks = UINT32_MAX / kAttnThreads;
 constexpr int kMaxD = 128, kMaxDv = 256;
 constexpr float kLog2e = 1.44269504088896340736f;
 
@@ -86,10 +88,16 @@ __device__ __forceinline__ void empty_row(const FwdArgs &a, int64_t row) {
         for (int c = lane; c < a.s.H * 4; c += kWave) a.stat[row * a.s.H * 4 + c] = 0.f;
 }
 
-// The n-th row without entries, or -1.
-__device__ __forceinline__ int64_t nth_empty(const nsd_plan &plan, int nseg, int all, int64_t n) {
-    if (all) return n < nseg ? n : -1;
-    return n < plan.nempty ? plan.empty_seg[n] : -1;
+// Calls f(segment) for the segments without entries that this wave takes: the
+// blocks past the first nmain walk them all, four at a time each.
+template <class F>
+__device__ __forceinline__ void for_empty(const nsd_plan &plan, int nseg, int all, int64_t nmain,
+                                          F f) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int64_t end = all ? nseg : plan.nempty;
+    const int64_t step = ((int64_t)gridDim.x - nmain) * kAttnWaves;
+    for (int64_t n = ((int64_t)blockIdx.x - nmain) * kAttnWaves + wave; n < end; n += step)
+        f(all ? n : (int64_t)plan.empty_seg[n]);
 }
 
 struct BwdArgs {
@@ -108,6 +116,22 @@ struct BwdArgs {
     int64_t nmain;
     int32_t all_empty;
 };
+
+// Rows and columns without entries have no gradient.  One wave each.
+template <class T>
+__device__ __forceinline__ void empty_row(const BwdArgs &a, int64_t row) {
+    const int lane = threadIdx.x % kWave;
+    T *o = static_cast<T *>(a.dQ) + row * a.s.ldq;
+    for (int c = lane; c < a.s.H * 2 * a.s.d; c += kWave) o[c] = T(0);
+    for (int c = lane; c < a.s.H * 2; c += kWave) a.D[row * a.s.H * 2 + c] = 0.f;
+}
+template <class T>
+__device__ __forceinline__ void empty_column(const BwdArgs &a, int64_t col) {
+    const int lane = threadIdx.x % kWave;
+    T *k = static_cast<T *>(a.dK) + col * a.s.ldk, *v = static_cast<T *>(a.dV) + col * a.s.ldv;
+    for (int c = lane; c < a.s.Hk * 2 * a.s.d; c += kWave) k[c] = T(0);
+    for (int c = lane; c < a.s.Hk * a.s.dv; c += kWave) v[c] = T(0);
+}
 
 // (row, first partial, partials) of the i-th long segment or decode row.
 __device__ __forceinline__ void long_segment(const nsd_plan &plan, const int32_t *ptr, int nsplit,

@@ -795,10 +795,8 @@ constexpr int waves(int nc, int nv) { return nc * nv <= 4 ? 2 : 1; }
 template <int NC, int NV, bool FULL, bool DECODE>
 __global__ __launch_bounds__(kAttnThreads, waves(NC, NV)) void mfma_fwd_kernel(FwdArgs a, Slab b) {
     if (!DECODE && (int64_t)blockIdx.x >= a.nmain) {
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-        const int64_t n = ((int64_t)blockIdx.x - a.nmain) * kAttnWaves + wave;
-        const int64_t row = nth_empty(a.plan, a.nrows, a.all_empty, n);
-        if (row >= 0) empty_row<bf16_t>(a, row);
+        for_empty(a.plan, a.nrows, a.all_empty, a.nmain,
+                  [&](int64_t row) { empty_row<bf16_t>(a, row); });
         return;
     }
     const Unit u(a.nmain, b.nslab);
@@ -1082,14 +1080,8 @@ template <int NC, int NV, bool FULL>
 __global__ __launch_bounds__(kAttnThreads, waves(NC, NV)) void mfma_weight_kernel(
     BwdArgs a, Slab b) {
     if ((int64_t)blockIdx.x >= a.nmain) {
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-        const int64_t n = ((int64_t)blockIdx.x - a.nmain) * kAttnWaves + wave;
-        const int64_t row = nth_empty(a.plan, a.nseg, a.all_empty, n);
-        if (row < 0) return;
-        const int lane = threadIdx.x % kWave;
-        bf16_t *o = static_cast<bf16_t *>(a.dQ) + row * a.s.ldq;
-        for (int c = lane; c < a.s.H * 2 * a.s.d; c += kWave) o[c] = 0;
-        for (int c = lane; c < a.s.H * 2; c += kWave) a.D[row * a.s.H * 2 + c] = 0.f;
+        for_empty(a.plan, a.nseg, a.all_empty, a.nmain,
+                  [&](int64_t row) { empty_row<bf16_t>(a, row); });
         return;
     }
     const Unit u(a.nmain, b.nslab);
@@ -1348,14 +1340,8 @@ template <int NK, int NV>
 __global__ __launch_bounds__(kAttnThreads, NK * NV == 1 ? 2 : 1) void mfma_col_kernel(
     BwdArgs a, Slab b) {
     if ((int64_t)blockIdx.x >= a.nmain) {
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-        const int64_t n = ((int64_t)blockIdx.x - a.nmain) * kAttnWaves + wave;
-        const int64_t col = nth_empty(a.plan, a.nseg, a.all_empty, n);
-        if (col < 0) return;
-        bf16_t *dK = static_cast<bf16_t *>(a.dK), *dV = static_cast<bf16_t *>(a.dV);
-        const int lane = threadIdx.x % kWave;
-        for (int c = lane; c < a.s.Hk * 2 * a.s.d; c += kWave) dK[col * a.s.ldk + c] = 0;
-        for (int c = lane; c < a.s.Hk * a.s.dv; c += kWave) dV[col * a.s.ldv + c] = 0;
+        for_empty(a.plan, a.nseg, a.all_empty, a.nmain,
+                  [&](int64_t col) { empty_column<bf16_t>(a, col); });
         return;
     }
     const Unit u(a.nmain, b.nslab);

@@ -37,6 +37,13 @@ def test_too_long_a_tensor_is_refused():
     assert e.value.status == nsd.NSD_ERR_TOO_LARGE
 
 
+def test_more_chunks_than_a_launch_has_blocks_are_refused():
+    many = [record(n=2 ** 31 - 5000)] * 33  # 2^24 chunks: a grid's threads take 32 bits
+    with pytest.raises(nsd.NsdError) as e:
+        nsd.nsd_adamw_plan_build(many, 32, torch.empty(4096, dtype=torch.uint8))
+    assert e.value.status == nsd.NSD_ERR_TOO_LARGE
+
+
 def test_a_small_table_is_refused():
     with pytest.raises(nsd.NsdError) as e:
         nsd.nsd_adamw_plan_build([record()], 32, torch.empty(8, dtype=torch.uint8))

@@ -85,6 +85,41 @@ def test_bad_arguments_are_refused():
                       torch.zeros(3, 32), torch.zeros(3, 64), 1.0)
 
 
+@pytest.mark.parametrize("dtype", [nsd.F32, nsd.BF16])
+def test_more_blocks_than_a_launch_has_are_refused(dtype):
+    """A grid's threads are counted in 32 bits: 2^24 blocks of 256 are one too many."""
+    s, P = shape(dtype=dtype), 0x1000
+
+    class Big:
+        """A workspace's address and size, no memory behind it."""
+        def data_ptr(self):
+            return P
+
+        def numel(self):
+            return 1 << 40
+
+        def element_size(self):
+            return 1
+
+    def refused(change):
+        A, At = csr(nrows=2 ** 26), csc(nrows=2 ** 26)
+        A.plan.long_seg = A.plan.long_first = A.plan.chunk_item = A.plan.chunk_ord = P
+        for name, value in change.items():
+            setattr(A.plan, name, value)
+        for f in (lambda: nsd.nsd_attn_diff(A, s, P, P, P, P, None, P, None, Big()),
+                  lambda: nsd.nsd_attn_diff_vjp(A, At, s, P, P, P, P, None, P, P, P, P, P, P, None,
+                                                Big())):
+            with pytest.raises(nsd.NsdError) as e:
+                f()
+            assert e.value.status == nsd.NSD_ERR_TOO_LARGE
+
+    refused(dict(nlong=2 ** 22))
+    refused(dict(nitems=2 ** 26))
+    with pytest.raises(nsd.NsdError) as e:
+        nsd.nsd_attn_diff_decode(2 ** 27, P, P, 1, s, P, P, P, P, None, P, None)
+    assert e.value.status == nsd.NSD_ERR_TOO_LARGE
+
+
 def test_rows_of_another_distance_are_refused():
     """Queries, keys and values from one projection: their gradients have the same
     row distances, which tensors of their own do not."""
@@ -511,6 +546,53 @@ def test_patterns_without_entries(nq, nk):
     c, T = make(rng, nq, nk, 2, 2, 8, 16, torch.float32, (none, none))
     out = run(c, T)
     assert all(not t.any() for t in out.values())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("nnz", [0, 3])
+@pytest.mark.parametrize("nq, H, Hk, d, dv, dtype", [(68_000_000, 1, 1, 1, 1, torch.float32),
+                                                     (9_000_001, 2, 1, 8, 8, torch.bfloat16)])
+def test_more_empty_rows_than_waves(nq, H, Hk, d, dv, dtype, nnz):
+    """Rows without keys are zeros and have no gradient, also where they alone would
+    take more blocks than a launch has."""
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB of free memory")
+    from paper_2303_07030_amd.operand import DeviceCsr
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    rows, nk = [1, nq // 2, nq - 2][:nnz], 5
+    rowptr = torch.zeros(nq + 1, dtype=torch.int32, device="cuda")
+    for r in rows:
+        rowptr[r + 1:] += 1
+    A = DeviceCsr(nq, nk, rowptr, torch.tensor([4, 0, 2][:nnz]), torch.zeros(nnz), item_len=32,
+                  perm_plans=False)
+
+    def rows_of(n, w):
+        return torch.randn(n, w, generator=g, device="cuda", dtype=dtype)
+
+    q, k, v, go = (rows_of(nq, H * 2 * d), rows_of(nk, Hk * 2 * d), rows_of(nk, Hk * dv),
+                   rows_of(nq, H * dv))
+    out = [torch.full_like(t, math.nan) for t in (go, q, k, v)]
+    lam = torch.full((H,), 0.25, device="cuda")
+    dlam = torch.full_like(lam, math.nan)
+    stat = torch.full((nq, H, 4), math.nan, device="cuda")
+    s = nsd.attn_desc(H, Hk, d, dv, q, k, v, out[0], 1.0)
+    ws = torch.empty(nsd.nsd_attn_diff_workspace_size(A.desc, A.csc, s), dtype=torch.uint8,
+                     device="cuda")
+    nsd.nsd_attn_diff(A.desc, s, q, k, v, lam, None, out[0], stat, ws)
+    nsd.nsd_attn_diff_vjp(A.desc, A.csc, s, q, k, v, lam, None, stat, go, *out[1:], dlam, None, ws)
+    # one key has all the weight: O is 3/4 of its value
+    want = torch.zeros_like(go)
+    for r, c in zip(rows, [4, 0, 2]):
+        want[r] = 0.75 * v[c].view(Hk, 1, dv).expand(Hk, H // Hk, dv).reshape(-1)
+    assert torch.equal(out[0], want)
+    empty = torch.ones(nq, dtype=torch.bool, device="cuda")
+    empty[rows] = False
+    assert not out[1][empty].any()
+    unused = [c for c in range(nk) if c not in [4, 0, 2][:nnz]]
+    assert not out[2][unused].any() and not out[3][unused].any()
+    assert bool(out[3][[4, 0, 2][:nnz]].ne(0).all())
+    assert bool(torch.isfinite(dlam).all())
 
 
 @pytest.mark.gpu
