@@ -24,6 +24,7 @@
 // leave a step of m / eps.  The random bits are a hash of the step, the tensor
 // and the entry: a step is reproducible, and needs no generator's state.
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdlib>
 #include <type_traits>
@@ -274,7 +275,7 @@ __device__ __forceinline__ void adam_block(const AdamTensor &t, const AdamScalar
         load4<FULL, float>(t.m, i, left, m);
         load4<FULL, float>(t.v, i, left, v);
     }
-    const float keep = 1.f - s.lr * t.wd;
+    const float decay = s.lr * t.wd;
 #pragma unroll
     for (int e = 0; e < kPer; ++e) {
         // each product and sum of the states rounded by itself: what a block's
@@ -299,8 +300,13 @@ __device__ __forceinline__ void adam_block(const AdamTensor &t, const AdamScalar
     }
 #pragma unroll
     for (int e = 0; e < kPer; ++e) {
+        // the decay joins the step and both leave the weight at once: 1 - lr wd,
+        // rounded by itself, is off by up to 2^-25, the same way at every step.  (An
+        // infinite weight stays so.)
         const float den = sq[e] * s.root + a.eps;
-        w[e] = w[e] * keep - s.rate * (m[e] * __builtin_amdgcn_rcpf(den));
+        const float step = s.rate * (m[e] * __builtin_amdgcn_rcpf(den));
+        const float held = __builtin_amdgcn_fmed3f(w[e], -FLT_MAX, FLT_MAX);
+        w[e] -= __builtin_fmaf(held, decay, step);
     }
     uint32_t rnd[kPer];
     if constexpr (EIGHT || KIND == kBf16) {

@@ -361,3 +361,28 @@ def test_second_moments_below_the_normal_numbers(weights):
     u = (1 - b2) * g.astype(np.float64) ** 2 / 2.0 ** -149
     tol = lr * (1.5 / (u - 1.5) + 16 * EPS32) + 2 * EPS32
     assert np.all(np.abs(got - (1.0 - lr)) <= tol)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("weights", ["f32", "copy"])
+@pytest.mark.parametrize("lr, wd", [(1e-4, 0.01), (2e-4, 0.01), (1e-5, 0.012), (1e-2, 0.05)])
+def test_a_small_decay_is_not_rounded_before_the_weight(lr, wd, weights, bits):
+    """Without gradients only w (1 - lr wd) is left: to the nearest, but for lr and
+    the product in 32 bits."""
+    from paper_2303_07030_amd.optim import AdamW
+    rng = np.random.default_rng(10)
+    w = rng.standard_normal(5000).astype(np.float32)
+    w[7], w[8] = np.inf, -np.inf
+    p = gpu(w, torch.float32 if weights == "f32" else torch.bfloat16)
+    copies = [gpu(w)] if weights == "copy" else None
+    opt = AdamW([p], [torch.zeros(5000, device="cuda")], lr=lr, weight_decay=wd, masters=copies,
+                state_bits=bits)
+    opt.step()
+    got = as64(copies[0] if copies else p)
+    assert got[7] == np.inf and got[8] == -np.inf
+    fine = np.isfinite(w)
+    want = w[fine].astype(np.float64) * (1 - lr * wd)
+    off = np.abs(got[fine] - want)
+    assert np.all(off <= np.spacing(np.abs(want).astype(np.float32)) / 2.0
+                  + 4 * EPS32 * lr * wd * np.abs(want))
