@@ -90,14 +90,13 @@ class AdamW:
         """One step.  lr changes the rate from now on; grad_scale (a device fp32
         scalar) multiplies every gradient.  step_dev (device int32, the number
         of this step) and lr_dev (device fp32) are read when the step runs: with
-        them a captured graph counts its replays."""
-        h = self.hyper
-        if step_dev is None:
-            self.t += 1
-            h.step = self.t
-        if lr is not None:
-            h.lr = lr
-        h.step_dev = None if step_dev is None else step_dev.data_ptr()
-        h.lr_dev = None if lr_dev is None else lr_dev.data_ptr()
-        h.grad_scale = None if grad_scale is None else grad_scale.data_ptr()
+        them a captured graph counts its replays.  The count is then the caller's:
+        `t`, the steps done, is not advanced, and has to be set before steps
+        without step_dev or a checkpoint of it.  A refused step changes nothing."""
+        last = self.hyper
+        t = self.t + 1 if step_dev is None else self.t
+        h = nsd.nsd_adamw(last.lr if lr is None else lr, last.beta1, last.beta2, last.eps, t,
+                          *(None if x is None else x.data_ptr()
+                            for x in (step_dev, lr_dev, grad_scale)))
         nsd.nsd_adamw_step(self.plan, h, stream)
+        self.t, self.hyper = t, h

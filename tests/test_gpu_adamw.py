@@ -386,3 +386,30 @@ def test_a_small_decay_is_not_rounded_before_the_weight(lr, wd, weights, bits):
     off = np.abs(got[fine] - want)
     assert np.all(off <= np.spacing(np.abs(want).astype(np.float32)) / 2.0
                   + 4 * EPS32 * lr * wd * np.abs(want))
+
+
+@pytest.mark.gpu
+def test_a_refused_step_changes_nothing():
+    from paper_2303_07030_amd.optim import AdamW
+    rng = np.random.default_rng(11)
+    w, g = rng.standard_normal(700).astype(np.float32), rng.standard_normal(700).astype(np.float32)
+    opts = [AdamW([gpu(w, torch.bfloat16)], [gpu(g)], state_bits=8, **H) for _ in range(2)]
+    opts[1].step(lr=0.02)
+    opts[0].step(lr=0.02)
+    for bad in (math.nan, math.inf):
+        with pytest.raises(nsd.NsdError):
+            opts[0].step(lr=bad)
+    assert opts[0].t == 1 and opts[0].hyper.lr == 0.02
+    for o in opts:
+        o.step()
+    a, b = ((o.params[0], o.m[0].view(torch.uint8), o.v[0].view(torch.uint8)) for o in opts)
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+    # the caller's count, then the optimizer's
+    count = torch.full((1,), 3, dtype=torch.int32, device="cuda")
+    opts[0].step(step_dev=count)
+    assert opts[0].t == 2
+    opts[0].t = 3
+    opts[1].step()
+    for o in opts:
+        o.step()
+    assert opts[0].t == opts[1].t == 4
