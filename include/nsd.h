@@ -927,7 +927,8 @@ nsd_status nsd_route_vjp(int32_t ntok, const nsd_router *s, const void *logits,
  *
  * A tensor is a flat array of n < 2^31 - 4096 values, at any address that its
  * type allows.  `param` (fp32 or bf16) and the states are updated in place;
- * `grad` (fp32 or bf16) is read.  `master` (bf16 weights only, or NULL) is the
+ * `grad` (fp32 or bf16) is read.  An array that is updated shares no memory with
+ * another; gradients may be one another's.  `master` (bf16 weights only, or NULL) is the
  * weights in fp32: the step updates it and writes its nearest bf16 to `param`.
  * Without it a bf16 weight is rounded to one of its neighbours at random.
  *

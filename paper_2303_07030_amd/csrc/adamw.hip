@@ -413,6 +413,53 @@ nsd_status check_tensors(int32_t n, const nsd_adamw_tensor *ts, int32_t state_bi
     return NSD_OK;
 }
 
+// An array of a tensor: its bytes, and whether a step writes it.
+struct AdamArray {
+    uintptr_t lo, hi;
+    int32_t tensor;
+    bool written;
+};
+
+// No array that a step writes may share memory with another: workgroups take
+// them in any order.  (Gradients may share theirs.)
+nsd_status check_apart(int32_t n, const nsd_adamw_tensor *ts, int32_t state_bits) {
+    if (n == 0) return NSD_OK;
+    constexpr int kArrays = 7;
+    AdamArray *all = static_cast<AdamArray *>(std::malloc((size_t)n * kArrays * sizeof(AdamArray)));
+    if (all == nullptr) return fail(NSD_ERR_HIP, "no host memory for %d tensors", n);
+    size_t count = 0;
+    for (int32_t i = 0; i < n; ++i) {
+        const nsd_adamw_tensor &t = ts[i];
+        auto add = [&](const void *p, int64_t values, int64_t bytes, bool written) {
+            const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
+            if (p && values > 0) all[count++] = {lo, lo + (uintptr_t)(values * bytes), i, written};
+        };
+        const int64_t state = state_bits / 8;
+        add(t.param, t.n, t.param_dtype == NSD_BF16 ? 2 : 4, true);
+        add(t.master, t.n, 4, true);
+        add(t.grad, t.n, t.grad_dtype == NSD_BF16 ? 2 : 4, false);
+        add(t.m, t.n, state, true);
+        add(t.v, t.n, state, true);
+        if (state_bits == 8) {
+            add(t.m_scale, ceil_div(t.n, kStateBlock), 4, true);
+            add(t.v_scale, ceil_div(t.n, kStateBlock), 4, true);
+        }
+    }
+    std::sort(all, all + count, [](const AdamArray &x, const AdamArray &y) { return x.lo < y.lo; });
+    // of the arrays before, the one that ends last, and the one that is written
+    size_t any = 0, written = count, a = count, b = count;
+    for (size_t i = 0; i < count && a == count; ++i) {
+        if (written < count && all[i].lo < all[written].hi) a = written, b = i;
+        else if (i > 0 && all[i].written && all[i].lo < all[any].hi) a = any, b = i;
+        if (i > 0 && all[i].hi > all[any].hi) any = i;
+        if (all[i].written && (written == count || all[i].hi > all[written].hi)) written = i;
+    }
+    const int32_t ta = a < count ? all[a].tensor : -1, tb = b < count ? all[b].tensor : -1;
+    std::free(all);
+    NSD_REQUIRE(ta < 0, "arrays of tensors %d and %d share memory that a step writes", ta, tb);
+    return NSD_OK;
+}
+
 // Table: the tensors' records, then the chunks' (device and host alike).
 size_t table_bytes(int32_t n, int64_t chunks) {
     return (size_t)n * sizeof(AdamTensor) + (size_t)chunks * sizeof(AdamChunk);
@@ -449,6 +496,7 @@ nsd_status nsd_adamw_plan_build(int32_t ntensors, const nsd_adamw_tensor *tensor
     if (need > 0 && (table == nullptr || table_size < need))
         return fail(NSD_ERR_WORKSPACE, "table %zu bytes at %p, need %zu", table_size, table, need);
     NSD_REQUIRE((reinterpret_cast<uintptr_t>(table) & 7) == 0, "table is not 8-byte aligned");
+    NSD_TRY(check_apart(ntensors, tensors, state_bits));
     if (need > 0) {
         char *host = static_cast<char *>(std::malloc(need));
         if (host == nullptr) return fail(NSD_ERR_HIP, "no host memory for %zu bytes", need);

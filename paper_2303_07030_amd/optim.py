@@ -12,9 +12,11 @@ import torch
 from . import nsd
 
 
-def _flat(t, what, n=None, dtypes=None):
+def _flat(t, what, device, n=None, dtypes=None):
     if not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{what}: not a contiguous device tensor")
+    if t.device != device:
+        raise ValueError(f"{what}: on {t.device}, the first tensor on {device}")
     if n is not None and t.numel() != n:
         raise ValueError(f"{what}: {t.numel()} values for {n}")
     if dtypes is not None and t.dtype not in dtypes:
@@ -66,15 +68,16 @@ class AdamW:
         self.records = []
         for i, p in enumerate(self.params):
             n = p.numel()
-            _flat(p, f"tensor {i}", dtypes=floats)
-            _flat(self.grads[i], f"gradient {i}", n, floats)
-            _flat(self.m[i], f"first moment {i}", n, (T_m,))
-            _flat(self.v[i], f"second moment {i}", n, (T_v,))
+            dev = self.params[0].device
+            _flat(p, f"tensor {i}", dev, dtypes=floats)
+            _flat(self.grads[i], f"gradient {i}", dev, n, floats)
+            _flat(self.m[i], f"first moment {i}", dev, n, (T_m,))
+            _flat(self.v[i], f"second moment {i}", dev, n, (T_v,))
             if self.masters[i] is not None:
-                _flat(self.masters[i], f"copy {i}", n, (torch.float32,))
+                _flat(self.masters[i], f"copy {i}", dev, n, (torch.float32,))
             if scales:
                 for s in (self.m_scale[i], self.v_scale[i]):
-                    _flat(s, f"scales {i}", -(-n // block), (torch.float32,))
+                    _flat(s, f"scales {i}", dev, -(-n // block), (torch.float32,))
             t = [p, self.masters[i], self.grads[i], self.m[i], self.v[i], self.m_scale[i],
                  self.v_scale[i]]
             self.records.append(nsd.nsd_adamw_tensor(

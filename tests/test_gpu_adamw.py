@@ -44,6 +44,51 @@ def test_more_chunks_than_a_launch_has_blocks_are_refused():
     assert e.value.status == nsd.NSD_ERR_TOO_LARGE
 
 
+def apart(n, first, **change):
+    """A record of bf16 weights whose arrays follow each other from `first` on."""
+    sizes = dict(param=2 * n, master=4 * n, grad=2 * n, m=n, v=n, m_scale=4 * -(-n // 256),
+                 v_scale=4 * -(-n // 256))
+    t = nsd.nsd_adamw_tensor(n, param_dtype=nsd.BF16, grad_dtype=nsd.BF16)
+    for name, size in sizes.items():
+        setattr(t, name, first)
+        first += size
+    for name, value in change.items():
+        setattr(t, name, value)
+    return t, first
+
+
+def test_arrays_that_share_memory_are_refused():
+    table = torch.empty(4096, dtype=torch.uint8)
+    a, end = apart(600, 0x1000)
+    for change in (dict(param=a.param), dict(param=a.param + 1198), dict(m=a.v), dict(grad=a.master),
+                   dict(v_scale=a.m_scale + 8), dict(m=a.grad), dict(master=end - 4)):
+        b, _ = apart(40, end, **change)
+        for records in ([a, b], [b, a], [a, apart(0, end)[0], b]):
+            with pytest.raises(nsd.NsdError) as e:
+                nsd.nsd_adamw_plan_build(records, 8, table)
+            assert e.value.status == nsd.NSD_ERR_INVALID_ARG and "share" in str(e.value)
+    for field in ("master", "grad", "m", "v", "m_scale", "v_scale"):  # within one tensor
+        c, _ = apart(600, 0x1000)
+        setattr(c, field, c.param)
+        with pytest.raises(nsd.NsdError) as e:
+            nsd.nsd_adamw_plan_build([c], 8, table)
+        assert e.value.status == nsd.NSD_ERR_INVALID_ARG and "share" in str(e.value)
+
+
+@pytest.mark.gpu
+def test_neighbours_and_shared_gradients_are_taken():
+    """Arrays side by side in one buffer, and one gradient of two tensors."""
+    from paper_2303_07030_amd.optim import AdamW
+    buf = torch.zeros(4 * 300, device="cuda")
+    p, m, v, g = buf.split(300)
+    g.fill_(0.5)
+    q = torch.zeros(300, device="cuda")
+    AdamW([p, q], [g, g], m=[m, torch.zeros_like(m)], v=[v, torch.zeros_like(v)], **H).step()
+    assert torch.equal(p, q) and bool((p < 0).all())
+    with pytest.raises(nsd.NsdError):
+        AdamW([p, p], [g, g])
+
+
 def test_a_small_table_is_refused():
     with pytest.raises(nsd.NsdError) as e:
         nsd.nsd_adamw_plan_build([record()], 32, torch.empty(8, dtype=torch.uint8))
