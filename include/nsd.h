@@ -883,7 +883,8 @@ nsd_status nsd_attn_diff_decode(int32_t nrows, const int32_t *rowptr, const int3
  *     n_e    = tokens that chose e,  N = tokens routed
  *     L      = weight E sum_e (n_e / sum n) (sum_t p_te / N)
  * A logit of -infinity closes an expert to a token: chosen only for want of
- * others, its gate is a stored 0 and it is not counted.  skip[t] != 0 (skip may
+ * others, its gate is a stored 0 that is not counted, and no gradient of that
+ * gate, whatever it is, comes back.  skip[t] != 0 (skip may
  * be NULL) leaves a token out of everything: its row stores 0 at the experts 0
  * to topk - 1.  A token with every expert closed is not routed either.  A NaN
  * makes its token's gates NaN.  logits: [ntok] rows of E values (nsd_dtype),

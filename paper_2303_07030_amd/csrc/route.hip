@@ -492,24 +492,26 @@ __global__ __launch_bounds__(kPlainThreads) void route_vjp_kernel(VjpArgs a) {
             const int j0 = min(g, a.k - 1);
             const int c0 = a.col[o + j0];
             const float dg0 = a.dgate[o + j0], ga0 = a.norm ? a.gate[o + j0] : 0.f;
+            // a closed expert's gate is 0, and its gradient may be anything
+            auto part = [](float ga, float dg) { return ga != 0.f ? ga * dg : 0.f; };
             float dot = 0.f;
             if (a.norm) {
-                dot = g < a.k ? ga0 * dg0 : 0.f;
-                for (int j = g + G; j < a.k; j += G) dot += a.gate[o + j] * a.dgate[o + j];
+                dot = g < a.k ? part(ga0, dg0) : 0.f;
+                for (int j = g + G; j < a.k; j += G) dot += part(a.gate[o + j], a.dgate[o + j]);
                 dot = slot_sum<G>(dot);
             }
 #pragma unroll
             for (int n = 0; n < NE; ++n) mine[e0 + n] = 0.f;
             wave_fence();
             auto put = [&](int c, float ga, float dg) {
-                if ((unsigned)c < (unsigned)a.E) mine[c] = a.norm ? ga * (dg - dot) : dg;
+                if ((unsigned)c < (unsigned)a.E) mine[c] = a.norm ? part(ga, dg - dot) : dg;
             };
             if (g < a.k) put(c0, ga0, dg0);
             for (int j = g + G; j < a.k; j += G)
                 put(a.col[o + j], a.norm ? a.gate[o + j] : 0.f, a.dgate[o + j]);
             wave_fence();
 #pragma unroll
-            for (int n = 0; n < NE; ++n) b[n] = mine[e0 + n];
+            for (int n = 0; n < NE; ++n) b[n] = x[n] == -INFINITY ? 0.f : mine[e0 + n];
             wave_fence();
         }
         const float inv = softmax_row<G, NE>(x, e);

@@ -307,3 +307,24 @@ def test_on_another_stream_and_in_a_graph():
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want))
         y.zero_()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("E, k", [(8, 4), (20, 7), (64, 8), (300, 40)])
+@pytest.mark.parametrize("norm", [False, True])
+def test_nothing_comes_back_through_the_gates_of_closed_experts(norm, E, k, dtype):
+    rng = np.random.default_rng(6)
+    T = 90
+    x = rows(rng, T, E, dtype, 0)
+    opened = torch.from_numpy(rng.integers(0, k, T)).cuda()  # fewer than k, of some none
+    order = torch.from_numpy(rng.random((T, E))).cuda().argsort(1).argsort(1)
+    x.masked_fill_(order >= opened[:, None], -math.inf)
+    dgate = torch.from_numpy(rng.standard_normal((T, k)).astype(np.float32)).cuda()
+    col, _, _, _, _ = run(x, k, norm, None, 0.3)
+    closed = x.gather(1, col.long()) == -math.inf
+    assert bool(closed.any(1).all())
+    want = run(x, k, norm, None, 0.3, 1.3, dgate.masked_fill(closed, 0.0))[4]
+    assert bool(torch.isfinite(want).all()) and bool(want.any())
+    for what in (math.nan, math.inf, -1e38):
+        assert torch.equal(run(x, k, norm, None, 0.3, 1.3, dgate.masked_fill(closed, what))[4], want)
