@@ -442,6 +442,21 @@ def test_what_is_not_finite_stays_with_the_rows_and_heads_that_use_it(H, Hk, d, 
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("H, Hk, d, dv", [(8, 8, 16, 32), (8, 4, 64, 128), (2, 1, 32, 64),
+                                          (12, 1, 37, 20)])
+@pytest.mark.parametrize("item_len", [8, 16, 33])
+def test_what_is_not_finite_stays_there_in_chunks_of_rows(item_len, H, Hk, d, dv, dtype,
+                                                          monkeypatch):
+    """The same with rows and columns of several work items each, whose parts are
+    joined afterwards."""
+    whole = run
+    monkeypatch.setitem(globals(), "run", lambda c, T, item_len=None: whole(c, T, split))
+    split = item_len
+    test_what_is_not_finite_stays_with_the_rows_and_heads_that_use_it(H, Hk, d, dv, dtype)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("pad, shift", [(0, 1), (3, 0), (8, 5)])
 @pytest.mark.parametrize("d, dv", [(8, 16), (37, 20), (64, 128)])
 def test_strides_and_alignment(pad, shift, d, dv, dtype):
@@ -692,6 +707,93 @@ def test_decode_in_a_cache_beyond_32_bit_offsets():
     k[at], v[at] = T["k"], T["v"]
     out = decode(dict(small), dict(T, k=k, v=v), np.array([0, 100]), cols, 100)
     check(small, T, out, backward=False)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("H, Hk", [(16, 8), (32, 8), (24, 2)])
+def test_decode_of_heads_that_share_keys_beyond_32_bit_offsets(H, Hk):
+    rng = np.random.default_rng(15)
+    d, dv, n = 64, 128, 300
+    slots = 2 ** 32 // (Hk * 2 * d) + 100_000
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB of free memory")
+    k = torch.empty(slots, Hk * 2 * d, dtype=torch.bfloat16, device="cuda")
+    v = torch.empty(slots, Hk * dv, dtype=torch.bfloat16, device="cuda")
+    cols = np.concatenate([rng.choice(slots // 2, n // 3, replace=False),
+                           slots - 1 - rng.choice(1000, n - n // 3, replace=False)])
+    row = np.repeat([0, 1], [n - 70, 70])
+    c, T = make(rng, 2, n, H, Hk, d, dv, torch.bfloat16, (row, np.arange(n)))
+    at = torch.from_numpy(cols).cuda()
+    k[at], v[at] = T["k"], T["v"]
+    for max_len in (1, n):  # one launch, and splits that are joined
+        out = decode(c, dict(T, k=k, v=v), np.array([0, n - 70, n]), cols, max_len)
+        check(c, T, out, backward=False)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("max_len", [1, 100, 700])
+@pytest.mark.parametrize("H, Hk, d, dv", [(8, 2, 64, 128), (16, 2, 16, 16), (12, 1, 37, 20),
+                                          (3, 3, 20, 37)])
+def test_decode_of_slots_that_are_not_finite(H, Hk, d, dv, max_len, dtype):
+    """Masked slots may hold anything; a used one that is not finite in one key head
+    stays with the rows and heads that read it."""
+    rng = np.random.default_rng(16)
+    lens = [400, 700, 3, 90]
+    rowptr = np.concatenate([[0], np.cumsum(lens)])
+    row, n = np.repeat(np.arange(4), lens), sum(lens)
+    nk, grp = n + 5, H // Hk
+    col = rng.permutation(nk)[:n]
+    bias = np.where(rng.random(n) < 0.2, -np.inf, rng.standard_normal(n))
+    bias[400:440] = -np.inf  # whole tiles
+    c, T = make(rng, 4, nk, H, Hk, d, dv, dtype, (row, col), bias)
+    clean = decode(c, T, rowptr, col, max_len)["o"]
+    check(c, T, dict(o=clean), backward=False)
+
+    def dirty(change):
+        k, v = T["k"].clone(), T["v"].clone()
+        change(k.view(nk, Hk, 2 * d), v.view(nk, Hk, dv))
+        return decode(c, dict(T, k=k, v=v), rowptr, col, max_len)["o"].view(4, H, dv)
+
+    masked = torch.from_numpy(col[bias == -np.inf]).cuda()
+    unread = torch.from_numpy(np.setdiff1d(np.arange(nk), col)).cuda()
+
+    def hide(k, v):
+        k[masked], v[masked] = math.nan, math.inf
+        k[unread], v[unread] = math.inf, math.nan
+
+    assert torch.equal(dirty(hide), clean.view(4, H, dv))
+    clean = clean.view(4, H, dv)
+    open_ = np.flatnonzero(bias > -np.inf)
+    for r, head, half, what in ((1, 0, 0, math.nan), (0, Hk - 1, 1, math.inf),
+                                (3, Hk - 1, 2, -math.inf), (1, 0, 2, math.nan)):
+        slot = int(col[open_[(open_ >= rowptr[r]) & (open_ < rowptr[r + 1])][-1]])
+
+        def spoil(k, v):
+            if half < 2:
+                k[slot, head, half * d] = what
+            else:
+                v[slot, head, dv // 2] = what
+
+        out = dirty(spoil)
+        hit = slice(head * grp, (head + 1) * grp)
+        want = torch.zeros(grp, dv, dtype=torch.bool, device="cuda")
+        if half == 2:    # a value: its column
+            want[:, dv // 2] = True
+        elif half == 1:  # an infinite score, or one of no weight
+            want[T["q"].view(4, H, 2, d)[r, hit, 1, 0] > 0] = True
+        else:
+            want[:] = True
+        assert torch.equal(~torch.isfinite(out[r, hit]), want)
+        rest = torch.ones(4, H, dtype=torch.bool, device="cuda")
+        rest[r, hit] = False
+        others = rest.clone()
+        others[r] = False
+        assert torch.equal(out[others], clean[others])
+        a, b = clean[rest].float(), out[rest].float()
+        assert bool(torch.isfinite(b).all())
+        # the row's other heads: walked apart, their weights are added in another order
+        assert float((a - b).abs().max()) <= 2.0 ** -7 * float(a.abs().max())
 
 
 @pytest.mark.gpu
