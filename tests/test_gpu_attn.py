@@ -404,6 +404,20 @@ def test_rows_that_share_columns(n, w, glob, step, H, Hk, d, dv, dtype):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("H, Hk, d, dv", [(8, 8, 16, 32), (8, 4, 64, 128), (4, 1, 37, 20)])
+@pytest.mark.parametrize("item_len", [64, 2000])
+def test_rows_that_share_columns_with_a_bias(item_len, H, Hk, d, dv, dtype):
+    rng = np.random.default_rng(31)
+    n = 280
+    pat = window(n, 64, 3)
+    bias = np.where(rng.random(pat[0].size) < 0.2, -np.inf, rng.standard_normal(pat[0].size))
+    bias[pat[0] == 100] = -np.inf
+    c, T = make(rng, n, n, H, Hk, d, dv, dtype, pat, bias)
+    check(c, T, run(c, T, item_len=item_len))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("H, Hk, d, dv", [(8, 8, 16, 32), (8, 4, 64, 128), (2, 1, 32, 64)])
 def test_what_is_not_finite_stays_with_the_rows_and_heads_that_use_it(H, Hk, d, dv, dtype):
     """A key and a value that are not finite, each in one head: other rows and other
