@@ -69,7 +69,7 @@ typedef enum nsd_status {
 
 /* Types of the arrays that may be held in fewer bits (attention, router,
  * optimizer): 32-bit floats, or bfloat16 (the upper half of one).  Whatever the
- * type, sums, softmax statistics and updates are computed in 32 bits. */
+ * type, weights, sums, softmax statistics and updates are computed in 32 bits. */
 typedef enum nsd_dtype { NSD_F32 = 0, NSD_BF16 = 1 } nsd_dtype;
 
 /* Duplicate coordinates in a COO input: summed (the "+=" of a singleton
@@ -834,7 +834,9 @@ nsd_status nsd_batax_jacobian(const nsd_csr *A, float beta, int64_t npairs, int3
  *                          the upstream dO (ldo) and nsd_attn_diff's stat on
  *                          the same inputs.  Gradients of a key head add up its
  *                          query heads'.
- * nsd_attn_diff_workspace_size  bytes for both; At NULL: for nsd_attn_diff.
+ * nsd_attn_diff_workspace_size  bytes for both; At NULL: for nsd_attn_diff.  The
+ *                          gradient holds 12 or 16 bytes for every entry and
+ *                          head.
  * nsd_attn_diff_decode     O for a few rows over long lists of keys: rowptr
  *                          [nrows + 1] and colind need no plan, and may change
  *                          from call to call (or from replay to replay of a

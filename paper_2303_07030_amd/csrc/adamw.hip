@@ -5,13 +5,16 @@
 //   w = w (1 - lr wd) - lr / (1 - b1^t) * m / (sqrt(v / (1 - b2^t)) + eps)
 //
 // HBM-bound: every array is read and written once (200M weights in bf16 with
-// 32-bit copies: 1.02 ms, 5.3 TB/s; with 8-bit states and no copies 421 us, 4.6
-// TB/s, instructions close behind).  The tensors' entries are
-// cut into chunks of kChunk, one workgroup each, found through a list that the
-// plan holds, so that tensors of one value and of billions share a launch and
-// a step has no pass over the host's list.  A wave takes 256 consecutive
-// entries, a lane four of them: the 256 are also what shares a scale in the
-// 8-bit states, so that the largest of a block is one butterfly of a wave.
+// 32-bit copies: 1.02 ms, 5.3 TB/s; with 8-bit states and no copies 420 to 430
+// us, 4.5 TB/s).  With 8-bit states the instructions are as close: steps without
+// a pause between them draw the engine clock from 2.1 GHz to 1.6 for some ten of
+// them, and take up to 650 us there, 460 after forty.
+// The tensors' entries are cut into chunks of kChunk, one workgroup each, found
+// through a list that the plan holds, so that tensors of one value and of
+// billions share a launch and a step has no pass over the host's list.  A wave
+// takes 256 consecutive entries, a lane four of them: the 256 are also what
+// shares a scale in the 8-bit states, so that the largest of a block is one
+// butterfly of a wave.
 //
 // States in 8 bits: m as e4m3 and v as e5m2, each over a 32-bit scale that
 // takes the block's largest value to the format's largest.  A value is rounded
@@ -20,9 +23,10 @@
 // distance (v moves by 1 - b2 of its distance to g^2, and codes of v lie a
 // quarter of their value apart) would never move.  e5m2's range, 2^31 down
 // from the block's largest, keeps every v whose square root is more than 2^-16
-// of the largest; one that is not zero is never rounded to zero, which would
-// leave a step of m / eps.  The random bits are a hash of the step, the tensor
-// and the entry: a step is reproducible, and needs no generator's state.
+// of the largest; one that is not zero is not rounded to zero (but with its whole
+// block, at a scale below 2^-126), which would leave a step of m / eps.  The
+// random bits are a hash of the step, the tensor and the entry: a step is
+// reproducible, and needs no generator's state.
 #include <algorithm>
 #include <cfloat>
 #include <cmath>
@@ -179,8 +183,8 @@ __device__ __forceinline__ float block_scale(const float (&x)[kPer], float inv_t
 // (and half a unit of those).  Below the smallest normal, codes are 2^(LOW -
 // MANT) apart (a second moment's at least the first, where it is not zero), and
 // NaN becomes the format's: all so rare (a ten-thousandth of a normal
-// distribution's m) that a wave takes them apart (200M weights 476 -> 406 us:
-// the step is bound by its instructions).
+// distribution's m) that a wave takes them apart (200M weights: 70 of
+// 476 us saved, the step being bound by its instructions).
 template <int MANT, int LOW, uint32_t MAX>
 __device__ __forceinline__ void encode(const float (&y)[kPer], const uint32_t (&rnd)[kPer],
                                        uint32_t (&code)[kPer]) {
@@ -409,7 +413,8 @@ nsd_status check_tensors(int32_t n, const nsd_adamw_tensor *ts, int32_t state_bi
         *chunks += ceil_div(t.n, kChunk);
     }
     // a launch's threads are counted in 32 bits
-    if (*chunks > UINT32_MAX / kAdamThreads) return fail(NSD_ERR_TOO_LARGE, "%lld chunks", (long long)*chunks);
+    if (*chunks > UINT32_MAX / kAdamThreads)
+        return fail(NSD_ERR_TOO_LARGE, "%lld chunks", (long long)*chunks);
     return NSD_OK;
 }
 

@@ -27,9 +27,10 @@
 // (the CSC) is then a plain weighted gather of q and dO, without a dot product
 // or an atomic.
 //
-// Measured: forward over 4M entries, 8 heads of d = 16, dv = 32 in bf16 743 us (5.5
-// TB/s of gathered rows); a training step of 1M entries in 100K rows, 4 heads of d
-// = 8 in fp32 475 us, most of it latency: 10 entries a row.
+// Measured: forward over 4M entries, 8 heads of d = 16, dv = 32 in bf16 750 us (5.5
+// TB/s of gathered rows; rows of 512 bytes alone gather at 7.2); a training step of
+// 1M entries in 100K rows, 4 heads of d = 8 in fp32 482 us, most of it latency: 10
+// entries a row.
 #include "attn.hpp"
 #include "attn_mfma.hpp"
 
@@ -1009,7 +1010,8 @@ nsd_status nsd_attn_item_len(int32_t nnz, const nsd_attn *s, int32_t *item_len) 
     // The vector form: 16 waves a SIMD of every head group's items, as long as the
     // other passes' at most (1M entries, 4 heads of 8: 472 us a training step at up
     // to 256, 509 at up to 2048).  On the matrix cores: eight, whose rows can share
-    // tiles only within an item (a window of 256: 1.93 ms at 256, 1.25 at 1088).
+    // tiles only within an item (a window of 256: 2.19 ms at 256, 1.31 at 1070, 1.48
+    // at 2048).
     const bool cores = cores_pay(s);
     const int64_t units = (int64_t)nnz * (cores ? make_slab(s).nslab : make_shape(s, s->heads).nhb);
     *item_len = (int32_t)(cores ? std::min<int64_t>(2048, std::max<int64_t>(32, units / 8192))

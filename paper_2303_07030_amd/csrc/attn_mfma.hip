@@ -33,9 +33,12 @@
 // with the products taken half by half of one head, everything else masked.
 //
 // Bound by HBM where a cache is read once (sixteen tokens over 24K keys each, 4 key
-// heads of d = 64: 194 us, 4.3 TB/s of rows in random order), by
-// issue and latency at two waves a SIMD where rows share keys (a training step of
-// 8192 rows, a window of 256 and 16 keys more, 8 heads over 4: 1.25 ms).
+// heads of d = 64: 201 us, 4.2 TB/s of rows in random order; 194 with weights of 16
+// bits), by issue and latency at two waves a SIMD where rows share keys (a training
+// step of 8192 rows, a window of 256 and 16 keys more, 8 heads over 4: 1.31 ms; 1.25
+// with weights of 16 bits).  At these widths (d = 64, dv = 128) the kernels need a
+// few registers more than two waves leave them: 12 to 84 bytes of scratch a lane, 96
+// to 164 where the key columns do not fill their chunks.
 #include "attn.hpp"
 #include "attn_mfma.hpp"
 
@@ -1421,14 +1424,21 @@ void with_cols(const Slab &b, F f) {
 
 }  // namespace
 
-// Which form is faster, by the query heads of a key head (measured on MI355X at
-// 1 to 4M entries, random patterns of 6 to 250 entries a row and windows of 32 and
-// 256; vector form against this one, us).  Two and more: 8 heads over 4, d = 64,
-// 60 a row 387 / 344 forward and 1234 / 1237 backward, a window of 32 346 / 154
-// and 1118 / 629; 16 over 4, d = 32 336 / 162 and 1305 / 1049.  One: the product
-// rows are half empty and the backward passes' coefficients as many as the heads:
-// 8 heads, d = 16, 60 a row 663 / 628 and 1569 / 2022, 3 heads, d = 32 502 / 661
-// and 1261 / 2108, so the vector form.
+// Which form is faster, by the query heads of a key head.  Measured at 4M entries,
+// dv = 2 d, the vector form / this one, us, forward and gradient:
+//   heads      a random 60 a row        a window of 32          a window of 256
+//   8 over 4, d = 64
+//          1453/1329  4588/5273    1283/582  3900/3420     931/428  2800/2303
+//   16 over 4, d = 32
+//          1282/716   5240/4486    1173/705  4873/3973     929/410  2869/2383
+//   4 over 4, d = 64
+//          1076/1442  2479/4181     645/396  1910/2063     492/631  1386/2221
+//   8 over 8, d = 16
+//           549/671   1373/2149     294/585  1145/2087     259/432   750/1646
+// One query head a key head leaves half the product rows empty, and the backward
+// passes have as many coefficients: the vector form, on windows too.  From two on
+// this one; where it loses is a gradient of two heads without shared columns, and
+// slabs of few columns (4 over 2, d = 16: 214/250 and 1140/1295 at 60 a row).
 bool cores_pay(const nsd_attn *s) { return fits_cores(s) && s->heads >= 2 * s->kv_heads; }
 
 Slab make_slab(const nsd_attn *s) {

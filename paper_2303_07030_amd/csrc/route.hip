@@ -18,7 +18,7 @@
 // lowest expert and a round has one winner.
 //
 // Measured at 131,072 tokens of 128 experts, 8 chosen, bf16: gates and statistics 35
-// us, totals 9, gradient 26 (2.9 TB/s); the first is bound by the instructions of the
+// us, totals 10, gradient 27 (2.8 TB/s); the first is bound by the instructions of the
 // selection.
 #include <algorithm>
 #include <type_traits>
