@@ -807,6 +807,10 @@ def nsd_route(ntok, s: nsd_router, logits, skip, weight, colind, gate, counts, l
 
 def nsd_route_vjp(ntok, s: nsd_router, logits, skip, colind, gate, counts, weight, seed, dgate,
                   dlogits, stream=None):
+    """dlogits: rows of the logits' type, one after the other whatever their ld."""
+    _dense(dlogits, "dlogits", ntok * s.experts, torch.bfloat16 if s.dtype == BF16
+           else torch.float32)
+    _dense(dgate, "dgate", ntok * s.topk, torch.float32)
     _check(_lib.nsd_route_vjp(ntok, C.byref(s), _p(logits), _p(skip), _p(colind), _p(gate),
                               _p(counts), weight, seed, _p(dgate), _p(dlogits),
                               _stream(stream)), "nsd_route_vjp")

@@ -57,6 +57,22 @@ def test_bad_arguments_are_refused():
 
 # ---------------------------------------------- definition in 64 bits (numpy)
 
+def test_gradients_that_are_not_whole_rows_are_refused():
+    """dlogits is written row after row: as part of wider rows, or of fewer bits than
+    the logits, it would be written beside its place."""
+    T, E, k, P = 6, 8, 2, 0x1000
+    s = nsd.router_desc(E, k, torch.zeros(T, E))
+    wide = torch.zeros(T, E + 4)
+    for dlogits, dgate, name in ((wide[:, :E], torch.zeros(T, k), "dlogits"),
+                                 (torch.zeros(T, E, dtype=torch.bfloat16), None, "dlogits"),
+                                 (torch.zeros(T - 1, E), None, "dlogits"),
+                                 (torch.zeros(T, E), wide[:, :k], "dgate"),
+                                 (torch.zeros(T, E), torch.zeros(T, k).double(), "dgate")):
+        with pytest.raises(ValueError, match=name):
+            nsd.nsd_route_vjp(T, s, P, None, P, P, P, 1.0, 1.0, dgate, dlogits)
+    nsd.nsd_route_vjp(0, s, P, None, P, P, P, 1.0, 1.0, torch.zeros(0, k), torch.zeros(0, E))
+
+
 def softmax64(x):
     m = x.max(1, keepdims=True)
     m = np.where(np.isinf(m) & (m < 0), 0.0, m)
