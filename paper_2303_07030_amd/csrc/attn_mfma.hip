@@ -1436,9 +1436,10 @@ void with_cols(const Slab &b, F f) {
 //   8 over 8, d = 16
 //           549/671   1373/2149     294/585  1145/2087     259/432   750/1646
 // One query head a key head leaves half the product rows empty, and the backward
-// passes have as many coefficients: the vector form, on windows too.  From two on
-// this one; where it loses is a gradient of two heads without shared columns, and
-// slabs of few columns (4 over 2, d = 16: 214/250 and 1140/1295 at 60 a row).
+// passes have as many coefficients: the vector form, on windows too (but for a
+// narrow one at d = 64).  From two on this one; where it loses is a gradient of
+// two heads without shared columns, and slabs of few columns (4 over 2, d = 16:
+// 214/250 and 1140/1295 at 60 a row).
 bool cores_pay(const nsd_attn *s) { return fits_cores(s) && s->heads >= 2 * s->kv_heads; }
 
 Slab make_slab(const nsd_attn *s) {
