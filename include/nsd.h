@@ -67,8 +67,8 @@ typedef enum nsd_status {
     NSD_ERR_HIP = 7          /* a HIP runtime error; see nsd_last_error() */
 } nsd_status;
 
-/* Types of the arrays that may be held in fewer bits (attention, router,
- * optimizer): 32-bit floats, or bfloat16 (the upper half of one).  Whatever the
+/* Types of the arrays that may be held in fewer bits (attention and what stands
+ * around it, router, optimizer): 32-bit floats, or bfloat16 (the upper half of one).  Whatever the
  * type, weights, sums, softmax statistics and updates are computed in 32 bits. */
 typedef enum nsd_dtype { NSD_F32 = 0, NSD_BF16 = 1 } nsd_dtype;
 
@@ -986,6 +986,140 @@ nsd_status nsd_adamw_plan_build(int32_t ntensors, const nsd_adamw_tensor *tensor
                                 int32_t state_bits, nsd_adamw_plan *plan, void *table,
                                 size_t table_bytes, void *stream);
 nsd_status nsd_adamw_step(const nsd_adamw_plan *plan, const nsd_adamw *h, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * Norm of all gradients, and the factor that clips them: what a step of AdamW
+ * takes as grad_scale, or what is applied in place.
+ *     norm_i = |f| (sum of g^2)^(1/2) of tensor i, or (order 0) its largest |f g|
+ *     norm   = the same over all tensors
+ *     scale  = f min(1, max_norm / (norm + 1e-6))
+ * with f = *grad_scale (1 where NULL).  Squares and sums are held in 64 bits, so
+ * that no gradient of 32 bits overflows or vanishes in them.  A NaN makes the
+ * norms that it belongs to and the factor NaN; an infinity makes norms infinite
+ * and the factor 0.
+ *
+ * A tensor is a flat array of n < 2^31 - 16384 values, at any address that its
+ * type allows.  Tensors may share memory; each counts by itself.
+ *
+ * nsd_grad_plan_size   bytes of the plan's device table (host output).
+ * nsd_grad_plan_build  writes the table from host records, whose addresses stay
+ *                      in it.  Synchronous.
+ * nsd_grad_norm        norm (fp64, one value) and scale (fp32, one value), and,
+ *                      when norms is not NULL, norms [ntensors] (fp64).  Async.
+ * nsd_grad_clip        every gradient times *scale, rounded to its type; nothing
+ *                      is written where *scale is 1.  Refused for a plan whose
+ *                      tensors share memory.  Async.
+ */
+typedef struct nsd_grad_tensor {
+    int64_t n;
+    void *grad;
+    int32_t dtype; /* nsd_dtype */
+} nsd_grad_tensor;
+
+typedef struct nsd_grad_plan {
+    int32_t ntensors, nchunks;
+    int32_t shared;    /* some tensors share memory */
+    const void *table; /* device, nsd_grad_plan_size bytes, 8-byte aligned */
+} nsd_grad_plan;
+
+typedef struct nsd_clip {
+    double max_norm;         /* > 0; infinity: nothing is clipped */
+    int32_t order;           /* 2, or 0 for the largest magnitude */
+    const float *grad_scale; /* device scalar f, or NULL */
+} nsd_clip;
+
+nsd_status nsd_grad_plan_size(int32_t ntensors, const nsd_grad_tensor *tensors, size_t *bytes);
+nsd_status nsd_grad_plan_build(int32_t ntensors, const nsd_grad_tensor *tensors,
+                               nsd_grad_plan *plan, void *table, size_t table_bytes,
+                               void *stream);
+nsd_status nsd_grad_norm_workspace_size(const nsd_grad_plan *plan, size_t *bytes);
+nsd_status nsd_grad_norm(const nsd_grad_plan *plan, const nsd_clip *h, double *norm, float *scale,
+                         double *norms, void *ws, size_t ws_bytes, void *stream);
+nsd_status nsd_grad_clip(const nsd_grad_plan *plan, const float *scale, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * Rows of a table by token, and the table's gradient: the product of a one-hot
+ * matrix (token t stores its word id_t) with the table W, and its transpose,
+ * without the matrix.
+ *     out_t = scale W[id_t]
+ *     dW_v  = scale sum over the tokens of word v of dout_t
+ * W: [vocab][width] (wtype, ldw values from one row to the next), out and dout:
+ * [ntok][width] (otype, ldo), dW: [vocab][width] (gtype, ldw).  A token whose id
+ * is outside [0, vocab) is padding: its row is 0 and it has no gradient.
+ *
+ * nsd_embed      out.
+ * nsd_embed_vjp  dW.  accumulate = 0: all of dW is written, 0 for words without
+ *                a token; 1: the sums are added to dW, and the other words' rows
+ *                are not touched (a head that shares the table wrote its gradient
+ *                there).  A word's tokens are added up in their order.
+ * Async.
+ */
+typedef struct nsd_embedding {
+    int32_t vocab, width;
+    int32_t wtype, otype, gtype; /* nsd_dtype */
+    float scale;
+    int64_t ldw, ldo; /* >= width */
+} nsd_embedding;
+
+nsd_status nsd_embed(int32_t ntok, const nsd_embedding *s, const int32_t *ids, const void *W,
+                     void *out, void *stream);
+nsd_status nsd_embed_vjp_workspace_size(int32_t ntok, const nsd_embedding *s, size_t *bytes);
+nsd_status nsd_embed_vjp(int32_t ntok, const nsd_embedding *s, const int32_t *ids,
+                         const void *dout, int32_t accumulate, void *dW, void *ws,
+                         size_t ws_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * Norm and rotation of every head's query and key, in one pass on the way from a
+ * projection to an attention (a head of nsd_attn counts as two, one a half):
+ *     n = x / sqrt(mean(x^2) + eps) * w         (norm = 0: n = x)
+ *     (y_a, y_b) = (n_a cos - n_b sin, n_a sin + n_b cos),  angle = pos_t freq_p
+ * for pair p of the first `rot` values of a head: values p and p + rot / 2, or
+ * (interleaved) 2 p and 2 p + 1.  The others are not rotated.  The angle and its
+ * part of a whole turn are computed in 64 bits, so that far positions keep their
+ * place.
+ * Q: [ntok][heads][d], K: [ntok][kv_heads][d], and the same for what is written,
+ * Qo and Ko, all of one nsd_dtype; ldq, ldk, ldqo, ldko values from one row to the
+ * next.  wq, wk: fp32 [d], or NULL for ones.  pos: int32 [ntok]; freq: fp64
+ * [rot / 2].  d <= 512, any alignment.  kv_heads = 0: queries alone (K, wk, Ko and
+ * their gradients are not read).
+ *
+ * nsd_qk_rotate      Qo and Ko.  They may be Q and K themselves (of the same row
+ *                    distances).
+ * nsd_qk_rotate_vjp  the upstream dQo (ldqo) and dKo (ldko) give dQ (ldq), dK (ldk)
+ *                    and, where not NULL, dwq and dwk (fp32 [d], sums over all
+ *                    tokens and heads).  dQ may be dQo itself (ldq = ldqo), dK dKo.
+ * nsd_qk_append      the serving form: token t's key and value go to row slot[t]
+ *                    of the caches Kc (ldko) and Vc (ldvo; rows of vwidth values
+ *                    copied from V's, ldv), as nsd_attn_diff_decode and others read
+ *                    them; its query to Qo.  A slot outside [0, nslots) leaves the
+ *                    caches as they are.  Slots of one call are distinct: of two
+ *                    tokens with one slot, either's values may be found there.
+ *                    vwidth = 0: no values.
+ * Async.
+ */
+typedef struct nsd_qk {
+    int32_t heads, kv_heads;
+    int32_t d, rot; /* rot: even, 0 <= rot <= d */
+    int32_t dtype;
+    int32_t interleaved, norm;
+    float eps; /* >= 0 */
+    int64_t ldq, ldk, ldqo, ldko;
+} nsd_qk;
+
+nsd_status nsd_qk_rotate(int32_t ntok, const nsd_qk *s, const void *Q, const void *K,
+                         const float *wq, const float *wk, const int32_t *pos,
+                         const double *freq, void *Qo, void *Ko, void *stream);
+nsd_status nsd_qk_rotate_vjp_workspace_size(int32_t ntok, const nsd_qk *s, size_t *bytes);
+nsd_status nsd_qk_rotate_vjp(int32_t ntok, const nsd_qk *s, const void *Q, const void *K,
+                             const float *wq, const float *wk, const int32_t *pos,
+                             const double *freq, const void *dQo, const void *dKo, void *dQ,
+                             void *dK, float *dwq, float *dwk, void *ws, size_t ws_bytes,
+                             void *stream);
+nsd_status nsd_qk_append(int32_t ntok, const nsd_qk *s, const void *Q, const void *K,
+                         const void *V, int32_t vwidth, int64_t ldv, int64_t ldvo,
+                         const float *wq, const float *wk, const int32_t *pos,
+                         const double *freq, const int32_t *slot, int32_t nslots, void *Qo,
+                         void *Kc, void *Vc, void *stream);
 
 #ifdef __cplusplus
 }

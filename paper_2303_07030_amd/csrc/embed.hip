@@ -1,0 +1,470 @@
+// Rows of a table by token, and the table's gradient.
+//
+//   out_t = s W[id_t],   dW_v = s (sum over the tokens t of word v of dout_t)
+//
+// Both are HBM-bound: the rows that tokens name are read and written once; the
+// gradient reads every token's row and writes the whole table.  The gradient
+// needs the tokens by word, in their order, without the host: each block of
+// embed_order_kernel takes 256 words, looks through all ids, counts those before
+// its words (the place of its tokens in the order) and those of each word, and
+// on a second look puts its tokens there.  One launch instead of a radix sort's
+// six; the ids come from L2 but for the first block.  Where words times tokens
+// are too many for that the radix sort is taken.
+//
+// The sums: a wave takes a word and a tile of columns and adds up its tokens' rows
+// in their order.  A word of more than kLong tokens (a few words are a tenth of a
+// text) is left to waves that take kLong places of the order each, whatever the
+// words there; their sums of long words are joined in order by a second launch.
+#include <algorithm>
+
+#include "values.hpp"
+
+namespace nsd {
+
+namespace {
+
+constexpr int kEmbedThreads = 256;
+constexpr int kEmbedWaves = kEmbedThreads / kWave;
+constexpr int64_t kMaxEmbedBlocks = UINT32_MAX / kEmbedThreads;
+constexpr int kLong = kWave;  // tokens that one wave adds up; places of a chunk
+
+constexpr int kOrderThreads = 1024;
+constexpr int kOrderWaves = kOrderThreads / kWave;
+constexpr int kOrderWords = 256;
+// Ids looked at by all blocks of embed_order_kernel up to which it is taken.
+constexpr int64_t kMaxLooks = int64_t(1) << 25;
+
+bool by_looking(int64_t ntok, int64_t vocab) {
+    return ceil_div(vocab, kOrderWords) * ntok <= kMaxLooks && ntok <= (1 << 17);
+}
+
+// ------------------------------------------------------------------- rows
+
+template <class TW, class TO, int N>
+__global__ __launch_bounds__(kEmbedThreads) void embed_kernel(
+    int64_t units, int32_t tiles, int32_t vocab, int32_t width, float scale,
+    const int32_t *__restrict__ ids, const TW *__restrict__ W, int64_t ldw, TO *__restrict__ out,
+    int64_t ldo) {
+    const int lane = threadIdx.x % kWave;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    for (int64_t u = (int64_t)blockIdx.x * kEmbedWaves + wave; u < units;
+         u += (int64_t)gridDim.x * kEmbedWaves) {
+        const int64_t t = u / tiles;
+        const int col = ((int)(u % tiles) * kWave + lane) * N;
+        const int id = ids[t];
+        if (col >= width) continue;
+        float x[N] = {};
+        if (id >= 0 && id < vocab) load_left<N, TW>(W + id * ldw + col, width - col, x);
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] *= scale;
+        if (id < 0 || id >= vocab)
+#pragma unroll
+            for (int e = 0; e < N; ++e) x[e] = 0.f;  // also where the scale is not finite
+        store_left<N, TO>(out + t * ldo + col, width - col, x);
+    }
+}
+
+// ------------------------------------------------------------ tokens by word
+
+// Places of the tokens of words [256 b, 256 b + 256) in the order by word: `perm` the
+// token, `word` its word, of every place; segptr the first place of every word.
+__global__ __launch_bounds__(kOrderThreads) void embed_order_kernel(
+    int32_t ntok, int32_t vocab, const int32_t *__restrict__ ids, int32_t *__restrict__ perm,
+    int32_t *__restrict__ word, int32_t *__restrict__ segptr) {
+    __shared__ int32_t count[kOrderWaves][kOrderWords];  // of a wave's tokens; then its next place
+    __shared__ int32_t below[kOrderWaves], scan[kOrderWords / kWave];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int lo = blockIdx.x * kOrderWords;
+    const int words = min(kOrderWords, vocab - lo);
+    for (int i = threadIdx.x; i < kOrderWaves * kOrderWords; i += kOrderThreads) (&count[0][0])[i] = 0;
+    __syncthreads();
+    // a wave's tokens are consecutive ones; eight loads are in flight at once
+    constexpr int kAhead = 8;
+    const int piece = (ntok / (kOrderWaves * kWave) + 1) * kWave;
+    const int first = (int)min((int64_t)wave * piece, (int64_t)ntok);
+    const int last = (int)min((int64_t)first + piece, (int64_t)ntok);
+    int before = 0;
+    for (int b = first; b < last; b += kWave * kAhead) {
+        int id[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int t = b + u * kWave + lane;
+            id[u] = t < last ? ids[t] : -1;
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            before += id[u] >= 0 && id[u] < lo;
+            if (id[u] >= lo && id[u] - lo < words) atomicAdd(&count[wave][id[u] - lo], 1);
+        }
+    }
+#pragma unroll
+    for (int m = 1; m < kWave; m <<= 1) before += __shfl_xor(before, m, kWave);
+    if (lane == 0) below[wave] = before;
+    __syncthreads();
+    int mine = 0, upto = 0;
+    if (threadIdx.x < kOrderWords) {
+        for (int w = 0; w < kOrderWaves; ++w) mine += count[w][threadIdx.x];
+        upto = mine;
+#pragma unroll
+        for (int m = 1; m < kWave; m <<= 1) {
+            const int x = __shfl_up(upto, m, kWave);
+            if (lane >= m) upto += x;
+        }
+        if (lane == kWave - 1) scan[wave] = upto;
+    }
+    __syncthreads();
+    if (threadIdx.x < kOrderWords) {
+        for (int w = 0; w < wave; ++w) upto += scan[w];
+        for (int w = 0; w < kOrderWaves; ++w) upto += below[w];
+        int at = upto - mine;
+        if (threadIdx.x < words) segptr[lo + threadIdx.x] = at;
+        if (threadIdx.x == words - 1 && lo + words == vocab) segptr[vocab] = upto;
+        for (int w = 0; w < kOrderWaves; ++w) {
+            const int n = count[w][threadIdx.x];
+            count[w][threadIdx.x] = at;
+            at += n;
+        }
+    }
+    __syncthreads();
+    for (int b = first; b < last; b += kWave * kAhead) {
+        int id[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int t = b + u * kWave + lane;
+            id[u] = t < last ? ids[t] : -1;
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int x = id[u] - lo;
+            const bool here = id[u] >= lo && x < words;
+            uint64_t same = __ballot(here);  // lanes with this lane's word
+            if (same == 0) continue;
+#pragma unroll
+            for (int bit = 0; bit < 8; ++bit) {
+                const uint64_t set = __ballot(here && (x >> bit & 1));
+                same &= x >> bit & 1 ? set : ~set;
+            }
+            if (here) {
+                const int place = count[wave][x];
+                const int rank = __popcll(same & ((1ull << lane) - 1));
+                perm[place + rank] = b + u * kWave + lane;
+                word[place + rank] = id[u];
+                if (rank == __popcll(same) - 1) count[wave][x] = place + rank + 1;
+            }
+            // the next look reads what another lane wrote
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+}
+
+// Ids as keys of a sort: padding behind every word.
+__global__ __launch_bounds__(kEmbedThreads) void embed_keys_kernel(int32_t ntok, int32_t vocab,
+                                                                   const int32_t *ids,
+                                                                   int32_t *key) {
+    const int64_t t = (int64_t)blockIdx.x * kEmbedThreads + threadIdx.x;
+    if (t < ntok) key[t] = ids[t] >= 0 && ids[t] < vocab ? ids[t] : vocab;
+}
+
+// ------------------------------------------------------------------- sums
+
+struct EmbedSum {
+    int32_t ntok, vocab, width, tiles, nchunks;
+    bool accumulate;
+    float scale;
+    const int32_t *perm, *word, *segptr;
+    int64_t ldw, ldo;
+    float *part;  // [chunk][2][width]: of the word at its first place, and of another at its last
+};
+
+// The sum of n <= 64 rows: lane from + i holds row i's token.  FULL: every lane's columns
+// exist.
+template <bool FULL, class TR, int N>
+__device__ __forceinline__ void add_some(const TR *__restrict__ rows, int64_t ld, int token, int from,
+                                         int n, int col, int left, float (&acc)[N]) {
+    constexpr int kAhead = 4;
+    int i = 0;
+    for (; i + kAhead <= n; i += kAhead) {
+        float x[kAhead][N];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int64_t t = __builtin_amdgcn_readlane(token, from + i + u);
+            load_left<N, TR>(rows + t * ld + col, FULL ? N : left, x[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int e = 0; e < N; ++e) acc[e] += x[u][e];
+    }
+    for (; i < n; ++i) {
+        float x[N];
+        const int64_t t = __builtin_amdgcn_readlane(token, from + i);
+        load_left<N, TR>(rows + t * ld + col, FULL ? N : left, x);
+#pragma unroll
+        for (int e = 0; e < N; ++e) acc[e] += x[e];
+    }
+}
+template <class TR, int N>
+__device__ __forceinline__ void add_rows(const EmbedSum &a, const TR *__restrict__ rows, int token,
+                                         int from, int n, int tile, int lane, float (&acc)[N]) {
+    const int col = (tile * kWave + lane) * N;
+    if ((tile + 1) * kWave * N <= a.width) {
+        add_some<true, TR, N>(rows, a.ldo, token, from, n, col, N, acc);
+    } else {  // lanes beyond the row stay: the others read their tokens
+        add_some<false, TR, N>(rows, a.ldo, token, from, n, min(col, a.width), max(a.width - col, 0), acc);
+    }
+}
+
+template <class TG, int N>
+__device__ __forceinline__ void put_sum(const EmbedSum &a, TG *dW, int64_t v, int col,
+                                        float (&acc)[N]) {
+    const int left = a.width - col;
+#pragma unroll
+    for (int e = 0; e < N; ++e) acc[e] *= a.scale;
+    TG *p = dW + v * a.ldw + col;
+    if (a.accumulate) {
+        float old[N];
+        load_left<N, TG>(p, left, old);
+#pragma unroll
+        for (int e = 0; e < N; ++e) acc[e] += old[e];
+    }
+    store_left<N, TG>(p, left, acc);
+}
+
+template <class TR, class TG, int N>
+__global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(EmbedSum a, int64_t row_units,
+                                                                  int64_t units,
+                                                                  const TR *__restrict__ dout,
+                                                                  TG *__restrict__ dW) {
+    const int lane = threadIdx.x % kWave;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    for (int64_t u = (int64_t)blockIdx.x * kEmbedWaves + wave; u < units;
+         u += (int64_t)gridDim.x * kEmbedWaves) {
+        const bool rows = u < row_units;
+        const int64_t item = (rows ? u : u - row_units) / a.tiles;
+        const int tile = (int)((rows ? u : u - row_units) % a.tiles);
+        const int col = (tile * kWave + lane) * N;
+        const int left = a.width - col;
+        if (rows) {  // a word: the item's own, or (accumulate) the one that starts at this place
+            int64_t v = item;
+            if (a.accumulate) {
+                if (item >= a.segptr[a.vocab]) continue;
+                v = a.word[item];
+                if (a.segptr[v] != item) continue;
+            }
+            const int lo = a.segptr[v], n = a.segptr[v + 1] - lo;
+            if (n > kLong) continue;
+            const int token = lane < n ? a.perm[lo + lane] : 0;
+            float acc[N] = {};
+            add_rows<TR, N>(a, dout, token, 0, n, tile, lane, acc);
+            if (left > 0) {
+                if (n == 0) {
+                    store_left<N, TG>(dW + v * a.ldw + col, left, acc);
+                } else {
+                    put_sum<TG, N>(a, dW, v, col, acc);
+                }
+            }
+        } else {  // kLong places
+            const int base = (int)item * kLong, end = min(base + kLong, a.segptr[a.vocab]);
+            if (base >= end) continue;
+            const bool on = base + lane < end;
+            const int token = on ? a.perm[base + lane] : 0;
+            const int w0 = a.word[base], w1 = a.word[end - 1];
+            for (int side = 0; side < (w1 != w0 ? 2 : 1); ++side) {
+                const int w = side ? w1 : w0;
+                const int s0 = a.segptr[w], s1 = a.segptr[w + 1];
+                if (s1 - s0 <= kLong) continue;
+                const int from = max(s0, base) - base, n = min(s1, end) - base - from;
+                float acc[N] = {};
+                add_rows<TR, N>(a, dout, token, from, n, tile, lane, acc);
+                if (left > 0)
+                    store_left<N, float>(a.part + (item * 2 + side) * a.width + col, left, acc);
+            }
+        }
+    }
+}
+
+constexpr int kJoinThreads = 512;
+constexpr int kJoinWaves = kJoinThreads / kWave;
+
+// The long word that starts in chunk blockIdx.x / tiles (there is one at most): the sums of
+// the chunks that it covers, consecutive ones by each wave, the waves' in their order.
+template <class TG, int N>
+__global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(EmbedSum a, TG *__restrict__ dW) {
+    __shared__ float sum[kJoinWaves][kWave * N];
+    const int lane = threadIdx.x % kWave;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int chunk = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles;
+    const int base = chunk * kLong, end = min(base + kLong, a.segptr[a.vocab]);
+    if (base >= end) return;
+    const int w = a.word[end - 1];
+    const int s0 = a.segptr[w], s1 = a.segptr[w + 1];
+    if (s1 - s0 <= kLong || s0 < base) return;
+    const int col = (tile * kWave + lane) * N, left = a.width - col;
+    const int nc = (s1 - 1) / kLong - chunk + 1;  // chunks that the word covers
+    const int per = (nc + kJoinWaves - 1) / kJoinWaves;
+    const int c0 = min(wave * per, nc), c1 = min(c0 + per, nc);
+    float acc[N] = {};
+    constexpr int kAhead = 8;
+    for (int c = c0; c < c1; c += kAhead) {
+        float x[kAhead][N];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int at = chunk + min(c + u, c1 - 1);
+            const int side = at == chunk && s0 > base ? 1 : 0;  // not the word at its first place
+            const int64_t p = (int64_t)at * 2 + side;
+            load_left<N, float>(a.part + p * a.width + min(col, a.width), c + u < c1 ? max(left, 0) : 0,
+                                x[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int e = 0; e < N; ++e) acc[e] += x[u][e];
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) sum[wave][lane * N + e] = acc[e];
+    __syncthreads();
+    if (wave > 0 || left <= 0) return;
+    for (int o = 1; o < kJoinWaves; ++o)
+#pragma unroll
+        for (int e = 0; e < N; ++e) acc[e] += sum[o][lane * N + e];
+    put_sum<TG, N>(a, dW, w, col, acc);
+}
+
+// ------------------------------------------------------------------- host
+
+nsd_status check_embedding(int32_t ntok, const nsd_embedding *s) {
+    NSD_REQUIRE(s != nullptr, "descriptor is NULL");
+    NSD_REQUIRE(ntok >= 0, "negative number of tokens");
+    NSD_REQUIRE(s->vocab >= 0 && s->width >= 1, "a table of %d rows of %d", s->vocab, s->width);
+    NSD_REQUIRE(known_dtype(s->wtype) && known_dtype(s->otype) && known_dtype(s->gtype),
+                "unknown type");
+    NSD_REQUIRE(s->ldw >= s->width && s->ldo >= s->width, "row distances below the width %d",
+                s->width);
+    if (s->vocab == INT32_MAX || ntok > INT32_MAX - 2 * kLong || s->width > INT32_MAX - 1024)
+        return fail(NSD_ERR_TOO_LARGE, "%d tokens, %d words of %d", ntok, s->vocab, s->width);
+    return NSD_OK;
+}
+
+int values_per_lane(int32_t a, int32_t b) { return a == NSD_BF16 && b == NSD_BF16 ? 8 : 4; }
+
+struct EmbedWs {
+    int32_t *perm, *word, *segptr, *key;
+    float *part;
+    void *sort;
+    size_t bytes;
+    EmbedWs(void *ws, int32_t ntok, const nsd_embedding *s) {
+        Carver c(ws);
+        perm = c.take<int32_t>(ntok);
+        word = c.take<int32_t>(ntok);
+        segptr = c.take<int32_t>((size_t)s->vocab + 1);
+        const int64_t nchunks = ntok > kLong ? ceil_div(ntok, kLong) : 0;
+        part = c.take<float>((size_t)nchunks * 2 * s->width);
+        key = nullptr;
+        sort = nullptr;
+        if (!by_looking(ntok, s->vocab)) {
+            key = c.take<int32_t>(ntok);
+            sort = c.take<char>(sort_ws_bytes(ntok, s->vocab + 1));
+        }
+        bytes = std::max<size_t>(c.bytes(), 256);
+    }
+};
+
+// f(row type, gradient or output type, values per lane) by the descriptor's types
+template <class F>
+nsd_status by_types(int32_t a, int32_t b, F f) {
+    if (a == NSD_F32) return b == NSD_F32 ? f(float(), float(), std::integral_constant<int, 4>())
+                                          : f(float(), Bf16(), std::integral_constant<int, 4>());
+    return b == NSD_F32 ? f(Bf16(), float(), std::integral_constant<int, 4>())
+                        : f(Bf16(), Bf16(), std::integral_constant<int, 8>());
+}
+
+}  // namespace
+
+}  // namespace nsd
+
+using namespace nsd;
+
+extern "C" {
+
+nsd_status nsd_embed(int32_t ntok, const nsd_embedding *s, const int32_t *ids, const void *W,
+                     void *out, void *stream) {
+    NSD_TRY(check_embedding(ntok, s));
+    if (ntok == 0) return NSD_OK;
+    NSD_REQUIRE(ids && out && (W || s->vocab == 0), "a NULL array");
+    const int tiles = (int)ceil_div(s->width, kWave * values_per_lane(s->wtype, s->otype));
+    const int64_t units = (int64_t)ntok * tiles;
+    const int64_t blocks = std::min(ceil_div(units, kEmbedWaves), kMaxEmbedBlocks);
+    return by_types(s->wtype, s->otype, [&](auto w, auto o, auto n) -> nsd_status {
+        using TW = decltype(w);
+        using TO = decltype(o);
+        embed_kernel<TW, TO, decltype(n)::value><<<blocks, kEmbedThreads, 0, as_stream(stream)>>>(
+            units, tiles, s->vocab, s->width, s->scale, ids, static_cast<const TW *>(W), s->ldw,
+            static_cast<TO *>(out), s->ldo);
+        return check_launch("embed_kernel");
+    });
+}
+
+nsd_status nsd_embed_vjp_workspace_size(int32_t ntok, const nsd_embedding *s, size_t *bytes) {
+    NSD_REQUIRE(bytes != nullptr, "bytes is NULL");
+    NSD_TRY(check_embedding(ntok, s));
+    *bytes = EmbedWs(nullptr, ntok, s).bytes;
+    return NSD_OK;
+}
+
+nsd_status nsd_embed_vjp(int32_t ntok, const nsd_embedding *s, const int32_t *ids,
+                         const void *dout, int32_t accumulate, void *dW, void *ws,
+                         size_t ws_bytes, void *stream) {
+    NSD_TRY(check_embedding(ntok, s));
+    if (s->vocab == 0 || (accumulate && ntok == 0)) return NSD_OK;
+    NSD_REQUIRE(dW && (ntok == 0 || (ids && dout)), "a NULL array");
+    const EmbedWs w(ws, ntok, s);
+    if (ws == nullptr || ws_bytes < w.bytes)
+        return fail(NSD_ERR_WORKSPACE, "workspace %zu bytes at %p, need %zu", ws_bytes, ws, w.bytes);
+    NSD_REQUIRE((reinterpret_cast<uintptr_t>(ws) & 255) == 0, "workspace is not 256-byte aligned");
+    const hipStream_t st = as_stream(stream);
+    if (w.key == nullptr) {
+        embed_order_kernel<<<ceil_div(s->vocab, kOrderWords), kOrderThreads, 0, st>>>(
+            ntok, s->vocab, ids, w.perm, w.word, w.segptr);
+        NSD_TRY(check_launch("embed_order_kernel"));
+    } else {
+        embed_keys_kernel<<<ceil_div(ntok, kEmbedThreads), kEmbedThreads, 0, st>>>(ntok, s->vocab, ids,
+                                                                                  w.key);
+        NSD_TRY(check_launch("embed_keys_kernel"));
+        NSD_TRY(radix_sort_pairs(ntok, s->vocab + 1, w.key, nullptr, w.word, w.perm, w.sort, st));
+        NSD_TRY(segptr_from_sorted(ntok, s->vocab, w.word, w.segptr, st));
+    }
+    EmbedSum a;
+    a.ntok = ntok;
+    a.vocab = s->vocab;
+    a.width = s->width;
+    a.tiles = (int)ceil_div(s->width, kWave * values_per_lane(s->otype, s->gtype));
+    a.nchunks = ntok > kLong ? (int)ceil_div(ntok, kLong) : 0;
+    a.accumulate = accumulate != 0;
+    a.scale = s->scale;
+    a.perm = w.perm;
+    a.word = w.word;
+    a.segptr = w.segptr;
+    a.ldw = s->ldw;
+    a.ldo = s->ldo;
+    a.part = w.part;
+    const int64_t row_units = (int64_t)(accumulate ? ntok : s->vocab) * a.tiles;
+    const int64_t units = row_units + (int64_t)a.nchunks * a.tiles;
+    const int64_t blocks = std::min(ceil_div(units, kEmbedWaves), kMaxEmbedBlocks);
+    return by_types(s->otype, s->gtype, [&](auto r, auto g, auto n) -> nsd_status {
+        using TR = decltype(r);
+        using TG = decltype(g);
+        constexpr int N = decltype(n)::value;
+        embed_sum_kernel<TR, TG, N><<<blocks, kEmbedThreads, 0, st>>>(
+            a, row_units, units, static_cast<const TR *>(dout), static_cast<TG *>(dW));
+        NSD_TRY(check_launch("embed_sum_kernel"));
+        if (a.nchunks == 0) return NSD_OK;
+        const int64_t joins = (int64_t)a.nchunks * a.tiles;
+        if (joins > UINT32_MAX / kJoinThreads)
+            return fail(NSD_ERR_TOO_LARGE, "%lld sums of long words", (long long)joins);
+        embed_join_kernel<TG, N><<<joins, kJoinThreads, 0, st>>>(a, static_cast<TG *>(dW));
+        return check_launch("embed_join_kernel");
+    });
+}
+
+}  // extern "C"

@@ -131,6 +131,32 @@ class nsd_adamw(C.Structure):
                 ("lr_dev", C.c_void_p), ("grad_scale", C.c_void_p)]
 
 
+class nsd_grad_tensor(C.Structure):
+    _fields_ = [("n", C.c_int64), ("grad", C.c_void_p), ("dtype", C.c_int32)]
+
+
+class nsd_grad_plan(C.Structure):
+    _fields_ = [("ntensors", C.c_int32), ("nchunks", C.c_int32), ("shared", C.c_int32),
+                ("table", C.c_void_p)]
+
+
+class nsd_clip(C.Structure):
+    _fields_ = [("max_norm", C.c_double), ("order", C.c_int32), ("grad_scale", C.c_void_p)]
+
+
+class nsd_embedding(C.Structure):
+    _fields_ = [("vocab", C.c_int32), ("width", C.c_int32), ("wtype", C.c_int32),
+                ("otype", C.c_int32), ("gtype", C.c_int32), ("scale", C.c_float),
+                ("ldw", C.c_int64), ("ldo", C.c_int64)]
+
+
+class nsd_qk(C.Structure):
+    _fields_ = [("heads", C.c_int32), ("kv_heads", C.c_int32), ("d", C.c_int32),
+                ("rot", C.c_int32), ("dtype", C.c_int32), ("interleaved", C.c_int32),
+                ("norm", C.c_int32), ("eps", C.c_float), ("ldq", C.c_int64), ("ldk", C.c_int64),
+                ("ldqo", C.c_int64), ("ldko", C.c_int64)]
+
+
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"libnsd.so is not built ({LIB_PATH}); run "
                       "`python -m paper_2303_07030_amd.build` first")
@@ -236,6 +262,21 @@ _SIGS = {
     "nsd_adamw_plan_build": (C.c_int, [_I, C.POINTER(nsd_adamw_tensor), _I,
                                        C.POINTER(nsd_adamw_plan), _P, _SZ, _P]),
     "nsd_adamw_step": (C.c_int, [C.POINTER(nsd_adamw_plan), C.POINTER(nsd_adamw), _P]),
+    "nsd_grad_plan_size": (C.c_int, [_I, C.POINTER(nsd_grad_tensor), C.POINTER(_SZ)]),
+    "nsd_grad_plan_build": (C.c_int, [_I, C.POINTER(nsd_grad_tensor), C.POINTER(nsd_grad_plan),
+                                      _P, _SZ, _P]),
+    "nsd_grad_norm_workspace_size": (C.c_int, [C.POINTER(nsd_grad_plan), C.POINTER(_SZ)]),
+    "nsd_grad_norm": (C.c_int, [C.POINTER(nsd_grad_plan), C.POINTER(nsd_clip), _P, _P, _P, _P,
+                                _SZ, _P]),
+    "nsd_grad_clip": (C.c_int, [C.POINTER(nsd_grad_plan), _P, _P]),
+    "nsd_embed": (C.c_int, [_I, C.POINTER(nsd_embedding), _P, _P, _P, _P]),
+    "nsd_embed_vjp_workspace_size": (C.c_int, [_I, C.POINTER(nsd_embedding), C.POINTER(_SZ)]),
+    "nsd_embed_vjp": (C.c_int, [_I, C.POINTER(nsd_embedding), _P, _P, _I, _P, _P, _SZ, _P]),
+    "nsd_qk_rotate": (C.c_int, [_I, C.POINTER(nsd_qk), _P, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "nsd_qk_rotate_vjp_workspace_size": (C.c_int, [_I, C.POINTER(nsd_qk), C.POINTER(_SZ)]),
+    "nsd_qk_rotate_vjp": (C.c_int, [_I, C.POINTER(nsd_qk)] + [_P] * 13 + [_SZ, _P]),
+    "nsd_qk_append": (C.c_int, [_I, C.POINTER(nsd_qk), _P, _P, _P, _I, C.c_int64, C.c_int64, _P,
+                                _P, _P, _P, _P, _I, _P, _P, _P, _P]),
     "nsd_loss_cp": (C.c_int, [_COO3, _P, _P, _P, _I, C.c_float, _P, _P, _P, _P, _P, _P, _SZ,
                               _P]),
 }
@@ -835,3 +876,173 @@ def nsd_adamw_plan_build(tensors, state_bits, table, stream=None) -> nsd_adamw_p
 
 def nsd_adamw_step(plan: nsd_adamw_plan, h: nsd_adamw, stream=None):
     _check(_lib.nsd_adamw_step(C.byref(plan), C.byref(h), _stream(stream)), "nsd_adamw_step")
+
+
+def nsd_grad_plan_size(tensors) -> int:
+    """tensors: a list of nsd_grad_tensor."""
+    b = _SZ(0)
+    _check(_lib.nsd_grad_plan_size(len(tensors), (nsd_grad_tensor * len(tensors))(*tensors),
+                                   C.byref(b)), "nsd_grad_plan_size")
+    return b.value
+
+
+def nsd_grad_plan_build(tensors, table, stream=None) -> nsd_grad_plan:
+    plan = nsd_grad_plan()
+    _check(_lib.nsd_grad_plan_build(len(tensors), (nsd_grad_tensor * len(tensors))(*tensors),
+                                    C.byref(plan), _p(table), _nbytes(table), _stream(stream)),
+           "nsd_grad_plan_build")
+    plan._keep = table
+    return plan
+
+
+def nsd_grad_norm_workspace_size(plan: nsd_grad_plan) -> int:
+    b = _SZ(0)
+    _check(_lib.nsd_grad_norm_workspace_size(C.byref(plan), C.byref(b)),
+           "nsd_grad_norm_workspace_size")
+    return b.value
+
+
+def nsd_grad_norm(plan: nsd_grad_plan, h: nsd_clip, norm, scale, norms, ws, stream=None):
+    _dense(norm, "norm", 1, torch.float64)
+    _dense(scale, "scale", 1, torch.float32)
+    _dense(norms, "norms", plan.ntensors, torch.float64)
+    _check(_lib.nsd_grad_norm(C.byref(plan), C.byref(h), _p(norm), _p(scale), _p(norms), _p(ws),
+                              _nbytes(ws), _stream(stream)), "nsd_grad_norm")
+
+
+def nsd_grad_clip(plan: nsd_grad_plan, scale, stream=None):
+    _dense(scale, "scale", 1, torch.float32)
+    _check(_lib.nsd_grad_clip(C.byref(plan), _p(scale), _stream(stream)), "nsd_grad_clip")
+
+
+def _type_of(dtype: int):
+    return torch.bfloat16 if dtype == BF16 else torch.float32
+
+
+def _row_distance(t, width, name):
+    """Values from one row of a matrix of `width` columns to the next."""
+    if t.dim() != 2 or t.shape[1] != width or (width > 1 and t.numel() and t.stride(1) != 1):
+        raise ValueError(f"{name}: {tuple(t.shape)}, strides {t.stride()}, are not rows of "
+                         f"{width} values")
+    return t.stride(0) if t.shape[0] > 1 else width
+
+
+def embed_desc(W, out, scale=1.0, grad=None) -> nsd_embedding:
+    """A table W [vocab, width] and rows out [ntok, width]: their types and row
+    distances are taken.  grad: the table's gradient (its type; its row distance
+    is W's), or an nsd_dtype; without it W's type."""
+    if W.dim() != 2:
+        raise ValueError(f"table: {tuple(W.shape)} are not rows")
+    width = W.shape[1]
+    s = nsd_embedding(W.shape[0], width, dtype_of(W), dtype_of(out),
+                      dtype_of(W if grad is None else grad), scale,
+                      _row_distance(W, width, "table"), _row_distance(out, width, "rows"))
+    if isinstance(grad, torch.Tensor):
+        _rows(grad, "gradient", s.vocab, width, s.ldw, _type_of(s.gtype))
+    return s
+
+
+def nsd_embed(ntok, s: nsd_embedding, ids, W, out, stream=None):
+    _dense(ids, "ids", ntok, torch.int32)
+    _rows(W, "W", s.vocab, s.width, s.ldw, _type_of(s.wtype))
+    _rows(out, "out", ntok, s.width, s.ldo, _type_of(s.otype))
+    _check(_lib.nsd_embed(ntok, C.byref(s), _p(ids), _p(W), _p(out), _stream(stream)),
+           "nsd_embed")
+
+
+def nsd_embed_vjp_workspace_size(ntok: int, s: nsd_embedding) -> int:
+    b = _SZ(0)
+    _check(_lib.nsd_embed_vjp_workspace_size(ntok, C.byref(s), C.byref(b)),
+           "nsd_embed_vjp_workspace_size")
+    return b.value
+
+
+def nsd_embed_vjp(ntok, s: nsd_embedding, ids, dout, accumulate, dW, ws, stream=None):
+    _dense(ids, "ids", ntok, torch.int32)
+    _rows(dout, "dout", ntok, s.width, s.ldo, _type_of(s.otype))
+    _rows(dW, "dW", s.vocab, s.width, s.ldw, _type_of(s.gtype))
+    _check(_lib.nsd_embed_vjp(ntok, C.byref(s), _p(ids), _p(dout), int(bool(accumulate)), _p(dW),
+                              _p(ws), _nbytes(ws), _stream(stream)), "nsd_embed_vjp")
+
+
+def qk_desc(heads, kv_heads, d, q, k, qo, ko, rot=None, interleaved=False, norm=True,
+            eps=1e-6) -> nsd_qk:
+    """The shape of a norm and rotation of q [ntok, heads * d] and k [ntok,
+    kv_heads * d] to qo and ko (rows of the same widths, ko of a cache's as well):
+    their type and row distances are taken.  kv_heads = 0: k and ko are None.
+    rot: the values of a head that are rotated, all by default."""
+    lds = []
+    for t, n, name in ((q, heads, "q"), (k, kv_heads, "k"), (qo, heads, "qo"),
+                       (ko, kv_heads, "ko")):
+        if t is None and n == 0:
+            lds.append(0)
+            continue
+        if t.dtype != q.dtype:
+            raise ValueError(f"{name}: {t.dtype} beside {q.dtype}")
+        lds.append(_row_distance(t, n * d, name))
+    return nsd_qk(heads, kv_heads, d, d // 2 * 2 if rot is None else rot, dtype_of(q),
+                  int(bool(interleaved)), int(bool(norm)), eps, *lds)
+
+
+def _qk_rows(ntok, s, rows, T):
+    """rows: (tensor, name, heads, row distance) of each matrix."""
+    for t, name, heads, ld in rows:
+        _rows(t, name, ntok, heads * s.d, ld, T)
+
+
+def _qk_small(ntok, s, wq, wk, pos, freq):
+    _dense(wq, "wq", s.d, torch.float32)
+    _dense(wk, "wk", s.d, torch.float32)
+    _dense(pos, "pos", ntok, torch.int32)
+    _dense(freq, "freq", s.rot // 2, torch.float64)
+
+
+def nsd_qk_rotate(ntok, s: nsd_qk, Q, K, wq, wk, pos, freq, Qo, Ko, stream=None):
+    _qk_rows(ntok, s, ((Q, "Q", s.heads, s.ldq), (K, "K", s.kv_heads, s.ldk),
+                       (Qo, "Qo", s.heads, s.ldqo), (Ko, "Ko", s.kv_heads, s.ldko)),
+             _type_of(s.dtype))
+    _qk_small(ntok, s, wq, wk, pos, freq)
+    _check(_lib.nsd_qk_rotate(ntok, C.byref(s), _p(Q), _p(K), _p(wq), _p(wk), _p(pos), _p(freq),
+                              _p(Qo), _p(Ko), _stream(stream)), "nsd_qk_rotate")
+
+
+def nsd_qk_rotate_vjp_workspace_size(ntok: int, s: nsd_qk) -> int:
+    b = _SZ(0)
+    _check(_lib.nsd_qk_rotate_vjp_workspace_size(ntok, C.byref(s), C.byref(b)),
+           "nsd_qk_rotate_vjp_workspace_size")
+    return b.value
+
+
+def nsd_qk_rotate_vjp(ntok, s: nsd_qk, Q, K, wq, wk, pos, freq, dQo, dKo, dQ, dK, dwq, dwk, ws,
+                      stream=None):
+    _qk_rows(ntok, s, ((Q, "Q", s.heads, s.ldq), (K, "K", s.kv_heads, s.ldk),
+                       (dQo, "dQo", s.heads, s.ldqo), (dKo, "dKo", s.kv_heads, s.ldko),
+                       (dQ, "dQ", s.heads, s.ldq), (dK, "dK", s.kv_heads, s.ldk)),
+             _type_of(s.dtype))
+    _qk_small(ntok, s, wq, wk, pos, freq)
+    _dense(dwq, "dwq", s.d, torch.float32)
+    _dense(dwk, "dwk", s.d, torch.float32)
+    _check(_lib.nsd_qk_rotate_vjp(ntok, C.byref(s), _p(Q), _p(K), _p(wq), _p(wk), _p(pos),
+                                  _p(freq), _p(dQo), _p(dKo), _p(dQ), _p(dK), _p(dwq), _p(dwk),
+                                  _p(ws), _nbytes(ws), _stream(stream)), "nsd_qk_rotate_vjp")
+
+
+def nsd_qk_append(ntok, s: nsd_qk, Q, K, V, wq, wk, pos, freq, slot, nslots, Qo, Kc, Vc,
+                  stream=None):
+    """V [ntok, any width] and Vc [nslots, the same]: their row distances are taken
+    (None: no values)."""
+    T = _type_of(s.dtype)
+    _qk_rows(ntok, s, ((Q, "Q", s.heads, s.ldq), (K, "K", s.kv_heads, s.ldk),
+                       (Qo, "Qo", s.heads, s.ldqo)), T)
+    _rows(Kc, "Kc", nslots, s.kv_heads * s.d, s.ldko, T)
+    _qk_small(ntok, s, wq, wk, pos, freq)
+    _dense(slot, "slot", ntok, torch.int32)
+    vwidth, ldv, ldvo = 0, 0, 0
+    if V is not None:
+        vwidth = V.shape[-1]
+        ldv, ldvo = _row_distance(V, vwidth, "V"), _row_distance(Vc, vwidth, "Vc")
+        _rows(V, "V", ntok, vwidth, ldv, T)
+        _rows(Vc, "Vc", nslots, vwidth, ldvo, T)
+    _check(_lib.nsd_qk_append(ntok, C.byref(s), _p(Q), _p(K), _p(V), vwidth, ldv, ldvo, _p(wq),
+                              _p(wk), _p(pos), _p(freq), _p(slot), nslots, _p(Qo), _p(Kc), _p(Vc),
+                              _stream(stream)), "nsd_qk_append")

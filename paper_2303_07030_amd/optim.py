@@ -1,11 +1,15 @@
-"""The optimizer's side of a training step: AdamW over a model's tensors.
+"""The optimizer's side of a training step: the norm of all gradients, and AdamW
+over a model's tensors.
 
-An AdamW holds the states of a list of device tensors and the plan by which
-one launch updates all of them (nsd_adamw_step).  It reads gradients where the
-gradient calls write them: the `grads` given at construction are caller
-buffers that are overwritten step by step.
+Both read gradients where the gradient calls write them: the `grads` given at
+construction are caller buffers that are overwritten step by step.  A GradNorm
+measures them (nsd_grad_norm) and holds the factor that clips them; an AdamW
+holds the states of a list of device tensors and the plan by which one launch
+updates all of them (nsd_adamw_step).
 """
 from __future__ import annotations
+
+import math
 
 import torch
 
@@ -24,6 +28,43 @@ def _flat(t, what, device, n=None, dtypes=None):
     return t
 
 
+class GradNorm:
+    """The norm of a list of fp32 or bf16 gradients and the factor that clips it to
+    max_norm.  order: 2, or math.inf for the largest magnitude.  measure() leaves
+    on the device `norm` (fp64, one value), `norms` (fp64, one for each tensor) and
+    `scale` (fp32, one value): what AdamW.step takes as grad_scale, or what clip()
+    multiplies the gradients by."""
+
+    def __init__(self, grads, max_norm=math.inf, order=2, stream=None):
+        if order not in (2, math.inf):
+            raise ValueError(f"norm of order {order} (2 or math.inf)")
+        self.grads = list(grads)
+        dev = self.grads[0].device if self.grads else torch.device("cuda")
+        for i, g in enumerate(self.grads):
+            _flat(g, f"gradient {i}", dev, dtypes=(torch.float32, torch.bfloat16))
+        records = [nsd.nsd_grad_tensor(g.numel(), g.data_ptr(), nsd.dtype_of(g))
+                   for g in self.grads]
+        table = torch.empty(nsd.nsd_grad_plan_size(records), dtype=torch.uint8, device=dev)
+        self.plan = nsd.nsd_grad_plan_build(records, table, stream)
+        self.max_norm, self.order = max_norm, order
+        self.norm = torch.zeros(1, dtype=torch.float64, device=dev)
+        self.norms = torch.zeros(len(records), dtype=torch.float64, device=dev)
+        self.scale = torch.ones(1, device=dev)
+        self.ws = torch.empty(nsd.nsd_grad_norm_workspace_size(self.plan), dtype=torch.uint8,
+                              device=dev)
+
+    def measure(self, grad_scale=None, stream=None):
+        """The norms of grad_scale (a device fp32 scalar, or None) times the gradients;
+        `scale` holds grad_scale as a factor."""
+        h = nsd.nsd_clip(self.max_norm, 2 if self.order == 2 else 0,
+                         None if grad_scale is None else grad_scale.data_ptr())
+        nsd.nsd_grad_norm(self.plan, h, self.norm, self.scale, self.norms, self.ws, stream)
+
+    def clip(self, stream=None):
+        """Every gradient times `scale`, in place."""
+        nsd.nsd_grad_clip(self.plan, self.scale, stream)
+
+
 class AdamW:
     """params: fp32 or bf16 tensors, updated in place; grads: as many, fp32 or
     bf16.  masters: the fp32 copies of bf16 weights (a list that may hold None),
@@ -31,11 +72,13 @@ class AdamW:
     states in 8-bit floats with a scale per nsd.ADAMW_BLOCK values.
     weight_decay: one number, or one per tensor.  m, v, m_scale, v_scale and
     step continue a run: its state tensors (updated in place) and the number
-    of steps done; without them the states start at zero."""
+    of steps done; without them the states start at zero.  max_norm: every step
+    measures the gradients first (`grad_norm`, a GradNorm) and clips what it takes
+    of them; the gradients themselves stay."""
 
     def __init__(self, params, grads, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8,
                  weight_decay=0.01, state_bits=32, masters=None, m=None, v=None, m_scale=None,
-                 v_scale=None, step=0, stream=None):
+                 v_scale=None, step=0, stream=None, max_norm=None):
         self.params, self.grads = list(params), list(grads)
         count = len(self.params)
         if state_bits not in (8, 32):
@@ -86,6 +129,8 @@ class AdamW:
         table = torch.empty(nsd.nsd_adamw_plan_size(self.records), dtype=torch.uint8,
                             device=self.params[0].device if count else "cuda")
         self.plan = nsd.nsd_adamw_plan_build(self.records, state_bits, table, stream)
+        self.grad_norm = None if max_norm is None else GradNorm(self.grads, max_norm,
+                                                                stream=stream)
         self.t = step
         self.hyper = nsd.nsd_adamw(lr, beta1, beta2, eps, step, None, None, None)
 
@@ -96,6 +141,9 @@ class AdamW:
         them a captured graph counts its replays.  The count is then the caller's:
         `t`, the steps done, is not advanced, and has to be set before steps
         without step_dev or a checkpoint of it.  A refused step changes nothing."""
+        if self.grad_norm is not None:
+            self.grad_norm.measure(grad_scale, stream)
+            grad_scale = self.grad_norm.scale
         last = self.hyper
         t = self.t + 1 if step_dev is None else self.t
         h = nsd.nsd_adamw(last.lr if lr is None else lr, last.beta1, last.beta2, last.eps, t,

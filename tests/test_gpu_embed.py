@@ -1,0 +1,267 @@
+"""Token rows and the table's gradient: against sums in 64 bits, for words without
+a token and with most of them, padding, rows that are parts of wider ones, the
+sums added to what a tied head left, and the refusals.
+
+Tolerances: a product in 32 bits is off by 2^-24 of itself, a sum of n terms in any
+order by n 2^-24 of its terms' magnitudes, and a value rounded to its type by half a
+step of it.
+"""
+import numpy as np
+import pytest
+import torch
+
+from paper_2303_07030_amd import nsd
+
+P = 0x1000
+T = {"f32": torch.float32, "bf16": torch.bfloat16}
+HALF = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
+
+
+# ------------------------------------------------------------- refusals
+
+def desc(**change):
+    return nsd.nsd_embedding(**{**dict(vocab=10, width=8, wtype=0, otype=0, gtype=0, scale=1.0,
+                                       ldw=8, ldo=8), **change})
+
+
+@pytest.mark.parametrize("change, status", [
+    (dict(vocab=-1), nsd.NSD_ERR_INVALID_ARG), (dict(width=0), nsd.NSD_ERR_INVALID_ARG),
+    (dict(wtype=2), nsd.NSD_ERR_INVALID_ARG), (dict(otype=-1), nsd.NSD_ERR_INVALID_ARG),
+    (dict(gtype=9), nsd.NSD_ERR_INVALID_ARG), (dict(ldw=7), nsd.NSD_ERR_INVALID_ARG),
+    (dict(ldo=7), nsd.NSD_ERR_INVALID_ARG), (dict(vocab=2 ** 31 - 1), nsd.NSD_ERR_TOO_LARGE)])
+def test_bad_descriptors_are_refused(change, status):
+    s = desc(**change)
+    for call in (lambda: nsd.nsd_embed(4, s, P, P, P),
+                 lambda: nsd.nsd_embed_vjp_workspace_size(4, s),
+                 lambda: nsd.nsd_embed_vjp(4, s, P, P, False, P, None)):
+        with pytest.raises(nsd.NsdError) as e:
+            call()
+        assert e.value.status == status
+
+
+def test_bad_arguments_are_refused():
+    s = desc()
+    for call in (lambda: nsd.nsd_embed(-1, s, P, P, P), lambda: nsd.nsd_embed(4, s, None, P, P),
+                 lambda: nsd.nsd_embed(4, s, P, None, P), lambda: nsd.nsd_embed(4, s, P, P, None),
+                 lambda: nsd.nsd_embed_vjp(4, s, None, P, False, P, None),
+                 lambda: nsd.nsd_embed_vjp(4, s, P, None, False, P, None),
+                 lambda: nsd.nsd_embed_vjp(4, s, P, P, False, None, None)):
+        with pytest.raises(nsd.NsdError) as e:
+            call()
+        assert e.value.status == nsd.NSD_ERR_INVALID_ARG
+    with pytest.raises(nsd.NsdError) as e:
+        nsd.nsd_embed_vjp(4, s, P, P, False, P, None)
+    assert e.value.status == nsd.NSD_ERR_WORKSPACE
+    nsd.nsd_embed(0, s, None, None, None)  # nothing to do
+    nsd.nsd_embed_vjp(0, s, None, None, True, None, None)
+
+
+def test_tensors_of_other_shapes_are_refused():
+    W, out = torch.zeros(10, 8), torch.zeros(4, 8)
+    s = nsd.embed_desc(W, out)
+    ids = torch.zeros(4, dtype=torch.int32)
+    for args, name in (((4, s, ids.long(), W, out), "ids"), ((5, s, ids, W, out), "ids"),
+                       ((4, s, ids, W[:9], out), "W"), ((4, s, ids, W, out.bfloat16()), "out"),
+                       ((4, s, ids, W, torch.zeros(4, 16)[:, ::2]), "out")):
+        with pytest.raises(ValueError, match=name):
+            nsd.nsd_embed(*args)
+    for args, name in (((ids, torch.zeros(4, 9)[:, :8], False, W), "dout"),
+                       ((ids, out, False, torch.zeros(10, 9)[:, :8]), "dW")):
+        with pytest.raises(ValueError, match=name):
+            nsd.nsd_embed_vjp(4, s, *args, None)
+    with pytest.raises(ValueError, match="table"):
+        nsd.embed_desc(torch.zeros(8, 10).t(), out)
+    with pytest.raises(ValueError, match="gradient"):
+        nsd.embed_desc(W, out, grad=torch.zeros(10, 9)[:, :8])
+
+
+def test_a_workspace_serves_smaller_batches():
+    for V in (1, 300, 50_000, 2_000_000):
+        s = desc(vocab=V, width=24, ldw=24, ldo=24)
+        sizes = [nsd.nsd_embed_vjp_workspace_size(n, s)
+                 for n in (0, 1, 64, 65, 4000, 2 ** 17 - 1, 2 ** 17, 2 ** 17 + 1, 300_000)]
+        assert sizes == sorted(sizes)
+
+
+# ------------------------------------------------------------- on the GPU
+
+def words(rng, n, V, hot):
+    """Ids with every kind of padding; `hot` of them one word."""
+    ids = rng.integers(0, V, n)
+    ids[rng.random(n) < hot] = V // 2
+    bad = rng.random(n) < 0.07
+    ids[bad] = rng.choice([-1, V, -2 ** 31, 2 ** 31 - 1], bad.sum())
+    return ids.astype(np.int32)
+
+
+def run(ids, V, w, scale, tw, to, tg, add, gap=0, seed=0):
+    """Both calls on seeded data, the rows `gap` values apart, with what lies between
+    and behind them checked: (W, dout, old dW, out, dW)."""
+    g = torch.Generator().manual_seed(seed)
+    n = len(ids)
+
+    def rows(m, dtype):
+        return torch.randn(m + 2, w + gap, generator=g).to(dtype).cuda()
+
+    W, out, dout, dW = rows(V, T[tw]), rows(n, T[to]), rows(n, T[to]), rows(V, T[tg])
+    before = out.clone(), dW.clone()
+    old = dW[:V, :w].double().cpu().numpy()
+    s = nsd.embed_desc(W[:V, :w], out[:n, :w], scale, grad=dW[:V, :w])
+    s.ldw, s.ldo = w + gap, w + gap  # (a single row has no distance)
+    idd = torch.from_numpy(ids).cuda()
+    nsd.nsd_embed(n, s, idd, W.view(-1)[: V * (w + gap)].view(V, w + gap)[:, :w], out[:n, :w])
+    ws = torch.empty(nsd.nsd_embed_vjp_workspace_size(n, s), dtype=torch.uint8, device="cuda")
+    ws.fill_(0x7F)
+    nsd.nsd_embed_vjp(n, s, idd, dout[:n, :w], add, dW[:V, :w], ws)
+    for t, b, m in ((out, before[0], n), (dW, before[1], V)):
+        assert torch.equal(t[m:], b[m:]) and torch.equal(t[:, w:], b[:, w:])
+    if n:
+        again = before[1].clone()
+        nsd.nsd_embed_vjp(n, s, idd, dout[:n, :w], add, again[:V, :w], ws)
+        assert torch.equal(again.view(torch.uint8), dW.view(torch.uint8))  # bit for bit
+    f64 = [t.double().cpu().numpy() for t in (W[:V, :w], dout[:n, :w], out[:n, :w], dW[:V, :w])]
+    return f64[0], f64[1], old, f64[2], f64[3]
+
+
+def check(ids, V, w, scale, tw, to, tg, add, **kw):
+    W, dout, old, out, dW = run(ids, V, w, scale, tw, to, tg, add, **kw)
+    scale = float(np.float32(scale))
+    on = (ids >= 0) & (ids < V)
+    ref = np.zeros_like(out)
+    ref[on] = W[ids[on]] * scale
+    assert np.all(np.abs(out - ref) <= (2.0 ** -23 + HALF[to]) * np.abs(ref))
+    ref, mag = np.zeros((V, w)), np.zeros((V, w))
+    np.add.at(ref, ids[on], dout[on] * scale)
+    np.add.at(mag, ids[on], np.abs(dout[on] * scale))
+    n = np.bincount(ids[on], minlength=V)[:, None]
+    if add:
+        ref, mag = ref + old, mag + np.abs(old)
+        assert np.array_equal(dW[n[:, 0] == 0], old[n[:, 0] == 0])
+    else:
+        assert np.all(dW[n[:, 0] == 0] == 0)
+    assert np.all(np.abs(dW - ref) <= (n + 3) * 2.0 ** -24 * mag + HALF[tg] * np.abs(ref))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [0, 1, 2, 63, 64, 65, 129, 1000, 5000])
+@pytest.mark.parametrize("V", [1, 5, 255, 256, 257, 3000])
+def test_tokens_and_words(n, V):
+    rng = np.random.default_rng(n * 7 + V)
+    check(words(rng, n, V, 0.3), V, 24, 1.5, "f32", "f32", "f32", bool(n % 2))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("w", [1, 3, 8, 255, 256, 257, 333, 512, 520, 1030])
+@pytest.mark.parametrize("types", [("f32", "f32", "f32"), ("bf16", "bf16", "bf16"),
+                                   ("bf16", "bf16", "f32"), ("f32", "bf16", "bf16"),
+                                   ("bf16", "f32", "bf16")])
+@pytest.mark.parametrize("add", [False, True])
+def test_widths_and_types(w, types, add):
+    rng = np.random.default_rng(w)
+    check(words(rng, 700, 90, 0.4), 90, w, w ** 0.5, *types, add, gap=(w * 7) % 5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n, V, hot", [(140_000, 600, 0.0), (140_000, 3, 0.9),
+                                       (131_072, 70_000, 0.1), (131_072, 256, 0.0),
+                                       (70_000, 2_000_000, 0.05)])
+def test_many_tokens(n, V, hot):
+    """Either way to the order by word, words of thousands of tokens."""
+    rng = np.random.default_rng(n + V)
+    check(words(rng, n, V, hot), V, 4, 0.5, "bf16", "bf16", "f32", True)
+
+
+@pytest.mark.gpu
+def test_one_word_alone():
+    ids = np.full(20_001, 7, np.int32)
+    check(ids, 9, 70, 1.0, "f32", "f32", "f32", False)
+    check(ids, 1, 70, 1.0, "f32", "f32", "f32", True)  # every id is padding
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lead", [0, 1, 63])
+def test_long_words_at_every_place(lead):
+    """Words of 63 to 66 and of 128 to 130 tokens, whose sums start and end at the
+    borders of what one wave takes."""
+    ids = np.concatenate([np.zeros(lead, np.int32)] +
+                         [np.full(m, i + 1, np.int32)
+                          for i, m in enumerate([64, 65, 63, 128, 66, 1, 129, 64, 130, 62])])
+    rng = np.random.default_rng(lead)
+    rng.shuffle(ids)
+    check(ids, 12, 40, 1.0, "f32", "f32", "f32", False)
+
+
+@pytest.mark.gpu
+def test_rows_without_a_number_are_their_words_alone():
+    """NaN and infinite rows of padding and of other words stay where they are."""
+    V, w, n = 50, 16, 400
+    rng = np.random.default_rng(0)
+    ids = rng.integers(0, V, n).astype(np.int32)
+    ids[::9] = -1
+    W = torch.randn(V, w)
+    W[3], W[4] = float("nan"), float("inf")
+    dout = torch.randn(n, w)
+    dout[::9] = float("nan")
+    first = int(np.nonzero(ids == 11)[0][0])
+    dout[first] = float("inf")
+    out, dW = torch.empty(n, w).cuda(), torch.empty(V, w).cuda()
+    W, dout, idd = W.cuda(), dout.cuda(), torch.from_numpy(ids).cuda()
+    s = nsd.embed_desc(W, out, float("inf"), grad=dW)
+    nsd.nsd_embed(n, s, idd, W, out)
+    assert torch.all(out[::9] == 0)
+    s.scale = 1.0
+    ws = torch.empty(nsd.nsd_embed_vjp_workspace_size(n, s), dtype=torch.uint8, device="cuda")
+    nsd.nsd_embed_vjp(n, s, idd, dout, False, dW, ws)
+    bad = torch.isinf(dW).all(1)
+    assert bad.nonzero().view(-1).tolist() == [11] and torch.isfinite(dW[~bad]).all()
+
+
+@pytest.mark.gpu
+def test_a_table_past_32_bit_offsets():
+    """The last rows of a table of more than 2^32 bytes."""
+    V, w = 2_200_000, 1024
+    W = torch.empty(V, w, dtype=torch.bfloat16, device="cuda")
+    W[-3:] = torch.randn(3, w).cuda()
+    ids = torch.tensor([V - 1, V - 3, V - 1, V - 2], dtype=torch.int32, device="cuda")
+    out = torch.empty(4, w, dtype=torch.bfloat16, device="cuda")
+    s = nsd.embed_desc(W, out)
+    nsd.nsd_embed(4, s, ids, W, out)
+    assert torch.equal(out, W[ids.long()])
+    dout = torch.randn(4, w, device="cuda").bfloat16()
+    kept = W[:10].clone()
+    before = W[-3:].float()
+    ws = torch.empty(nsd.nsd_embed_vjp_workspace_size(4, s), dtype=torch.uint8, device="cuda")
+    nsd.nsd_embed_vjp(4, s, ids, dout, True, W, ws)
+    d = dout.float()
+    want = before + torch.stack([d[1], d[3], d[0] + d[2]])
+    assert (W[-3:].float() - want).abs().max() <= 2.0 ** -8 * want.abs().max() + 1e-5
+    assert torch.equal(W[:10].view(torch.int16), kept.view(torch.int16))
+
+
+@pytest.mark.gpu
+def test_a_captured_step_follows_the_ids():
+    V, w, n = 3000, 200, 6000
+    rng = np.random.default_rng(1)
+    W, dout = torch.randn(V, w, device="cuda"), torch.randn(n, w, device="cuda")
+    out, dW = torch.empty(n, w, device="cuda"), torch.empty(V, w, device="cuda")
+    ids = torch.from_numpy(words(rng, n, V, 0.2)).cuda()
+    s = nsd.embed_desc(W, out, 2.0, grad=dW)
+    ws = torch.empty(nsd.nsd_embed_vjp_workspace_size(n, s), dtype=torch.uint8, device="cuda")
+
+    def step():
+        nsd.nsd_embed(n, s, ids, W, out)
+        nsd.nsd_embed_vjp(n, s, ids, dout, False, dW, ws)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        ids.copy_(torch.from_numpy(words(rng, n, V, 0.2)))
+        step()
+        want = out.clone(), dW.clone()
+        out.fill_(7), dW.fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(dW, want[1])

@@ -1,0 +1,366 @@
+"""Norm and rotation of queries and keys, their gradient, and the serving form:
+against plain formulas in 64 bits, the gradient against differences, far positions,
+rows that are parts of wider ones, calls in place, slots of a cache, and the
+refusals.
+
+Tolerances (u = 2^-24).  A mean of d squares is off by (d + 1) u of itself, its root's
+reciprocal by half of that and 3 u, a normalised value by (d / 2 + 6) u.  The angle less
+its whole turns is rounded to 32 bits (pi u at most), its sine and cosine by 2 u more:
+8 u of the pair's magnitude with the products' and the sum's roundings.  So a rotated
+value is off by (d / 2 + 16) u (|n_a| + |n_b|) and half a step of its type.
+"""
+import numpy as np
+import pytest
+import torch
+
+from paper_2303_07030_amd import nsd
+
+P = 0x1000
+U = 2.0 ** -24
+T = {"f32": torch.float32, "bf16": torch.bfloat16}
+HALF = {"f32": U, "bf16": 2.0 ** -8}
+
+
+# ------------------------------------------------------------- refusals
+
+def desc(**change):
+    return nsd.nsd_qk(**{**dict(heads=4, kv_heads=2, d=8, rot=8, dtype=0, interleaved=0, norm=1,
+                                eps=1e-6, ldq=32, ldk=16, ldqo=32, ldko=16), **change})
+
+
+def calls(s, n=4):
+    return (lambda: nsd.nsd_qk_rotate(n, s, P, P, P, P, P, P, 2 * P, 2 * P),
+            lambda: nsd.nsd_qk_rotate_vjp_workspace_size(n, s),
+            lambda: nsd.nsd_qk_rotate_vjp(n, s, P, P, P, P, P, P, P, P, 2 * P, 2 * P, None, None,
+                                          None),
+            lambda: nsd.nsd_qk_append(n, s, P, P, None, P, P, P, P, P, 9, 2 * P, 2 * P, None))
+
+
+@pytest.mark.parametrize("change, status", [
+    (dict(heads=-1), nsd.NSD_ERR_INVALID_ARG), (dict(kv_heads=-1), nsd.NSD_ERR_INVALID_ARG),
+    (dict(d=0, rot=0), nsd.NSD_ERR_INVALID_ARG), (dict(rot=7), nsd.NSD_ERR_INVALID_ARG),
+    (dict(rot=10), nsd.NSD_ERR_INVALID_ARG), (dict(rot=-2), nsd.NSD_ERR_INVALID_ARG),
+    (dict(dtype=3), nsd.NSD_ERR_INVALID_ARG), (dict(eps=-1.0), nsd.NSD_ERR_INVALID_ARG),
+    (dict(eps=float("nan")), nsd.NSD_ERR_INVALID_ARG),
+    (dict(ldq=31), nsd.NSD_ERR_INVALID_ARG), (dict(ldk=15), nsd.NSD_ERR_INVALID_ARG),
+    (dict(ldqo=31), nsd.NSD_ERR_INVALID_ARG), (dict(ldko=15), nsd.NSD_ERR_INVALID_ARG),
+    (dict(d=513, ldq=4000, ldk=4000, ldqo=4000, ldko=4000), nsd.NSD_ERR_UNSUPPORTED)])
+def test_bad_descriptors_are_refused(change, status):
+    for call in calls(desc(**change)):
+        with pytest.raises(nsd.NsdError) as e:
+            call()
+        assert e.value.status == status
+
+
+def test_bad_arguments_are_refused():
+    s, bad = desc(), nsd.NSD_ERR_INVALID_ARG
+    wide = desc(ldqo=40)
+    for call in (*(lambda c=c: c() for c in calls(s, -1)),
+                 lambda: nsd.nsd_qk_rotate(4, s, None, P, P, P, P, P, P, P),
+                 lambda: nsd.nsd_qk_rotate(4, s, P, None, P, P, P, P, P, P),
+                 lambda: nsd.nsd_qk_rotate(4, s, P, P, P, P, None, P, P, P),
+                 lambda: nsd.nsd_qk_rotate(4, s, P, P, P, P, P, None, P, P),
+                 lambda: nsd.nsd_qk_rotate(4, s, P, P, P, P, P, P, None, P),
+                 lambda: nsd.nsd_qk_rotate(4, wide, P, 2 * P, P, P, P, P, P, 2 * P),  # in place
+                 lambda: nsd.nsd_qk_rotate_vjp(4, desc(norm=0), P, P, P, P, P, P, P, P, P, P, P,
+                                               None, None),  # weights without a norm
+                 lambda: nsd.nsd_qk_append(4, s, P, P, None, P, P, P, P, None, 9, P, P, None),
+                 lambda: nsd.nsd_qk_append(4, s, P, P, None, P, P, P, P, P, -1, P, P, None)):
+        with pytest.raises(nsd.NsdError) as e:
+            call()
+        assert e.value.status == bad
+    with pytest.raises(nsd.NsdError) as e:
+        nsd.nsd_qk_rotate_vjp(4, s, P, P, P, P, P, P, P, P, P, P, P, P, None)
+    assert e.value.status == nsd.NSD_ERR_WORKSPACE
+    nsd.nsd_qk_rotate(0, s, None, None, None, None, None, None, None, None)
+
+
+def test_tensors_of_other_shapes_are_refused():
+    q, k = torch.zeros(4, 32), torch.zeros(4, 16)
+    s = nsd.qk_desc(4, 2, 8, q, k, q, k)
+    pos, freq = torch.zeros(4, dtype=torch.int32), torch.zeros(4, dtype=torch.float64)
+    good = dict(Q=q, K=k, wq=None, wk=None, pos=pos, freq=freq, Qo=q, Ko=k)
+    for name, t in (("Q", q[:3]), ("K", k.bfloat16()), ("wq", torch.zeros(7)),
+                    ("pos", pos.long()), ("freq", freq.float()), ("Qo", torch.zeros(4, 33)[:, :32]),
+                    ("Ko", torch.zeros(4, 32)[:, ::2])):
+        with pytest.raises(ValueError, match=name):
+            nsd.nsd_qk_rotate(4, s, **{**good, name: t})
+    with pytest.raises(ValueError, match="q:"):
+        nsd.qk_desc(4, 2, 8, q[:, :30], k, q, k)
+    with pytest.raises(ValueError, match="ko"):
+        nsd.qk_desc(4, 2, 8, q, k, q, k.bfloat16())
+    with pytest.raises(ValueError, match="Vc"):
+        nsd.nsd_qk_append(4, s, q, k, torch.zeros(4, 6), None, None, pos, freq, pos, 4, q, k,
+                          torch.zeros(4, 7))
+
+
+# ------------------------------------------------- the definition in 64 bits
+
+def pairs_of(d, rot, interleaved):
+    p = np.arange(rot // 2)
+    return (2 * p, 2 * p + 1) if interleaved else (p, p + rot // 2)
+
+
+def turned(n, angle, rot, interleaved, back=False):
+    """n [tokens, heads, d] and the magnitudes of its pairs."""
+    a, b = pairs_of(n.shape[-1], rot, interleaved)
+    c, s = np.cos(angle)[:, None], np.sin(angle)[:, None] * (-1 if back else 1)
+    y, mag = n.copy(), np.abs(n)
+    y[..., a] = n[..., a] * c - n[..., b] * s
+    y[..., b] = n[..., a] * s + n[..., b] * c
+    mag[..., a] = mag[..., b] = np.abs(n[..., a]) + np.abs(n[..., b])
+    return y, mag
+
+
+def forward64(x, w, angle, rot, interleaved, norm, eps):
+    n = x
+    if norm:
+        n = x / np.sqrt((x * x).mean(-1, keepdims=True) + eps) * w
+    return turned(n, angle, rot, interleaved)
+
+
+def backward64(x, w, dy, angle, rot, interleaved, norm, eps):
+    """(dx, its magnitude, dw, its magnitude)."""
+    g, m = turned(dy, angle, rot, interleaved, back=True)
+    if not norm:
+        return g, m, None, None
+    r = 1.0 / np.sqrt((x * x).mean(-1, keepdims=True) + eps)
+    u = x * r
+    dx = r * (g * w - u * (g * w * u).mean(-1, keepdims=True))
+    mag = r * (m * np.abs(w) + np.abs(u) * (m * np.abs(w * u)).mean(-1, keepdims=True))
+    return dx, mag, (g * u).sum((0, 1)), (m * np.abs(u)).sum((0, 1))
+
+
+def test_the_gradient_is_that_of_the_definition():
+    rng = np.random.default_rng(0)
+    x, dy = rng.standard_normal((2, 3, 2, 10))
+    w, angle = rng.standard_normal(10), rng.standard_normal((3, 3))
+    for interleaved in (False, True):
+        args = (angle, 6, interleaved, True, 1e-3)
+        dx, _, dw, _ = backward64(x, w, dy, *args)
+        h = 1e-6
+        for t, grad in ((x, dx), (w, dw)):
+            for i in np.ndindex(t.shape):
+                side = []
+                for sign in (1, -1):
+                    old = t[i]
+                    t[i] = old + sign * h
+                    side.append((forward64(x, w, *args)[0] * dy).sum())
+                    t[i] = old
+                assert abs((side[0] - side[1]) / (2 * h) - grad[i]) <= 1e-7
+
+
+# ------------------------------------------------------------- on the GPU
+
+def make(n, H, Hk, d, rot, dtype, far, seed=0, gap=0):
+    g = torch.Generator().manual_seed(seed)
+
+    def rows(heads):
+        return torch.randn(n + 1, heads * d + gap, generator=g).to(T[dtype]).cuda()[:n, :heads * d]
+
+    t = dict(q=rows(H), k=rows(Hk), qo=rows(H), ko=rows(Hk), dqo=rows(H), dko=rows(Hk),
+             dq=rows(H), dk=rows(Hk))
+    t["wq"], t["wk"] = torch.randn(d, generator=g).cuda(), torch.randn(d, generator=g).cuda()
+    t["pos"] = torch.randint(-far, far, (n,), generator=g, dtype=torch.int32).cuda()
+    t["freq"] = (10_000.0 ** (-torch.arange(0, rot, 2, dtype=torch.float64) / max(rot, 1))).cuda()
+    return t
+
+
+def np64(t):
+    return t.double().cpu().numpy()
+
+
+def compare(n, H, Hk, d, rot, dtype, interleaved, norm=True, eps=1e-6, far=5000, gap=0, seed=0,
+            weights=True):
+    t = make(n, H, Hk, d, rot, dtype, far, seed, gap)
+    s = nsd.qk_desc(H, Hk, d, t["q"], t["k"], t["qo"], t["ko"], rot, interleaved, norm, eps)
+    wq, wk = (t["wq"], t["wk"]) if norm and weights else (None, None)
+    small = (wq, wk, t["pos"], t["freq"])
+    nsd.nsd_qk_rotate(n, s, t["q"], t["k"], *small, t["qo"], t["ko"])
+    ws = torch.full((nsd.nsd_qk_rotate_vjp_workspace_size(n, s),), 0x7F, dtype=torch.uint8,
+                    device="cuda")
+    gw = [torch.full((d,), 7.0, device="cuda") if norm else None for _ in range(2)]
+    nsd.nsd_qk_rotate_vjp(n, s, t["q"], t["k"], *small, t["dqo"], t["dko"], t["dq"], t["dk"], *gw,
+                          ws)
+    angle = np64(t["pos"])[:, None] * np64(t["freq"])
+    args = (angle, rot, interleaved, norm, float(np.float32(eps)))
+    half = HALF[dtype]
+    for x, w, y, dy, dx, dw in (("q", wq, "qo", "dqo", "dq", gw[0]),
+                                ("k", wk, "ko", "dko", "dk", gw[1])):
+        x, y, dy, dx = (np64(t[i]).reshape(n, -1, d) for i in (x, y, dy, dx))
+        heads = x.shape[1]
+        w = np.ones(d) if w is None else np64(w)
+        ref, mag = forward64(x, w, *args)
+        assert np.all(np.abs(y - ref) <= (d / 2 + 16) * U * mag + half * np.abs(ref))
+        ref, mag, refw, magw = backward64(x, w, dy, *args)
+        # the normalised value twice, the mean of d products of it
+        assert np.all(np.abs(dx - ref) <= (2 * d + 40) * U * mag + half * np.abs(ref))
+        if norm:  # a sum over tokens and heads
+            room = (d + 40 + n * heads) * U * magw
+            assert np.all(np.abs(np64(dw) - refw) <= room)
+    return t, s, small
+
+
+SHAPES = [(1, 1, 1, 1, 0), (3, 2, 1, 2, 2), (5, 3, 1, 7, 6), (5, 3, 3, 8, 8), (70, 4, 2, 16, 16),
+          (33, 6, 3, 40, 24), (9, 16, 4, 64, 64), (65, 5, 1, 64, 32), (7, 9, 3, 66, 66),
+          (20, 12, 4, 128, 128), (20, 3, 1, 130, 64), (6, 2, 2, 256, 256), (5, 3, 1, 511, 510),
+          (3, 2, 2, 512, 128), (4, 1, 1, 24, 8)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n, H, Hk, d, rot", SHAPES)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_heads(n, H, Hk, d, rot, dtype, interleaved):
+    compare(n, H, Hk, d, rot, dtype, interleaved, gap=n % 3)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [1, 100, 4099, 9001])
+@pytest.mark.parametrize("norm, weights", [(True, True), (True, False), (False, True)])
+def test_tokens(n, norm, weights):
+    compare(n, 5, 2, 32, 32, "f32", False, norm, weights=weights, far=2 ** 30)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rows_of_zeros_and_large_values(interleaved):
+    """eps keeps a row of zeros; large values overflow in no square of bf16 range up to
+    2^63."""
+    n, H, Hk, d = 40, 3, 2, 48
+    t = make(n, H, Hk, d, d, "bf16", 100)
+    t["q"][5] = 0
+    t["q"][6] *= 2.0 ** 40
+    s = nsd.qk_desc(H, Hk, d, t["q"], t["k"], t["qo"], t["ko"], d, interleaved)
+    nsd.nsd_qk_rotate(n, s, t["q"], t["k"], None, None, t["pos"], t["freq"], t["qo"], t["ko"])
+    assert torch.all(t["qo"][5] == 0) and torch.isfinite(t["qo"].float()).all()
+    ref, mag = forward64(np64(t["q"]).reshape(n, H, d), 1.0, np64(t["pos"])[:, None] *
+                         np64(t["freq"]), d, interleaved, True, float(np.float32(1e-6)))
+    got = np64(t["qo"]).reshape(n, H, d)
+    assert np.all(np.abs(got - ref) <= (d / 2 + 16) * U * mag + 2.0 ** -8 * np.abs(ref))
+
+
+@pytest.mark.gpu
+def test_weights_with_eps_of_zero():
+    """Lanes without a head of their own leave the weights' gradients alone."""
+    compare(11, 3, 1, 16, 16, "f32", False, eps=0.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 50])
+def test_in_place(d):
+    t, s, small = compare(37, 4, 2, d, d, "bf16", False)
+    q, k = t["q"].clone(), t["k"].clone()
+    nsd.nsd_qk_rotate(37, s, q, k, *small, q, k)
+    assert torch.equal(q, t["qo"]) and torch.equal(k, t["ko"])
+    dq, dk = t["dqo"].clone(), t["dko"].clone()
+    ws = torch.empty(nsd.nsd_qk_rotate_vjp_workspace_size(37, s), dtype=torch.uint8, device="cuda")
+    gw = torch.empty(2, d, device="cuda")
+    nsd.nsd_qk_rotate_vjp(37, s, t["q"], t["k"], *small, dq, dk, dq, dk, gw[0], gw[1], ws)
+    assert torch.equal(dq, t["dq"]) and torch.equal(dk, t["dk"])
+
+
+@pytest.mark.gpu
+def test_queries_alone():
+    n, H, d = 19, 3, 24
+    t = make(n, H, 1, d, d, "f32", 100)
+    s = nsd.qk_desc(H, 0, d, t["q"], None, t["qo"], None)
+    nsd.nsd_qk_rotate(n, s, t["q"], None, t["wq"], None, t["pos"], t["freq"], t["qo"], None)
+    both = nsd.qk_desc(H, 1, d, t["q"], t["k"], t["qo"], t["ko"])
+    want = torch.empty_like(t["qo"])
+    nsd.nsd_qk_rotate(n, both, t["q"], t["k"], t["wq"], t["wk"], t["pos"], t["freq"], want, t["ko"])
+    assert torch.equal(want, t["qo"])
+    ws = torch.empty(nsd.nsd_qk_rotate_vjp_workspace_size(n, s), dtype=torch.uint8, device="cuda")
+    dw = torch.full((2, d), 5.0, device="cuda")
+    nsd.nsd_qk_rotate_vjp(n, s, t["q"], None, t["wq"], None, t["pos"], t["freq"], t["dqo"], None,
+                          t["dq"], None, dw[0], dw[1], ws)
+    assert torch.all(dw[1] == 0) and torch.isfinite(dw[0]).all()
+
+
+@pytest.mark.gpu
+def test_no_tokens_leave_zero_weights_gradients():
+    t = make(1, 2, 1, 8, 8, "f32", 5)
+    s = nsd.qk_desc(2, 1, 8, t["q"], t["k"], t["qo"], t["ko"])
+    ws = torch.empty(nsd.nsd_qk_rotate_vjp_workspace_size(0, s), dtype=torch.uint8, device="cuda")
+    gw = torch.full((2, 8), 5.0, device="cuda")
+    nsd.nsd_qk_rotate_vjp(0, s, None, None, None, None, None, None, None, None, None, None, gw[0],
+                          gw[1], ws)
+    assert torch.all(gw == 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n, d, dv, dtype", [(1, 64, 128, "bf16"), (8, 64, 128, "bf16"),
+                                             (33, 20, 13, "f32"), (300, 128, 96, "bf16"),
+                                             (5, 7, 0, "bf16")])
+def test_appending_to_a_cache(n, d, dv, dtype):
+    H, Hk, slots = 6, 2, 2 * n + 3
+    t = make(n, H, Hk, d, d // 2 * 2, dtype, 10_000, gap=1)
+    g = torch.Generator().manual_seed(1)
+    kc = torch.randn(slots + 1, Hk * d + 3, generator=g).to(T[dtype]).cuda()
+    vc = torch.randn(slots + 1, Hk * dv + 5, generator=g).to(T[dtype]).cuda()
+    v = torch.randn(n, Hk * dv + 2, generator=g).to(T[dtype]).cuda()[:, :Hk * dv]
+    slot = torch.randperm(slots, generator=g)[:n].int()
+    if n > 4:
+        slot[1], slot[2], slot[3] = -1, slots, 2 ** 31 - 1
+    before = kc.clone(), vc.clone()
+    s = nsd.qk_desc(H, Hk, d, t["q"], t["k"], t["qo"], kc[:, :Hk * d], d // 2 * 2)
+    values = (v, vc[:slots, :Hk * dv]) if dv else (None, None)
+    nsd.nsd_qk_append(n, s, t["q"], t["k"], values[0], t["wq"], t["wk"], t["pos"], t["freq"],
+                      slot.cuda(), slots, t["qo"], kc[:slots, :Hk * d], values[1])
+    # the rotated rows are those of the other call, bit for bit
+    rows = nsd.qk_desc(H, Hk, d, t["q"], t["k"], t["qo"], t["ko"], d // 2 * 2)
+    qo = t["qo"].clone()
+    nsd.nsd_qk_rotate(n, rows, t["q"], t["k"], t["wq"], t["wk"], t["pos"], t["freq"], t["qo"],
+                      t["ko"])
+    assert torch.equal(qo, t["qo"])
+    wk, wv = before
+    for i, x in enumerate(slot.tolist()):
+        if 0 <= x < slots:
+            wk[x, :Hk * d] = t["ko"][i]
+            if dv:
+                wv[x, :Hk * dv] = v[i]
+    assert torch.equal(kc, wk) and torch.equal(vc, wv)
+
+
+@pytest.mark.gpu
+def test_a_cache_past_32_bit_offsets():
+    n, Hk, d, slots = 3, 8, 128, 2_200_000
+    t = make(n, 8, Hk, d, d, "bf16", 100)
+    kc = torch.empty(slots, Hk * d, dtype=torch.bfloat16, device="cuda")
+    slot = torch.tensor([slots - 1, 0, slots - 2], dtype=torch.int32, device="cuda")
+    s = nsd.qk_desc(8, Hk, d, t["q"], t["k"], t["qo"], kc)
+    nsd.nsd_qk_append(n, s, t["q"], t["k"], t["k"], None, None, t["pos"], t["freq"], slot, slots,
+                      t["qo"], kc, kc.roll(0))
+    rows = nsd.qk_desc(8, Hk, d, t["q"], t["k"], t["qo"], t["ko"])
+    nsd.nsd_qk_rotate(n, rows, t["q"], t["k"], None, None, t["pos"], t["freq"], t["qo"], t["ko"])
+    assert torch.equal(kc[slot.long()], t["ko"])
+
+
+@pytest.mark.gpu
+def test_a_captured_step_follows_its_inputs():
+    n = 50
+    t, s, small = compare(n, 4, 2, 64, 64, "bf16", False)
+    ws = torch.empty(nsd.nsd_qk_rotate_vjp_workspace_size(n, s), dtype=torch.uint8, device="cuda")
+    gw = torch.empty(2, 64, device="cuda")
+
+    def step():
+        nsd.nsd_qk_rotate(n, s, t["q"], t["k"], *small, t["qo"], t["ko"])
+        nsd.nsd_qk_rotate_vjp(n, s, t["q"], t["k"], *small, t["dqo"], t["dko"], t["dq"], t["dk"],
+                              gw[0], gw[1], ws)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    outs = [t[i] for i in ("qo", "ko", "dq", "dk")] + [gw]
+    for i in range(3):
+        t["q"].copy_(torch.randn_like(t["q"].float()))
+        t["pos"].add_(17)
+        step()
+        want = [o.clone() for o in outs]
+        for o in outs:
+            o.fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
