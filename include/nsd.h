@@ -1121,6 +1121,62 @@ nsd_status nsd_qk_append(int32_t ntok, const nsd_qk *s, const void *Q, const voi
                          const double *freq, const int32_t *slot, int32_t nslots, void *Qo,
                          void *Kc, void *Vc, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Linear attention with a decay for each head, over packed sequences: token t of a
+ * sequence sees every token j <= t, the weight of which falls with the distance,
+ *     S_t = exp(g_h) S_{t-1} + k_t^T v_t        (S of the head: d x dv, S_{-1} = S0)
+ *     o_t = scale q_t S_t
+ * so that a sequence is carried on by its states alone.  Q: [ntok][heads][d], K:
+ * [ntok][kv_heads][d], V: [ntok][kv_heads][dv], O: [ntok][heads][dv], all of one
+ * nsd_dtype, with ldq, ldk, ldv, ldo values from one row to the next; head h reads
+ * key head h / (heads / kv_heads).  d, dv <= 256, any alignment.  decay: fp32 [heads],
+ * the g_h: at most 0 (-infinity: a token sees itself alone).  States are fp32,
+ * [heads][d][dv] for each sequence or slot, whatever the type of the rows.
+ *
+ * Sequence s is the rows seqptr[s] to seqptr[s + 1] - 1 (int32 [nseq + 1],
+ * non-decreasing, within [0, ntok]); it may be empty.  Rows of no sequence are not
+ * read, and left as they are in what is written.  A number that is not finite shows
+ * in its own sequence and head from its token on, and in no earlier token.
+ *
+ * nsd_attn_decay       O and, where not NULL, S1 [nseq]: the states after each
+ *                      sequence (of an empty one, S0).  S0 [nseq] or NULL (zero).
+ *                      S1 may be S0.  max_len (host): sequences are split for up to
+ *                      so many tokens; a longer one is right, and slower.
+ * nsd_attn_decay_vjp   gradients of Q, K, V (type and row distances of theirs) and,
+ *                      where not NULL, decay [heads] and S0 [nseq], for the upstream
+ *                      dO (ldo) and dS1 [nseq] or NULL (zero).  Nothing that is
+ *                      written shares memory with what is read.  Gradients of a key
+ *                      head add up its query heads'.
+ * nsd_attn_decay_workspace_size  bytes for either call with these sizes.
+ * nsd_attn_decay_step  one token for each row, its state in slot[r] of `state`
+ *                      [nslots] (slot NULL: in r), updated in place.  Rows that name
+ *                      one slot are tokens of it in the rows' order.  A slot outside
+ *                      [0, nslots) is padding: its row of O is 0.
+ * Async.
+ */
+typedef struct nsd_decay {
+    int32_t heads, kv_heads; /* heads is a multiple of kv_heads */
+    int32_t d, dv;
+    int32_t dtype;
+    float scale;
+    int64_t ldq, ldk, ldv, ldo;
+} nsd_decay;
+
+nsd_status nsd_attn_decay_workspace_size(int32_t ntok, int32_t nseq, int32_t max_len,
+                                         const nsd_decay *s, int32_t gradient, size_t *bytes);
+nsd_status nsd_attn_decay(int32_t ntok, int32_t nseq, const int32_t *seqptr, int32_t max_len,
+                          const nsd_decay *s, const void *Q, const void *K, const void *V,
+                          const float *decay, const float *S0, void *O, float *S1, void *ws,
+                          size_t ws_bytes, void *stream);
+nsd_status nsd_attn_decay_vjp(int32_t ntok, int32_t nseq, const int32_t *seqptr, int32_t max_len,
+                              const nsd_decay *s, const void *Q, const void *K, const void *V,
+                              const float *decay, const float *S0, const void *dO,
+                              const float *dS1, void *dQ, void *dK, void *dV, float *ddecay,
+                              float *dS0, void *ws, size_t ws_bytes, void *stream);
+nsd_status nsd_attn_decay_step(int32_t nrows, const int32_t *slot, int32_t nslots,
+                               const nsd_decay *s, const void *Q, const void *K, const void *V,
+                               const float *decay, float *state, void *O, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,617 @@
+// Linear attention with a decay for each head: the scan over chunks of tokens that its
+// forward pass and every gradient run, on the matrix cores.
+//
+//   S_t = e^g S_{t-1} + k_t^T v_t,   o_t = s q_t S_t
+//
+// A chunk of C tokens, with S the state before it, n = i - j and w = e^g:
+//   O = [ s w^(i+1) Q S ] + [ s w^n (Q K^T) for n >= 0 ] V,
+//   S = w^C S + (w^(C-1-j) K)^T V
+// The gradients are the same scan with the roles changed.  With R the state that comes
+// back from the tokens behind (R_t = w R_{t+1} + s q_t^T do_t):
+//   dq: queries dO, keys V, values K, states S^T;   forwards
+//   dk: queries V, keys dO, values Q, states R^T;   backwards
+//   dv: queries K, keys Q, values dO, states R;     backwards
+// (backwards, the state is held with its next decay in it, so that the state of no
+// token is the upstream of the last state: powers i and C - j instead of i + 1 and
+// C - 1 - j).  The gradient of g is the sum of do_t times the derivative of o_t, a
+// scan of S and its derivative T = dS/dg:
+//   dO/dg: weights n w^n,  s w^(i+1) ((i+1) Q S + Q T);   T = w^C (T + C S) + sum
+//   (C-1-j) w^(C-1-j) k^T v
+//
+// A block of four waves takes a segment of a sequence, a head and 64 or 128 columns of
+// the values.  A wave's own columns of the state stay in its registers, in 32 bits, in
+// the layout that the products leave and, with the contraction's order within 32
+// places permuted (place() below), the next product takes.  Queries, keys (both ways
+// round), transposed values and the scores are shared through LDS; the next chunk's
+// rows are in flight meanwhile.
+//
+// bf16: products of bf16 rows are exact, and what is not a bf16 number (scores, states,
+// decayed values) is a sum of two or three of them: two keep 16 bits, far below the
+// rounding of a bf16 result; the states that are carried on, and the gradient of g,
+// are held in 32 bits and take three.  fp32: fp32 products, half the chunk.
+#pragma once
+
+#include <type_traits>
+
+#include "values.hpp"
+
+namespace nsd {
+namespace decay {
+
+constexpr int kScanThreads = 256;
+constexpr int kScanWaves = kScanThreads / kWave;
+constexpr int kMaxWidth = 256;
+
+template <class T>
+constexpr int kChunkOf = sizeof(T) == 2 ? 64 : 32;
+
+// One of the rows' matrices: head h of a query head is at (h / grp) * width.
+struct Rows {
+    const void *p;
+    int64_t ld;
+    int32_t width, grp;
+};
+
+struct Scan {
+    int32_t ntok, nseq, H;
+    const int32_t *seqptr;
+    int32_t seg_len;          // tokens of a segment
+    int32_t nseg;             // segment numbers there are (some of no tokens)
+    Rows q, k, v;
+    void *out;                // [ntok][..]: head h at h * v.width
+    int64_t ldo;
+    bool out32;               // a float for each query head, to be added up
+    bool rev;
+    float s_score, s_inter, s_update;
+    const float *decay;       // g [H]
+    // states [index][H][per], element (k, v) at k * sk + v * sv
+    const float *start;       // NULL: zero
+    float *end;               // NULL: not wanted
+    bool start_by_seq, end_by_seq;
+    int32_t sk, sv;
+    int64_t per;
+    // gradient of g: dO, the states that come back to a segment's end, one sum for each block
+    Rows up;
+    const float *back;
+    bool back_by_seq;
+    float *sums;
+};
+
+// Segment `id`: sequence s has the numbers from seqptr[s] / seg_len + s on, which are enough for
+// it whatever the lengths; those it does not need have no tokens.
+struct Segment {
+    int32_t seq, first, n;  // its first token and its tokens (0: none)
+    bool on;                // it is one: also the first of an empty sequence
+    __device__ __forceinline__ Segment(const Scan &a, int id) {
+        int lo = 0, hi = a.nseq - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) / 2;
+            if (a.seqptr[mid] / a.seg_len + mid <= id) lo = mid;
+            else hi = mid - 1;
+        }
+        seq = lo;
+        const int begin = max(a.seqptr[lo], 0), end = min(a.seqptr[lo + 1], a.ntok);
+        const int c = id - (a.seqptr[lo] / a.seg_len + lo);
+        const int64_t at = begin + (int64_t)c * a.seg_len;
+        on = c == 0 || (c > 0 && at < end);
+        first = (int)min(at, (int64_t)a.ntok);
+        n = on ? (int)max(min((int64_t)end - at, (int64_t)a.seg_len), (int64_t)0) : 0;
+    }
+};
+
+typedef float f32x4v __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8v __attribute__((ext_vector_type(8)));
+
+// Eight values of a lane: places of 32 of the contraction, of row (lane % 16).
+template <class T>
+struct Frag;
+template <>
+struct Frag<Bf16> {
+    u32x4v v;
+};
+template <>
+struct Frag<float> {
+    float v[8];
+};
+
+template <class T>
+__device__ __forceinline__ Frag<T> fragment(const T *p) {
+    Frag<T> f;
+    __builtin_memcpy(&f, __builtin_assume_aligned(p, 16), sizeof f);
+    return f;
+}
+
+// c[4 g + r][n] += sum of a[4 g + r][.] b[n][.]: rows of a in the lane's four values, the row
+// of b by lane % 16.
+__device__ __forceinline__ void mma(f32x4v &c, const Frag<Bf16> &a, const Frag<Bf16> &b) {
+    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, a.v),
+                                                __builtin_bit_cast(bf16x8v, b.v), c, 0, 0, 0);
+}
+__device__ __forceinline__ void mma(f32x4v &c, const Frag<float> &a, const Frag<float> &b) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[e], b.v[e], c, 0, 0, 0);
+}
+
+// x as a sum of N numbers of T (one is enough in 32 bits).
+template <class T, int N>
+constexpr int kParts = sizeof(T) == 2 ? N : 1;
+
+template <class T, int N, int M>
+__device__ __forceinline__ void split(const float (&x)[M], T (&part)[kParts<T, N>][M]) {
+#pragma unroll
+    for (int e = 0; e < M; ++e) {
+        if constexpr (sizeof(T) == 4) {
+            part[0][e] = x[e];
+        } else {
+            float left = x[e];
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                part[i][e] = narrowed<Bf16>(left);
+                if (i + 1 < N) left -= widened(part[i][e]);
+            }
+        }
+    }
+}
+template <class T, int N>
+__device__ __forceinline__ void split(const float (&x)[8], Frag<T> (&f)[kParts<T, N>]) {
+    T part[kParts<T, N>][8];
+    split<T, N, 8>(x, part);
+#pragma unroll
+    for (int i = 0; i < kParts<T, N>; ++i) __builtin_memcpy(&f[i], part[i], sizeof f[i]);
+}
+
+// Where value k of a row lies in LDS, k a multiple of four: of 32 values lane group g takes 4 g
+// to 4 g + 3 and 16 + 4 g to 16 + 4 g + 3, as the products leave a state's rows.
+__device__ __forceinline__ int place(int k) {
+    const int u = k % 32 / 4;
+    return k / 32 * 32 + (u % 4) * 8 + (u / 4) * 4;
+}
+
+// A chunk's rows of one matrix on their way to LDS: four rows and CV columns a unit.
+template <class T, int W>
+struct Stage {
+    static constexpr int C = kChunkOf<T>;
+    static constexpr int CV = sizeof(T) == 2 && W >= 128 ? 8 : 4;
+    static constexpr int PIECES = W / CV;
+    static constexpr int UNITS = C / 4 * PIECES;
+    static constexpr int U = (UNITS + kScanThreads - 1) / kScanThreads;
+    T x[U][4][CV];
+
+    // rows i < len from token t0 + i * dir; columns from col0 on
+    __device__ __forceinline__ void load(const Rows &m, int h, int col0, int64_t t0, int dir, int len) {
+        const T *p = static_cast<const T *>(m.p) + (int64_t)(h / m.grp) * m.width + col0;
+        const int width = m.width - col0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int unit = threadIdx.x + u * kScanThreads;
+            const int i0 = unit / PIECES * 4, c = unit % PIECES * CV;
+            const int left = width - c;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+#pragma unroll
+                for (int e = 0; e < CV; ++e) x[u][r][e] = T(0);
+                if ((UNITS % kScanThreads && unit >= UNITS) || i0 + r >= len || left <= 0) continue;
+                const T *row = p + (t0 + (int64_t)(i0 + r) * dir) * m.ld + c;
+                if (left >= CV) {
+                    __builtin_memcpy(x[u][r], row, sizeof x[u][r]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < CV; ++e)
+                        if (e < left) x[u][r][e] = row[e];
+                }
+            }
+        }
+    }
+    // rows of ld values, columns in the order of place()
+    __device__ __forceinline__ void store(T *to, int ld) const {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int unit = threadIdx.x + u * kScanThreads;
+            if (UNITS % kScanThreads && unit >= UNITS) continue;
+            const int i0 = unit / PIECES * 4, c = unit % PIECES * CV;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int e = 0; e < CV; e += 4)
+                    __builtin_memcpy(__builtin_assume_aligned(to + (i0 + r) * ld + place(c + e), 8),
+                                     &x[u][r][e], 4 * sizeof(T));
+        }
+    }
+    // columns as rows of ld values
+    __device__ __forceinline__ void store_transposed(T *to, int ld) const {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int unit = threadIdx.x + u * kScanThreads;
+            if (UNITS % kScanThreads && unit >= UNITS) continue;
+            const int i0 = unit / PIECES * 4, c = unit % PIECES * CV;
+#pragma unroll
+            for (int e = 0; e < CV; ++e) {
+                const T t[4] = {x[u][0][e], x[u][1][e], x[u][2][e], x[u][3][e]};
+                __builtin_memcpy(__builtin_assume_aligned(to + (c + e) * ld + i0, 8), t, sizeof t);
+            }
+        }
+    }
+    __device__ __forceinline__ bool finite() const {
+        uint32_t top = 0;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int e = 0; e < CV; ++e) {
+                    if constexpr (sizeof(T) == 4) top = max(top, __float_as_uint(x[u][r][e]) & 0x7F800000u);
+                    else top = max(top, (uint32_t)x[u][r][e] & 0x7F80u);
+                }
+        return top < (sizeof(T) == 4 ? 0x7F800000u : 0x7F80u);
+    }
+};
+
+// What a scan does: outputs; the states at the segments' ends alone; the gradient of g.
+enum Kind { kOutput, kState, kDerivative };
+
+// LDS of a block.
+template <class T, int KD, int NV, Kind KIND>
+struct Shared {
+    static constexpr int C = kChunkOf<T>;
+    static constexpr int VB = kScanWaves * 16 * NV;
+    static constexpr int PAD = 16 / sizeof(T);
+    static constexpr int LDK = KD + PAD, LDC = C + PAD;
+    static constexpr int SP = KIND == kState ? 0 : kParts<T, KIND == kDerivative ? 3 : 2>;
+    static constexpr int QK = KIND == kState ? 0 : C * LDK;
+    static constexpr size_t bytes =
+        sizeof(T) * (2 * QK + (size_t)KD * LDC + (size_t)VB * LDC + (size_t)SP * C * LDC);
+};
+
+// KD: width of queries and keys, padded; NV: 16 columns of values by a wave; blocks: of the
+// segments' heads' columns, nvb for each head.
+template <class T, int KD, int NV, Kind KIND>
+__global__ __launch_bounds__(kScanThreads) void scan_kernel(Scan a, int32_t nvb) {
+    using Sh = Shared<T, KD, NV, KIND>;
+    constexpr int C = Sh::C, VB = Sh::VB, LDK = Sh::LDK, LDC = Sh::LDC;
+    constexpr int KT = KD / 16, KF = KD / 32, IT = C / 16, JF = C / 32;
+    constexpr int NS = KIND == kDerivative ? 3 : 2;  // parts of scores and states
+    constexpr int SP = kParts<T, NS>, VP = kParts<T, 3>;
+    constexpr bool DERIV = KIND == kDerivative;
+    __shared__ __align__(16) char lds_bytes[Sh::bytes];
+    T *const ldsQ = reinterpret_cast<T *>(lds_bytes);
+    T *const ldsK = ldsQ + Sh::QK;
+    T *const ldsKt = ldsK + Sh::QK;
+    T *const ldsVt = ldsKt + KD * LDC;
+    T *const ldsP = ldsVt + VB * LDC;
+    __shared__ float power[C + 2];
+    __shared__ int unusual[2];
+    __shared__ float wave_sum[kScanWaves];
+
+    const int lane = threadIdx.x % kWave, n16 = lane % 16, g = lane / 16;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int64_t unit = xcd_contiguous_tile();
+    const int vb = (int)(unit % nvb), h = (int)(unit / nvb % a.H);
+    const Segment seg(a, (int)(unit / nvb / a.H));
+    if (!seg.on) {
+        if (DERIV && threadIdx.x == 0) a.sums[unit] = 0.f;
+        return;
+    }
+    const int col0 = vb * VB;                      // the block's first column
+    const int colw = wave * 16 * NV;               // the wave's, within the block
+    const int rev = a.rev ? 1 : 0;
+    const double gd = (double)a.decay[h];
+    if (threadIdx.x < C + 2)  // powers of the decay, exact to their last bit; also of -infinity
+        power[threadIdx.x] = threadIdx.x ? (float)exp(gd * (double)threadIdx.x) : 1.f;
+    if (threadIdx.x < 2) unusual[threadIdx.x] = 0;
+
+    // this lane's part of the state: rows 16 kt + 4 g + r, column n16 of each 16
+    const int64_t sidx = ((int64_t)(a.start_by_seq ? seg.seq : (int)(unit / nvb / a.H)) * a.H + h) * a.per;
+    f32x4v S[KT][NV], D[DERIV ? KT : 1][NV];
+    auto each_state = [&](auto f) {
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int nv = 0; nv < NV; ++nv)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int k = 16 * kt + 4 * g + r, c = col0 + colw + 16 * nv + n16;
+                    f(kt, nv, r, k < a.k.width && c < a.v.width, (int64_t)k * a.sk + (int64_t)c * a.sv);
+                }
+    };
+    each_state([&](int kt, int nv, int r, bool in, int64_t at) {
+        S[kt][nv][r] = in && a.start ? a.start[sidx + at] : 0.f;
+        if (DERIV) D[kt][nv][r] = 0.f;
+    });
+
+    Stage<T, KD> xq, xk;
+    Stage<T, VB> xv;
+    const int64_t first = rev ? (int64_t)seg.first + seg.n - 1 : seg.first;
+    const int dir = rev ? -1 : 1;
+    auto load = [&](int pos, int len) {
+        const int64_t t0 = first + (int64_t)pos * dir;
+        if (KIND != kState) xq.load(a.q, h, 0, t0, dir, len);
+        xk.load(a.k, h, 0, t0, dir, len);
+        xv.load(a.v, h, col0, t0, dir, len);
+    };
+    // powers of whole chunks in more bits than one number has: thousands of chunks multiply them
+    auto low_part = [&](int n) { return (float)(exp(gd * (double)n) - (double)(float)exp(gd * (double)n)); };
+    const float whole_low = low_part(C);
+    float dsum = 0.f;
+    int single = 0, turn = 0;  // tokens that are still taken one by one
+    int pos = 0, len = min(C, seg.n);
+    if (seg.n > 0) load(0, len);
+    while (pos < seg.n) {
+        // ---- the chunk's rows to LDS
+        if (KIND != kState) {
+            xq.store(ldsQ, LDK);
+            xk.store(ldsK, LDK);
+        }
+        xk.store_transposed(ldsKt, LDC);
+        xv.store_transposed(ldsVt, LDC);
+        if (KIND != kState && !xv.finite()) unusual[turn] = 1;
+        __syncthreads();
+        // A product with a score of 0 keeps an infinite or missing number of a later token out
+        // of an earlier one's output no more than a sum would: such chunks go token by token.
+        if (KIND != kState && unusual[turn] && len > 1) {
+            single = len;
+            len = 1;
+            load(pos, 1);
+            __syncthreads();
+            continue;
+        }
+        if (threadIdx.x == 0) unusual[turn ^ 1] = 0;
+        if (single > 0) --single;
+        const int next = pos + len, next_len = single > 0 ? 1 : min(C, seg.n - next);
+        if (next < seg.n) load(next, next_len);
+        const float keep = power[len];
+
+        f32x4v O[IT][NV], OD[DERIV ? IT : 1][NV];
+        if constexpr (KIND != kState) {
+            // ---- scores: tile (it, jt) of 16 x 16, jt <= it, shared out among the waves
+            constexpr int TILES = IT * (IT + 1) / 2;
+#pragma unroll
+            for (int tile0 = 0; tile0 < TILES; tile0 += kScanWaves) {
+                const int tile = tile0 + wave;
+                if (tile >= TILES) break;
+                const int it = tile >= 6 ? 3 : tile >= 3 ? 2 : tile >= 1 ? 1 : 0;
+                const int jt = tile - it * (it + 1) / 2;
+                f32x4v acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int f = 0; f < KF; ++f)
+                    mma(acc, fragment(ldsK + (16 * jt + n16) * LDK + 32 * f + 8 * g),
+                        fragment(ldsQ + (16 * it + n16) * LDK + 32 * f + 8 * g));
+                const int i = 16 * it + n16, j = 16 * jt + 4 * g;
+                float p[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int n = i - j - r;
+                    const float w = power[max(n, 0)] * (DERIV ? (float)n : 1.f);
+                    p[r] = n >= 0 ? acc[r] * a.s_score * w : 0.f;
+                }
+                T part[SP][4];
+                split<T, NS, 4>(p, part);
+#pragma unroll
+                for (int s = 0; s < SP; ++s) {
+                    T *to = ldsP + (s * C + i) * LDC + j;
+                    __builtin_memcpy(__builtin_assume_aligned(to, 8), part[s], 4 * sizeof(T));
+                    if (jt == it && it % 2 == 0) {  // the rest of the 32 columns that products take
+                        const T none[4] = {T(0), T(0), T(0), T(0)};
+                        __builtin_memcpy(__builtin_assume_aligned(to + 16, 8), none, sizeof none);
+                    }
+                }
+            }
+            __syncthreads();
+            // ---- from the state
+#pragma unroll
+            for (int it = 0; it < IT; ++it)
+#pragma unroll
+                for (int nv = 0; nv < NV; ++nv) {
+                    O[it][nv] = f32x4v{0.f, 0.f, 0.f, 0.f};
+                    if (DERIV) OD[it][nv] = f32x4v{0.f, 0.f, 0.f, 0.f};
+                }
+#pragma unroll
+            for (int f = 0; f < KF; ++f) {
+                Frag<T> sf[NV][SP], df[DERIV ? NV : 1][SP];
+#pragma unroll
+                for (int nv = 0; nv < NV; ++nv) {
+                    float x[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = S[2 * f + e / 4][nv][e % 4];
+                    split<T, NS>(x, sf[nv]);
+                    if constexpr (DERIV) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) x[e] = D[2 * f + e / 4][nv][e % 4];
+                        split<T, NS>(x, df[nv]);
+                    }
+                }
+#pragma unroll
+                for (int it = 0; it < IT; ++it) {
+                    const Frag<T> qf = fragment(ldsQ + (16 * it + n16) * LDK + 32 * f + 8 * g);
+#pragma unroll
+                    for (int nv = 0; nv < NV; ++nv)
+#pragma unroll
+                        for (int s = 0; s < SP; ++s) {
+                            mma(O[it][nv], sf[nv][s], qf);
+                            if constexpr (DERIV) mma(OD[it][nv], df[nv][s], qf);
+                        }
+                }
+            }
+#pragma unroll
+            for (int it = 0; it < IT; ++it) {
+                const int i = 16 * it + n16;
+                const float w = a.s_inter * power[i + 1 - rev];
+#pragma unroll
+                for (int nv = 0; nv < NV; ++nv)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        O[it][nv][r] = DERIV ? w * __builtin_fmaf((float)(i + 1), O[it][nv][r],
+                                                                  OD[it][nv][r])
+                                             : w * O[it][nv][r];
+            }
+        }
+        // ---- from the chunk's own tokens, and the state behind them
+        const float keep_low = len == C ? whole_low : low_part(len);
+        if constexpr (DERIV) {
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                for (int nv = 0; nv < NV; ++nv)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float x = __builtin_fmaf((float)len, S[kt][nv][r], D[kt][nv][r]);
+                        D[kt][nv][r] = __builtin_fmaf(x, keep, x * keep_low);
+                    }
+        }
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int nv = 0; nv < NV; ++nv)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    S[kt][nv][r] = __builtin_fmaf(S[kt][nv][r], keep, S[kt][nv][r] * keep_low);
+#pragma unroll
+        for (int f = 0; f < JF; ++f) {
+            Frag<T> vf[NV], vs[NV][VP], vd[DERIV ? NV : 1][VP];
+#pragma unroll
+            for (int nv = 0; nv < NV; ++nv) {
+                const T *from = ldsVt + (colw + 16 * nv + n16) * LDC + 32 * f + 8 * g;
+                vf[nv] = fragment(from);
+                T v[8];
+                __builtin_memcpy(v, &vf[nv], sizeof v);
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int after = len - 1 - (32 * f + 8 * g + e) + rev;
+                    x[e] = after >= 0 ? widened(v[e]) * a.s_update * power[after] : 0.f;
+                }
+                split<T, 3>(x, vs[nv]);
+                if constexpr (DERIV) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        x[e] *= (float)max(len - 1 - (32 * f + 8 * g + e), 0);
+                    split<T, 3>(x, vd[nv]);
+                }
+            }
+            if constexpr (KIND != kState) {
+#pragma unroll
+                for (int it = 2 * f; it < IT; ++it)
+#pragma unroll
+                    for (int s = 0; s < SP; ++s) {
+                        const Frag<T> pf =
+                            fragment(ldsP + (s * C + 16 * it + n16) * LDC + 32 * f + 8 * g);
+#pragma unroll
+                        for (int nv = 0; nv < NV; ++nv) mma(O[it][nv], vf[nv], pf);
+                    }
+            }
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) {
+                const Frag<T> kf = fragment(ldsKt + (16 * kt + n16) * LDC + 32 * f + 8 * g);
+#pragma unroll
+                for (int nv = 0; nv < NV; ++nv)
+#pragma unroll
+                    for (int s = 0; s < VP; ++s) {
+                        mma(S[kt][nv], kf, vs[nv][s]);
+                        if constexpr (DERIV) mma(D[kt][nv], kf, vd[nv][s]);
+                    }
+            }
+        }
+        // ---- outputs: row i by lane % 16, four columns each
+        if constexpr (KIND != kState) {
+#pragma unroll
+            for (int it = 0; it < IT; ++it) {
+                const int i = 16 * it + n16;
+                if (i >= len) continue;
+                const int64_t t = first + (int64_t)(pos + i) * dir;
+#pragma unroll
+                for (int nv = 0; nv < NV; ++nv) {
+                    const int c = col0 + colw + 16 * nv + 4 * g, left = a.v.width - c;
+                    if (left <= 0) continue;
+                    const float x[4] = {O[it][nv][0], O[it][nv][1], O[it][nv][2], O[it][nv][3]};
+                    if constexpr (DERIV) {
+                        float up[4];
+                        load_left<4, T>(static_cast<const T *>(a.up.p) + t * a.up.ld +
+                                            (int64_t)(h / a.up.grp) * a.up.width + c, left, up);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) dsum = r < left ? __builtin_fmaf(x[r], up[r], dsum) : dsum;
+                    } else if (a.out32) {
+                        store_left<4, float>(static_cast<float *>(a.out) + t * a.ldo +
+                                                 (int64_t)h * a.v.width + c, left, x);
+                    } else {
+                        store_left<4, T>(static_cast<T *>(a.out) + t * a.ldo +
+                                             (int64_t)h * a.v.width + c, left, x);
+                    }
+                }
+            }
+        }
+        __syncthreads();
+        pos = next;
+        len = next_len;
+        turn ^= 1;
+    }
+    if (a.end) {
+        const int64_t to = ((int64_t)(a.end_by_seq ? seg.seq : (int)(unit / nvb / a.H)) * a.H + h) * a.per;
+        each_state([&](int kt, int nv, int r, bool in, int64_t at) {
+            if (in) a.end[to + at] = S[kt][nv][r];
+        });
+    }
+    if constexpr (DERIV) {  // what the segment adds to the states behind it
+        if (a.back) {
+            const int64_t at0 =
+                ((int64_t)(a.back_by_seq ? seg.seq : (int)(unit / nvb / a.H)) * a.H + h) * a.per;
+            each_state([&](int kt, int nv, int r, bool in, int64_t at) {
+                if (in) dsum = __builtin_fmaf(D[kt][nv][r], a.back[at0 + at], dsum);
+            });
+        }
+#pragma unroll
+        for (int m = 1; m < kWave; m <<= 1) dsum += __shfl_xor(dsum, m, kWave);
+        if (lane == 0) wave_sum[wave] = dsum;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            float t = 0.f;
+            for (int w = 0; w < kScanWaves; ++w) t += wave_sum[w];
+            a.sums[unit] = t;
+        }
+    }
+}
+
+// Blocks of a head's columns for values of `width` and queries of `kw`.
+inline int columns_of(Kind kind, int kw, int width) {
+    return kind != kDerivative && width > 64 && kw <= 128 ? 128 : 64;
+}
+
+nsd_status launch_scan_f32(Kind kind, const Scan &a, hipStream_t st);
+nsd_status launch_scan_bf16(Kind kind, const Scan &a, hipStream_t st);
+
+template <class T, int KD, int NV, Kind KIND>
+nsd_status launch_one(const Scan &a, hipStream_t st) {
+    const int nvb = (int)ceil_div(a.v.width, kScanWaves * 16 * NV);
+    const int64_t blocks = (int64_t)a.nseg * a.H * nvb;
+    if (blocks == 0) return NSD_OK;
+    scan_kernel<T, KD, NV, KIND><<<blocks, kScanThreads, 0, st>>>(a, nvb);
+    return check_launch("scan_kernel");
+}
+
+template <class T, Kind KIND>
+nsd_status launch_kind(const Scan &a, hipStream_t st) {
+    const bool wide = columns_of(KIND, a.k.width, a.v.width) == 128;
+    auto by_width = [&](auto kd) -> nsd_status {
+        constexpr int KD = decltype(kd)::value;
+        if constexpr (KIND != kDerivative && KD <= 128) {
+            if (wide) return launch_one<T, KD, 2, KIND>(a, st);
+        }
+        return launch_one<T, KD, 1, KIND>(a, st);
+    };
+    if (a.k.width <= 32) return by_width(std::integral_constant<int, 32>());
+    if (a.k.width <= 64) return by_width(std::integral_constant<int, 64>());
+    if (a.k.width <= 128) return by_width(std::integral_constant<int, 128>());
+    return by_width(std::integral_constant<int, 256>());
+}
+
+template <class T>
+nsd_status launch_any(Kind kind, const Scan &a, hipStream_t st) {
+    switch (kind) {
+        case kOutput: return launch_kind<T, kOutput>(a, st);
+        case kState: return launch_kind<T, kState>(a, st);
+        default: return launch_kind<T, kDerivative>(a, st);
+    }
+}
+
+}  // namespace decay
+}  // namespace nsd

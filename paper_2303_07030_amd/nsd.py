@@ -157,6 +157,12 @@ class nsd_qk(C.Structure):
                 ("ldqo", C.c_int64), ("ldko", C.c_int64)]
 
 
+class nsd_decay(C.Structure):
+    _fields_ = [("heads", C.c_int32), ("kv_heads", C.c_int32), ("d", C.c_int32),
+                ("dv", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float),
+                ("ldq", C.c_int64), ("ldk", C.c_int64), ("ldv", C.c_int64), ("ldo", C.c_int64)]
+
+
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"libnsd.so is not built ({LIB_PATH}); run "
                       "`python -m paper_2303_07030_amd.build` first")
@@ -277,6 +283,12 @@ _SIGS = {
     "nsd_qk_rotate_vjp": (C.c_int, [_I, C.POINTER(nsd_qk)] + [_P] * 13 + [_SZ, _P]),
     "nsd_qk_append": (C.c_int, [_I, C.POINTER(nsd_qk), _P, _P, _P, _I, C.c_int64, C.c_int64, _P,
                                 _P, _P, _P, _P, _I, _P, _P, _P, _P]),
+    "nsd_attn_decay_workspace_size": (C.c_int, [_I, _I, _I, C.POINTER(nsd_decay), _I,
+                                                C.POINTER(_SZ)]),
+    "nsd_attn_decay": (C.c_int, [_I, _I, _P, _I, C.POINTER(nsd_decay)] + [_P] * 8 + [_SZ, _P]),
+    "nsd_attn_decay_vjp": (C.c_int, [_I, _I, _P, _I, C.POINTER(nsd_decay)] + [_P] * 13 +
+                           [_SZ, _P]),
+    "nsd_attn_decay_step": (C.c_int, [_I, _P, _I, C.POINTER(nsd_decay)] + [_P] * 7),
     "nsd_loss_cp": (C.c_int, [_COO3, _P, _P, _P, _I, C.c_float, _P, _P, _P, _P, _P, _P, _SZ,
                               _P]),
 }
@@ -1046,3 +1058,70 @@ def nsd_qk_append(ntok, s: nsd_qk, Q, K, V, wq, wk, pos, freq, slot, nslots, Qo,
     _check(_lib.nsd_qk_append(ntok, C.byref(s), _p(Q), _p(K), _p(V), vwidth, ldv, ldvo, _p(wq),
                               _p(wk), _p(pos), _p(freq), _p(slot), nslots, _p(Qo), _p(Kc), _p(Vc),
                               _stream(stream)), "nsd_qk_append")
+
+
+def decay_desc(heads, kv_heads, d, dv, q, k, v, o, scale) -> nsd_decay:
+    """The shape of an attention with a decay over q [ntok, heads * d], k [ntok,
+    kv_heads * d], v [ntok, kv_heads * dv] and o [ntok, heads * dv]: their type and
+    row distances are taken."""
+    lds = []
+    for t, width, name in ((q, heads * d, "q"), (k, kv_heads * d, "k"), (v, kv_heads * dv, "v"),
+                           (o, heads * dv, "o")):
+        if t.dtype != q.dtype:
+            raise ValueError(f"{name}: {t.dtype} beside {q.dtype}")
+        lds.append(_row_distance(t, width, name))
+    return nsd_decay(heads, kv_heads, d, dv, dtype_of(q), scale, *lds)
+
+
+def _decay_rows(n, s, **rows):
+    """rows: which of the call's matrices each is (Q: "q", dQ: "q", ...)."""
+    shape = dict(Q=(s.heads * s.d, s.ldq), K=(s.kv_heads * s.d, s.ldk),
+                 V=(s.kv_heads * s.dv, s.ldv), O=(s.heads * s.dv, s.ldo))
+    for name, t in rows.items():
+        _rows(t, name, n, *shape[name.lstrip("d")], _type_of(s.dtype))
+
+
+def nsd_attn_decay_workspace_size(ntok, nseq, max_len, s: nsd_decay, gradient=False) -> int:
+    b = _SZ(0)
+    _check(_lib.nsd_attn_decay_workspace_size(ntok, nseq, max_len, C.byref(s),
+                                              int(bool(gradient)), C.byref(b)),
+           "nsd_attn_decay_workspace_size")
+    return b.value
+
+
+def _decay_small(nseq, s, seqptr, decay, **states):
+    _dense(seqptr, "seqptr", nseq + 1, torch.int32)
+    _dense(decay, "decay", s.heads, torch.float32)
+    for name, t in states.items():
+        _dense(t, name, nseq * s.heads * s.d * s.dv, torch.float32)
+
+
+def nsd_attn_decay(ntok, nseq, seqptr, max_len, s: nsd_decay, Q, K, V, decay, S0, O, S1, ws,
+                   stream=None):
+    _decay_rows(ntok, s, Q=Q, K=K, V=V, O=O)
+    _decay_small(nseq, s, seqptr, decay, S0=S0, S1=S1)
+    _check(_lib.nsd_attn_decay(ntok, nseq, _p(seqptr), max_len, C.byref(s), _p(Q), _p(K), _p(V),
+                               _p(decay), _p(S0), _p(O), _p(S1), _p(ws), _nbytes(ws),
+                               _stream(stream)), "nsd_attn_decay")
+
+
+def nsd_attn_decay_vjp(ntok, nseq, seqptr, max_len, s: nsd_decay, Q, K, V, decay, S0, dO, dS1, dQ,
+                       dK, dV, ddecay, dS0, ws, stream=None):
+    _decay_rows(ntok, s, Q=Q, K=K, V=V, dO=dO, dQ=dQ, dK=dK, dV=dV)
+    _decay_small(nseq, s, seqptr, decay, S0=S0, dS1=dS1, dS0=dS0)
+    _dense(ddecay, "ddecay", s.heads, torch.float32)
+    _check(_lib.nsd_attn_decay_vjp(ntok, nseq, _p(seqptr), max_len, C.byref(s), _p(Q), _p(K),
+                                   _p(V), _p(decay), _p(S0), _p(dO), _p(dS1), _p(dQ), _p(dK),
+                                   _p(dV), _p(ddecay), _p(dS0), _p(ws), _nbytes(ws),
+                                   _stream(stream)), "nsd_attn_decay_vjp")
+
+
+def nsd_attn_decay_step(nrows, slot, nslots, s: nsd_decay, Q, K, V, decay, state, O,
+                        stream=None):
+    _decay_rows(nrows, s, Q=Q, K=K, V=V, O=O)
+    _dense(slot, "slot", nrows, torch.int32)
+    _dense(decay, "decay", s.heads, torch.float32)
+    _dense(state, "state", nslots * s.heads * s.d * s.dv, torch.float32)
+    _check(_lib.nsd_attn_decay_step(nrows, _p(slot), nslots, C.byref(s), _p(Q), _p(K), _p(V),
+                                    _p(decay), _p(state), _p(O), _stream(stream)),
+           "nsd_attn_decay_step")

@@ -1,0 +1,546 @@
+"""Linear attention with a decay for each head: outputs, states and every gradient
+against the sums over pairs of tokens in 64 bits, the gradients' formulas against
+differences, packed sequences of every length, sequences cut into segments, heads that
+share keys, states carried on, single tokens, numbers that are not finite, and the
+refusals.
+
+Tolerances (u = 2^-24).  All results are sums of products with positive weights, so the
+same formulas on magnitudes bound what roundings add up to: a sum of n terms in any
+order is off by n u of them.  A result passes a sum over a head's values (d or dv), one
+over the tokens, and for each chunk of 32 tokens and more two roundings of a decay:
+(d + dv + 2 len + 32) u of the magnitudes.  Where a power or a product is below 2^-126, the
+least normal number, it is off by less than that, whatever multiplies it: 2^-126 of the
+magnitudes without a decay, and of each of the products that a result adds up.  bf16 rows multiply exactly; scores and
+states enter the products of bf16 results as two bf16 numbers each, off by 2^-16; those
+of states and of the decay's gradient as three, off by 2^-24.  A value rounded to its
+type is off by half a step.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2303_07030_amd import nsd
+
+P = 0x1000
+U = 2.0 ** -24
+T = {"f32": torch.float32, "bf16": torch.bfloat16}
+HALF = {"f32": U, "bf16": 2.0 ** -8}
+PARTS = {"f32": 0.0, "bf16": 2 * 2.0 ** -16}
+
+
+# ------------------------------------------------------------- refusals
+
+def desc(**change):
+    return nsd.nsd_decay(**{**dict(heads=4, kv_heads=2, d=8, dv=6, dtype=0, scale=1.0, ldq=32,
+                                   ldk=16, ldv=12, ldo=24), **change})
+
+
+def calls(s, ntok=10, nseq=2, max_len=10, ws=None):
+    return (lambda: nsd.nsd_attn_decay_workspace_size(ntok, nseq, max_len, s),
+            lambda: nsd.nsd_attn_decay(ntok, nseq, P, max_len, s, P, P, P, P, None, P, None, ws),
+            lambda: nsd.nsd_attn_decay_vjp(ntok, nseq, P, max_len, s, P, P, P, P, None, P, None,
+                                           P, P, P, None, None, ws))
+
+
+@pytest.mark.parametrize("change, status", [
+    (dict(heads=0), nsd.NSD_ERR_INVALID_ARG), (dict(kv_heads=0), nsd.NSD_ERR_INVALID_ARG),
+    (dict(kv_heads=3), nsd.NSD_ERR_INVALID_ARG), (dict(d=0), nsd.NSD_ERR_INVALID_ARG),
+    (dict(dv=0), nsd.NSD_ERR_INVALID_ARG), (dict(dtype=4), nsd.NSD_ERR_INVALID_ARG),
+    (dict(ldq=31), nsd.NSD_ERR_INVALID_ARG), (dict(ldk=15), nsd.NSD_ERR_INVALID_ARG),
+    (dict(ldv=11), nsd.NSD_ERR_INVALID_ARG), (dict(ldo=23), nsd.NSD_ERR_INVALID_ARG),
+    (dict(d=257, ldq=2000, ldk=2000), nsd.NSD_ERR_UNSUPPORTED),
+    (dict(dv=257, ldv=2000, ldo=2000), nsd.NSD_ERR_UNSUPPORTED),
+    (dict(heads=4098, ldq=99999, ldo=99999), nsd.NSD_ERR_UNSUPPORTED)])
+def test_bad_descriptors_are_refused(change, status):
+    s = desc(**change)
+    for call in (*calls(s), lambda: nsd.nsd_attn_decay_step(4, P, 9, s, P, P, P, P, P, P)):
+        with pytest.raises(nsd.NsdError) as e:
+            call()
+        assert e.value.status == status
+
+
+def test_bad_arguments_are_refused():
+    s, bad, big = desc(), nsd.NSD_ERR_INVALID_ARG, nsd.NSD_ERR_TOO_LARGE
+    ws = torch.empty(1 << 16, dtype=torch.uint8)
+    for many, status in ((calls(s, ntok=-1), bad), (calls(s, nseq=-1), bad),
+                         (calls(s, max_len=-1), bad), (calls(s, ntok=2 ** 30 + 1), big),
+                         (calls(s, nseq=2 ** 30), big)):
+        for call in many:
+            with pytest.raises(nsd.NsdError) as e:
+                call()
+            assert e.value.status == status
+    for call in calls(s)[1:]:
+        with pytest.raises(nsd.NsdError) as e:
+            call()
+        assert e.value.status == nsd.NSD_ERR_WORKSPACE
+    for hole in (2, 5, 6, 7, 8, 10):
+        args = [10, 2, P, 10, s, P, P, P, P, None, P, None, ws]
+        args[hole] = None
+        with pytest.raises(nsd.NsdError) as e:
+            nsd.nsd_attn_decay(*args)
+        assert e.value.status == bad
+    for hole in (2, 5, 6, 7, 8, 10, 12, 13, 14):
+        args = [10, 2, P, 10, s, P, P, P, P, None, P, None, P, P, P, None, None, ws]
+        args[hole] = None
+        with pytest.raises(nsd.NsdError) as e:
+            nsd.nsd_attn_decay_vjp(*args)
+        assert e.value.status == bad
+    for place in (9, 11):  # dS0 over what is read
+        args = [10, 2, P, 10, s, P, P, P, P, None, P, None, P, P, P, None, 2 * P, ws]
+        args[place] = 2 * P
+        with pytest.raises(nsd.NsdError, match="shares memory"):
+            nsd.nsd_attn_decay_vjp(*args)
+    for args in ((-1, P, 9), (4, P, -1), (4, None, 3)):
+        with pytest.raises(nsd.NsdError) as e:
+            nsd.nsd_attn_decay_step(*args, s, P, P, P, P, P, P)
+        assert e.value.status == bad
+    for hole in range(4, 10):
+        args = [4, P, 9, s, P, P, P, P, P, P]
+        args[hole] = None
+        with pytest.raises(nsd.NsdError) as e:
+            nsd.nsd_attn_decay_step(*args)
+        assert e.value.status == bad
+    nsd.nsd_attn_decay(0, 0, None, 0, s, None, None, None, None, None, None, None, None)
+    nsd.nsd_attn_decay_step(0, None, 0, s, None, None, None, None, None, None)
+
+
+def test_tensors_of_other_shapes_are_refused():
+    q, k, v, o = (torch.zeros(5, w) for w in (32, 16, 12, 24))
+    s = nsd.decay_desc(4, 2, 8, 6, q, k, v, o, 1.0)
+    ptr, g, S = torch.zeros(3, dtype=torch.int32), torch.zeros(4), torch.zeros(2, 4, 8, 6)
+    good = dict(Q=q, K=k, V=v, decay=g, S0=S, O=o, S1=S)
+    for name, t in (("Q", q[:4]), ("K", k.bfloat16()), ("V", torch.zeros(5, 13)[:, :12]),
+                    ("O", torch.zeros(5, 48)[:, ::2]), ("decay", g[:3]), ("S0", S[:1]),
+                    ("S1", S.double())):
+        with pytest.raises(ValueError, match=name):
+            nsd.nsd_attn_decay(5, 2, ptr, 5, s, **{**good, name: t}, ws=None)
+    with pytest.raises(ValueError, match="seqptr"):
+        nsd.nsd_attn_decay(5, 2, ptr[:2], 5, s, **good, ws=None)
+    with pytest.raises(ValueError, match="dK"):
+        nsd.nsd_attn_decay_vjp(5, 2, ptr, 5, s, q, k, v, g, S, o, S, q, k[:, :15], v, None, None,
+                               None)
+    with pytest.raises(ValueError, match="state"):
+        nsd.nsd_attn_decay_step(2, None, 3, s, q, k, v, g, S, o)
+    with pytest.raises(ValueError, match="v:"):
+        nsd.decay_desc(4, 2, 8, 6, q, k, v[:, :11], o, 1.0)
+    with pytest.raises(ValueError, match="o:"):
+        nsd.decay_desc(4, 2, 8, 6, q, k, v, o.bfloat16(), 1.0)
+
+
+# ------------------------------------------------- the definition in 64 bits
+
+def definition(x, lens, scale, magnitude=False):
+    """Outputs, states and gradients of x (arrays q [n, H, d], k [n, Hk, d], v, g [H], s0
+    [B, H, d, dv], and the upstream do, ds1), sums over all pairs of tokens; of the
+    magnitudes of everything where that is asked for."""
+    a = {i: (np.abs(t) if magnitude and i != "g" else t) for i, t in x.items()}
+    q, k, v, g, s0, do, ds1 = (a[i] for i in ("q", "k", "v", "g", "s0", "do", "ds1"))
+    n, H, d = q.shape
+    grp = H // k.shape[1]
+    out = dict(o=np.zeros((n, H, v.shape[-1])), s1=np.zeros_like(s0), dq=np.zeros_like(q),
+               dk=np.zeros_like(k), dv=np.zeros_like(v), dg=np.zeros(H), ds0=np.zeros_like(s0))
+    first = x.get("first", 0)
+
+    def power(n_, h):
+        with np.errstate(invalid="ignore"):
+            return np.where(n_ == 0, 1.0, np.exp(g[h] * n_))
+
+    for b, m in enumerate(lens):
+        rows = slice(first, first + m)
+        first += m
+        t = np.arange(m, dtype=float)
+        apart = t[:, None] - t
+        for h in range(H):
+            e = h // grp
+            qq, kk, vv, up = q[rows, h], k[rows, e], v[rows, e], do[rows, h]
+            w = np.where(apart >= 0, power(np.maximum(apart, 0), h), 0.0) * scale
+            sc, u = qq @ kk.T, up @ vv.T
+            since = power(t + 1, h)[:, None] * scale
+            rest = power(m - 1 - t, h)[:, None]
+            whole = power(np.float64(m), h)
+            S, R = s0[b, h], ds1[b, h]
+            out["o"][rows, h] = (w * sc) @ vv + since * (qq @ S)
+            out["s1"][b, h] = (rest * kk).T @ vv + whole * S
+            out["dq"][rows, h] = (w * u) @ kk + since * (up @ S.T)
+            out["dk"][rows, e] += (w * u).T @ qq + rest * (vv @ R.T)
+            out["dv"][rows, e] += (w * sc).T @ up + rest * (kk @ R)
+            out["ds0"][b, h] = (since * qq).T @ up + whole * R
+            out["dg"][h] += (w * apart * sc * u).sum() + \
+                ((t + 1)[:, None] * since * (qq @ S) * up).sum() + \
+                ((m - 1 - t)[:, None] * rest * (kk @ R) * vv).sum() + m * whole * (S * R).sum()
+    return out
+
+
+def test_the_gradients_are_those_of_the_definition():
+    rng = np.random.default_rng(0)
+    lens, H, Hk, d, dv, scale = [4, 0, 1, 3], 4, 2, 3, 2, 0.7
+    n = sum(lens)
+    x = dict(q=rng.standard_normal((n, H, d)), k=rng.standard_normal((n, Hk, d)),
+             v=rng.standard_normal((n, Hk, dv)), g=-rng.random(H),
+             s0=rng.standard_normal((4, H, d, dv)), do=rng.standard_normal((n, H, dv)),
+             ds1=rng.standard_normal((4, H, d, dv)))
+    got = definition(x, lens, scale)
+    h = 1e-6
+    for name, grad in (("q", "dq"), ("k", "dk"), ("v", "dv"), ("g", "dg"), ("s0", "ds0")):
+        for i in np.ndindex(x[name].shape):
+            side = []
+            for sign in (1, -1):
+                old = x[name][i]
+                x[name][i] = old + sign * h
+                y = definition(x, lens, scale)
+                side.append((y["o"] * x["do"]).sum() + (y["s1"] * x["ds1"]).sum())
+                x[name][i] = old
+            assert abs((side[0] - side[1]) / (2 * h) - got[grad][i]) <= 1e-7, (name, i)
+    # and the definition's outputs are the recurrence's
+    for h in range(H):
+        S, first = x["s0"].copy(), 0
+        for b, m in enumerate(lens):
+            for t in range(first, first + m):
+                S[b, h] = np.exp(x["g"][h]) * S[b, h] + \
+                    np.outer(x["k"][t, h // 2], x["v"][t, h // 2])
+                assert np.allclose(scale * x["q"][t, h] @ S[b, h], got["o"][t, h], atol=1e-12)
+            first += m
+        assert np.allclose(S[:, h], got["s1"][:, h], atol=1e-12)
+
+
+# ------------------------------------------------------------- on the GPU
+
+class Case:
+    """Seeded rows of packed sequences on the GPU, `gap` values between them, `lead` rows
+    before the sequences and some behind."""
+
+    def __init__(self, lens, H, Hk, d, dv, dtype, decays=None, gap=0, lead=0, seed=0, scale=0.3):
+        self.lens, self.H, self.Hk, self.d, self.dv = lens, H, Hk, d, dv
+        self.dtype, self.scale, self.lead, self.B = dtype, float(np.float32(scale)), lead, len(lens)
+        self.n = lead + sum(lens) + 3
+        self.gen = torch.Generator().manual_seed(seed)
+        w = dict(q=H * d, k=Hk * d, v=Hk * dv, do=H * dv)
+        self.wide = {i: self.rows(x, gap) for i, x in w.items()}
+        self.t = {i: self.wide[i][:, :x] for i, x in w.items()}
+        outs = dict(o=H * dv, dq=H * d, dk=Hk * d, dv=Hk * dv)
+        self.wide_out = {i: self.rows(x, gap) for i, x in outs.items()}
+        self.out = {i: self.wide_out[i][:, :x] for i, x in outs.items()}
+        if decays is None:
+            decays = [-(2.0 ** -x) for x in np.linspace(0.5, 9, H)]
+        self.g = torch.tensor(decays, dtype=torch.float32).cuda()
+        self.s0, self.ds1 = (torch.randn(self.B, H, d, dv, generator=self.gen).cuda()
+                             for _ in range(2))
+        self.seqptr = torch.tensor(np.cumsum([lead] + list(lens)), dtype=torch.int32).cuda()
+        self.desc = nsd.decay_desc(H, Hk, d, dv, self.t["q"], self.t["k"], self.t["v"],
+                                   self.out["o"], scale)
+
+    def rows(self, width, gap):
+        return torch.randn(self.n, width + gap, generator=self.gen).to(T[self.dtype]).cuda()
+
+    def ws(self, max_len, gradient):
+        n = nsd.nsd_attn_decay_workspace_size(self.n, self.B, max_len, self.desc, gradient)
+        return torch.full((n,), 0x7F, dtype=torch.uint8, device="cuda")
+
+    def forward(self, max_len=None, start=True, s1=None):
+        max_len = max(self.lens) if max_len is None else max_len
+        s1 = torch.full_like(self.s0, 7.0) if s1 is None else s1
+        nsd.nsd_attn_decay(self.n, self.B, self.seqptr, max_len, self.desc, self.t["q"],
+                           self.t["k"], self.t["v"], self.g, self.s0 if start else None,
+                           self.out["o"], s1, self.ws(max_len, False))
+        return s1
+
+    def backward(self, max_len=None, start=True, decay=True):
+        max_len = max(self.lens) if max_len is None else max_len
+        dg = torch.full((self.H,), 7.0, device="cuda") if decay else None
+        ds0 = torch.full_like(self.s0, 7.0) if start else None
+        nsd.nsd_attn_decay_vjp(self.n, self.B, self.seqptr, max_len, self.desc, self.t["q"],
+                               self.t["k"], self.t["v"], self.g, self.s0 if start else None,
+                               self.t["do"], self.ds1 if start else None, self.out["dq"],
+                               self.out["dk"], self.out["dv"], dg, ds0, self.ws(max_len, True))
+        return dg, ds0
+
+    def arrays(self, start=True):
+        def a(t, *shape):
+            return t.double().cpu().numpy().reshape(*shape)
+        n, H, Hk, d, dv = self.n, self.H, self.Hk, self.d, self.dv
+        zero = 1.0 if start else 0.0
+        return dict(q=a(self.t["q"], n, H, d), k=a(self.t["k"], n, Hk, d),
+                    v=a(self.t["v"], n, Hk, dv), do=a(self.t["do"], n, H, dv), g=a(self.g, H),
+                    s0=a(self.s0, *self.s0.shape) * zero, ds1=a(self.ds1, *self.s0.shape) * zero,
+                    first=self.lead)
+
+    def check(self, max_len=None, start=True, decay=True):
+        before = {i: t.clone() for i, t in self.wide_out.items()}
+        s1 = self.forward(max_len, start)
+        dg, ds0 = self.backward(max_len, start, decay)
+        x = self.arrays(start)
+        ref = definition(x, self.lens, self.scale)
+        mag = definition({**x, "first": self.lead}, self.lens, self.scale, magnitude=True)
+        flat = definition({**x, "g": np.zeros(self.H)}, self.lens, self.scale, magnitude=True)
+        longest = max(self.lens + [0])
+        room = (self.d + self.dv + 2 * longest + 32) * U
+        tiny = {i: 2.0 ** -126 * (t + longest + self.d + self.dv) for i, t in flat.items()}
+
+        def near(name, got, want, tol):
+            worst = np.max(np.abs(got - want) / np.maximum(tol, 1e-300), initial=0.0)
+            assert worst <= 1.0, (name, worst)
+
+        live = slice(self.lead, self.lead + sum(self.lens))
+        for name, t in self.out.items():
+            got = t.double().cpu().numpy().reshape(ref[name].shape)[live]
+            near(name, got, ref[name][live], (room + PARTS[self.dtype]) * mag[name][live] +
+                 HALF[self.dtype] * np.abs(ref[name][live]) + tiny[name][live])
+            # rows of no sequence, and what lies between rows
+            w = t.shape[1]
+            wide, old = self.wide_out[name], before[name]
+            assert torch.equal(wide[:, w:], old[:, w:])
+            assert torch.equal(wide[:live.start], old[:live.start])
+            assert torch.equal(wide[live.stop:], old[live.stop:])
+        states = [("s1", s1)] + ([("ds0", ds0)] if start else []) + ([("dg", dg)] if decay else [])
+        for name, t in states:
+            got = t.double().cpu().numpy()
+            # the decay's gradient adds up over heads' columns and tokens once more
+            more = sum(self.lens) * U if name == "dg" else 0.0
+            near(name, got, ref[name], (room + more) * mag[name] + tiny[name])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lens", [[1], [2], [31, 0, 33], [32], [63, 1, 65], [64, 64], [127, 128, 129],
+                                  [0], [0, 0, 5], [255, 256], [200, 1, 0, 77]])
+def test_lengths(lens, dtype):
+    Case(lens, 2, 2, 16, 24, dtype, lead=2).check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d, dv", [(1, 1), (3, 5), (16, 16), (31, 33), (32, 64), (40, 72), (64, 64),
+                                   (64, 128), (65, 130), (128, 128), (100, 200), (130, 20),
+                                   (20, 130), (256, 256), (255, 129)])
+def test_widths(d, dv, dtype):
+    Case([70, 33], 2, 1, d, dv, dtype, gap=d % 3).check(start=d % 2 == 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("H, Hk", [(1, 1), (6, 3), (8, 1), (5, 5)])
+def test_heads(H, Hk, dtype):
+    Case([90, 40], H, Hk, 24, 40, dtype, gap=1).check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d, dv, H, Hk", [(16, 16, 2, 1), (64, 128, 1, 1), (40, 72, 2, 2)])
+@pytest.mark.parametrize("lens", [[1000], [513, 0, 1, 700, 256], [257, 512, 3]])
+def test_sequences_in_segments(lens, d, dv, H, Hk, dtype):
+    """Sequences past the segments' length (256 here)."""
+    c = Case(lens, H, Hk, d, dv, dtype, lead=1)
+    whole = nsd.nsd_attn_decay_workspace_size(c.n, c.B, 1, c.desc)
+    assert nsd.nsd_attn_decay_workspace_size(c.n, c.B, max(lens), c.desc) > whole
+    c.check()
+    c.check(start=False)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_longer_than_said(dtype):
+    Case([300, 700], 2, 1, 32, 32, dtype).check(max_len=1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lens", [[130, 40], [600]])
+def test_decays(lens, dtype):
+    """None, hardly any, all at once, and so strong that powers vanish."""
+    Case(lens, 5, 5, 16, 16, dtype, decays=[0.0, -1e-6, -20.0, -100.0, -0.5]).check()
+    c = Case(lens, 2, 2, 16, 16, dtype, decays=[-math.inf, -math.inf])
+    c.check(decay=False)
+
+
+@pytest.mark.gpu
+def test_results_are_the_same_every_time():
+    c = Case([700, 300], 4, 2, 64, 64, "bf16")
+    runs = []
+    for _ in range(3):
+        s1 = c.forward()
+        dg, ds0 = c.backward()
+        runs.append([t.clone() for t in (*c.out.values(), s1, dg, ds0)])
+    for other in runs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(runs[0], other))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("max_len", [1, 10_000])
+@pytest.mark.parametrize("bad", [math.inf, math.nan])
+def test_numbers_that_are_not_finite_stay_behind_their_token(bad, max_len, dtype):
+    lens, H, d = [200, 400, 90], 2, 32
+    room = (2 * d + 2 * max(lens) + 32) * U
+    mag = definition(Case(lens, H, H, d, d, dtype).arrays(), lens, 0.3, magnitude=True)
+    for name in ("v", "k", "q", "do"):
+        c = Case(lens, H, H, d, d, dtype)
+        want_s1 = c.forward(max_len)
+        want_dg = c.backward(max_len)
+        want = {i: t.clone() for i, t in c.out.items()}
+        at = 200 + 77
+        c.t[name][at, d + 3] = bad  # of sequence 1, head 1
+        s1 = c.forward(max_len)
+        c.backward(max_len)
+        for out, later in (("o", True), ("dq", True), ("dk", False), ("dv", False)):
+            got = c.out[out].view(c.n, H, -1)
+            old = want[out].view(c.n, H, -1)
+            touched = torch.zeros(c.n, H, dtype=torch.bool, device="cuda")
+            span = slice(at, 600) if later else slice(200, at + 1)
+            touched[span, 1] = True
+            other = torch.ones(c.n, H, dtype=torch.bool, device="cuda")
+            other[200:600, 1] = False  # other sequences and heads: the same bits
+            assert torch.equal(got[other], old[other]), (name, out)
+            # the head's tokens on the other side: summed in another order at most
+            clean = (~touched & ~other).cpu().numpy()
+            diff = (got.double() - old.double()).cpu().numpy()[clean]
+            assert np.all(np.abs(diff) <= 2 * (room + PARTS[dtype]) * mag[out][clean] +
+                          2 * HALF[dtype] * old.double().abs().cpu().numpy()[clean]), (name, out)
+        assert torch.equal(s1[[0, 2]], want_s1[[0, 2]]) and torch.equal(s1[1, 0], want_s1[1, 0])
+        if name in ("v", "k"):
+            assert not torch.isfinite(s1[1, 1]).all()
+        if name in ("v", "q", "k"):
+            assert not torch.isfinite(c.out["o"].view(c.n, H, -1)[at, 1].float()).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_states_carry_a_sequence_on(dtype):
+    """Two calls, the second from the first's states, are one call; in place, too."""
+    c = Case([600], 3, 3, 40, 24, dtype)
+    s1 = c.forward(start=False)
+    o = c.out["o"].clone()
+    x = c.arrays(False)
+    mag = definition(x, [600], c.scale, magnitude=True)
+    state = torch.zeros_like(s1)
+    ends = [0, 65, 66, 300, 600]
+    for a, b in zip(ends, ends[1:]):
+        ptr = torch.tensor([a, b], dtype=torch.int32, device="cuda")
+        nsd.nsd_attn_decay(c.n, 1, ptr, b - a, c.desc, c.t["q"], c.t["k"], c.t["v"], c.g, state,
+                           c.out["o"], state, c.ws(b - a, False))
+    room = 2 * (40 + 24 + 1200 + 32) * U
+    got, want = (t[:600].double().cpu().numpy().reshape(600, 3, 24) for t in (c.out["o"], o))
+    assert np.all(np.abs(got - want) <= (room + 2 * PARTS[dtype]) * mag["o"][:600]
+                  + 2 * HALF[dtype] * np.abs(want))
+    assert np.all((state - s1).abs().double().cpu().numpy() <= room * mag["s1"])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d, dv, H, Hk", [(16, 16, 2, 1), (64, 128, 4, 4), (40, 72, 6, 3), (5, 7, 3, 1),
+                                          (256, 256, 1, 1), (1, 1, 2, 2), (64, 130, 2, 2)])
+@pytest.mark.parametrize("rows", [1, 5, 300])
+def test_single_tokens(rows, d, dv, H, Hk, dtype):
+    """One token each on states in scattered slots, some rows padding."""
+    c = Case([rows], H, Hk, d, dv, dtype, gap=1)
+    slots = rows + 4
+    state = torch.randn(slots, H, d, dv, generator=c.gen).cuda()
+    slot = torch.randperm(slots, generator=c.gen)[:rows].int()
+    if rows > 3:
+        slot[1], slot[2] = -1, slots
+    old = state.clone()
+    nsd.nsd_attn_decay_step(rows, slot.cuda(), slots, c.desc, c.t["q"], c.t["k"], c.t["v"], c.g,
+                            state, c.out["o"])
+    x = c.arrays()
+    S = old.double().cpu().numpy()
+    want, mag = S.copy(), np.abs(S)
+    o, om = np.zeros((rows, H, dv)), np.zeros((rows, H, dv))
+    grp = H // Hk
+    for r, sl in enumerate(slot.tolist()):
+        if not 0 <= sl < slots:
+            continue
+        for h in range(H):
+            kv = np.outer(x["k"][r, h // grp], x["v"][r, h // grp])
+            want[sl, h] = np.exp(x["g"][h]) * S[sl, h] + kv
+            mag[sl, h] = np.exp(x["g"][h]) * np.abs(S[sl, h]) + np.abs(kv)
+            o[r, h] = c.scale * x["q"][r, h] @ want[sl, h]
+            om[r, h] = c.scale * np.abs(x["q"][r, h]) @ mag[sl, h]
+    assert np.all(np.abs(state.double().cpu().numpy() - want) <= 4 * U * mag)
+    got = c.out["o"][:rows].double().cpu().numpy().reshape(rows, H, dv)
+    assert np.all(np.abs(got - o) <= (d + 8) * U * om + HALF[dtype] * np.abs(o))
+    untouched = [i for i in range(slots) if i not in slot.tolist()]
+    assert torch.equal(state[untouched], old[untouched])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_that_share_a_slot_are_its_tokens(dtype):
+    """As the chunked call on their tokens in order."""
+    H, d, dv = 2, 24, 40
+    order = [3, 0, 3, 3, 1, 0, 3]
+    c = Case([7], H, H, d, dv, dtype)
+    state = torch.randn(5, H, d, dv, generator=c.gen).cuda()
+    old = state.clone()
+    slot = torch.tensor(order, dtype=torch.int32, device="cuda")
+    nsd.nsd_attn_decay_step(7, slot, 5, c.desc, c.t["q"], c.t["k"], c.t["v"], c.g, state,
+                            c.out["o"])
+    one, o1 = old.clone(), torch.zeros_like(c.out["o"][:7])
+    for r, sl in enumerate(order):
+        s = nsd.decay_desc(H, H, d, dv, c.t["q"][:1], c.t["k"][:1], c.t["v"][:1], o1[:1], c.scale)
+        nsd.nsd_attn_decay_step(1, slot[r:r + 1], 5, s, c.t["q"][r:r + 1], c.t["k"][r:r + 1],
+                                c.t["v"][r:r + 1], c.g, one, o1[r:r + 1])
+    tol = (d + 8) * U * 50
+    assert (state - one).abs().max().item() <= tol
+    assert (c.out["o"][:7].float() - o1.float()).abs().max().item() <= \
+        tol + 2 * HALF[dtype] * o1.float().abs().max().item()
+    assert torch.equal(state[[2, 4]], old[[2, 4]])
+
+
+@pytest.mark.gpu
+def test_steps_go_on_where_a_prompt_ends():
+    """A prompt by chunks, then tokens one by one, against one call over all."""
+    H, Hk, d, dv, n = 4, 2, 32, 48, 150
+    c = Case([n], H, Hk, d, dv, "f32")
+    s1 = c.forward(start=False)
+    want = c.out["o"].clone()
+    state = torch.zeros(1, H, d, dv, device="cuda")
+    ptr = torch.tensor([0, 140], dtype=torch.int32, device="cuda")
+    nsd.nsd_attn_decay(c.n, 1, ptr, 140, c.desc, c.t["q"], c.t["k"], c.t["v"], c.g, None,
+                       c.out["o"], state, c.ws(140, False))
+    for t in range(140, n):
+        row = [c.t[i][t:t + 1].contiguous() for i in ("q", "k", "v")]
+        o = torch.empty(1, H * dv, device="cuda")
+        s = nsd.decay_desc(H, Hk, d, dv, *row, o, c.scale)
+        nsd.nsd_attn_decay_step(1, None, 1, s, *row, c.g, state, o)
+        c.out["o"][t] = o[0]
+    mag = definition(c.arrays(False), [n], c.scale, magnitude=True)
+    room = 2 * (d + dv + 2 * n + 32) * U
+    assert np.all((c.out["o"][:n] - want[:n]).abs().double().cpu().numpy().reshape(n, H, dv)
+                  <= room * mag["o"][:n])
+    assert np.all((state - s1).abs().double().cpu().numpy() <= room * mag["s1"])
+
+
+@pytest.mark.gpu
+def test_a_captured_step_follows_its_inputs():
+    """Both calls captured; rows and sequences change between replays."""
+    c = Case([500, 100, 200], 4, 2, 32, 64, "bf16")
+    ws = [c.ws(800, False), c.ws(800, True)]
+    s1, ds0 = torch.empty_like(c.s0), torch.empty_like(c.s0)
+    dg = torch.empty(4, device="cuda")
+
+    def step():
+        args = (c.n, 3, c.seqptr, 800, c.desc, c.t["q"], c.t["k"], c.t["v"], c.g, c.s0)
+        nsd.nsd_attn_decay(*args, c.out["o"], s1, ws[0])
+        nsd.nsd_attn_decay_vjp(*args, c.t["do"], c.ds1, c.out["dq"], c.out["dk"], c.out["dv"], dg,
+                               ds0, ws[1])
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    outs = [*c.out.values(), s1, ds0, dg]
+    for lens in ([0, 800, 0], [1, 2, 797], [300, 250, 250]):
+        c.seqptr.copy_(torch.tensor(np.cumsum([0] + lens), dtype=torch.int32))
+        c.wide["q"].copy_(torch.randn(c.wide["q"].shape))
+        step()
+        want = [o.clone() for o in outs]
+        for o in outs:
+            o.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(outs, want):
+            if a.dim() == 2:
+                a, b = a[:800], b[:800]
+            assert torch.equal(a, b)
