@@ -1129,8 +1129,8 @@ nsd_status nsd_qk_append(int32_t ntok, const nsd_qk *s, const void *Q, const voi
  * so that a sequence is carried on by its states alone.  Q: [ntok][heads][d], K:
  * [ntok][kv_heads][d], V: [ntok][kv_heads][dv], O: [ntok][heads][dv], all of one
  * nsd_dtype, with ldq, ldk, ldv, ldo values from one row to the next; head h reads
- * key head h / (heads / kv_heads).  d, dv <= 256, any alignment.  decay: fp32 [heads],
- * the g_h: at most 0 (-infinity: a token sees itself alone).  States are fp32,
+ * key head h / (heads / kv_heads).  d, dv <= 256, distances up to 2^22 values, any
+ * alignment.  decay: fp32 [heads], the g_h: at most 0 (-infinity: a token sees itself alone).  States are fp32,
  * [heads][d][dv] for each sequence or slot, whatever the type of the rows.
  *
  * Sequence s is the rows seqptr[s] to seqptr[s + 1] - 1 (int32 [nseq + 1],

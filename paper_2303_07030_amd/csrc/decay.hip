@@ -225,6 +225,8 @@ __global__ __launch_bounds__(kStepThreads) void decay_step_kernel(Step a) {
 
 // ------------------------------------------------------------------- host
 
+constexpr int kMaxDistance = 1 << 22;
+
 nsd_status check_decay(const nsd_decay *s) {
     NSD_REQUIRE(s != nullptr, "descriptor is NULL");
     NSD_REQUIRE(s->heads >= 1 && s->kv_heads >= 1 && s->heads % s->kv_heads == 0,
@@ -237,6 +239,9 @@ nsd_status check_decay(const nsd_decay *s) {
     NSD_REQUIRE(s->ldq >= (int64_t)s->heads * s->d && s->ldk >= (int64_t)s->kv_heads * s->d &&
                     s->ldv >= (int64_t)s->kv_heads * s->dv && s->ldo >= (int64_t)s->heads * s->dv,
                 "row distances below the heads' widths");
+    // a chunk's places in its rows are counted in 32 bits
+    if (std::max({s->ldq, s->ldk, s->ldv, s->ldo}) > kMaxDistance)
+        return fail(NSD_ERR_UNSUPPORTED, "rows more than %d values apart", kMaxDistance);
     return NSD_OK;
 }
 

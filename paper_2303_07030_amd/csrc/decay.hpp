@@ -170,52 +170,68 @@ __device__ __forceinline__ int place(int k) {
 }
 
 // A chunk's rows of one matrix on their way to LDS: four rows and CV columns a unit.
-template <class T, int W>
+// TAIL: the rows' widths are no multiples of CV.
+template <class T, int W, bool TAIL>
 struct Stage {
     static constexpr int C = kChunkOf<T>;
     static constexpr int CV = sizeof(T) == 2 && W >= 128 ? 8 : 4;
     static constexpr int PIECES = W / CV;
     static constexpr int UNITS = C / 4 * PIECES;
     static constexpr int U = (UNITS + kScanThreads - 1) / kScanThreads;
+    static constexpr bool EXACT = UNITS % kScanThreads == 0;
     T x[U][4][CV];
 
-    // rows i < len from token t0 + i * dir; columns from col0 on
-    __device__ __forceinline__ void load(const Rows &m, int h, int col0, int64_t t0, int dir, int len) {
-        const T *p = static_cast<const T *>(m.p) + (int64_t)(h / m.grp) * m.width + col0;
-        const int width = m.width - col0;
+    // (threads beyond the units repeat the last one, and store nothing)
+    __device__ __forceinline__ int unit(int u) const {
+        const int n = (int)threadIdx.x + u * kScanThreads;
+        return EXACT ? n : min(n, UNITS - 1);
+    }
+    // Rows i < len (at least one) from token t0 on, or back; columns from col0 on.  Nothing here
+    // depends on a lane's place: what is beyond a row or the chunk reads a neighbour of it,
+    // and is cleared by clear().
+    __device__ __forceinline__ void load(const Rows &m, int h, int col0, int64_t t0, bool rev, int len) {
+        const T *base = static_cast<const T *>(m.p) + (rev ? t0 - (len - 1) : t0) * m.ld +
+                        (int64_t)(h / m.grp) * m.width + col0;
+        const int width = m.width - col0, ld = (int)m.ld;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int unit = threadIdx.x + u * kScanThreads;
-            const int i0 = unit / PIECES * 4, c = unit % PIECES * CV;
-            const int left = width - c;
+            const int i0 = unit(u) / PIECES * 4, c = unit(u) % PIECES * CV;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-#pragma unroll
-                for (int e = 0; e < CV; ++e) x[u][r][e] = T(0);
-                if ((UNITS % kScanThreads && unit >= UNITS) || i0 + r >= len || left <= 0) continue;
-                const T *row = p + (t0 + (int64_t)(i0 + r) * dir) * m.ld + c;
-                if (left >= CV) {
-                    __builtin_memcpy(x[u][r], row, sizeof x[u][r]);
+                const int i = min(i0 + r, len - 1);
+                const uint32_t row = (uint32_t)((rev ? len - 1 - i : i) * ld);
+                if constexpr (!TAIL) {
+                    __builtin_memcpy(x[u][r], base + (row + (uint32_t)min(c, width - CV)), sizeof x[u][r]);
                 } else {
 #pragma unroll
-                    for (int e = 0; e < CV; ++e)
-                        if (e < left) x[u][r][e] = row[e];
+                    for (int e = 0; e < CV; ++e) x[u][r][e] = base[row + (uint32_t)min(c + e, width - 1)];
                 }
             }
+        }
+    }
+    __device__ __forceinline__ void clear(int width, int len) {
+        if (len == C && width >= W) return;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i0 = unit(u) / PIECES * 4, c = unit(u) % PIECES * CV;
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int e = 0; e < CV; ++e)
+                    if (i0 + r >= len || c + (TAIL ? e : 0) >= width) x[u][r][e] = T(0);
         }
     }
     // rows of ld values, columns in the order of place()
     __device__ __forceinline__ void store(T *to, int ld) const {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int unit = threadIdx.x + u * kScanThreads;
-            if (UNITS % kScanThreads && unit >= UNITS) continue;
-            const int i0 = unit / PIECES * 4, c = unit % PIECES * CV;
+            if (!EXACT && (int)threadIdx.x + u * kScanThreads >= UNITS) continue;
+            const int i0 = unit(u) / PIECES * 4, c = unit(u) % PIECES * CV;
 #pragma unroll
             for (int r = 0; r < 4; ++r)
 #pragma unroll
-                for (int e = 0; e < CV; e += 4)
-                    __builtin_memcpy(__builtin_assume_aligned(to + (i0 + r) * ld + place(c + e), 8),
+                for (int e = 0; e < CV; e += 4)  // (a multiple of eight and the four behind it)
+                    __builtin_memcpy(__builtin_assume_aligned(to + i0 * ld + place(c) + r * ld + 2 * e, 8),
                                      &x[u][r][e], 4 * sizeof(T));
         }
     }
@@ -223,9 +239,8 @@ struct Stage {
     __device__ __forceinline__ void store_transposed(T *to, int ld) const {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int unit = threadIdx.x + u * kScanThreads;
-            if (UNITS % kScanThreads && unit >= UNITS) continue;
-            const int i0 = unit / PIECES * 4, c = unit % PIECES * CV;
+            if (!EXACT && (int)threadIdx.x + u * kScanThreads >= UNITS) continue;
+            const int i0 = unit(u) / PIECES * 4, c = unit(u) % PIECES * CV;
 #pragma unroll
             for (int e = 0; e < CV; ++e) {
                 const T t[4] = {x[u][0][e], x[u][1][e], x[u][2][e], x[u][3][e]};
@@ -251,44 +266,44 @@ struct Stage {
 // What a scan does: outputs; the states at the segments' ends alone; the gradient of g.
 enum Kind { kOutput, kState, kDerivative };
 
-// LDS of a block.
+// LDS of a block: queries, keys (the scores take their place), keys and values by columns.
 template <class T, int KD, int NV, Kind KIND>
 struct Shared {
     static constexpr int C = kChunkOf<T>;
     static constexpr int VB = kScanWaves * 16 * NV;
     static constexpr int PAD = 16 / sizeof(T);
     static constexpr int LDK = KD + PAD, LDC = C + PAD;
-    static constexpr int SP = KIND == kState ? 0 : kParts<T, KIND == kDerivative ? 3 : 2>;
-    static constexpr int QK = KIND == kState ? 0 : C * LDK;
-    static constexpr size_t bytes =
-        sizeof(T) * (2 * QK + (size_t)KD * LDC + (size_t)VB * LDC + (size_t)SP * C * LDC);
+    static constexpr int NS = KIND == kDerivative ? 3 : 2;  // parts of scores and states
+    static constexpr int SP = kParts<T, NS>;
+    static constexpr int Q = KIND == kState ? 0 : C * LDK;
+    static constexpr int KP = KIND == kState ? 0 : C * LDK > SP * C * LDC ? C * LDK : SP * C * LDC;
+    static constexpr int VALUES = Q + KP + KD * LDC + VB * LDC;
 };
 
 // KD: width of queries and keys, padded; NV: 16 columns of values by a wave; blocks: of the
 // segments' heads' columns, nvb for each head.
-template <class T, int KD, int NV, Kind KIND>
-__global__ __launch_bounds__(kScanThreads) void scan_kernel(Scan a, int32_t nvb) {
+template <class T, int KD, int NV, Kind KIND, bool TAIL>
+__global__ __launch_bounds__(kScanThreads, KD <= 128 ? 2 : 1) void scan_kernel(Scan a, int32_t nvb) {
     using Sh = Shared<T, KD, NV, KIND>;
     constexpr int C = Sh::C, VB = Sh::VB, LDK = Sh::LDK, LDC = Sh::LDC;
     constexpr int KT = KD / 16, KF = KD / 32, IT = C / 16, JF = C / 32;
-    constexpr int NS = KIND == kDerivative ? 3 : 2;  // parts of scores and states
-    constexpr int SP = kParts<T, NS>, VP = kParts<T, 3>;
+    constexpr int NS = Sh::NS, SP = Sh::SP, VP = kParts<T, 3>;
     constexpr bool DERIV = KIND == kDerivative;
-    __shared__ __align__(16) char lds_bytes[Sh::bytes];
-    T *const ldsQ = reinterpret_cast<T *>(lds_bytes);
-    T *const ldsK = ldsQ + Sh::QK;
-    T *const ldsKt = ldsK + Sh::QK;
+    __shared__ __align__(16) T lds[Sh::VALUES];
+    T *const ldsQ = lds;
+    T *const ldsK = ldsQ + Sh::Q;
+    T *const ldsP = ldsK;
+    T *const ldsKt = ldsK + Sh::KP;
     T *const ldsVt = ldsKt + KD * LDC;
-    T *const ldsP = ldsVt + VB * LDC;
-    __shared__ float power[C + 2];
+    __shared__ float power[C + 2], power_low[C + 2];
     __shared__ int unusual[2];
     __shared__ float wave_sum[kScanWaves];
 
     const int lane = threadIdx.x % kWave, n16 = lane % 16, g = lane / 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int64_t unit = xcd_contiguous_tile();
-    const int vb = (int)(unit % nvb), h = (int)(unit / nvb % a.H);
-    const Segment seg(a, (int)(unit / nvb / a.H));
+    const int unit = (int)xcd_contiguous_tile();
+    const int vb = unit % nvb, h = unit / nvb % a.H, id = unit / nvb / a.H;
+    const Segment seg(a, id);
     if (!seg.on) {
         if (DERIV && threadIdx.x == 0) a.sums[unit] = 0.f;
         return;
@@ -296,15 +311,19 @@ __global__ __launch_bounds__(kScanThreads) void scan_kernel(Scan a, int32_t nvb)
     const int col0 = vb * VB;                      // the block's first column
     const int colw = wave * 16 * NV;               // the wave's, within the block
     const int rev = a.rev ? 1 : 0;
-    const double gd = (double)a.decay[h];
-    if (threadIdx.x < C + 2)  // powers of the decay, exact to their last bit; also of -infinity
-        power[threadIdx.x] = threadIdx.x ? (float)exp(gd * (double)threadIdx.x) : 1.f;
+    if (threadIdx.x < C + 2) {
+        // powers of the decay in two numbers, also of -infinity: what one would leave out adds up
+        // over the thousands of chunks that multiply them
+        const double x = threadIdx.x ? exp((double)a.decay[h] * (double)threadIdx.x) : 1.0;
+        power[threadIdx.x] = (float)x;
+        power_low[threadIdx.x] = (float)(x - (double)(float)x);
+    }
     if (threadIdx.x < 2) unusual[threadIdx.x] = 0;
 
     // this lane's part of the state: rows 16 kt + 4 g + r, column n16 of each 16
-    const int64_t sidx = ((int64_t)(a.start_by_seq ? seg.seq : (int)(unit / nvb / a.H)) * a.H + h) * a.per;
     f32x4v S[KT][NV], D[DERIV ? KT : 1][NV];
-    auto each_state = [&](auto f) {
+    auto each_state = [&](const float *from, bool by_seq, auto f) {
+        const float *const p = from + ((int64_t)(by_seq ? seg.seq : id) * a.H + h) * a.per;
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
@@ -312,253 +331,259 @@ __global__ __launch_bounds__(kScanThreads) void scan_kernel(Scan a, int32_t nvb)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int k = 16 * kt + 4 * g + r, c = col0 + colw + 16 * nv + n16;
-                    f(kt, nv, r, k < a.k.width && c < a.v.width, (int64_t)k * a.sk + (int64_t)c * a.sv);
+                    const uint32_t at = (uint32_t)(min(k, a.k.width - 1) * a.sk + min(c, a.v.width - 1) * a.sv);
+                    f(kt, nv, r, k < a.k.width && c < a.v.width, p + at);
                 }
     };
-    each_state([&](int kt, int nv, int r, bool in, int64_t at) {
-        S[kt][nv][r] = in && a.start ? a.start[sidx + at] : 0.f;
-        if (DERIV) D[kt][nv][r] = 0.f;
-    });
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int nv = 0; nv < NV; ++nv) {
+            S[kt][nv] = f32x4v{0.f, 0.f, 0.f, 0.f};
+            if (DERIV) D[kt][nv] = f32x4v{0.f, 0.f, 0.f, 0.f};
+        }
+    if (a.start)
+        each_state(a.start, a.start_by_seq, [&](int kt, int nv, int r, bool in, const float *p) {
+            const float x = *p;
+            S[kt][nv][r] = in ? x : 0.f;
+        });
 
-    Stage<T, KD> xq, xk;
-    Stage<T, VB> xv;
+    Stage<T, KD, TAIL> xq, xk;
+    Stage<T, VB, TAIL> xv;
     const int64_t first = rev ? (int64_t)seg.first + seg.n - 1 : seg.first;
     const int dir = rev ? -1 : 1;
-    auto load = [&](int pos, int len) {
-        const int64_t t0 = first + (int64_t)pos * dir;
-        if (KIND != kState) xq.load(a.q, h, 0, t0, dir, len);
-        xk.load(a.k, h, 0, t0, dir, len);
-        xv.load(a.v, h, col0, t0, dir, len);
-    };
-    // powers of whole chunks in more bits than one number has: thousands of chunks multiply them
-    auto low_part = [&](int n) { return (float)(exp(gd * (double)n) - (double)(float)exp(gd * (double)n)); };
-    const float whole_low = low_part(C);
     float dsum = 0.f;
-    int single = 0, turn = 0;  // tokens that are still taken one by one
-    int pos = 0, len = min(C, seg.n);
-    if (seg.n > 0) load(0, len);
-    while (pos < seg.n) {
-        // ---- the chunk's rows to LDS
-        if (KIND != kState) {
-            xq.store(ldsQ, LDK);
-            xk.store(ldsK, LDK);
+    int single = 0, turn = 0;  // single: tokens that are still taken one by one
+    int pos = 0, len = 0, next = 0, next_len = min(C, seg.n);
+    for (;;) {
+        // ---- the next chunk's rows are on their way while this one's are multiplied
+        if (next < seg.n) {
+            const int64_t t0 = first + (int64_t)next * dir;
+            if (KIND != kState) xq.load(a.q, h, 0, t0, a.rev, next_len);
+            xk.load(a.k, h, 0, t0, a.rev, next_len);
+            xv.load(a.v, h, col0, t0, a.rev, next_len);
         }
-        xk.store_transposed(ldsKt, LDC);
-        xv.store_transposed(ldsVt, LDC);
-        if (KIND != kState && !xv.finite()) unusual[turn] = 1;
-        __syncthreads();
-        // A product with a score of 0 keeps an infinite or missing number of a later token out
-        // of an earlier one's output no more than a sum would: such chunks go token by token.
-        if (KIND != kState && unusual[turn] && len > 1) {
-            single = len;
-            len = 1;
-            load(pos, 1);
-            __syncthreads();
-            continue;
-        }
-        if (threadIdx.x == 0) unusual[turn ^ 1] = 0;
-        if (single > 0) --single;
-        const int next = pos + len, next_len = single > 0 ? 1 : min(C, seg.n - next);
-        if (next < seg.n) load(next, next_len);
-        const float keep = power[len];
-
-        f32x4v O[IT][NV], OD[DERIV ? IT : 1][NV];
-        if constexpr (KIND != kState) {
-            // ---- scores: tile (it, jt) of 16 x 16, jt <= it, shared out among the waves
-            constexpr int TILES = IT * (IT + 1) / 2;
+        if (len > 0) {
+            f32x4v O[IT][NV], OD[DERIV ? IT : 1][NV];
+            if constexpr (KIND != kState) {
+                // ---- scores: tile (it, jt) of 16 x 16, jt <= it, shared out among the waves
+                constexpr int TILES = IT * (IT + 1) / 2;
+                constexpr int ROUNDS = (TILES + kScanWaves - 1) / kScanWaves;
+                float p[ROUNDS][4];
+                int it[ROUNDS], jt[ROUNDS];
 #pragma unroll
-            for (int tile0 = 0; tile0 < TILES; tile0 += kScanWaves) {
-                const int tile = tile0 + wave;
-                if (tile >= TILES) break;
-                const int it = tile >= 6 ? 3 : tile >= 3 ? 2 : tile >= 1 ? 1 : 0;
-                const int jt = tile - it * (it + 1) / 2;
-                f32x4v acc = {0.f, 0.f, 0.f, 0.f};
+                for (int u = 0; u < ROUNDS; ++u) {
+                    const int tile = min(u * kScanWaves + wave, TILES - 1);  // (the last one again)
+                    it[u] = tile >= 6 ? 3 : tile >= 3 ? 2 : tile >= 1 ? 1 : 0;
+                    jt[u] = tile - it[u] * (it[u] + 1) / 2;
+                    f32x4v acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int f = 0; f < KF; ++f)
-                    mma(acc, fragment(ldsK + (16 * jt + n16) * LDK + 32 * f + 8 * g),
-                        fragment(ldsQ + (16 * it + n16) * LDK + 32 * f + 8 * g));
-                const int i = 16 * it + n16, j = 16 * jt + 4 * g;
-                float p[4];
+                    for (int f = 0; f < KF; ++f)
+                        mma(acc, fragment(ldsK + (16 * jt[u] + n16) * LDK + 32 * f + 8 * g),
+                            fragment(ldsQ + (16 * it[u] + n16) * LDK + 32 * f + 8 * g));
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int n = i - j - r;
-                    const float w = power[max(n, 0)] * (DERIV ? (float)n : 1.f);
-                    p[r] = n >= 0 ? acc[r] * a.s_score * w : 0.f;
-                }
-                T part[SP][4];
-                split<T, NS, 4>(p, part);
-#pragma unroll
-                for (int s = 0; s < SP; ++s) {
-                    T *to = ldsP + (s * C + i) * LDC + j;
-                    __builtin_memcpy(__builtin_assume_aligned(to, 8), part[s], 4 * sizeof(T));
-                    if (jt == it && it % 2 == 0) {  // the rest of the 32 columns that products take
-                        const T none[4] = {T(0), T(0), T(0), T(0)};
-                        __builtin_memcpy(__builtin_assume_aligned(to + 16, 8), none, sizeof none);
+                    for (int r = 0; r < 4; ++r) {
+                        const int n = 16 * it[u] + n16 - (16 * jt[u] + 4 * g + r);
+                        const float w = power[max(n, 0)] * (DERIV ? (float)n : 1.f);
+                        p[u][r] = n >= 0 ? acc[r] * a.s_score * w : 0.f;
                     }
                 }
-            }
-            __syncthreads();
-            // ---- from the state
+                __syncthreads();  // the keys were read: the scores take their place
 #pragma unroll
-            for (int it = 0; it < IT; ++it)
+                for (int u = 0; u < ROUNDS; ++u) {
+                    T part[SP][4];
+                    split<T, NS, 4>(p[u], part);
 #pragma unroll
-                for (int nv = 0; nv < NV; ++nv) {
-                    O[it][nv] = f32x4v{0.f, 0.f, 0.f, 0.f};
-                    if (DERIV) OD[it][nv] = f32x4v{0.f, 0.f, 0.f, 0.f};
+                    for (int s = 0; s < SP; ++s) {
+                        T *to = ldsP + (s * C + 16 * it[u] + n16) * LDC + 16 * jt[u] + 4 * g;
+                        __builtin_memcpy(__builtin_assume_aligned(to, 8), part[s], 4 * sizeof(T));
+                        if (jt[u] == it[u] && it[u] % 2 == 0) {  // the rest of 32 columns
+                            const T none[4] = {T(0), T(0), T(0), T(0)};
+                            __builtin_memcpy(__builtin_assume_aligned(to + 16, 8), none, sizeof none);
+                        }
+                    }
                 }
+                // ---- from the state
 #pragma unroll
-            for (int f = 0; f < KF; ++f) {
-                Frag<T> sf[NV][SP], df[DERIV ? NV : 1][SP];
+                for (int it = 0; it < IT; ++it)
 #pragma unroll
-                for (int nv = 0; nv < NV; ++nv) {
-                    float x[8];
+                    for (int nv = 0; nv < NV; ++nv) {
+                        O[it][nv] = f32x4v{0.f, 0.f, 0.f, 0.f};
+                        if (DERIV) OD[it][nv] = f32x4v{0.f, 0.f, 0.f, 0.f};
+                    }
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = S[2 * f + e / 4][nv][e % 4];
-                    split<T, NS>(x, sf[nv]);
-                    if constexpr (DERIV) {
+                for (int f = 0; f < KF; ++f) {
+                    Frag<T> sf[NV][SP], df[DERIV ? NV : 1][SP];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) x[e] = D[2 * f + e / 4][nv][e % 4];
-                        split<T, NS>(x, df[nv]);
+                    for (int nv = 0; nv < NV; ++nv) {
+                        float x[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) x[e] = S[2 * f + e / 4][nv][e % 4];
+                        split<T, NS>(x, sf[nv]);
+                        if constexpr (DERIV) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) x[e] = D[2 * f + e / 4][nv][e % 4];
+                            split<T, NS>(x, df[nv]);
+                        }
+                    }
+#pragma unroll
+                    for (int it = 0; it < IT; ++it) {
+                        const Frag<T> qf = fragment(ldsQ + (16 * it + n16) * LDK + 32 * f + 8 * g);
+#pragma unroll
+                        for (int nv = 0; nv < NV; ++nv)
+#pragma unroll
+                            for (int s = 0; s < SP; ++s) {
+                                mma(O[it][nv], sf[nv][s], qf);
+                                if constexpr (DERIV) mma(OD[it][nv], df[nv][s], qf);
+                            }
                     }
                 }
 #pragma unroll
                 for (int it = 0; it < IT; ++it) {
-                    const Frag<T> qf = fragment(ldsQ + (16 * it + n16) * LDK + 32 * f + 8 * g);
+                    const int i = 16 * it + n16;
+                    const float w = a.s_inter * power[i + 1 - rev];
 #pragma unroll
                     for (int nv = 0; nv < NV; ++nv)
 #pragma unroll
-                        for (int s = 0; s < SP; ++s) {
-                            mma(O[it][nv], sf[nv][s], qf);
-                            if constexpr (DERIV) mma(OD[it][nv], df[nv][s], qf);
-                        }
+                        for (int r = 0; r < 4; ++r)
+                            O[it][nv][r] = DERIV ? w * __builtin_fmaf((float)(i + 1), O[it][nv][r],
+                                                                      OD[it][nv][r])
+                                                 : w * O[it][nv][r];
                 }
+                __syncthreads();
             }
-#pragma unroll
-            for (int it = 0; it < IT; ++it) {
-                const int i = 16 * it + n16;
-                const float w = a.s_inter * power[i + 1 - rev];
-#pragma unroll
-                for (int nv = 0; nv < NV; ++nv)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        O[it][nv][r] = DERIV ? w * __builtin_fmaf((float)(i + 1), O[it][nv][r],
-                                                                  OD[it][nv][r])
-                                             : w * O[it][nv][r];
-            }
-        }
-        // ---- from the chunk's own tokens, and the state behind them
-        const float keep_low = len == C ? whole_low : low_part(len);
-        if constexpr (DERIV) {
+            // ---- from the chunk's own tokens, and the state behind them
+            const float keep = power[len], keep_low = power_low[len];
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
                 for (int nv = 0; nv < NV; ++nv)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        const float x = __builtin_fmaf((float)len, S[kt][nv][r], D[kt][nv][r]);
-                        D[kt][nv][r] = __builtin_fmaf(x, keep, x * keep_low);
+                        if constexpr (DERIV) {
+                            const float x = __builtin_fmaf((float)len, S[kt][nv][r], D[kt][nv][r]);
+                            D[kt][nv][r] = __builtin_fmaf(x, keep, x * keep_low);
+                        }
+                        S[kt][nv][r] = __builtin_fmaf(S[kt][nv][r], keep, S[kt][nv][r] * keep_low);
                     }
-        }
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-            for (int nv = 0; nv < NV; ++nv)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    S[kt][nv][r] = __builtin_fmaf(S[kt][nv][r], keep, S[kt][nv][r] * keep_low);
-#pragma unroll
-        for (int f = 0; f < JF; ++f) {
-            Frag<T> vf[NV], vs[NV][VP], vd[DERIV ? NV : 1][VP];
-#pragma unroll
-            for (int nv = 0; nv < NV; ++nv) {
-                const T *from = ldsVt + (colw + 16 * nv + n16) * LDC + 32 * f + 8 * g;
-                vf[nv] = fragment(from);
-                T v[8];
-                __builtin_memcpy(v, &vf[nv], sizeof v);
-                float x[8];
+            for (int f = 0; f < JF; ++f) {
+                Frag<T> vf[NV], vs[NV][VP], vd[DERIV ? NV : 1][VP];
+                float w[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const int after = len - 1 - (32 * f + 8 * g + e) + rev;
-                    x[e] = after >= 0 ? widened(v[e]) * a.s_update * power[after] : 0.f;
+                    w[e] = after >= 0 ? a.s_update * power[max(after, 0)] : 0.f;
                 }
-                split<T, 3>(x, vs[nv]);
-                if constexpr (DERIV) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        x[e] *= (float)max(len - 1 - (32 * f + 8 * g + e), 0);
-                    split<T, 3>(x, vd[nv]);
-                }
-            }
-            if constexpr (KIND != kState) {
-#pragma unroll
-                for (int it = 2 * f; it < IT; ++it)
-#pragma unroll
-                    for (int s = 0; s < SP; ++s) {
-                        const Frag<T> pf =
-                            fragment(ldsP + (s * C + 16 * it + n16) * LDC + 32 * f + 8 * g);
-#pragma unroll
-                        for (int nv = 0; nv < NV; ++nv) mma(O[it][nv], vf[nv], pf);
-                    }
-            }
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
-                const Frag<T> kf = fragment(ldsKt + (16 * kt + n16) * LDC + 32 * f + 8 * g);
-#pragma unroll
-                for (int nv = 0; nv < NV; ++nv)
-#pragma unroll
-                    for (int s = 0; s < VP; ++s) {
-                        mma(S[kt][nv], kf, vs[nv][s]);
-                        if constexpr (DERIV) mma(D[kt][nv], kf, vd[nv][s]);
-                    }
-            }
-        }
-        // ---- outputs: row i by lane % 16, four columns each
-        if constexpr (KIND != kState) {
-#pragma unroll
-            for (int it = 0; it < IT; ++it) {
-                const int i = 16 * it + n16;
-                if (i >= len) continue;
-                const int64_t t = first + (int64_t)(pos + i) * dir;
 #pragma unroll
                 for (int nv = 0; nv < NV; ++nv) {
-                    const int c = col0 + colw + 16 * nv + 4 * g, left = a.v.width - c;
-                    if (left <= 0) continue;
-                    const float x[4] = {O[it][nv][0], O[it][nv][1], O[it][nv][2], O[it][nv][3]};
-                    if constexpr (DERIV) {
-                        float up[4];
-                        load_left<4, T>(static_cast<const T *>(a.up.p) + t * a.up.ld +
-                                            (int64_t)(h / a.up.grp) * a.up.width + c, left, up);
+                    vf[nv] = fragment(ldsVt + (colw + 16 * nv + n16) * LDC + 32 * f + 8 * g);
+                    T v[8];
+                    __builtin_memcpy(v, &vf[nv], sizeof v);
+                    float x[8];
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) dsum = r < left ? __builtin_fmaf(x[r], up[r], dsum) : dsum;
-                    } else if (a.out32) {
-                        store_left<4, float>(static_cast<float *>(a.out) + t * a.ldo +
+                    for (int e = 0; e < 8; ++e) x[e] = widened(v[e]) * w[e];
+                    split<T, 3>(x, vs[nv]);
+                    if constexpr (DERIV) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            x[e] *= (float)max(len - 1 - (32 * f + 8 * g + e), 0);
+                        split<T, 3>(x, vd[nv]);
+                    }
+                }
+                if constexpr (KIND != kState) {
+#pragma unroll
+                    for (int it = 2 * f; it < IT; ++it)
+#pragma unroll
+                        for (int s = 0; s < SP; ++s) {
+                            const Frag<T> pf =
+                                fragment(ldsP + (s * C + 16 * it + n16) * LDC + 32 * f + 8 * g);
+#pragma unroll
+                            for (int nv = 0; nv < NV; ++nv) mma(O[it][nv], vf[nv], pf);
+                        }
+                }
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt) {
+                    const Frag<T> kf = fragment(ldsKt + (16 * kt + n16) * LDC + 32 * f + 8 * g);
+#pragma unroll
+                    for (int nv = 0; nv < NV; ++nv)
+#pragma unroll
+                        for (int s = 0; s < VP; ++s) {
+                            mma(S[kt][nv], kf, vs[nv][s]);
+                            if constexpr (DERIV) mma(D[kt][nv], kf, vd[nv][s]);
+                        }
+                }
+            }
+            // ---- outputs: row i by lane % 16, four columns each
+            if constexpr (KIND != kState) {
+#pragma unroll
+                for (int it = 0; it < IT; ++it) {
+                    const int i = 16 * it + n16;
+                    const int64_t t = first + (int64_t)(pos + i) * dir;
+#pragma unroll
+                    for (int nv = 0; nv < NV; ++nv) {
+                        const int c = col0 + colw + 16 * nv + 4 * g, left = TAIL ? a.v.width - c : 4;
+                        if (i >= len || c >= a.v.width) continue;
+                        const float x[4] = {O[it][nv][0], O[it][nv][1], O[it][nv][2], O[it][nv][3]};
+                        if constexpr (DERIV) {
+                            float up[4];
+                            load_left<4, T>(static_cast<const T *>(a.up.p) + t * a.up.ld +
+                                                (int64_t)(h / a.up.grp) * a.up.width + c, left, up);
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                dsum = r < left ? __builtin_fmaf(x[r], up[r], dsum) : dsum;
+                        } else if (a.out32) {
+                            store_left<4, float>(static_cast<float *>(a.out) + t * a.ldo +
+                                                     (int64_t)h * a.v.width + c, left, x);
+                        } else {
+                            store_left<4, T>(static_cast<T *>(a.out) + t * a.ldo +
                                                  (int64_t)h * a.v.width + c, left, x);
-                    } else {
-                        store_left<4, T>(static_cast<T *>(a.out) + t * a.ldo +
-                                             (int64_t)h * a.v.width + c, left, x);
+                        }
                     }
                 }
             }
+            __syncthreads();
         }
-        __syncthreads();
+        if (next >= seg.n) break;
+        // ---- to LDS
         pos = next;
         len = next_len;
-        turn ^= 1;
-    }
-    if (a.end) {
-        const int64_t to = ((int64_t)(a.end_by_seq ? seg.seq : (int)(unit / nvb / a.H)) * a.H + h) * a.per;
-        each_state([&](int kt, int nv, int r, bool in, int64_t at) {
-            if (in) a.end[to + at] = S[kt][nv][r];
-        });
-    }
-    if constexpr (DERIV) {  // what the segment adds to the states behind it
-        if (a.back) {
-            const int64_t at0 =
-                ((int64_t)(a.back_by_seq ? seg.seq : (int)(unit / nvb / a.H)) * a.H + h) * a.per;
-            each_state([&](int kt, int nv, int r, bool in, int64_t at) {
-                if (in) dsum = __builtin_fmaf(D[kt][nv][r], a.back[at0 + at], dsum);
-            });
+        for (;;) {
+            xk.clear(a.k.width, len);
+            xv.clear(a.v.width - col0, len);
+            if (KIND != kState) {
+                xq.clear(a.q.width, len);
+                xq.store(ldsQ, LDK);
+                xk.store(ldsK, LDK);
+            }
+            xk.store_transposed(ldsKt, LDC);
+            xv.store_transposed(ldsVt, LDC);
+            if (KIND != kState && !xv.finite()) unusual[turn] = 1;
+            __syncthreads();
+            // A product with a score of 0 keeps an infinite or missing number of a later token
+            // out of an earlier one's output no more than a sum would: such chunks go token by
+            // token.
+            if (KIND == kState || !unusual[turn] || len == 1) break;
+            single = len;
+            len = 1;
+            __syncthreads();
         }
+        turn ^= 1;
+        if (threadIdx.x == 0) unusual[turn] = 0;  // (written again behind the next barrier)
+        if (single > 0) --single;
+        next = pos + len;
+        next_len = single > 0 ? 1 : min(C, seg.n - next);
+    }
+    if (a.end)
+        each_state(a.end, a.end_by_seq, [&](int kt, int nv, int r, bool in, const float *p) {
+            if (in) *const_cast<float *>(p) = S[kt][nv][r];
+        });
+    if constexpr (DERIV) {  // what the segment adds to the states behind it
+        if (a.back)
+            each_state(a.back, a.back_by_seq, [&](int kt, int nv, int r, bool in, const float *p) {
+                const float x = *p;
+                dsum = in ? __builtin_fmaf(D[kt][nv][r], x, dsum) : dsum;
+            });
 #pragma unroll
         for (int m = 1; m < kWave; m <<= 1) dsum += __shfl_xor(dsum, m, kWave);
         if (lane == 0) wave_sum[wave] = dsum;
@@ -584,7 +609,12 @@ nsd_status launch_one(const Scan &a, hipStream_t st) {
     const int nvb = (int)ceil_div(a.v.width, kScanWaves * 16 * NV);
     const int64_t blocks = (int64_t)a.nseg * a.H * nvb;
     if (blocks == 0) return NSD_OK;
-    scan_kernel<T, KD, NV, KIND><<<blocks, kScanThreads, 0, st>>>(a, nvb);
+    // whole pieces of the rows, whatever their alignment
+    constexpr int CV = 16 / sizeof(T);
+    if (a.k.width % CV == 0 && a.v.width % CV == 0)
+        scan_kernel<T, KD, NV, KIND, false><<<blocks, kScanThreads, 0, st>>>(a, nvb);
+    else
+        scan_kernel<T, KD, NV, KIND, true><<<blocks, kScanThreads, 0, st>>>(a, nvb);
     return check_launch("scan_kernel");
 }
 

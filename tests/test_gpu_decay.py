@@ -52,6 +52,7 @@ def calls(s, ntok=10, nseq=2, max_len=10, ws=None):
     (dict(ldv=11), nsd.NSD_ERR_INVALID_ARG), (dict(ldo=23), nsd.NSD_ERR_INVALID_ARG),
     (dict(d=257, ldq=2000, ldk=2000), nsd.NSD_ERR_UNSUPPORTED),
     (dict(dv=257, ldv=2000, ldo=2000), nsd.NSD_ERR_UNSUPPORTED),
+    (dict(ldk=2 ** 22 + 1), nsd.NSD_ERR_UNSUPPORTED),
     (dict(heads=4098, ldq=99999, ldo=99999), nsd.NSD_ERR_UNSUPPORTED)])
 def test_bad_descriptors_are_refused(change, status):
     s = desc(**change)
