@@ -18,7 +18,7 @@ namespace decay {
 
 namespace {
 
-constexpr int kJoinThreads = 256;
+constexpr int kJoinThreads = 256, kMaxScanThreads = 512;
 
 // One element of a head's state of a sequence through the sequence's segments.
 template <int VEC>
@@ -263,7 +263,7 @@ nsd_status check_sizes(int32_t ntok, int32_t nseq, int32_t max_len, const nsd_de
     const int64_t scans = ((int64_t)ntok / segment_tokens(ntok, max_len, s) + nseq) * s->heads *
                           ceil_div(std::max(s->d, s->dv), 64);
     const int64_t joins = join_blocks(nseq, s->heads, (int64_t)s->d * s->dv);
-    if (ntok > INT32_MAX / 2 || std::max(scans, joins) > UINT32_MAX / kScanThreads)
+    if (ntok > INT32_MAX / 2 || std::max(scans, joins) > UINT32_MAX / kMaxScanThreads)
         return fail(NSD_ERR_TOO_LARGE, "%d tokens, %d sequences of %d heads", ntok, nseq, s->heads);
     return NSD_OK;
 }
@@ -281,7 +281,7 @@ struct DecayWs {
         const bool grouped = s->heads != s->kv_heads;
         forth = c.take<float>(states);
         back = dk = dv = sums = nullptr;
-        nvb = (int)ceil_div(s->dv, 64);
+        nvb = (int)ceil_div(s->dv, block_columns(s->dv));
         if (gradient) {
             back = c.take<float>(states);
             dk = c.take<float>(grouped ? (size_t)ntok * s->heads * s->d : 0);

@@ -18,12 +18,12 @@
 //   dO/dg: weights n w^n,  s w^(i+1) ((i+1) Q S + Q T);   T = w^C (T + C S) + sum
 //   (C-1-j) w^(C-1-j) k^T v
 //
-// A block of four waves takes a segment of a sequence, a head and 64 or 128 columns of
-// the values.  A wave's own columns of the state stay in its registers, in 32 bits, in
-// the layout that the products leave and, with the contraction's order within 32
-// places permuted (place() below), the next product takes.  Queries, keys (both ways
-// round), transposed values and the scores are shared through LDS; the next chunk's
-// rows are in flight meanwhile.
+// A block of four or eight waves takes a segment of a sequence, a head and 64 or 128
+// columns of the values, 16 a wave.  A wave's own columns of the state stay in its
+// registers, in 32 bits, in the layout that the products leave and, with the
+// contraction's order within 32 places permuted (place() below), the next product
+// takes.  Queries, keys (both ways round), transposed values and the scores are shared
+// through LDS; the next chunk's rows are in flight meanwhile.
 //
 // bf16: products of bf16 rows are exact, and what is not a bf16 number (scores, states,
 // decayed values) is a sum of two or three of them: two keep 16 bits, far below the
@@ -38,8 +38,6 @@
 namespace nsd {
 namespace decay {
 
-constexpr int kScanThreads = 256;
-constexpr int kScanWaves = kScanThreads / kWave;
 constexpr int kMaxWidth = 256;
 
 template <class T>
@@ -169,21 +167,40 @@ __device__ __forceinline__ int place(int k) {
     return k / 32 * 32 + (u % 4) * 8 + (u / 4) * 4;
 }
 
-// A chunk's rows of one matrix on their way to LDS: four rows and CV columns a unit.
-// TAIL: the rows' widths are no multiples of CV.
-template <class T, int W, bool TAIL>
+// Where place j of row `row` lies in LDS, of rows of C places (128 bytes): 16 bytes are moved
+// together, and rows that lanes write or read at once lie on different banks.
+template <class T>
+__device__ __forceinline__ int spread(int row, int j) {
+    constexpr int B = 16 / sizeof(T);
+    const int x = ((row >> 1 ^ row >> 3) & 1) | (row >> 1 & 2) | (row >> 2 & 4);
+    return row * kChunkOf<T> + ((j / B ^ x) * B | j % B);
+}
+template <class T>
+__device__ __forceinline__ Frag<T> fragment_of(const T *rows, int row, int j) {
+    constexpr int B = 16 / sizeof(T);
+    Frag<T> f;
+#pragma unroll
+    for (int b = 0; b < 8; b += B)
+        __builtin_memcpy(reinterpret_cast<char *>(&f) + b * sizeof(T),
+                         __builtin_assume_aligned(rows + spread<T>(row, j + b), 16), 16);
+    return f;
+}
+
+// A chunk's rows of one matrix on their way to LDS: four rows and four columns a unit.
+// TAIL: the rows' widths are no multiples of four.
+template <class T, int W, int THREADS, bool TAIL>
 struct Stage {
     static constexpr int C = kChunkOf<T>;
-    static constexpr int CV = sizeof(T) == 2 && W >= 128 ? 8 : 4;
+    static constexpr int CV = 4;
     static constexpr int PIECES = W / CV;
     static constexpr int UNITS = C / 4 * PIECES;
-    static constexpr int U = (UNITS + kScanThreads - 1) / kScanThreads;
-    static constexpr bool EXACT = UNITS % kScanThreads == 0;
+    static constexpr int U = (UNITS + THREADS - 1) / THREADS;
+    static constexpr bool EXACT = UNITS % THREADS == 0;
     T x[U][4][CV];
 
     // (threads beyond the units repeat the last one, and store nothing)
     __device__ __forceinline__ int unit(int u) const {
-        const int n = (int)threadIdx.x + u * kScanThreads;
+        const int n = (int)threadIdx.x + u * THREADS;
         return EXACT ? n : min(n, UNITS - 1);
     }
     // Rows i < len (at least one) from token t0 on, or back; columns from col0 on.  Nothing here
@@ -225,26 +242,24 @@ struct Stage {
     __device__ __forceinline__ void store(T *to, int ld) const {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (!EXACT && (int)threadIdx.x + u * kScanThreads >= UNITS) continue;
+            if (!EXACT && (int)threadIdx.x + u * THREADS >= UNITS) continue;
             const int i0 = unit(u) / PIECES * 4, c = unit(u) % PIECES * CV;
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int e = 0; e < CV; e += 4)  // (a multiple of eight and the four behind it)
-                    __builtin_memcpy(__builtin_assume_aligned(to + i0 * ld + place(c) + r * ld + 2 * e, 8),
-                                     &x[u][r][e], 4 * sizeof(T));
+                __builtin_memcpy(__builtin_assume_aligned(to + i0 * ld + place(c) + r * ld, 8), x[u][r],
+                                 sizeof x[u][r]);
         }
     }
-    // columns as rows of ld values
-    __device__ __forceinline__ void store_transposed(T *to, int ld) const {
+    // columns as rows of C places
+    __device__ __forceinline__ void store_transposed(T *to) const {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (!EXACT && (int)threadIdx.x + u * kScanThreads >= UNITS) continue;
+            if (!EXACT && (int)threadIdx.x + u * THREADS >= UNITS) continue;
             const int i0 = unit(u) / PIECES * 4, c = unit(u) % PIECES * CV;
 #pragma unroll
             for (int e = 0; e < CV; ++e) {
                 const T t[4] = {x[u][0][e], x[u][1][e], x[u][2][e], x[u][3][e]};
-                __builtin_memcpy(__builtin_assume_aligned(to + (c + e) * ld + i0, 8), t, sizeof t);
+                __builtin_memcpy(__builtin_assume_aligned(to + spread<T>(c + e, i0), 8), t, sizeof t);
             }
         }
     }
@@ -267,25 +282,24 @@ struct Stage {
 enum Kind { kOutput, kState, kDerivative };
 
 // LDS of a block: queries, keys (the scores take their place), keys and values by columns.
-template <class T, int KD, int NV, Kind KIND>
+template <class T, int KD, int NW, Kind KIND>
 struct Shared {
     static constexpr int C = kChunkOf<T>;
-    static constexpr int VB = kScanWaves * 16 * NV;
-    static constexpr int PAD = 16 / sizeof(T);
-    static constexpr int LDK = KD + PAD, LDC = C + PAD;
+    static constexpr int VB = NW * 16;
+    static constexpr int LDK = KD + 16 / sizeof(T);
     static constexpr int NS = KIND == kDerivative ? 3 : 2;  // parts of scores and states
     static constexpr int SP = kParts<T, NS>;
     static constexpr int Q = KIND == kState ? 0 : C * LDK;
-    static constexpr int KP = KIND == kState ? 0 : C * LDK > SP * C * LDC ? C * LDK : SP * C * LDC;
-    static constexpr int VALUES = Q + KP + KD * LDC + VB * LDC;
+    static constexpr int KP = KIND == kState ? 0 : LDK > SP * C ? C * LDK : SP * C * C;
+    static constexpr int VALUES = Q + KP + KD * C + VB * C;
 };
 
-// KD: width of queries and keys, padded; NV: 16 columns of values by a wave; blocks: of the
-// segments' heads' columns, nvb for each head.
-template <class T, int KD, int NV, Kind KIND, bool TAIL>
-__global__ __launch_bounds__(kScanThreads, KD <= 128 ? 2 : 1) void scan_kernel(Scan a, int32_t nvb) {
-    using Sh = Shared<T, KD, NV, KIND>;
-    constexpr int C = Sh::C, VB = Sh::VB, LDK = Sh::LDK, LDC = Sh::LDC;
+// KD: width of queries and keys, padded; NW: waves, 16 columns of the values each; blocks: of
+// the segments' heads' columns, nvb for each head.
+template <class T, int KD, int NW, Kind KIND, bool TAIL>
+__global__ __launch_bounds__(NW * kWave, KD <= 128 ? 2 : 1) void scan_kernel(Scan a, int32_t nvb) {
+    using Sh = Shared<T, KD, NW, KIND>;
+    constexpr int C = Sh::C, VB = Sh::VB, LDK = Sh::LDK;
     constexpr int KT = KD / 16, KF = KD / 32, IT = C / 16, JF = C / 32;
     constexpr int NS = Sh::NS, SP = Sh::SP, VP = kParts<T, 3>;
     constexpr bool DERIV = KIND == kDerivative;
@@ -294,10 +308,11 @@ __global__ __launch_bounds__(kScanThreads, KD <= 128 ? 2 : 1) void scan_kernel(S
     T *const ldsK = ldsQ + Sh::Q;
     T *const ldsP = ldsK;
     T *const ldsKt = ldsK + Sh::KP;
-    T *const ldsVt = ldsKt + KD * LDC;
+    T *const ldsVt = ldsKt + KD * C;
     __shared__ float power[C + 2], power_low[C + 2];
+    __shared__ float behind[2 * C];  // s_update w^(C - 1 - j (+ 1)) of place j, 0 from C on
     __shared__ int unusual[2];
-    __shared__ float wave_sum[kScanWaves];
+    __shared__ float wave_sum[NW];
 
     const int lane = threadIdx.x % kWave, n16 = lane % 16, g = lane / 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -308,48 +323,47 @@ __global__ __launch_bounds__(kScanThreads, KD <= 128 ? 2 : 1) void scan_kernel(S
         if (DERIV && threadIdx.x == 0) a.sums[unit] = 0.f;
         return;
     }
-    const int col0 = vb * VB;                      // the block's first column
-    const int colw = wave * 16 * NV;               // the wave's, within the block
     const int rev = a.rev ? 1 : 0;
+    const int col0 = vb * VB, colw = wave * 16;  // first columns: the block's; the wave's in it
     if (threadIdx.x < C + 2) {
         // powers of the decay in two numbers, also of -infinity: what one would leave out adds up
         // over the thousands of chunks that multiply them
-        const double x = threadIdx.x ? exp((double)a.decay[h] * (double)threadIdx.x) : 1.0;
-        power[threadIdx.x] = (float)x;
-        power_low[threadIdx.x] = (float)(x - (double)(float)x);
+        const int n = threadIdx.x;
+        const double x = n ? exp((double)a.decay[h] * (double)n) : 1.0;
+        power[n] = (float)x;
+        power_low[n] = (float)(x - (double)(float)x);
+        if (n >= rev && n < C + rev) behind[C - 1 + rev - n] = a.s_update * (float)x;
+        if (n < C) behind[C + n] = 0.f;
     }
     if (threadIdx.x < 2) unusual[threadIdx.x] = 0;
 
-    // this lane's part of the state: rows 16 kt + 4 g + r, column n16 of each 16
-    f32x4v S[KT][NV], D[DERIV ? KT : 1][NV];
+    // this lane's part of the state: rows 16 kt + 4 g + r, column n16 of the wave's
+    f32x4v S[KT], D[DERIV ? KT : 1];
     auto each_state = [&](const float *from, bool by_seq, auto f) {
         const float *const p = from + ((int64_t)(by_seq ? seg.seq : id) * a.H + h) * a.per;
+        const int c = col0 + colw + n16;
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-            for (int nv = 0; nv < NV; ++nv)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int k = 16 * kt + 4 * g + r, c = col0 + colw + 16 * nv + n16;
-                    const uint32_t at = (uint32_t)(min(k, a.k.width - 1) * a.sk + min(c, a.v.width - 1) * a.sv);
-                    f(kt, nv, r, k < a.k.width && c < a.v.width, p + at);
-                }
+            for (int r = 0; r < 4; ++r) {
+                const int k = 16 * kt + 4 * g + r;
+                const uint32_t at = (uint32_t)(min(k, a.k.width - 1) * a.sk + min(c, a.v.width - 1) * a.sv);
+                f(kt, r, k < a.k.width && c < a.v.width, p + at);
+            }
     };
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-        for (int nv = 0; nv < NV; ++nv) {
-            S[kt][nv] = f32x4v{0.f, 0.f, 0.f, 0.f};
-            if (DERIV) D[kt][nv] = f32x4v{0.f, 0.f, 0.f, 0.f};
-        }
+    for (int kt = 0; kt < KT; ++kt) {
+        S[kt] = f32x4v{0.f, 0.f, 0.f, 0.f};
+        if (DERIV) D[kt] = f32x4v{0.f, 0.f, 0.f, 0.f};
+    }
     if (a.start)
-        each_state(a.start, a.start_by_seq, [&](int kt, int nv, int r, bool in, const float *p) {
+        each_state(a.start, a.start_by_seq, [&](int kt, int r, bool in, const float *p) {
             const float x = *p;
-            S[kt][nv][r] = in ? x : 0.f;
+            S[kt][r] = in ? x : 0.f;
         });
 
-    Stage<T, KD, TAIL> xq, xk;
-    Stage<T, VB, TAIL> xv;
+    Stage<T, KD, NW * kWave, TAIL> xq, xk;
+    Stage<T, VB, NW * kWave, TAIL> xv;
     const int64_t first = rev ? (int64_t)seg.first + seg.n - 1 : seg.first;
     const int dir = rev ? -1 : 1;
     float dsum = 0.f;
@@ -364,26 +378,25 @@ __global__ __launch_bounds__(kScanThreads, KD <= 128 ? 2 : 1) void scan_kernel(S
             xv.load(a.v, h, col0, t0, a.rev, next_len);
         }
         if (len > 0) {
-            f32x4v O[IT][NV], OD[DERIV ? IT : 1][NV];
+            f32x4v O[IT], OD[DERIV ? IT : 1];
             if constexpr (KIND != kState) {
                 // ---- scores: tile (it, jt) of 16 x 16, jt <= it, shared out among the waves
                 constexpr int TILES = IT * (IT + 1) / 2;
-                constexpr int ROUNDS = (TILES + kScanWaves - 1) / kScanWaves;
+                constexpr int ROUNDS = (TILES + NW - 1) / NW;
                 float p[ROUNDS][4];
-                int it[ROUNDS], jt[ROUNDS];
+                auto it_of = [](int t) { return t >= 6 ? 3 : t >= 3 ? 2 : t >= 1 ? 1 : 0; };
 #pragma unroll
                 for (int u = 0; u < ROUNDS; ++u) {
-                    const int tile = min(u * kScanWaves + wave, TILES - 1);  // (the last one again)
-                    it[u] = tile >= 6 ? 3 : tile >= 3 ? 2 : tile >= 1 ? 1 : 0;
-                    jt[u] = tile - it[u] * (it[u] + 1) / 2;
+                    const int tile = u * NW + wave, it = it_of(tile), jt = tile - it * (it + 1) / 2;
+                    if (tile >= TILES) break;
                     f32x4v acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int f = 0; f < KF; ++f)
-                        mma(acc, fragment(ldsK + (16 * jt[u] + n16) * LDK + 32 * f + 8 * g),
-                            fragment(ldsQ + (16 * it[u] + n16) * LDK + 32 * f + 8 * g));
+                        mma(acc, fragment(ldsK + (16 * jt + n16) * LDK + 32 * f + 8 * g),
+                            fragment(ldsQ + (16 * it + n16) * LDK + 32 * f + 8 * g));
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        const int n = 16 * it[u] + n16 - (16 * jt[u] + 4 * g + r);
+                        const int n = 16 * it + n16 - (16 * jt + 4 * g + r);
                         const float w = power[max(n, 0)] * (DERIV ? (float)n : 1.f);
                         p[u][r] = n >= 0 ? acc[r] * a.s_score * w : 0.f;
                     }
@@ -391,51 +404,50 @@ __global__ __launch_bounds__(kScanThreads, KD <= 128 ? 2 : 1) void scan_kernel(S
                 __syncthreads();  // the keys were read: the scores take their place
 #pragma unroll
                 for (int u = 0; u < ROUNDS; ++u) {
+                    const int tile = u * NW + wave, it = it_of(tile), jt = tile - it * (it + 1) / 2;
+                    if (tile >= TILES) break;
                     T part[SP][4];
                     split<T, NS, 4>(p[u], part);
 #pragma unroll
                     for (int s = 0; s < SP; ++s) {
-                        T *to = ldsP + (s * C + 16 * it[u] + n16) * LDC + 16 * jt[u] + 4 * g;
-                        __builtin_memcpy(__builtin_assume_aligned(to, 8), part[s], 4 * sizeof(T));
-                        if (jt[u] == it[u] && it[u] % 2 == 0) {  // the rest of 32 columns
+                        T *const to = ldsP + s * C * C;
+                        __builtin_memcpy(__builtin_assume_aligned(
+                                             to + spread<T>(16 * it + n16, 16 * jt + 4 * g), 8),
+                                         part[s], 4 * sizeof(T));
+                        if (jt == it && it % 2 == 0) {  // the rest of 32 columns
                             const T none[4] = {T(0), T(0), T(0), T(0)};
-                            __builtin_memcpy(__builtin_assume_aligned(to + 16, 8), none, sizeof none);
+                            __builtin_memcpy(__builtin_assume_aligned(
+                                                 to + spread<T>(16 * it + n16, 16 * jt + 16 + 4 * g), 8),
+                                             none, sizeof none);
                         }
                     }
                 }
                 // ---- from the state
 #pragma unroll
-                for (int it = 0; it < IT; ++it)
-#pragma unroll
-                    for (int nv = 0; nv < NV; ++nv) {
-                        O[it][nv] = f32x4v{0.f, 0.f, 0.f, 0.f};
-                        if (DERIV) OD[it][nv] = f32x4v{0.f, 0.f, 0.f, 0.f};
-                    }
+                for (int it = 0; it < IT; ++it) {
+                    O[it] = f32x4v{0.f, 0.f, 0.f, 0.f};
+                    if (DERIV) OD[it] = f32x4v{0.f, 0.f, 0.f, 0.f};
+                }
 #pragma unroll
                 for (int f = 0; f < KF; ++f) {
-                    Frag<T> sf[NV][SP], df[DERIV ? NV : 1][SP];
+                    Frag<T> sf[SP], df[SP];
+                    float x[8];
 #pragma unroll
-                    for (int nv = 0; nv < NV; ++nv) {
-                        float x[8];
+                    for (int e = 0; e < 8; ++e) x[e] = S[2 * f + e / 4][e % 4];
+                    split<T, NS>(x, sf);
+                    if constexpr (DERIV) {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) x[e] = S[2 * f + e / 4][nv][e % 4];
-                        split<T, NS>(x, sf[nv]);
-                        if constexpr (DERIV) {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) x[e] = D[2 * f + e / 4][nv][e % 4];
-                            split<T, NS>(x, df[nv]);
-                        }
+                        for (int e = 0; e < 8; ++e) x[e] = D[2 * f + e / 4][e % 4];
+                        split<T, NS>(x, df);
                     }
 #pragma unroll
                     for (int it = 0; it < IT; ++it) {
                         const Frag<T> qf = fragment(ldsQ + (16 * it + n16) * LDK + 32 * f + 8 * g);
 #pragma unroll
-                        for (int nv = 0; nv < NV; ++nv)
-#pragma unroll
-                            for (int s = 0; s < SP; ++s) {
-                                mma(O[it][nv], sf[nv][s], qf);
-                                if constexpr (DERIV) mma(OD[it][nv], df[nv][s], qf);
-                            }
+                        for (int s = 0; s < SP; ++s) {
+                            mma(O[it], sf[s], qf);
+                            if constexpr (DERIV) mma(OD[it], df[s], qf);
+                        }
                     }
                 }
 #pragma unroll
@@ -443,12 +455,9 @@ __global__ __launch_bounds__(kScanThreads, KD <= 128 ? 2 : 1) void scan_kernel(S
                     const int i = 16 * it + n16;
                     const float w = a.s_inter * power[i + 1 - rev];
 #pragma unroll
-                    for (int nv = 0; nv < NV; ++nv)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            O[it][nv][r] = DERIV ? w * __builtin_fmaf((float)(i + 1), O[it][nv][r],
-                                                                      OD[it][nv][r])
-                                                 : w * O[it][nv][r];
+                    for (int r = 0; r < 4; ++r)
+                        O[it][r] = DERIV ? w * __builtin_fmaf((float)(i + 1), O[it][r], OD[it][r])
+                                         : w * O[it][r];
                 }
                 __syncthreads();
             }
@@ -457,88 +466,67 @@ __global__ __launch_bounds__(kScanThreads, KD <= 128 ? 2 : 1) void scan_kernel(S
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-                for (int nv = 0; nv < NV; ++nv)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        if constexpr (DERIV) {
-                            const float x = __builtin_fmaf((float)len, S[kt][nv][r], D[kt][nv][r]);
-                            D[kt][nv][r] = __builtin_fmaf(x, keep, x * keep_low);
-                        }
-                        S[kt][nv][r] = __builtin_fmaf(S[kt][nv][r], keep, S[kt][nv][r] * keep_low);
+                for (int r = 0; r < 4; ++r) {
+                    if constexpr (DERIV) {
+                        const float x = __builtin_fmaf((float)len, S[kt][r], D[kt][r]);
+                        D[kt][r] = __builtin_fmaf(x, keep, x * keep_low);
                     }
-#pragma unroll
-            for (int f = 0; f < JF; ++f) {
-                Frag<T> vf[NV], vs[NV][VP], vd[DERIV ? NV : 1][VP];
-                float w[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int after = len - 1 - (32 * f + 8 * g + e) + rev;
-                    w[e] = after >= 0 ? a.s_update * power[max(after, 0)] : 0.f;
+                    S[kt][r] = __builtin_fmaf(S[kt][r], keep, S[kt][r] * keep_low);
                 }
 #pragma unroll
-                for (int nv = 0; nv < NV; ++nv) {
-                    vf[nv] = fragment(ldsVt + (colw + 16 * nv + n16) * LDC + 32 * f + 8 * g);
-                    T v[8];
-                    __builtin_memcpy(v, &vf[nv], sizeof v);
-                    float x[8];
+            for (int f = 0; f < JF; ++f) {
+                const Frag<T> vf = fragment_of(ldsVt, colw + n16, 32 * f + 8 * g);
+                Frag<T> vs[VP], vd[VP];
+                T v[8];
+                __builtin_memcpy(v, &vf, sizeof v);
+                float x[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = widened(v[e]) * w[e];
-                    split<T, 3>(x, vs[nv]);
-                    if constexpr (DERIV) {
+                for (int e = 0; e < 8; ++e) x[e] = widened(v[e]) * behind[C - len + 32 * f + 8 * g + e];
+                split<T, 3>(x, vs);
+                if constexpr (DERIV) {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            x[e] *= (float)max(len - 1 - (32 * f + 8 * g + e), 0);
-                        split<T, 3>(x, vd[nv]);
-                    }
+                    for (int e = 0; e < 8; ++e) x[e] *= (float)max(len - 1 - (32 * f + 8 * g + e), 0);
+                    split<T, 3>(x, vd);
                 }
                 if constexpr (KIND != kState) {
 #pragma unroll
                     for (int it = 2 * f; it < IT; ++it)
 #pragma unroll
-                        for (int s = 0; s < SP; ++s) {
-                            const Frag<T> pf =
-                                fragment(ldsP + (s * C + 16 * it + n16) * LDC + 32 * f + 8 * g);
-#pragma unroll
-                            for (int nv = 0; nv < NV; ++nv) mma(O[it][nv], vf[nv], pf);
-                        }
+                        for (int s = 0; s < SP; ++s)
+                            mma(O[it], vf, fragment_of(ldsP + s * C * C, 16 * it + n16, 32 * f + 8 * g));
                 }
 #pragma unroll
                 for (int kt = 0; kt < KT; ++kt) {
-                    const Frag<T> kf = fragment(ldsKt + (16 * kt + n16) * LDC + 32 * f + 8 * g);
+                    const Frag<T> kf = fragment_of(ldsKt, 16 * kt + n16, 32 * f + 8 * g);
 #pragma unroll
-                    for (int nv = 0; nv < NV; ++nv)
-#pragma unroll
-                        for (int s = 0; s < VP; ++s) {
-                            mma(S[kt][nv], kf, vs[nv][s]);
-                            if constexpr (DERIV) mma(D[kt][nv], kf, vd[nv][s]);
-                        }
+                    for (int s = 0; s < VP; ++s) {
+                        mma(S[kt], kf, vs[s]);
+                        if constexpr (DERIV) mma(D[kt], kf, vd[s]);
+                    }
                 }
             }
             // ---- outputs: row i by lane % 16, four columns each
             if constexpr (KIND != kState) {
+                const int c = col0 + colw + 4 * g, left = TAIL ? a.v.width - c : 4;
 #pragma unroll
                 for (int it = 0; it < IT; ++it) {
                     const int i = 16 * it + n16;
                     const int64_t t = first + (int64_t)(pos + i) * dir;
+                    if (i >= len || c >= a.v.width) continue;
+                    const float x[4] = {O[it][0], O[it][1], O[it][2], O[it][3]};
+                    if constexpr (DERIV) {
+                        float up[4];
+                        load_left<4, T>(static_cast<const T *>(a.up.p) + t * a.up.ld +
+                                            (int64_t)(h / a.up.grp) * a.up.width + c, left, up);
 #pragma unroll
-                    for (int nv = 0; nv < NV; ++nv) {
-                        const int c = col0 + colw + 16 * nv + 4 * g, left = TAIL ? a.v.width - c : 4;
-                        if (i >= len || c >= a.v.width) continue;
-                        const float x[4] = {O[it][nv][0], O[it][nv][1], O[it][nv][2], O[it][nv][3]};
-                        if constexpr (DERIV) {
-                            float up[4];
-                            load_left<4, T>(static_cast<const T *>(a.up.p) + t * a.up.ld +
-                                                (int64_t)(h / a.up.grp) * a.up.width + c, left, up);
-#pragma unroll
-                            for (int r = 0; r < 4; ++r)
-                                dsum = r < left ? __builtin_fmaf(x[r], up[r], dsum) : dsum;
-                        } else if (a.out32) {
-                            store_left<4, float>(static_cast<float *>(a.out) + t * a.ldo +
-                                                     (int64_t)h * a.v.width + c, left, x);
-                        } else {
-                            store_left<4, T>(static_cast<T *>(a.out) + t * a.ldo +
+                        for (int r = 0; r < 4; ++r)
+                            dsum = r < left ? __builtin_fmaf(x[r], up[r], dsum) : dsum;
+                    } else if (a.out32) {
+                        store_left<4, float>(static_cast<float *>(a.out) + t * a.ldo +
                                                  (int64_t)h * a.v.width + c, left, x);
-                        }
+                    } else {
+                        store_left<4, T>(static_cast<T *>(a.out) + t * a.ldo +
+                                             (int64_t)h * a.v.width + c, left, x);
                     }
                 }
             }
@@ -556,8 +544,8 @@ __global__ __launch_bounds__(kScanThreads, KD <= 128 ? 2 : 1) void scan_kernel(S
                 xq.store(ldsQ, LDK);
                 xk.store(ldsK, LDK);
             }
-            xk.store_transposed(ldsKt, LDC);
-            xv.store_transposed(ldsVt, LDC);
+            xk.store_transposed(ldsKt);
+            xv.store_transposed(ldsVt);
             if (KIND != kState && !xv.finite()) unusual[turn] = 1;
             __syncthreads();
             // A product with a score of 0 keeps an infinite or missing number of a later token
@@ -575,14 +563,14 @@ __global__ __launch_bounds__(kScanThreads, KD <= 128 ? 2 : 1) void scan_kernel(S
         next_len = single > 0 ? 1 : min(C, seg.n - next);
     }
     if (a.end)
-        each_state(a.end, a.end_by_seq, [&](int kt, int nv, int r, bool in, const float *p) {
-            if (in) *const_cast<float *>(p) = S[kt][nv][r];
+        each_state(a.end, a.end_by_seq, [&](int kt, int r, bool in, const float *p) {
+            if (in) *const_cast<float *>(p) = S[kt][r];
         });
     if constexpr (DERIV) {  // what the segment adds to the states behind it
         if (a.back)
-            each_state(a.back, a.back_by_seq, [&](int kt, int nv, int r, bool in, const float *p) {
+            each_state(a.back, a.back_by_seq, [&](int kt, int r, bool in, const float *p) {
                 const float x = *p;
-                dsum = in ? __builtin_fmaf(D[kt][nv][r], x, dsum) : dsum;
+                dsum = in ? __builtin_fmaf(D[kt][r], x, dsum) : dsum;
             });
 #pragma unroll
         for (int m = 1; m < kWave; m <<= 1) dsum += __shfl_xor(dsum, m, kWave);
@@ -590,48 +578,42 @@ __global__ __launch_bounds__(kScanThreads, KD <= 128 ? 2 : 1) void scan_kernel(S
         __syncthreads();
         if (threadIdx.x == 0) {
             float t = 0.f;
-            for (int w = 0; w < kScanWaves; ++w) t += wave_sum[w];
+            for (int w = 0; w < NW; ++w) t += wave_sum[w];
             a.sums[unit] = t;
         }
     }
 }
 
-// Blocks of a head's columns for values of `width` and queries of `kw`.
-inline int columns_of(Kind kind, int kw, int width) {
-    return kind != kDerivative && width > 64 && kw <= 128 ? 128 : 64;
-}
+// Columns of the values that a block takes.
+inline int block_columns(int width) { return width > 64 ? 128 : 64; }
 
 nsd_status launch_scan_f32(Kind kind, const Scan &a, hipStream_t st);
 nsd_status launch_scan_bf16(Kind kind, const Scan &a, hipStream_t st);
 
-template <class T, int KD, int NV, Kind KIND>
+template <class T, int KD, int NW, Kind KIND>
 nsd_status launch_one(const Scan &a, hipStream_t st) {
-    const int nvb = (int)ceil_div(a.v.width, kScanWaves * 16 * NV);
+    const int nvb = (int)ceil_div(a.v.width, NW * 16);
     const int64_t blocks = (int64_t)a.nseg * a.H * nvb;
     if (blocks == 0) return NSD_OK;
-    // whole pieces of the rows, whatever their alignment
-    constexpr int CV = 16 / sizeof(T);
-    if (a.k.width % CV == 0 && a.v.width % CV == 0)
-        scan_kernel<T, KD, NV, KIND, false><<<blocks, kScanThreads, 0, st>>>(a, nvb);
+    if (a.k.width % 4 == 0 && a.v.width % 4 == 0)  // whole pieces of the rows, at any address
+        scan_kernel<T, KD, NW, KIND, false><<<blocks, NW * kWave, 0, st>>>(a, nvb);
     else
-        scan_kernel<T, KD, NV, KIND, true><<<blocks, kScanThreads, 0, st>>>(a, nvb);
+        scan_kernel<T, KD, NW, KIND, true><<<blocks, NW * kWave, 0, st>>>(a, nvb);
     return check_launch("scan_kernel");
+}
+
+template <class T, int KD, Kind KIND>
+nsd_status launch_columns(const Scan &a, hipStream_t st) {
+    return block_columns(a.v.width) == 128 ? launch_one<T, KD, 8, KIND>(a, st)
+                                           : launch_one<T, KD, 4, KIND>(a, st);
 }
 
 template <class T, Kind KIND>
 nsd_status launch_kind(const Scan &a, hipStream_t st) {
-    const bool wide = columns_of(KIND, a.k.width, a.v.width) == 128;
-    auto by_width = [&](auto kd) -> nsd_status {
-        constexpr int KD = decltype(kd)::value;
-        if constexpr (KIND != kDerivative && KD <= 128) {
-            if (wide) return launch_one<T, KD, 2, KIND>(a, st);
-        }
-        return launch_one<T, KD, 1, KIND>(a, st);
-    };
-    if (a.k.width <= 32) return by_width(std::integral_constant<int, 32>());
-    if (a.k.width <= 64) return by_width(std::integral_constant<int, 64>());
-    if (a.k.width <= 128) return by_width(std::integral_constant<int, 128>());
-    return by_width(std::integral_constant<int, 256>());
+    if (a.k.width <= 32) return launch_columns<T, 32, KIND>(a, st);
+    if (a.k.width <= 64) return launch_columns<T, 64, KIND>(a, st);
+    if (a.k.width <= 128) return launch_columns<T, 128, KIND>(a, st);
+    return launch_columns<T, 256, KIND>(a, st);
 }
 
 template <class T>
