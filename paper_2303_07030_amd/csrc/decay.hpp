@@ -136,19 +136,33 @@ __device__ __forceinline__ void mma(f32x4v &c, const Frag<float> &a, const Frag<
 template <class T, int N>
 constexpr int kParts = sizeof(T) == 2 ? N : 1;
 
+// The parts but the last are cut, not rounded: an upper half is a bf16 number as it stands,
+// what is left is exact, and eight bits of 24 are gone with each.
 template <class T, int N, int M>
 __device__ __forceinline__ void split(const float (&x)[M], T (&part)[kParts<T, N>][M]) {
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int e = 0; e < M; ++e) {
-        if constexpr (sizeof(T) == 4) {
-            part[0][e] = x[e];
-        } else {
-            float left = x[e];
+        for (int e = 0; e < M; ++e) part[0][e] = x[e];
+    } else {
+        float left[M];
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                part[i][e] = narrowed<Bf16>(left);
-                if (i + 1 < N) left -= widened(part[i][e]);
+        for (int e = 0; e < M; ++e) left[e] = x[e];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            uint32_t pair[M / 2];
+#pragma unroll
+            for (int e = 0; e < M; e += 2) {
+                if (i + 1 < N) {
+                    const uint32_t a = __float_as_uint(left[e]), b = __float_as_uint(left[e + 1]);
+                    pair[e / 2] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+                    left[e] -= __uint_as_float(a & 0xFFFF0000u);
+                    left[e + 1] -= __uint_as_float(b & 0xFFFF0000u);
+                } else {
+                    const Bf16 two[2] = {narrowed<Bf16>(left[e]), narrowed<Bf16>(left[e + 1])};
+                    __builtin_memcpy(&pair[e / 2], two, 4);
+                }
             }
+            __builtin_memcpy(part[i], pair, sizeof pair);
         }
     }
 }
@@ -172,19 +186,31 @@ __device__ __forceinline__ int place(int k) {
 template <class T>
 __device__ __forceinline__ int spread(int row, int j) {
     constexpr int B = 16 / sizeof(T);
-    const int x = ((row >> 1 ^ row >> 3) & 1) | (row >> 1 & 2) | (row >> 2 & 4);
+    const int x = sizeof(T) == 2 ? ((row >> 1 ^ row >> 3) & 1) | (row >> 1 & 2) | (row >> 2 & 4)
+                                 : row >> 1 & 7;
     return row * kChunkOf<T> + ((j / B ^ x) * B | j % B);
 }
+
+// A lane's fragments of such rows: row 16 tile + lane % 16, places 32 f + 8 (lane / 16) on.
+// One address for all of them, the rest known at compile time (or the same for all lanes).
 template <class T>
-__device__ __forceinline__ Frag<T> fragment_of(const T *rows, int row, int j) {
-    constexpr int B = 16 / sizeof(T);
-    Frag<T> f;
+struct Spread {
+    const T *p[sizeof(T) / 2];  // of each 16 bytes
+    __device__ __forceinline__ Spread(const T *rows, int n16, int g) {
 #pragma unroll
-    for (int b = 0; b < 8; b += B)
-        __builtin_memcpy(reinterpret_cast<char *>(&f) + b * sizeof(T),
-                         __builtin_assume_aligned(rows + spread<T>(row, j + b), 16), 16);
-    return f;
-}
+        for (int b = 0; b < (int)sizeof(T) / 2; ++b) p[b] = rows + spread<T>(n16, 8 * g + b * 4);
+    }
+    __device__ __forceinline__ Frag<T> at(int tile, int f) const {
+        Frag<T> x;
+        // (bf16: tile and f turn the same bit of a place's 16 bytes, the lane none of it)
+        const int off = tile * 16 * kChunkOf<T> + (sizeof(T) == 2 ? ((f ^ tile) & 1) * 32 : 0);
+#pragma unroll
+        for (int b = 0; b < (int)sizeof(T) / 2; ++b)
+            __builtin_memcpy(reinterpret_cast<char *>(&x) + 16 * b,
+                             __builtin_assume_aligned(p[b] + off, 16), 16);
+        return x;
+    }
+};
 
 // A chunk's rows of one matrix on their way to LDS: four rows and four columns a unit.
 // TAIL: the rows' widths are no multiples of four.
@@ -196,7 +222,8 @@ struct Stage {
     static constexpr int UNITS = C / 4 * PIECES;
     static constexpr int U = (UNITS + THREADS - 1) / THREADS;
     static constexpr bool EXACT = UNITS % THREADS == 0;
-    T x[U][4][CV];
+    static constexpr int WD = CV * sizeof(T) / 4;
+    uint32_t x[U][4][WD];  // as they were loaded: nothing waits for them before clear()
 
     // (threads beyond the units repeat the last one, and store nothing)
     __device__ __forceinline__ int unit(int u) const {
@@ -205,23 +232,35 @@ struct Stage {
     }
     // Rows i < len (at least one) from token t0 on, or back; columns from col0 on.  Nothing here
     // depends on a lane's place: what is beyond a row or the chunk reads a neighbour of it,
-    // and is cleared by clear().
+    // and is cleared by clear().  A whole chunk's four rows have one place and four bases.
     __device__ __forceinline__ void load(const Rows &m, int h, int col0, int64_t t0, bool rev, int len) {
-        const T *base = static_cast<const T *>(m.p) + (rev ? t0 - (len - 1) : t0) * m.ld +
-                        (int64_t)(h / m.grp) * m.width + col0;
-        const int width = m.width - col0, ld = (int)m.ld;
+        const char *base = reinterpret_cast<const char *>(
+            static_cast<const T *>(m.p) + (rev ? t0 - (len - 1) : t0) * m.ld +
+            (int64_t)(h / m.grp) * m.width + col0);
+        const int width = m.width - col0;
+        const uint32_t row = (uint32_t)m.ld * sizeof(T);  // bytes
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int i0 = unit(u) / PIECES * 4, c = unit(u) % PIECES * CV;
+            if (!TAIL && len == C) {
+                const uint32_t at = (uint32_t)(rev ? C - 4 - i0 : i0) * row + min(c, width - CV) * sizeof(T);
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    __builtin_memcpy(x[u][r], base + (uint32_t)(rev ? 3 - r : r) * row + at, sizeof x[u][r]);
+                continue;
+            }
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int i = min(i0 + r, len - 1);
-                const uint32_t row = (uint32_t)((rev ? len - 1 - i : i) * ld);
+                const uint32_t at = (uint32_t)(rev ? len - 1 - i : i) * row;
                 if constexpr (!TAIL) {
-                    __builtin_memcpy(x[u][r], base + (row + (uint32_t)min(c, width - CV)), sizeof x[u][r]);
+                    __builtin_memcpy(x[u][r], base + (at + min(c, width - CV) * sizeof(T)), sizeof x[u][r]);
                 } else {
+                    T t[CV];
 #pragma unroll
-                    for (int e = 0; e < CV; ++e) x[u][r][e] = base[row + (uint32_t)min(c + e, width - 1)];
+                    for (int e = 0; e < CV; ++e)
+                        __builtin_memcpy(&t[e], base + (at + min(c + e, width - 1) * sizeof(T)), sizeof(T));
+                    __builtin_memcpy(x[u][r], t, sizeof t);
                 }
             }
         }
@@ -232,10 +271,13 @@ struct Stage {
         for (int u = 0; u < U; ++u) {
             const int i0 = unit(u) / PIECES * 4, c = unit(u) % PIECES * CV;
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
+            for (int d = 0; d < WD; ++d) {
+                const int e = TAIL ? c + d * (CV / WD) : c;  // the first value of the four bytes
+                uint32_t keep = e < width ? ~0u : 0u;
+                if (TAIL && sizeof(T) == 2 && e + 1 == width) keep = 0xFFFFu;
 #pragma unroll
-                for (int e = 0; e < CV; ++e)
-                    if (i0 + r >= len || c + (TAIL ? e : 0) >= width) x[u][r][e] = T(0);
+                for (int r = 0; r < 4; ++r) x[u][r][d] &= i0 + r < len ? keep : 0u;
+            }
         }
     }
     // rows of ld values, columns in the order of place()
@@ -256,25 +298,44 @@ struct Stage {
         for (int u = 0; u < U; ++u) {
             if (!EXACT && (int)threadIdx.x + u * THREADS >= UNITS) continue;
             const int i0 = unit(u) / PIECES * 4, c = unit(u) % PIECES * CV;
+            // (two columns of a multiple of four keep their 16 bytes' places, the others turn one bit)
+            T *const at[2] = {to + spread<T>(c, i0), to + spread<T>(c + 2, i0) - 2 * C};
 #pragma unroll
             for (int e = 0; e < CV; ++e) {
-                const T t[4] = {x[u][0][e], x[u][1][e], x[u][2][e], x[u][3][e]};
-                __builtin_memcpy(__builtin_assume_aligned(to + spread<T>(c + e, i0), 8), t, sizeof t);
+                uint32_t t[WD];
+                if constexpr (sizeof(T) == 2) {
+                    const uint32_t half = e % 2 ? 0x07060302u : 0x05040100u;
+                    t[0] = __builtin_amdgcn_perm(x[u][1][e / 2], x[u][0][e / 2], half);
+                    t[1] = __builtin_amdgcn_perm(x[u][3][e / 2], x[u][2][e / 2], half);
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) t[r] = x[u][r][e];
+                }
+                __builtin_memcpy(__builtin_assume_aligned(at[e / 2] + e * C, 8), t, sizeof t);
             }
         }
     }
     __device__ __forceinline__ bool finite() const {
-        uint32_t top = 0;
+        bool all = true;
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
+            for (int d = 0; d < WD; ++d) {
+                if constexpr (sizeof(T) == 4) {
+                    uint32_t top = 0;
 #pragma unroll
-                for (int e = 0; e < CV; ++e) {
-                    if constexpr (sizeof(T) == 4) top = max(top, __float_as_uint(x[u][r][e]) & 0x7F800000u);
-                    else top = max(top, (uint32_t)x[u][r][e] & 0x7F80u);
+                    for (int r = 0; r < 4; ++r) top = max(top, x[u][r][d] & 0x7F800000u);
+                    all = all && top < 0x7F800000u;
+                } else {
+                    typedef uint16_t two __attribute__((ext_vector_type(2)));
+                    two top = {0, 0};
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        top = __builtin_elementwise_max(top, __builtin_bit_cast(two, x[u][r][d] & 0x7F807F80u));
+                    all = all && top.x < 0x7F80 && top.y < 0x7F80;
                 }
-        return top < (sizeof(T) == 4 ? 0x7F800000u : 0x7F80u);
+            }
+        return all;
     }
 };
 
@@ -309,8 +370,9 @@ __global__ __launch_bounds__(NW * kWave, KD <= 128 ? 2 : 1) void scan_kernel(Sca
     T *const ldsP = ldsK;
     T *const ldsKt = ldsK + Sh::KP;
     T *const ldsVt = ldsKt + KD * C;
-    __shared__ float power[C + 2], power_low[C + 2];
-    __shared__ float behind[2 * C];  // s_update w^(C - 1 - j (+ 1)) of place j, 0 from C on
+    __shared__ float power[C + 2], power_less[C + 2];
+    __shared__ float weight[2 * C];  // s_score w^n (DERIV: n w^n) at C + n, 0 below C
+    __shared__ __align__(16) float behind[2 * C];  // s_update w^(C - 1 - j (+ 1)) at j, 0 from C on
     __shared__ int unusual[2];
     __shared__ float wave_sum[NW];
 
@@ -326,16 +388,22 @@ __global__ __launch_bounds__(NW * kWave, KD <= 128 ? 2 : 1) void scan_kernel(Sca
     const int rev = a.rev ? 1 : 0;
     const int col0 = vb * VB, colw = wave * 16;  // first columns: the block's; the wave's in it
     if (threadIdx.x < C + 2) {
-        // powers of the decay in two numbers, also of -infinity: what one would leave out adds up
-        // over the thousands of chunks that multiply them
+        // Powers of the decay, and what they are less than 1: near 1 the roundings of a power
+        // itself would add up over the thousands of chunks that multiply it.
         const int n = threadIdx.x;
         const double x = n ? exp((double)a.decay[h] * (double)n) : 1.0;
         power[n] = (float)x;
-        power_low[n] = (float)(x - (double)(float)x);
+        power_less[n] = (float)(x - 1.0);
         if (n >= rev && n < C + rev) behind[C - 1 + rev - n] = a.s_update * (float)x;
-        if (n < C) behind[C + n] = 0.f;
+        if (n < C) {
+            behind[C + n] = weight[n] = 0.f;
+            weight[C + n] = a.s_score * (float)x * (DERIV ? (float)n : 1.f);
+        }
     }
     if (threadIdx.x < 2) unusual[threadIdx.x] = 0;
+    // this lane's places in what the products read: all others are a constant from them
+    const Spread<T> by_k(ldsKt, n16, g), by_v(ldsVt, n16, g), by_p(ldsP, n16, g);
+    const T *const byQ = ldsQ + n16 * LDK + 8 * g, *const byK = ldsK + n16 * LDK + 8 * g;
 
     // this lane's part of the state: rows 16 kt + 4 g + r, column n16 of the wave's
     f32x4v S[KT], D[DERIV ? KT : 1];
@@ -385,6 +453,7 @@ __global__ __launch_bounds__(NW * kWave, KD <= 128 ? 2 : 1) void scan_kernel(Sca
                 constexpr int ROUNDS = (TILES + NW - 1) / NW;
                 float p[ROUNDS][4];
                 auto it_of = [](int t) { return t >= 6 ? 3 : t >= 3 ? 2 : t >= 1 ? 1 : 0; };
+                const int apart = n16 - 4 * g;  // of the lane's row and its first column in a tile
 #pragma unroll
                 for (int u = 0; u < ROUNDS; ++u) {
                     const int tile = u * NW + wave, it = it_of(tile), jt = tile - it * (it + 1) / 2;
@@ -392,14 +461,13 @@ __global__ __launch_bounds__(NW * kWave, KD <= 128 ? 2 : 1) void scan_kernel(Sca
                     f32x4v acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int f = 0; f < KF; ++f)
-                        mma(acc, fragment(ldsK + (16 * jt + n16) * LDK + 32 * f + 8 * g),
-                            fragment(ldsQ + (16 * it + n16) * LDK + 32 * f + 8 * g));
+                        mma(acc, fragment(byK + 16 * jt * LDK + 32 * f), fragment(byQ + 16 * it * LDK + 32 * f));
+                    const float *const w = weight + C + 16 * (it - jt) + apart;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int n = 16 * it + n16 - (16 * jt + 4 * g + r);
-                        const float w = power[max(n, 0)] * (DERIV ? (float)n : 1.f);
-                        p[u][r] = n >= 0 ? acc[r] * a.s_score * w : 0.f;
-                    }
+                    for (int r = 0; r < 4; ++r) p[u][r] = acc[r] * w[-r];
+                    if (it == jt)  // later tokens: 0, whatever their products are
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) p[u][r] = apart >= r ? p[u][r] : 0.f;
                 }
                 __syncthreads();  // the keys were read: the scores take their place
 #pragma unroll
@@ -442,7 +510,7 @@ __global__ __launch_bounds__(NW * kWave, KD <= 128 ? 2 : 1) void scan_kernel(Sca
                     }
 #pragma unroll
                     for (int it = 0; it < IT; ++it) {
-                        const Frag<T> qf = fragment(ldsQ + (16 * it + n16) * LDK + 32 * f + 8 * g);
+                        const Frag<T> qf = fragment(byQ + 16 * it * LDK + 32 * f);
 #pragma unroll
                         for (int s = 0; s < SP; ++s) {
                             mma(O[it], sf[s], qf);
@@ -462,26 +530,42 @@ __global__ __launch_bounds__(NW * kWave, KD <= 128 ? 2 : 1) void scan_kernel(Sca
                 __syncthreads();
             }
             // ---- from the chunk's own tokens, and the state behind them
-            const float keep = power[len], keep_low = power_low[len];
+            const float keep = power[len], less = power_less[len];
+            if (keep > 0.5f) {  // a slow decay by what it takes away
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt)
+                for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    if constexpr (DERIV) {
-                        const float x = __builtin_fmaf((float)len, S[kt][r], D[kt][r]);
-                        D[kt][r] = __builtin_fmaf(x, keep, x * keep_low);
+                    for (int r = 0; r < 4; ++r) {
+                        if constexpr (DERIV) {
+                            const float x = __builtin_fmaf((float)len, S[kt][r], D[kt][r]);
+                            D[kt][r] = __builtin_fmaf(x, less, x);
+                        }
+                        S[kt][r] = __builtin_fmaf(S[kt][r], less, S[kt][r]);
                     }
-                    S[kt][r] = __builtin_fmaf(S[kt][r], keep, S[kt][r] * keep_low);
-                }
+            } else {
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        if constexpr (DERIV) D[kt][r] = __builtin_fmaf((float)len, S[kt][r], D[kt][r]) * keep;
+                        S[kt][r] *= keep;
+                    }
+            }
 #pragma unroll
             for (int f = 0; f < JF; ++f) {
-                const Frag<T> vf = fragment_of(ldsVt, colw + n16, 32 * f + 8 * g);
+                const Frag<T> vf = by_v.at(wave, f);
                 Frag<T> vs[VP], vd[VP];
                 T v[8];
                 __builtin_memcpy(v, &vf, sizeof v);
                 float x[8];
+                if (len == C) {
+                    __builtin_memcpy(x, __builtin_assume_aligned(behind + 32 * f + 8 * g, 16), sizeof x);
+                } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = widened(v[e]) * behind[C - len + 32 * f + 8 * g + e];
+                    for (int e = 0; e < 8; ++e) x[e] = behind[C - len + 32 * f + 8 * g + e];
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] *= widened(v[e]);
                 split<T, 3>(x, vs);
                 if constexpr (DERIV) {
 #pragma unroll
@@ -493,11 +577,11 @@ __global__ __launch_bounds__(NW * kWave, KD <= 128 ? 2 : 1) void scan_kernel(Sca
                     for (int it = 2 * f; it < IT; ++it)
 #pragma unroll
                         for (int s = 0; s < SP; ++s)
-                            mma(O[it], vf, fragment_of(ldsP + s * C * C, 16 * it + n16, 32 * f + 8 * g));
+                            mma(O[it], vf, by_p.at(s * (C / 16) + it, f));
                 }
 #pragma unroll
                 for (int kt = 0; kt < KT; ++kt) {
-                    const Frag<T> kf = fragment_of(ldsKt, 16 * kt + n16, 32 * f + 8 * g);
+                    const Frag<T> kf = by_k.at(kt, f);
 #pragma unroll
                     for (int s = 0; s < VP; ++s) {
                         mma(S[kt], kf, vs[s]);
@@ -508,25 +592,30 @@ __global__ __launch_bounds__(NW * kWave, KD <= 128 ? 2 : 1) void scan_kernel(Sca
             // ---- outputs: row i by lane % 16, four columns each
             if constexpr (KIND != kState) {
                 const int c = col0 + colw + 4 * g, left = TAIL ? a.v.width - c : 4;
+                // rows from the chunk's first token on, or to it: a base and the lane's place
+                const int64_t t0 = first + (int64_t)pos * dir - (a.rev ? C - 1 : 0);
+                const uint32_t row = a.rev ? 15 - n16 : n16;
+                auto place_of = [&](auto *p, int64_t ld, int64_t head, int it) {
+                    return p + (t0 + (a.rev ? C - 16 - 16 * it : 16 * it)) * ld + head +
+                           (row * (uint32_t)ld + (uint32_t)c);
+                };
 #pragma unroll
                 for (int it = 0; it < IT; ++it) {
-                    const int i = 16 * it + n16;
-                    const int64_t t = first + (int64_t)(pos + i) * dir;
-                    if (i >= len || c >= a.v.width) continue;
+                    if (16 * it + n16 >= len || c >= a.v.width) continue;
                     const float x[4] = {O[it][0], O[it][1], O[it][2], O[it][3]};
                     if constexpr (DERIV) {
                         float up[4];
-                        load_left<4, T>(static_cast<const T *>(a.up.p) + t * a.up.ld +
-                                            (int64_t)(h / a.up.grp) * a.up.width + c, left, up);
+                        load_left<4, T>(place_of(static_cast<const T *>(a.up.p), a.up.ld,
+                                                 (int64_t)(h / a.up.grp) * a.up.width, it), left, up);
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
                             dsum = r < left ? __builtin_fmaf(x[r], up[r], dsum) : dsum;
                     } else if (a.out32) {
-                        store_left<4, float>(static_cast<float *>(a.out) + t * a.ldo +
-                                                 (int64_t)h * a.v.width + c, left, x);
+                        store_left<4, float>(place_of(static_cast<float *>(a.out), a.ldo,
+                                                      (int64_t)h * a.v.width, it), left, x);
                     } else {
-                        store_left<4, T>(static_cast<T *>(a.out) + t * a.ldo +
-                                             (int64_t)h * a.v.width + c, left, x);
+                        store_left<4, T>(place_of(static_cast<T *>(a.out), a.ldo,
+                                                  (int64_t)h * a.v.width, it), left, x);
                     }
                 }
             }
