@@ -226,14 +226,14 @@ struct Stage {
     uint32_t x[U][4][WD];  // as they were loaded: nothing waits for them before clear()
 
     // (threads beyond the units repeat the last one, and store nothing)
-    __device__ __forceinline__ int unit(int u) const {
-        const int n = (int)threadIdx.x + u * THREADS;
+    static __device__ __forceinline__ int unit(int tid, int u) {
+        const int n = tid + u * THREADS;
         return EXACT ? n : min(n, UNITS - 1);
     }
     // Rows i < len (at least one) from token t0 on, or back; columns from col0 on.  Nothing here
     // depends on a lane's place: what is beyond a row or the chunk reads a neighbour of it,
     // and is cleared by clear().  A whole chunk's four rows have one place and four bases.
-    __device__ __forceinline__ void load(const Rows &m, int h, int col0, int64_t t0, bool rev, int len) {
+    __device__ __forceinline__ void load(int tid, const Rows &m, int h, int col0, int64_t t0, bool rev, int len) {
         const char *base = reinterpret_cast<const char *>(
             static_cast<const T *>(m.p) + (rev ? t0 - (len - 1) : t0) * m.ld +
             (int64_t)(h / m.grp) * m.width + col0);
@@ -241,12 +241,12 @@ struct Stage {
         const uint32_t row = (uint32_t)m.ld * sizeof(T);  // bytes
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int i0 = unit(u) / PIECES * 4, c = unit(u) % PIECES * CV;
+            const int i0 = unit(tid, u) / PIECES * 4, c = unit(tid, u) % PIECES * CV;
             if (!TAIL && len == C) {
                 const uint32_t at = (uint32_t)(rev ? C - 4 - i0 : i0) * row + min(c, width - CV) * sizeof(T);
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    __builtin_memcpy(x[u][r], base + (uint32_t)(rev ? 3 - r : r) * row + at, sizeof x[u][r]);
+                    __builtin_memcpy(x[u][r], base + (uint64_t)((uint32_t)(rev ? 3 - r : r) * row) + at, sizeof x[u][r]);
                 continue;
             }
 #pragma unroll
@@ -265,11 +265,11 @@ struct Stage {
             }
         }
     }
-    __device__ __forceinline__ void clear(int width, int len) {
+    __device__ __forceinline__ void clear(int tid, int width, int len) {
         if (len == C && width >= W) return;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int i0 = unit(u) / PIECES * 4, c = unit(u) % PIECES * CV;
+            const int i0 = unit(tid, u) / PIECES * 4, c = unit(tid, u) % PIECES * CV;
 #pragma unroll
             for (int d = 0; d < WD; ++d) {
                 const int e = TAIL ? c + d * (CV / WD) : c;  // the first value of the four bytes
@@ -281,11 +281,11 @@ struct Stage {
         }
     }
     // rows of ld values, columns in the order of place()
-    __device__ __forceinline__ void store(T *to, int ld) const {
+    __device__ __forceinline__ void store(int tid, T *to, int ld) const {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (!EXACT && (int)threadIdx.x + u * THREADS >= UNITS) continue;
-            const int i0 = unit(u) / PIECES * 4, c = unit(u) % PIECES * CV;
+            if (!EXACT && tid + u * THREADS >= UNITS) continue;
+            const int i0 = unit(tid, u) / PIECES * 4, c = unit(tid, u) % PIECES * CV;
 #pragma unroll
             for (int r = 0; r < 4; ++r)
                 __builtin_memcpy(__builtin_assume_aligned(to + i0 * ld + place(c) + r * ld, 8), x[u][r],
@@ -293,11 +293,11 @@ struct Stage {
         }
     }
     // columns as rows of C places
-    __device__ __forceinline__ void store_transposed(T *to) const {
+    __device__ __forceinline__ void store_transposed(int tid, T *to) const {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (!EXACT && (int)threadIdx.x + u * THREADS >= UNITS) continue;
-            const int i0 = unit(u) / PIECES * 4, c = unit(u) % PIECES * CV;
+            if (!EXACT && tid + u * THREADS >= UNITS) continue;
+            const int i0 = unit(tid, u) / PIECES * 4, c = unit(tid, u) % PIECES * CV;
             // (two columns of a multiple of four keep their 16 bytes' places, the others turn one bit)
             T *const at[2] = {to + spread<T>(c, i0), to + spread<T>(c + 2, i0) - 2 * C};
 #pragma unroll
@@ -401,10 +401,6 @@ __global__ __launch_bounds__(NW * kWave, KD <= 128 ? 2 : 1) void scan_kernel(Sca
         }
     }
     if (threadIdx.x < 2) unusual[threadIdx.x] = 0;
-    // this lane's places in what the products read: all others are a constant from them
-    const Spread<T> by_k(ldsKt, n16, g), by_v(ldsVt, n16, g), by_p(ldsP, n16, g);
-    const T *const byQ = ldsQ + n16 * LDK + 8 * g, *const byK = ldsK + n16 * LDK + 8 * g;
-
     // this lane's part of the state: rows 16 kt + 4 g + r, column n16 of the wave's
     f32x4v S[KT], D[DERIV ? KT : 1];
     auto each_state = [&](const float *from, bool by_seq, auto f) {
@@ -438,14 +434,16 @@ __global__ __launch_bounds__(NW * kWave, KD <= 128 ? 2 : 1) void scan_kernel(Sca
     int single = 0, turn = 0;  // single: tokens that are still taken one by one
     int pos = 0, len = 0, next = 0, next_len = min(C, seg.n);
     for (;;) {
-        // ---- the next chunk's rows are on their way while this one's are multiplied
-        if (next < seg.n) {
-            const int64_t t0 = first + (int64_t)next * dir;
-            if (KIND != kState) xq.load(a.q, h, 0, t0, a.rev, next_len);
-            xk.load(a.k, h, 0, t0, a.rev, next_len);
-            xv.load(a.v, h, col0, t0, a.rev, next_len);
-        }
+        // What follows from the thread's number is found again for each chunk: kept across the
+        // loop it would take more registers than the state.
+        int tid = threadIdx.x;
+        opaque(tid);
         if (len > 0) {
+            const int n16 = tid % 16, g = tid % kWave / 16;
+            // this lane's places in what the products read: all others are a constant from them
+            const Spread<T> by_k(ldsKt, n16, g), by_v(ldsVt, n16, g), by_p(ldsP, n16, g);
+            const T *const byQ = ldsQ + n16 * LDK + 8 * g, *const byK = ldsK + n16 * LDK + 8 * g;
+
             f32x4v O[IT], OD[DERIV ? IT : 1];
             if constexpr (KIND != kState) {
                 // ---- scores: tile (it, jt) of 16 x 16, jt <= it, shared out among the waves
@@ -622,19 +620,25 @@ __global__ __launch_bounds__(NW * kWave, KD <= 128 ? 2 : 1) void scan_kernel(Sca
             __syncthreads();
         }
         if (next >= seg.n) break;
-        // ---- to LDS
+        // ---- the next chunk's rows to LDS
+        {
+            const int64_t t0 = first + (int64_t)next * dir;
+            if (KIND != kState) xq.load(tid, a.q, h, 0, t0, a.rev, next_len);
+            xk.load(tid, a.k, h, 0, t0, a.rev, next_len);
+            xv.load(tid, a.v, h, col0, t0, a.rev, next_len);
+        }
         pos = next;
         len = next_len;
         for (;;) {
-            xk.clear(a.k.width, len);
-            xv.clear(a.v.width - col0, len);
+            xk.clear(tid, a.k.width, len);
+            xv.clear(tid, a.v.width - col0, len);
             if (KIND != kState) {
-                xq.clear(a.q.width, len);
-                xq.store(ldsQ, LDK);
-                xk.store(ldsK, LDK);
+                xq.clear(tid, a.q.width, len);
+                xq.store(tid, ldsQ, LDK);
+                xk.store(tid, ldsK, LDK);
             }
-            xk.store_transposed(ldsKt);
-            xv.store_transposed(ldsVt);
+            xk.store_transposed(tid, ldsKt);
+            xv.store_transposed(tid, ldsVt);
             if (KIND != kState && !xv.finite()) unusual[turn] = 1;
             __syncthreads();
             // A product with a score of 0 keeps an infinite or missing number of a later token
