@@ -181,33 +181,45 @@ __device__ __forceinline__ int place(int k) {
     return k / 32 * 32 + (u % 4) * 8 + (u / 4) * 4;
 }
 
-// Where place j of row `row` lies in LDS, of rows of C places (128 bytes): 16 bytes are moved
-// together, and rows that lanes write or read at once lie on different banks.
+// Banks.  LDS has 64 of them; a read of 16 bytes a lane takes lanes 0-3, 12-15, 20-27 at once,
+// then 4-11, 16-19, 28-31, and so on (found by counting conflicts over row distances), a write
+// of 8 bytes 16 consecutive lanes over half of them.  The 16 bytes of a row that a lane
+// group reads are therefore turned by bits of the row's number, so that neither reads
+// nor writes (Stage's) of bf16 meet: 45% of the cycles of LDS were conflicts before.
+
+// Of rows by token, KD values and 16 bytes apart.
+template <class T>
+__device__ __forceinline__ int turned(int row) {
+    return sizeof(T) == 2 ? ((row >> 2 ^ row >> 3) & 1) * 8 : 0;
+}
+
+// Place j of row `row` of rows of C places (128 bytes).
 template <class T>
 __device__ __forceinline__ int spread(int row, int j) {
     constexpr int B = 16 / sizeof(T);
-    const int x = sizeof(T) == 2 ? ((row >> 1 ^ row >> 3) & 1) | (row >> 1 & 2) | (row >> 2 & 4)
+    const int x = sizeof(T) == 2 ? (row >> 2 & 1) | ((row >> 1 ^ row >> 2) & 2) | ((row << 1 ^ row >> 2) & 4)
                                  : row >> 1 & 7;
     return row * kChunkOf<T> + ((j / B ^ x) * B | j % B);
 }
 
 // A lane's fragments of such rows: row 16 tile + lane % 16, places 32 f + 8 (lane / 16) on.
-// One address for all of them, the rest known at compile time (or the same for all lanes).
+// Two addresses for all of them, the rest known at compile time (or the same for all lanes).
 template <class T>
 struct Spread {
-    const T *p[sizeof(T) / 2];  // of each 16 bytes
+    const T *p[2];  // bf16: of even and of odd f + tile; fp32: of either half of the places
     __device__ __forceinline__ Spread(const T *rows, int n16, int g) {
 #pragma unroll
-        for (int b = 0; b < (int)sizeof(T) / 2; ++b) p[b] = rows + spread<T>(n16, 8 * g + b * 4);
+        for (int b = 0; b < 2; ++b) p[b] = rows + spread<T>(n16, 8 * g + b * (sizeof(T) == 2 ? 32 : 4));
     }
     __device__ __forceinline__ Frag<T> at(int tile, int f) const {
         Frag<T> x;
-        // (bf16: tile and f turn the same bit of a place's 16 bytes, the lane none of it)
-        const int off = tile * 16 * kChunkOf<T> + (sizeof(T) == 2 ? ((f ^ tile) & 1) * 32 : 0);
+        const int off = tile * 16 * kChunkOf<T>;
 #pragma unroll
-        for (int b = 0; b < (int)sizeof(T) / 2; ++b)
+        for (int b = 0; b < (int)sizeof(T) / 2; ++b) {
+            const bool odd = sizeof(T) == 2 ? (f ^ tile) & 1 : b;
             __builtin_memcpy(reinterpret_cast<char *>(&x) + 16 * b,
-                             __builtin_assume_aligned(p[b] + off, 16), 16);
+                             __builtin_assume_aligned((odd ? p[1] : p[0]) + off, 16), 16);
+        }
         return x;
     }
 };
@@ -230,6 +242,8 @@ struct Stage {
         const int n = tid + u * THREADS;
         return EXACT ? n : min(n, UNITS - 1);
     }
+    // (neighbouring lanes take either half of the same eight rows)
+    static __device__ __forceinline__ int row_of(int n) { return (n / (2 * PIECES) * 2 + n % 2) * 4; }
     // Rows i < len (at least one) from token t0 on, or back; columns from col0 on.  Nothing here
     // depends on a lane's place: what is beyond a row or the chunk reads a neighbour of it,
     // and is cleared by clear().  A whole chunk's four rows have one place and four bases.
@@ -241,7 +255,7 @@ struct Stage {
         const uint32_t row = (uint32_t)m.ld * sizeof(T);  // bytes
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int i0 = unit(tid, u) / PIECES * 4, c = unit(tid, u) % PIECES * CV;
+            const int i0 = row_of(unit(tid, u)), c = unit(tid, u) / 2 % PIECES * CV;
             if (!TAIL && len == C) {
                 const uint32_t at = (uint32_t)(rev ? C - 4 - i0 : i0) * row + min(c, width - CV) * sizeof(T);
 #pragma unroll
@@ -269,7 +283,7 @@ struct Stage {
         if (len == C && width >= W) return;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int i0 = unit(tid, u) / PIECES * 4, c = unit(tid, u) % PIECES * CV;
+            const int i0 = row_of(unit(tid, u)), c = unit(tid, u) / 2 % PIECES * CV;
 #pragma unroll
             for (int d = 0; d < WD; ++d) {
                 const int e = TAIL ? c + d * (CV / WD) : c;  // the first value of the four bytes
@@ -285,10 +299,10 @@ struct Stage {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (!EXACT && tid + u * THREADS >= UNITS) continue;
-            const int i0 = unit(tid, u) / PIECES * 4, c = unit(tid, u) % PIECES * CV;
+            const int i0 = row_of(unit(tid, u)), c = unit(tid, u) / 2 % PIECES * CV;
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                __builtin_memcpy(__builtin_assume_aligned(to + i0 * ld + place(c) + r * ld, 8), x[u][r],
+                __builtin_memcpy(__builtin_assume_aligned(to + i0 * ld + (place(c) ^ turned<T>(i0)) + r * ld, 8), x[u][r],
                                  sizeof x[u][r]);
         }
     }
@@ -297,7 +311,7 @@ struct Stage {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (!EXACT && tid + u * THREADS >= UNITS) continue;
-            const int i0 = unit(tid, u) / PIECES * 4, c = unit(tid, u) % PIECES * CV;
+            const int i0 = row_of(unit(tid, u)), c = unit(tid, u) / 2 % PIECES * CV;
             // (two columns of a multiple of four keep their 16 bytes' places, the others turn one bit)
             T *const at[2] = {to + spread<T>(c, i0), to + spread<T>(c + 2, i0) - 2 * C};
 #pragma unroll
@@ -433,16 +447,27 @@ __global__ __launch_bounds__(NW * kWave, KD <= 128 ? 2 : 1) void scan_kernel(Sca
     float dsum = 0.f;
     int single = 0, turn = 0;  // single: tokens that are still taken one by one
     int pos = 0, len = 0, next = 0, next_len = min(C, seg.n);
+    // The next chunk's rows are on their way while one is multiplied where that leaves the card
+    // as many waves; the other blocks of a CU hide them else.
+    constexpr bool AHEAD = KIND == kState || (KIND == kOutput && KD <= 64);
+    auto load = [&](int tid) {
+        const int64_t t0 = first + (int64_t)next * dir;
+        if (KIND != kState) xq.load(tid, a.q, h, 0, t0, a.rev, next_len);
+        xk.load(tid, a.k, h, 0, t0, a.rev, next_len);
+        xv.load(tid, a.v, h, col0, t0, a.rev, next_len);
+    };
     for (;;) {
         // What follows from the thread's number is found again for each chunk: kept across the
         // loop it would take more registers than the state.
         int tid = threadIdx.x;
         opaque(tid);
+        if (AHEAD && next < seg.n) load(tid);
         if (len > 0) {
             const int n16 = tid % 16, g = tid % kWave / 16;
             // this lane's places in what the products read: all others are a constant from them
             const Spread<T> by_k(ldsKt, n16, g), by_v(ldsVt, n16, g), by_p(ldsP, n16, g);
-            const T *const byQ = ldsQ + n16 * LDK + 8 * g, *const byK = ldsK + n16 * LDK + 8 * g;
+            const T *const byQ = ldsQ + n16 * LDK + (8 * g ^ turned<T>(n16));
+            const T *const byK = byQ + (ldsK - ldsQ);
 
             f32x4v O[IT], OD[DERIV ? IT : 1];
             if constexpr (KIND != kState) {
@@ -621,12 +646,7 @@ __global__ __launch_bounds__(NW * kWave, KD <= 128 ? 2 : 1) void scan_kernel(Sca
         }
         if (next >= seg.n) break;
         // ---- the next chunk's rows to LDS
-        {
-            const int64_t t0 = first + (int64_t)next * dir;
-            if (KIND != kState) xq.load(tid, a.q, h, 0, t0, a.rev, next_len);
-            xk.load(tid, a.k, h, 0, t0, a.rev, next_len);
-            xv.load(tid, a.v, h, col0, t0, a.rev, next_len);
-        }
+        if (!AHEAD) load(tid);
         pos = next;
         len = next_len;
         for (;;) {
