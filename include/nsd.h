@@ -998,7 +998,7 @@ nsd_status nsd_adamw_step(const nsd_adamw_plan *plan, const nsd_adamw *h, void *
  * norms that it belongs to and the factor NaN; an infinity makes norms infinite
  * and the factor 0.
  *
- * A tensor is a flat array of n < 2^31 - 16384 values, at any address that its
+ * A tensor is a flat array of n < 2^31 - 8192 values, at any address that its
  * type allows.  Tensors may share memory; each counts by itself.
  *
  * nsd_grad_plan_size   bytes of the plan's device table (host output).

@@ -206,11 +206,11 @@ __device__ __forceinline__ int spread(int row, int j) {
 // Two addresses for all of them, the rest known at compile time (or the same for all lanes).
 template <class T>
 struct Spread {
-    const T *p[2];  // bf16: of even and of odd f + tile; fp32: of either half of the places
-    __device__ __forceinline__ Spread(const T *rows, int n16, int g) {
-#pragma unroll
-        for (int b = 0; b < 2; ++b) p[b] = rows + spread<T>(n16, 8 * g + b * (sizeof(T) == 2 ? 32 : 4));
-    }
+    const T *p;
+    int other;  // bf16: of odd f + tile; fp32: of the second half of the places
+    __device__ __forceinline__ Spread(const T *rows, int n16, int g)
+        : p(rows + spread<T>(n16, 8 * g)),
+          other(spread<T>(n16, 8 * g + (sizeof(T) == 2 ? 32 : 4)) - spread<T>(n16, 8 * g)) {}
     __device__ __forceinline__ Frag<T> at(int tile, int f) const {
         Frag<T> x;
         const int off = tile * 16 * kChunkOf<T>;
@@ -218,7 +218,7 @@ struct Spread {
         for (int b = 0; b < (int)sizeof(T) / 2; ++b) {
             const bool odd = sizeof(T) == 2 ? (f ^ tile) & 1 : b;
             __builtin_memcpy(reinterpret_cast<char *>(&x) + 16 * b,
-                             __builtin_assume_aligned((odd ? p[1] : p[0]) + off, 16), 16);
+                             __builtin_assume_aligned(p + off + (odd ? other : 0), 16), 16);
         }
         return x;
     }
@@ -369,15 +369,29 @@ struct Shared {
     static constexpr int VALUES = Q + KP + KD * C + VB * C;
 };
 
+// Waves of a SIMD, which say how many registers one may have: two blocks of eight waves a CU
+// where the state leaves room for it (a training step's scans 404 and 163 us with one block, 348
+// and 160 with two).
+constexpr int waves_of(int kd, int nw, Kind kind) {
+    return kd > 128 ? 1 : nw == 4 || (kind == kDerivative && kd > 64) ? 2 : 4;
+}
+
 // KD: width of queries and keys, padded; NW: waves, 16 columns of the values each; blocks: of
 // the segments' heads' columns, nvb for each head.
 template <class T, int KD, int NW, Kind KIND, bool TAIL>
-__global__ __launch_bounds__(NW * kWave, KD <= 128 ? 2 : 1) void scan_kernel(Scan a, int32_t nvb) {
+__global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kernel(Scan a, int32_t nvb) {
     using Sh = Shared<T, KD, NW, KIND>;
     constexpr int C = Sh::C, VB = Sh::VB, LDK = Sh::LDK;
     constexpr int KT = KD / 16, KF = KD / 32, IT = C / 16, JF = C / 32;
     constexpr int NS = Sh::NS, SP = Sh::SP, VP = kParts<T, 3>;
     constexpr bool DERIV = KIND == kDerivative;
+    // Operands of the next products on their way during these: where LDS, not registers, says how
+    // many blocks a CU has.
+    constexpr bool PIPE = NW == 4 && KIND != kState;
+    auto hold = [] {
+        if constexpr (PIPE) __builtin_amdgcn_sched_barrier(0);
+    };
+    constexpr int GR = KT < IT ? KT : IT;  // rows of the state that a step of their products takes
     __shared__ __align__(16) T lds[Sh::VALUES];
     T *const ldsQ = lds;
     T *const ldsK = ldsQ + Sh::Q;
@@ -416,7 +430,7 @@ __global__ __launch_bounds__(NW * kWave, KD <= 128 ? 2 : 1) void scan_kernel(Sca
     }
     if (threadIdx.x < 2) unusual[threadIdx.x] = 0;
     // this lane's part of the state: rows 16 kt + 4 g + r, column n16 of the wave's
-    f32x4v S[KT], D[DERIV ? KT : 1];
+    f32x4v S[KT], D[KT];  // (D: of DERIV alone)
     auto each_state = [&](const float *from, bool by_seq, auto f) {
         const float *const p = from + ((int64_t)(by_seq ? seg.seq : id) * a.H + h) * a.per;
         const int c = col0 + colw + n16;
@@ -469,7 +483,7 @@ __global__ __launch_bounds__(NW * kWave, KD <= 128 ? 2 : 1) void scan_kernel(Sca
             const T *const byQ = ldsQ + n16 * LDK + (8 * g ^ turned<T>(n16));
             const T *const byK = byQ + (ldsK - ldsQ);
 
-            f32x4v O[IT], OD[DERIV ? IT : 1];
+            f32x4v O[IT];
             if constexpr (KIND != kState) {
                 // ---- scores: tile (it, jt) of 16 x 16, jt <= it, shared out among the waves
                 constexpr int TILES = IT * (IT + 1) / 2;
@@ -513,46 +527,52 @@ __global__ __launch_bounds__(NW * kWave, KD <= 128 ? 2 : 1) void scan_kernel(Sca
                         }
                     }
                 }
-                // ---- from the state
+                // ---- from the state (DERIV: (i + 1) times that, and from its derivative)
 #pragma unroll
-                for (int it = 0; it < IT; ++it) {
-                    O[it] = f32x4v{0.f, 0.f, 0.f, 0.f};
-                    if (DERIV) OD[it] = f32x4v{0.f, 0.f, 0.f, 0.f};
-                }
+                for (int it = 0; it < IT; ++it) O[it] = f32x4v{0.f, 0.f, 0.f, 0.f};
+                Frag<T> qf[2][IT];
+                auto load_q = [&](int f) {
 #pragma unroll
-                for (int f = 0; f < KF; ++f) {
-                    Frag<T> sf[SP], df[SP];
-                    float x[8];
+                    for (int it = 0; it < IT; ++it) qf[f & 1][it] = fragment(byQ + 16 * it * LDK + 32 * f);
+                };
+                auto from_state = [&](const f32x4v (&state)[KT]) {
+                    if (PIPE) load_q(0);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = S[2 * f + e / 4][e % 4];
-                    split<T, NS>(x, sf);
-                    if constexpr (DERIV) {
+                    for (int f = 0; f < KF; ++f) {
+                        if (!PIPE) load_q(f);
+                        else if (f + 1 < KF) load_q(f + 1);
+                        hold();
+                        Frag<T> sf[SP];
+                        float x[8];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) x[e] = D[2 * f + e / 4][e % 4];
-                        split<T, NS>(x, df);
+                        for (int e = 0; e < 8; ++e) x[e] = state[2 * f + e / 4][e % 4];
+                        split<T, NS>(x, sf);
+#pragma unroll
+                        for (int s = 0; s < SP; ++s)
+#pragma unroll
+                            for (int it = 0; it < IT; ++it) mma(O[it], sf[s], qf[f & 1][it]);
+                        hold();
                     }
+                };
+                from_state(S);
+                if constexpr (DERIV) {
 #pragma unroll
-                    for (int it = 0; it < IT; ++it) {
-                        const Frag<T> qf = fragment(byQ + 16 * it * LDK + 32 * f);
+                    for (int it = 0; it < IT; ++it)
 #pragma unroll
-                        for (int s = 0; s < SP; ++s) {
-                            mma(O[it], sf[s], qf);
-                            if constexpr (DERIV) mma(OD[it], df[s], qf);
-                        }
-                    }
+                        for (int r = 0; r < 4; ++r) O[it][r] *= (float)(16 * it + n16 + 1);
+                    from_state(D);
                 }
-#pragma unroll
-                for (int it = 0; it < IT; ++it) {
-                    const int i = 16 * it + n16;
-                    const float w = a.s_inter * power[i + 1 - rev];
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        O[it][r] = DERIV ? w * __builtin_fmaf((float)(i + 1), O[it][r], OD[it][r])
-                                         : w * O[it][r];
-                }
-                __syncthreads();
             }
-            // ---- from the chunk's own tokens, and the state behind them
+            // ---- the state behind the chunk
+            Frag<T> vf[JF], kf[2][GR];
+            auto load_k = [&](int step) {
+#pragma unroll
+                for (int i = 0; i < GR; ++i)
+                    kf[step & 1][i] = by_k.at(step % (KT / GR) * GR + i, step / (KT / GR));
+            };
+#pragma unroll
+            for (int f = 0; f < JF; ++f) vf[f] = by_v.at(wave, f);
+            if (PIPE) load_k(0);
             const float keep = power[len], less = power_less[len];
             if (keep > 0.5f) {  // a slow decay by what it takes away
 #pragma unroll
@@ -574,12 +594,20 @@ __global__ __launch_bounds__(NW * kWave, KD <= 128 ? 2 : 1) void scan_kernel(Sca
                         S[kt][r] *= keep;
                     }
             }
+            if constexpr (KIND != kState) {
+#pragma unroll
+                for (int it = 0; it < IT; ++it) {
+                    const int i = 16 * it + n16;
+                    const float w = a.s_inter * power[i + 1 - rev];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) O[it][r] *= w;
+                }
+            }
 #pragma unroll
             for (int f = 0; f < JF; ++f) {
-                const Frag<T> vf = by_v.at(wave, f);
                 Frag<T> vs[VP], vd[VP];
                 T v[8];
-                __builtin_memcpy(v, &vf, sizeof v);
+                __builtin_memcpy(v, &vf[f], sizeof v);
                 float x[8];
                 if (len == C) {
                     __builtin_memcpy(x, __builtin_assume_aligned(behind + 32 * f + 8 * g, 16), sizeof x);
@@ -595,21 +623,40 @@ __global__ __launch_bounds__(NW * kWave, KD <= 128 ? 2 : 1) void scan_kernel(Sca
                     for (int e = 0; e < 8; ++e) x[e] *= (float)max(len - 1 - (32 * f + 8 * g + e), 0);
                     split<T, 3>(x, vd);
                 }
-                if constexpr (KIND != kState) {
 #pragma unroll
-                    for (int it = 2 * f; it < IT; ++it)
+                for (int kg = 0; kg < KT / GR; ++kg) {
+                    const int step = f * (KT / GR) + kg;
+                    if (!PIPE) load_k(step);
+                    else if (step + 1 < JF * (KT / GR)) load_k(step + 1);
+                    hold();
 #pragma unroll
-                        for (int s = 0; s < SP; ++s)
-                            mma(O[it], vf, by_p.at(s * (C / 16) + it, f));
+                    for (int s = 0; s < VP; ++s)
+#pragma unroll
+                        for (int i = 0; i < GR; ++i) {
+                            mma(S[kg * GR + i], kf[step & 1][i], vs[s]);
+                            if constexpr (DERIV) mma(D[kg * GR + i], kf[step & 1][i], vd[s]);
+                        }
+                    hold();
                 }
+            }
+            // ---- from the chunk's own tokens
+            if constexpr (KIND != kState) {
+                __syncthreads();
+                Frag<T> pf[2][IT];
+                auto load_p = [&](int step) {
 #pragma unroll
-                for (int kt = 0; kt < KT; ++kt) {
-                    const Frag<T> kf = by_k.at(kt, f);
+                    for (int it = step / SP * 2; it < IT; ++it)
+                        pf[step & 1][it] = by_p.at(step % SP * (C / 16) + it, step / SP);
+                };
+                if (PIPE) load_p(0);
 #pragma unroll
-                    for (int s = 0; s < VP; ++s) {
-                        mma(S[kt], kf, vs[s]);
-                        if constexpr (DERIV) mma(D[kt], kf, vd[s]);
-                    }
+                for (int step = 0; step < JF * SP; ++step) {
+                    if (!PIPE) load_p(step);
+                    else if (step + 1 < JF * SP) load_p(step + 1);
+                    hold();
+#pragma unroll
+                    for (int it = step / SP * 2; it < IT; ++it) mma(O[it], vf[step / SP], pf[step & 1][it]);
+                    hold();
                 }
             }
             // ---- outputs: row i by lane % 16, four columns each

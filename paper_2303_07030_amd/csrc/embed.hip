@@ -7,9 +7,9 @@
 // needs the tokens by word, in their order, without the host: each block of
 // embed_order_kernel takes 256 words, looks through all ids, counts those before
 // its words (the place of its tokens in the order) and those of each word, and
-// on a second look puts its tokens there.  One launch instead of a radix sort's
-// six; the ids come from L2 but for the first block.  Where words times tokens
-// are too many for that the radix sort is taken.
+// puts its tokens there.  One launch instead of a radix sort's six; the ids come
+// from L2 but for the first block.  Where words times tokens are too many for
+// that the radix sort is taken.
 //
 // The sums: a wave takes a word and a tile of columns and adds up its tokens' rows
 // in their order.  A word of more than kLong tokens (a few words are a tenth of a
@@ -68,33 +68,66 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_kernel(
 
 // Places of the tokens of words [256 b, 256 b + 256) in the order by word: `perm` the
 // token, `word` its word, of every place; segptr the first place of every word.
+//
+// A wave looks through consecutive tokens, four a lane, and keeps those of the block's words
+// in a list in LDS, in their order; what does not fit (a word that takes most of the batch)
+// it looks up again.
+constexpr int kOrderList = 2048;  // of a wave
+constexpr int kOrderStep = 4 * kWave;
+
 __global__ __launch_bounds__(kOrderThreads) void embed_order_kernel(
     int32_t ntok, int32_t vocab, const int32_t *__restrict__ ids, int32_t *__restrict__ perm,
     int32_t *__restrict__ word, int32_t *__restrict__ segptr) {
     __shared__ int32_t count[kOrderWaves][kOrderWords];  // of a wave's tokens; then its next place
+    __shared__ uint32_t list[kOrderWaves][kOrderList];   // token less the wave's first, and word
     __shared__ int32_t below[kOrderWaves], scan[kOrderWords / kWave];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const int lo = blockIdx.x * kOrderWords;
     const int words = min(kOrderWords, vocab - lo);
     for (int i = threadIdx.x; i < kOrderWaves * kOrderWords; i += kOrderThreads) (&count[0][0])[i] = 0;
     __syncthreads();
-    // a wave's tokens are consecutive ones; eight loads are in flight at once
-    constexpr int kAhead = 8;
-    const int piece = (ntok / (kOrderWaves * kWave) + 1) * kWave;
+    const int piece = (ntok / (kOrderWaves * kOrderStep) + 1) * kOrderStep;
     const int first = (int)min((int64_t)wave * piece, (int64_t)ntok);
     const int last = (int)min((int64_t)first + piece, (int64_t)ntok);
-    int before = 0;
-    for (int b = first; b < last; b += kWave * kAhead) {
-        int id[kAhead];
+    const uint64_t lower = (1ull << lane) - 1;
+    int before = 0, kept = 0, done = last;  // done: the tokens from here on are not in the list
+    constexpr int kAhead = 4;
+    for (int b = first; b < last; b += kOrderStep * kAhead) {
+        int id[kAhead][4];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            const int t = b + u * kWave + lane;
-            id[u] = t < last ? ids[t] : -1;
+            const int t = b + u * kOrderStep + lane * 4;
+            if (t + 4 <= last) {
+                __builtin_memcpy(id[u], ids + t, sizeof id[u]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) id[u][e] = t + e < last ? ids[t + e] : -1;
+            }
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            before += id[u] >= 0 && id[u] < lo;
-            if (id[u] >= lo && id[u] - lo < words) atomicAdd(&count[wave][id[u] - lo], 1);
+            const int t = b + u * kOrderStep;
+            uint64_t here[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                before += id[u][e] >= 0 && id[u][e] < lo;
+                here[e] = __ballot(id[u][e] >= lo && id[u][e] - lo < words);
+            }
+            if ((here[0] | here[1] | here[2] | here[3]) == 0) continue;
+            int at = kept;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) at += __popcll(here[e] & lower);
+            if (kept + kOrderStep > kOrderList) done = min(done, t);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (!(here[e] >> lane & 1)) continue;
+                const int x = id[u][e] - lo;
+                atomicAdd(&count[wave][x], 1);
+                if (done == last) list[wave][at++] = (uint32_t)(t + lane * 4 + e - first) << 8 | x;
+            }
+            if (done == last)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) kept += __popcll(here[e]);
         }
     }
 #pragma unroll
@@ -126,35 +159,33 @@ __global__ __launch_bounds__(kOrderThreads) void embed_order_kernel(
         }
     }
     __syncthreads();
-    for (int b = first; b < last; b += kWave * kAhead) {
-        int id[kAhead];
+    // a token a lane, in their order; x: its word in the block, or none of them
+    auto put = [&](bool here, int x, int t) {
+        uint64_t same = __ballot(here);  // lanes with this lane's word
+        if (same == 0) return;
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const int t = b + u * kWave + lane;
-            id[u] = t < last ? ids[t] : -1;
+        for (int bit = 0; bit < 8; ++bit) {
+            const uint64_t set = __ballot(here && (x >> bit & 1));
+            same &= x >> bit & 1 ? set : ~set;
         }
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const int x = id[u] - lo;
-            const bool here = id[u] >= lo && x < words;
-            uint64_t same = __ballot(here);  // lanes with this lane's word
-            if (same == 0) continue;
-#pragma unroll
-            for (int bit = 0; bit < 8; ++bit) {
-                const uint64_t set = __ballot(here && (x >> bit & 1));
-                same &= x >> bit & 1 ? set : ~set;
-            }
-            if (here) {
-                const int place = count[wave][x];
-                const int rank = __popcll(same & ((1ull << lane) - 1));
-                perm[place + rank] = b + u * kWave + lane;
-                word[place + rank] = id[u];
-                if (rank == __popcll(same) - 1) count[wave][x] = place + rank + 1;
-            }
-            // the next look reads what another lane wrote
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
+        if (here) {
+            const int place = count[wave][x], rank = __popcll(same & lower);
+            perm[place + rank] = t;
+            word[place + rank] = lo + x;
+            if (rank == __popcll(same) - 1) count[wave][x] = place + rank + 1;
         }
+        // the next ones read what another lane wrote
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    };
+    for (int i = 0; i < kept; i += kWave) {
+        const bool here = i + lane < kept;
+        const uint32_t v = here ? list[wave][i + lane] : 0;
+        put(here, (int)(v & 255), first + (int)(v >> 8));
+    }
+    for (int b = done; b < last; b += kWave) {
+        const int id = b + lane < last ? ids[b + lane] : -1;
+        put(id >= lo && id - lo < words, id - lo, b + lane);
     }
 }
 

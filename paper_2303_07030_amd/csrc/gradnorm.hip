@@ -21,15 +21,14 @@ namespace nsd {
 namespace {
 
 constexpr int kGradThreads = 256;
-constexpr int64_t kChunk = 16384;
+constexpr int64_t kChunk = 8192;
 
 struct GradTensor {
-    void *g;
-    int32_t n, dtype;
     int32_t first_chunk, nchunks;
 };
-struct GradChunk {
-    int32_t tensor, first;  // the tensor, and the first value in it
+struct GradChunk {  // all that a block needs, so that it waits for one read before the values'
+    void *g;
+    int32_t n, dtype;
 };
 
 // Largest magnitudes are compared as bits: in their order a NaN is above infinity.
@@ -70,16 +69,16 @@ __device__ __forceinline__ void over_block(Partial<MAX> &p) {
 }
 
 template <bool MAX, class T>
-__device__ __forceinline__ void take_chunk(Partial<MAX> &p, const T *g, int64_t first, int64_t end) {
+__device__ __forceinline__ void take_chunk(Partial<MAX> &p, const T *g, int end) {
     constexpr int N = 16 / sizeof(T);
     Partial<MAX> q[4];  // independent sums: a chain of one would wait for every value
-    constexpr int64_t step = (int64_t)kGradThreads * N;
-    for (int64_t b = first; b < end; b += 4 * step) {
+    constexpr int step = kGradThreads * N;
+    for (int b = 0; b < end; b += 4 * step) {
         float x[4][N];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            const int64_t i = b + u * step + (int64_t)threadIdx.x * N;
-            load_left<N, T>(g + min(i, end), (int)max(min(end - i, (int64_t)N), (int64_t)0), x[u]);
+            const int i = b + u * step + (int)threadIdx.x * N;
+            load_left<N, T>(g + min(i, end), max(min(end - i, N), 0), x[u]);
         }
 #pragma unroll
         for (int e = 0; e < N; ++e)
@@ -92,13 +91,11 @@ __device__ __forceinline__ void take_chunk(Partial<MAX> &p, const T *g, int64_t 
 
 template <bool MAX>
 __global__ __launch_bounds__(kGradThreads) void grad_chunk_kernel(
-    const GradTensor *__restrict__ tensors, const GradChunk *__restrict__ chunks, double *part) {
+    const GradChunk *__restrict__ chunks, double *part) {
     const GradChunk c = chunks[blockIdx.x];
-    const GradTensor t = tensors[c.tensor];
-    const int64_t end = min(c.first + kChunk, (int64_t)t.n);
     Partial<MAX> p;
-    if (t.dtype == NSD_F32) take_chunk<MAX, float>(p, static_cast<const float *>(t.g), c.first, end);
-    else take_chunk<MAX, Bf16>(p, static_cast<const Bf16 *>(t.g), c.first, end);
+    if (c.dtype == NSD_F32) take_chunk<MAX, float>(p, static_cast<const float *>(c.g), c.n);
+    else take_chunk<MAX, Bf16>(p, static_cast<const Bf16 *>(c.g), c.n);
     over_block<MAX, kGradThreads>(p);
     if (threadIdx.x == 0) part[blockIdx.x] = p.value();
 }
@@ -115,7 +112,14 @@ __global__ __launch_bounds__(kJoinThreads) void grad_join_kernel(
         n = tensors[blockIdx.x - 1].nchunks;
     }
     Partial<MAX> p;
-    for (int i = threadIdx.x; i < n; i += kJoinThreads) p.join(part[first + i]);
+    for (int i = threadIdx.x; i < n; i += 8 * kJoinThreads) {
+        double v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            v[u] = i + u * kJoinThreads < n ? part[first + i + u * kJoinThreads] : 0.0;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) p.join(v[u]);
+    }
     over_block<MAX, kJoinThreads>(p);
     if (threadIdx.x > 0) return;
     const double f = grad_scale ? (double)*grad_scale : 1.0;
@@ -130,36 +134,33 @@ __global__ __launch_bounds__(kJoinThreads) void grad_join_kernel(
 }
 
 template <class T>
-__device__ __forceinline__ void scale_chunk(T *g, int64_t first, int64_t end, float s) {
+__device__ __forceinline__ void scale_chunk(T *g, int end, float s) {
     constexpr int N = 16 / sizeof(T);
-    constexpr int64_t step = (int64_t)kGradThreads * N;
-    for (int64_t b = first; b < end; b += 4 * step) {
+    constexpr int step = kGradThreads * N;
+    for (int b = 0; b < end; b += 4 * step) {
         float x[4][N];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            const int64_t i = b + u * step + (int64_t)threadIdx.x * N;
-            load_left<N, T>(g + min(i, end), (int)max(min(end - i, (int64_t)N), (int64_t)0), x[u]);
+            const int i = b + u * step + (int)threadIdx.x * N;
+            load_left<N, T>(g + min(i, end), max(min(end - i, N), 0), x[u]);
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            const int64_t i = b + u * step + (int64_t)threadIdx.x * N;
+            const int i = b + u * step + (int)threadIdx.x * N;
 #pragma unroll
             for (int e = 0; e < N; ++e) x[u][e] *= s;
-            store_left<N, T>(g + min(i, end), (int)max(min(end - i, (int64_t)N), (int64_t)0), x[u]);
+            store_left<N, T>(g + min(i, end), max(min(end - i, N), 0), x[u]);
         }
     }
 }
 
 __global__ __launch_bounds__(kGradThreads) void grad_scale_kernel(
-    const GradTensor *__restrict__ tensors, const GradChunk *__restrict__ chunks,
-    const float *__restrict__ scale) {
+    const GradChunk *__restrict__ chunks, const float *__restrict__ scale) {
     const float s = *scale;
     if (s == 1.f) return;
     const GradChunk c = chunks[blockIdx.x];
-    const GradTensor t = tensors[c.tensor];
-    const int64_t end = min(c.first + kChunk, (int64_t)t.n);
-    if (t.dtype == NSD_F32) scale_chunk<float>(static_cast<float *>(t.g), c.first, end, s);
-    else scale_chunk<Bf16>(static_cast<Bf16 *>(t.g), c.first, end, s);
+    if (c.dtype == NSD_F32) scale_chunk<float>(static_cast<float *>(c.g), c.n, s);
+    else scale_chunk<Bf16>(static_cast<Bf16 *>(c.g), c.n, s);
 }
 
 nsd_status check_grads(int32_t n, const nsd_grad_tensor *ts, int64_t *chunks) {
@@ -257,8 +258,10 @@ nsd_status nsd_grad_plan_build(int32_t ntensors, const nsd_grad_tensor *tensors,
         for (int32_t i = 0; i < ntensors; ++i) {
             const nsd_grad_tensor &t = tensors[i];
             const int32_t own = (int32_t)ceil_div(t.n, kChunk);
-            ts[i] = GradTensor{t.grad, (int32_t)t.n, t.dtype, at, own};
-            for (int32_t c = 0; c < own; ++c) cs[at++] = GradChunk{i, (int32_t)(c * kChunk)};
+            ts[i] = GradTensor{at, own};
+            for (int32_t c = 0; c < own; ++c)
+                cs[at++] = GradChunk{static_cast<char *>(t.grad) + c * kChunk * dtype_bytes(t.dtype),
+                                     (int32_t)std::min(kChunk, t.n - c * kChunk), t.dtype};
         }
         hipError_t e = hipMemcpyAsync(table, host, need, hipMemcpyHostToDevice, as_stream(stream));
         if (e == hipSuccess) e = hipStreamSynchronize(as_stream(stream));
@@ -300,7 +303,7 @@ nsd_status nsd_grad_norm(const nsd_grad_plan *plan, const nsd_clip *h, double *n
     auto launch = [&](auto max) -> nsd_status {
         constexpr bool MAX = decltype(max)::value;
         if (plan->nchunks > 0) {
-            grad_chunk_kernel<MAX><<<plan->nchunks, kGradThreads, 0, st>>>(ts, chunks_of(plan), part);
+            grad_chunk_kernel<MAX><<<plan->nchunks, kGradThreads, 0, st>>>(chunks_of(plan), part);
             NSD_TRY(check_launch("grad_chunk_kernel"));
         }
         grad_join_kernel<MAX><<<1 + (norms ? plan->ntensors : 0), kJoinThreads, 0, st>>>(
@@ -316,7 +319,7 @@ nsd_status nsd_grad_clip(const nsd_grad_plan *plan, const float *scale, void *st
     NSD_REQUIRE(!plan->shared, "tensors that share memory would be scaled more than once");
     if (plan->nchunks == 0) return NSD_OK;
     grad_scale_kernel<<<plan->nchunks, kGradThreads, 0, as_stream(stream)>>>(
-        tensors_of(plan), chunks_of(plan), scale);
+        chunks_of(plan), scale);
     return check_launch("grad_scale_kernel");
 }
 

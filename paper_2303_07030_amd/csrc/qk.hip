@@ -52,10 +52,13 @@ struct QkArgs {
     float *part;  // [block][2][d]
 };
 
+// How a lane's values lie: anyhow; its a and b four consecutive ones each; a and b in turn,
+// eight consecutive ones.
+enum Lie { kAnyhow, kHalves, kNext };
+
 // The pairs p0 to p0 + 3 of a head, as a lane holds them: values a and b of pair e.  Values
-// that are not rotated pair up as they come.  VEC: a lane's a and b are four consecutive
-// values each (interleaved: eight in turn).
-template <class T, bool VEC>
+// that are not rotated pair up as they come.
+template <class T, Lie LIE>
 struct Head {
     float a[kPairs], b[kPairs];
     static __device__ __forceinline__ int place_a(const QkArgs &s, int p) {
@@ -69,17 +72,15 @@ struct Head {
         for (int e = 0; e < kPairs; ++e) a[e] = b[e] = 0.f;
     }
     __device__ __forceinline__ void load(const QkArgs &s, const T *x, int p0) {
-        if constexpr (VEC) {
-            if (s.interleaved) {
-                float t[2 * kPairs];
-                load_values<2 * kPairs, T>(x + 2 * p0, t);
+        if constexpr (LIE == kNext) {
+            float t[2 * kPairs];
+            load_values<2 * kPairs, T>(x + 2 * p0, t);
 #pragma unroll
-                for (int e = 0; e < kPairs; ++e) a[e] = t[2 * e], b[e] = t[2 * e + 1];
-            } else {
-                const int at = place_a(s, p0);
-                load_values<kPairs, T>(x + at, a);
-                load_values<kPairs, T>(x + (p0 < s.rot / 2 ? at + s.rot / 2 : at + kPairs), b);
-            }
+            for (int e = 0; e < kPairs; ++e) a[e] = t[2 * e], b[e] = t[2 * e + 1];
+        } else if constexpr (LIE == kHalves) {
+            const int at = place_a(s, p0);
+            load_values<kPairs, T>(x + at, a);
+            load_values<kPairs, T>(x + (p0 < s.rot / 2 ? at + s.rot / 2 : at + kPairs), b);
         } else {
 #pragma unroll
             for (int e = 0; e < kPairs; ++e) {
@@ -90,17 +91,15 @@ struct Head {
         }
     }
     __device__ __forceinline__ void store(const QkArgs &s, T *x, int p0) const {
-        if constexpr (VEC) {
-            if (s.interleaved) {
-                float t[2 * kPairs];
+        if constexpr (LIE == kNext) {
+            float t[2 * kPairs];
 #pragma unroll
-                for (int e = 0; e < kPairs; ++e) t[2 * e] = a[e], t[2 * e + 1] = b[e];
-                store_row_values<2 * kPairs, T>(x + 2 * p0, t);
-            } else {
-                const int at = place_a(s, p0);
-                store_row_values<kPairs, T>(x + at, a);
-                store_row_values<kPairs, T>(x + (p0 < s.rot / 2 ? at + s.rot / 2 : at + kPairs), b);
-            }
+            for (int e = 0; e < kPairs; ++e) t[2 * e] = a[e], t[2 * e + 1] = b[e];
+            store_row_values<2 * kPairs, T>(x + 2 * p0, t);
+        } else if constexpr (LIE == kHalves) {
+            const int at = place_a(s, p0);
+            store_row_values<kPairs, T>(x + at, a);
+            store_row_values<kPairs, T>(x + (p0 < s.rot / 2 ? at + s.rot / 2 : at + kPairs), b);
         } else {
 #pragma unroll
             for (int e = 0; e < kPairs; ++e) {
@@ -139,9 +138,9 @@ struct Head {
 };
 
 // A lane's view of the weights of a head.
-template <bool VEC>
+template <Lie LIE>
 __device__ __forceinline__ void load_weights(const QkArgs &s, const float *w, int p0, bool on,
-                                             Head<float, VEC> &h) {
+                                             Head<float, LIE> &h) {
 #pragma unroll
     for (int e = 0; e < kPairs; ++e) h.a[e] = h.b[e] = 1.f;
     if (w != nullptr && s.norm && on) h.load(s, w, p0);
@@ -205,16 +204,16 @@ __device__ __forceinline__ void copy_row(const T *__restrict__ from, T *__restri
 }
 
 // Unit u: part u % parts of token u / parts.  Heads 0 to H - 1 are queries, the others keys.
-template <class T, int G, bool VEC>
+template <class T, int G, Lie LIE>
 __global__ __launch_bounds__(kQkThreads) void qk_rotate_kernel(QkArgs s, int64_t units) {
     __shared__ float2 lds[kQkWaves][G * kPairs];
     constexpr int SLOTS = kWave / G;
     const int lane = threadIdx.x % kWave, slot = lane / G, p0 = lane % G * kPairs;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const bool on = p0 < s.pairs;
-    Head<float, VEC> wq, wk;
-    load_weights<VEC>(s, s.wq, p0, on, wq);
-    load_weights<VEC>(s, s.wk, p0, on, wk);
+    Head<float, LIE> wq, wk;
+    load_weights<LIE>(s, s.wq, p0, on, wq);
+    load_weights<LIE>(s, s.wk, p0, on, wk);
     const float mean = 1.f / (float)s.d;
     for (int64_t u = (int64_t)blockIdx.x * kQkWaves + wave; u < units;
          u += (int64_t)gridDim.x * kQkWaves) {
@@ -232,7 +231,7 @@ __global__ __launch_bounds__(kQkThreads) void qk_rotate_kernel(QkArgs s, int64_t
         angle.find(s, lds[wave], s.pos ? s.pos[t] : 0, lane, p0);
         const int heads = s.H + s.Hk;
         for (int h0 = part * SLOTS * kHeadsAhead; h0 < heads; h0 += s.parts * SLOTS * kHeadsAhead) {
-            Head<T, VEC> x[kHeadsAhead];
+            Head<T, LIE> x[kHeadsAhead];
 #pragma unroll
             for (int i = 0; i < kHeadsAhead; ++i) {
                 const int h = h0 + i * SLOTS + slot;
@@ -265,7 +264,7 @@ __global__ __launch_bounds__(kQkThreads) void qk_rotate_kernel(QkArgs s, int64_t
 }
 
 // Tokens by a wave, in order with a stride: dQ, dK, and the block's share of dw.
-template <class T, int G, bool VEC>
+template <class T, int G, Lie LIE>
 __global__ __launch_bounds__(kQkThreads) void qk_rotate_vjp_kernel(QkArgs s, int64_t units) {
     __shared__ float2 lds[kQkWaves][G * kPairs];
     __shared__ float sum[kQkWaves][2][2 * G * kPairs];
@@ -273,9 +272,9 @@ __global__ __launch_bounds__(kQkThreads) void qk_rotate_vjp_kernel(QkArgs s, int
     const int lane = threadIdx.x % kWave, slot = lane / G, p0 = lane % G * kPairs;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const bool on = p0 < s.pairs;
-    Head<float, VEC> wq, wk, gw[2];
-    load_weights<VEC>(s, s.wq, p0, on, wq);
-    load_weights<VEC>(s, s.wk, p0, on, wk);
+    Head<float, LIE> wq, wk, gw[2];
+    load_weights<LIE>(s, s.wq, p0, on, wq);
+    load_weights<LIE>(s, s.wk, p0, on, wk);
     gw[0].zero();
     gw[1].zero();
     const float mean = 1.f / (float)s.d;
@@ -293,10 +292,10 @@ __global__ __launch_bounds__(kQkThreads) void qk_rotate_vjp_kernel(QkArgs s, int
             const T *y0 = side ? static_cast<const T *>(s.Ko) + t * s.ldko
                                : static_cast<const T *>(s.Qo) + t * s.ldqo;
             T *g0 = side ? static_cast<T *>(s.dK) + t * s.ldk : static_cast<T *>(s.dQ) + t * s.ldq;
-            const Head<float, VEC> &w = side ? wk : wq;
+            const Head<float, LIE> &w = side ? wk : wq;
             for (int h0 = part * SLOTS * kHeadsAhead; h0 < heads;
                  h0 += s.parts * SLOTS * kHeadsAhead) {
-                Head<T, VEC> x[kHeadsAhead], y[kHeadsAhead];
+                Head<T, LIE> x[kHeadsAhead], y[kHeadsAhead];
 #pragma unroll
                 for (int i = 0; i < kHeadsAhead; ++i) {
                     const int h = h0 + i * SLOTS + slot;
@@ -354,11 +353,11 @@ __global__ __launch_bounds__(kQkThreads) void qk_rotate_vjp_kernel(QkArgs s, int
         const int side = i / (2 * G * kPairs), j = i % (2 * G * kPairs), p = j / 2;
         if (p >= s.pairs) continue;
         int at;
-        if (VEC && !s.interleaved && p >= s.rot / 2) {  // as Head::load pairs them
+        if (LIE == kHalves && p >= s.rot / 2) {  // as Head::load pairs them
             const int q = p / kPairs * kPairs;
-            at = Head<T, VEC>::place_a(s, q) + p % kPairs + (j % 2) * kPairs;
+            at = Head<T, LIE>::place_a(s, q) + p % kPairs + (j % 2) * kPairs;
         } else {
-            at = j % 2 ? Head<T, VEC>::place_b(s, p) : Head<T, VEC>::place_a(s, p);
+            at = j % 2 ? Head<T, LIE>::place_b(s, p) : Head<T, LIE>::place_a(s, p);
         }
         if (at >= s.d) continue;
         float v = 0.f;
@@ -441,8 +440,9 @@ int slot_lanes(int d) {
     while (g * kPairs * 2 < d) g <<= 1;
     return g;
 }
-bool in_fours(const nsd_qk *s) {
-    return s->d % (2 * kPairs) == 0 && (s->interleaved || s->rot / 2 % kPairs == 0);
+Lie lie_of(const nsd_qk *s) {
+    if (s->d % (2 * kPairs) != 0 || (!s->interleaved && s->rot / 2 % kPairs != 0)) return kAnyhow;
+    return s->interleaved ? kNext : kHalves;
 }
 
 // Waves for a token: one, but where that leaves the card without work the heads are shared
@@ -458,7 +458,11 @@ template <class F>
 nsd_status by_head(const nsd_qk *s, F f) {
     auto shape = [&](auto t) -> nsd_status {
         auto lanes = [&](auto g) -> nsd_status {
-            return in_fours(s) ? f(t, g, std::true_type()) : f(t, g, std::false_type());
+            switch (lie_of(s)) {
+                case kHalves: return f(t, g, std::integral_constant<Lie, kHalves>());
+                case kNext: return f(t, g, std::integral_constant<Lie, kNext>());
+                default: return f(t, g, std::integral_constant<Lie, kAnyhow>());
+            }
         };
         switch (slot_lanes(s->d)) {
             case 1: return lanes(std::integral_constant<int, 1>());
@@ -477,8 +481,8 @@ nsd_status launch_rotate(const nsd_qk *s, QkArgs a, hipStream_t st) {
     a.parts = head_parts(a.ntok, s, a.H + a.Hk);
     const int64_t units = (int64_t)a.ntok * a.parts;
     const int64_t blocks = std::min(ceil_div(units, kQkWaves), kMaxQkBlocks);
-    return by_head(s, [&](auto t, auto g, auto vec) -> nsd_status {
-        qk_rotate_kernel<decltype(t), decltype(g)::value, decltype(vec)::value>
+    return by_head(s, [&](auto t, auto g, auto lie) -> nsd_status {
+        qk_rotate_kernel<decltype(t), decltype(g)::value, decltype(lie)::value>
             <<<blocks, kQkThreads, 0, st>>>(a, units);
         return check_launch("qk_rotate_kernel");
     });
@@ -568,8 +572,8 @@ nsd_status nsd_qk_rotate_vjp(int32_t ntok, const nsd_qk *s, const void *Q, const
     if (any) {
         a.parts = head_parts(ntok, s, std::max(s->heads, s->kv_heads));
         blocks = grad_blocks(ntok, s);
-        NSD_TRY(by_head(s, [&](auto t, auto g, auto vec) -> nsd_status {
-            qk_rotate_vjp_kernel<decltype(t), decltype(g)::value, decltype(vec)::value>
+        NSD_TRY(by_head(s, [&](auto t, auto g, auto lie) -> nsd_status {
+            qk_rotate_vjp_kernel<decltype(t), decltype(g)::value, decltype(lie)::value>
                 <<<blocks, kQkThreads, 0, st>>>(a, grad_units(ntok, s));
             return check_launch("qk_rotate_vjp_kernel");
         }));

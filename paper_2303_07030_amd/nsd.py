@@ -316,9 +316,17 @@ def _nbytes(t):
     return 0 if t is None else t.numel() * t.element_size()
 
 
+_has_gpu = None
+
+
 def _stream(s):
     if s is None:
-        return torch.cuda.current_stream().cuda_stream if torch.cuda.is_available() else None
+        global _has_gpu
+        if _has_gpu is None:
+            _has_gpu = torch.cuda.is_available()
+        # the handle alone: a Stream object costs as much as a small call
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if _has_gpu \
+            else None
     return s if isinstance(s, int) else s.cuda_stream
 
 
@@ -767,6 +775,9 @@ def _rows(t, name, n, width, ld, dtype):
     """A tensor that a call takes as `n` rows of `width` values, `ld` from one to
     the next: one of another distance would be read, or written, past its end."""
     if not isinstance(t, torch.Tensor):
+        return
+    if t.dtype is dtype and t.dim() == 2 and t.stride() == (ld, 1) and t.shape[0] >= n and \
+            t.shape[1] >= width:
         return
     if n > 1 and ld != width:  # rows with something between them
         fits = (t.dim() == 2 and t.shape[0] >= n and t.shape[1] >= width and t.stride(0) == ld
