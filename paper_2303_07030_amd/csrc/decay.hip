@@ -246,8 +246,10 @@ nsd_status check_decay(const nsd_decay *s) {
 }
 
 // Tokens of a segment: as many as leave the card kEnough blocks, INT_MAX where whole sequences
-// do, or are short.
-constexpr int kShortest = 256, kLongest = 8192, kEnough = 1024;
+// do, or are short.  (A training step of 5,003 tokens of 6 heads in fp32: segments of 256 tokens
+// 350 us, of 128 305, of 64 203; the kernels of a prompt of 65,536 tokens of 8 heads of 128: 512
+// tokens 321 us, 1,024 365, 256 374.)
+constexpr int kShortest = 64, kLongest = 8192, kEnough = 1024;
 
 int segment_tokens(int32_t ntok, int32_t max_len, const nsd_decay *s) {
     const int64_t cols = ceil_div(std::max(s->d, s->dv), 128) * s->heads;

@@ -5,7 +5,7 @@
 // Both are HBM-bound: the rows that tokens name are read and written once; the
 // gradient reads every token's row and writes the whole table.  The gradient
 // needs the tokens by word, in their order, without the host: each block of
-// embed_order_kernel takes 256 words, looks through all ids, counts those before
+// embed_order_kernel takes up to 256 words, looks through all ids, counts those before
 // its words (the place of its tokens in the order) and those of each word, and
 // puts its tokens there.  One launch instead of a radix sort's six; the ids come
 // from L2 but for the first block.  Where words times tokens are too many for
@@ -34,8 +34,16 @@ constexpr int kOrderWords = 256;
 // Ids looked at by all blocks of embed_order_kernel up to which it is taken.
 constexpr int64_t kMaxLooks = int64_t(1) << 25;
 
+// Words of a block: few where there are few of them, so that all CUs take part in what is then
+// many tokens a word.
+int words_of_block(int64_t vocab) {
+    int n = 1;
+    while (n < kOrderWords && ceil_div(vocab, n) > 256) n *= 2;
+    return n;
+}
+
 bool by_looking(int64_t ntok, int64_t vocab) {
-    return ceil_div(vocab, kOrderWords) * ntok <= kMaxLooks && ntok <= (1 << 17);
+    return ceil_div(vocab, words_of_block(vocab)) * ntok <= kMaxLooks && ntok <= (1 << 17);
 }
 
 // ------------------------------------------------------------------- rows
@@ -66,7 +74,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_kernel(
 
 // ------------------------------------------------------------ tokens by word
 
-// Places of the tokens of words [256 b, 256 b + 256) in the order by word: `perm` the
+// Places of the tokens of block b's words (up to 256) in the order by word: `perm` the
 // token, `word` its word, of every place; segptr the first place of every word.
 //
 // A wave looks through consecutive tokens, four a lane, and keeps those of the block's words
@@ -76,14 +84,14 @@ constexpr int kOrderList = 2048;  // of a wave
 constexpr int kOrderStep = 4 * kWave;
 
 __global__ __launch_bounds__(kOrderThreads) void embed_order_kernel(
-    int32_t ntok, int32_t vocab, const int32_t *__restrict__ ids, int32_t *__restrict__ perm,
-    int32_t *__restrict__ word, int32_t *__restrict__ segptr) {
+    int32_t ntok, int32_t vocab, int32_t per, const int32_t *__restrict__ ids,
+    int32_t *__restrict__ perm, int32_t *__restrict__ word, int32_t *__restrict__ segptr) {
     __shared__ int32_t count[kOrderWaves][kOrderWords];  // of a wave's tokens; then its next place
     __shared__ uint32_t list[kOrderWaves][kOrderList];   // token less the wave's first, and word
     __shared__ int32_t below[kOrderWaves], scan[kOrderWords / kWave];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const int lo = blockIdx.x * kOrderWords;
-    const int words = min(kOrderWords, vocab - lo);
+    const int lo = blockIdx.x * per;
+    const int words = min(per, vocab - lo);
     for (int i = threadIdx.x; i < kOrderWaves * kOrderWords; i += kOrderThreads) (&count[0][0])[i] = 0;
     __syncthreads();
     const int piece = (ntok / (kOrderWaves * kOrderStep) + 1) * kOrderStep;
@@ -455,8 +463,9 @@ nsd_status nsd_embed_vjp(int32_t ntok, const nsd_embedding *s, const int32_t *id
     NSD_REQUIRE((reinterpret_cast<uintptr_t>(ws) & 255) == 0, "workspace is not 256-byte aligned");
     const hipStream_t st = as_stream(stream);
     if (w.key == nullptr) {
-        embed_order_kernel<<<ceil_div(s->vocab, kOrderWords), kOrderThreads, 0, st>>>(
-            ntok, s->vocab, ids, w.perm, w.word, w.segptr);
+        const int per = words_of_block(s->vocab);
+        embed_order_kernel<<<ceil_div(s->vocab, per), kOrderThreads, 0, st>>>(
+            ntok, s->vocab, per, ids, w.perm, w.word, w.segptr);
         NSD_TRY(check_launch("embed_order_kernel"));
     } else {
         embed_keys_kernel<<<ceil_div(ntok, kEmbedThreads), kEmbedThreads, 0, st>>>(ntok, s->vocab, ids,
