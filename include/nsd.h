@@ -1051,7 +1051,7 @@ nsd_status nsd_grad_clip(const nsd_grad_plan *plan, const float *scale, void *st
  * nsd_embed_vjp  dW.  accumulate = 0: all of dW is written, 0 for words without
  *                a token; 1: the sums are added to dW, and the other words' rows
  *                are not touched (a head that shares the table wrote its gradient
- *                there).  A word's tokens are added up in their order.
+ *                there).
  * Async.
  */
 typedef struct nsd_embedding {

@@ -11,8 +11,8 @@
 // from L2 but for the first block.  Where words times tokens are too many for
 // that the radix sort is taken.
 //
-// The sums: a wave takes a word and a tile of columns and adds up its tokens' rows
-// in their order.  A word of more than kLong tokens (a few words are a tenth of a
+// The sums: a wave takes a word and one or two tiles of columns and adds up its tokens'
+// rows, in one order.  A word of more than kLong tokens (a few words are a tenth of a
 // text) is left to waves that take kLong places of the order each, whatever the
 // words there; their sums of long words are joined in order by a second launch.
 #include <algorithm>
@@ -48,27 +48,39 @@ bool by_looking(int64_t ntok, int64_t vocab) {
 
 // ------------------------------------------------------------------- rows
 
+// Lanes that a row's columns take, a power of two up to 64: a wave takes 64 / lanes rows.
+int row_lanes(int32_t width, int values) {
+    int g = 1;
+    while (g < kWave && (int64_t)g * values < width) g <<= 1;
+    return g;
+}
+
+// A wave takes a token and a tile of columns, or 64 / lanes tokens of narrow rows.
 template <class TW, class TO, int N>
 __global__ __launch_bounds__(kEmbedThreads) void embed_kernel(
-    int64_t units, int32_t tiles, int32_t vocab, int32_t width, float scale,
-    const int32_t *__restrict__ ids, const TW *__restrict__ W, int64_t ldw, TO *__restrict__ out,
-    int64_t ldo) {
+    int32_t ntok, int64_t units, int32_t tiles, int32_t lanes, int32_t vocab, int32_t width,
+    float scale, const int32_t *__restrict__ ids, const TW *__restrict__ W, int64_t ldw,
+    TO *__restrict__ out, int64_t ldo) {
     const int lane = threadIdx.x % kWave;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     for (int64_t u = (int64_t)blockIdx.x * kEmbedWaves + wave; u < units;
          u += (int64_t)gridDim.x * kEmbedWaves) {
-        const int64_t t = u / tiles;
-        const int col = ((int)(u % tiles) * kWave + lane) * N;
+        int64_t t = u;
+        int tile = 0;
+        if (tiles > 1) {
+            t = u / tiles;
+            tile = (int)(u % tiles);
+        }
+        t = t * (kWave / lanes) + lane / lanes;
+        const int col = (tile * kWave + lane % lanes) * N;
+        if (t >= ntok || col >= width) continue;
         const int id = ids[t];
-        if (col >= width) continue;
+        const bool word = id >= 0 && id < vocab;
         float x[N] = {};
-        if (id >= 0 && id < vocab) load_left<N, TW>(W + id * ldw + col, width - col, x);
+        if (word) load_cols<N, TW>(W + id * ldw, col, width, x);
 #pragma unroll
-        for (int e = 0; e < N; ++e) x[e] *= scale;
-        if (id < 0 || id >= vocab)
-#pragma unroll
-            for (int e = 0; e < N; ++e) x[e] = 0.f;  // also where the scale is not finite
-        store_left<N, TO>(out + t * ldo + col, width - col, x);
+        for (int e = 0; e < N; ++e) x[e] = word ? x[e] * scale : 0.f;  // whatever the scale is
+        store_cols<N, TO>(out + t * ldo, col, width, x);
     }
 }
 
@@ -208,7 +220,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_keys_kernel(int32_t ntok,
 // ------------------------------------------------------------------- sums
 
 struct EmbedSum {
-    int32_t ntok, vocab, width, tiles, nchunks;
+    int32_t ntok, vocab, width, tiles, lanes, nchunks;
     bool accumulate;
     float scale;
     const int32_t *perm, *word, *segptr;
@@ -216,74 +228,78 @@ struct EmbedSum {
     float *part;  // [chunk][2][width]: of the word at its first place, and of another at its last
 };
 
-// The sum of n <= 64 rows: lane from + i holds row i's token.  FULL: every lane's columns
-// exist.
-template <bool FULL, class TR, int N>
-__device__ __forceinline__ void add_some(const TR *__restrict__ rows, int64_t ld, int token, int from,
-                                         int n, int col, int left, float (&acc)[N]) {
-    constexpr int kAhead = 4;
-    int i = 0;
-    for (; i + kAhead <= n; i += kAhead) {
-        float x[kAhead][N];
+// Sums of n <= 64 rows' columns: lane from + i holds row i's token.  A slot of `lanes` lanes takes
+// every (64 / lanes)th row; their sums are joined at the end, in one order.  NT tiles of a row.
+template <class TR, int N, int NT, bool WIDE>
+__device__ __forceinline__ void add_rows(const EmbedSum &a, const TR *__restrict__ rows, int token,
+                                         int from, int n, int tile, int lane,
+                                         float (&acc)[NT][N]) {
+    constexpr int kAhead = 8 / NT;
+    const int slots = kWave / a.lanes, slot = lane / a.lanes;
+    const int col = (tile * kWave + lane % a.lanes) * N;
+    for (int i = 0; i < n; i += kAhead * slots) {
+        Piece<N, TR, WIDE> x[kAhead][NT];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            const int64_t t = __builtin_amdgcn_readlane(token, from + i + u);
-            load_left<N, TR>(rows + t * ld + col, FULL ? N : left, x[u]);
+            if (i + u * slots >= n) break;
+            // (a slot past the end repeats the last row, and does not add it)
+            const int64_t t = slots == 1 ? __builtin_amdgcn_readlane(token, from + i + u)
+                                         : __shfl(token, from + min(i + u * slots + slot, n - 1), kWave);
+#pragma unroll
+            for (int k = 0; k < NT; ++k) x[u][k].load(rows + t * a.ldo, col + k * kWave * N, a.width);
         }
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
+        for (int u = 0; u < kAhead; ++u) {
+            if (i + u * slots >= n) break;
+            if (i + u * slots + slot < n)
 #pragma unroll
-            for (int e = 0; e < N; ++e) acc[e] += x[u][e];
-    }
-    for (; i < n; ++i) {
-        float x[N];
-        const int64_t t = __builtin_amdgcn_readlane(token, from + i);
-        load_left<N, TR>(rows + t * ld + col, FULL ? N : left, x);
+                for (int k = 0; k < NT; ++k)
 #pragma unroll
-        for (int e = 0; e < N; ++e) acc[e] += x[e];
+                    for (int e = 0; e < N; ++e) acc[k][e] += x[u][k].value(e);
+        }
     }
-}
-template <class TR, int N>
-__device__ __forceinline__ void add_rows(const EmbedSum &a, const TR *__restrict__ rows, int token,
-                                         int from, int n, int tile, int lane, float (&acc)[N]) {
-    const int col = (tile * kWave + lane) * N;
-    if ((tile + 1) * kWave * N <= a.width) {
-        add_some<true, TR, N>(rows, a.ldo, token, from, n, col, N, acc);
-    } else {  // lanes beyond the row stay: the others read their tokens
-        add_some<false, TR, N>(rows, a.ldo, token, from, n, min(col, a.width), max(a.width - col, 0), acc);
-    }
+    for (int m = a.lanes; m < kWave; m <<= 1)
+#pragma unroll
+        for (int k = 0; k < NT; ++k)
+#pragma unroll
+            for (int e = 0; e < N; ++e) acc[k][e] += __shfl_xor(acc[k][e], m, kWave);
 }
 
 template <class TG, int N>
 __device__ __forceinline__ void put_sum(const EmbedSum &a, TG *dW, int64_t v, int col,
                                         float (&acc)[N]) {
-    const int left = a.width - col;
 #pragma unroll
     for (int e = 0; e < N; ++e) acc[e] *= a.scale;
-    TG *p = dW + v * a.ldw + col;
+    TG *const row = dW + v * a.ldw;
     if (a.accumulate) {
         float old[N];
-        load_left<N, TG>(p, left, old);
+        load_cols<N, TG>(row, col, a.width, old);
 #pragma unroll
         for (int e = 0; e < N; ++e) acc[e] += old[e];
     }
-    store_left<N, TG>(p, left, acc);
+    store_cols<N, TG>(row, col, a.width, acc);
 }
 
-template <class TR, class TG, int N>
+// Units: of words and NT tiles of columns, then of kLong places and NT tiles.
+template <class TR, class TG, int N, int NT, bool WIDE>
 __global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(EmbedSum a, int64_t row_units,
                                                                   int64_t units,
                                                                   const TR *__restrict__ dout,
                                                                   TG *__restrict__ dW) {
     const int lane = threadIdx.x % kWave;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int groups = (a.tiles + NT - 1) / NT;
     for (int64_t u = (int64_t)blockIdx.x * kEmbedWaves + wave; u < units;
          u += (int64_t)gridDim.x * kEmbedWaves) {
         const bool rows = u < row_units;
-        const int64_t item = (rows ? u : u - row_units) / a.tiles;
-        const int tile = (int)((rows ? u : u - row_units) % a.tiles);
-        const int col = (tile * kWave + lane) * N;
-        const int left = a.width - col;
+        int64_t item = rows ? u : u - row_units;
+        int tile = 0;
+        if (groups > 1) {
+            tile = (int)(item % groups) * NT;
+            item /= groups;
+        }
+        const int col0 = (tile * kWave + lane % a.lanes) * N;
+        const bool first = lane < a.lanes;  // of the slots that hold the same sums
         if (rows) {  // a word: the item's own, or (accumulate) the one that starts at this place
             int64_t v = item;
             if (a.accumulate) {
@@ -294,14 +310,14 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(EmbedSum a, in
             const int lo = a.segptr[v], n = a.segptr[v + 1] - lo;
             if (n > kLong) continue;
             const int token = lane < n ? a.perm[lo + lane] : 0;
-            float acc[N] = {};
-            add_rows<TR, N>(a, dout, token, 0, n, tile, lane, acc);
-            if (left > 0) {
-                if (n == 0) {
-                    store_left<N, TG>(dW + v * a.ldw + col, left, acc);
-                } else {
-                    put_sum<TG, N>(a, dW, v, col, acc);
-                }
+            float acc[NT][N] = {};
+            add_rows<TR, N, NT, WIDE>(a, dout, token, 0, n, tile, lane, acc);
+#pragma unroll
+            for (int k = 0; k < NT; ++k) {
+                const int col = col0 + k * kWave * N;
+                if (!first || col >= a.width) continue;
+                if (n == 0) store_cols<N, TG>(dW + v * a.ldw, col, a.width, acc[k]);
+                else put_sum<TG, N>(a, dW, v, col, acc[k]);
             }
         } else {  // kLong places
             const int base = (int)item * kLong, end = min(base + kLong, a.segptr[a.vocab]);
@@ -314,10 +330,14 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_sum_kernel(EmbedSum a, in
                 const int s0 = a.segptr[w], s1 = a.segptr[w + 1];
                 if (s1 - s0 <= kLong) continue;
                 const int from = max(s0, base) - base, n = min(s1, end) - base - from;
-                float acc[N] = {};
-                add_rows<TR, N>(a, dout, token, from, n, tile, lane, acc);
-                if (left > 0)
-                    store_left<N, float>(a.part + (item * 2 + side) * a.width + col, left, acc);
+                float acc[NT][N] = {};
+                add_rows<TR, N, NT, WIDE>(a, dout, token, from, n, tile, lane, acc);
+#pragma unroll
+                for (int k = 0; k < NT; ++k) {
+                    const int col = col0 + k * kWave * N;
+                    if (first && col < a.width)
+                        store_cols<N, float>(a.part + (item * 2 + side) * a.width, col, a.width, acc[k]);
+                }
             }
         }
     }
@@ -339,7 +359,7 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(EmbedSum a, TG
     const int w = a.word[end - 1];
     const int s0 = a.segptr[w], s1 = a.segptr[w + 1];
     if (s1 - s0 <= kLong || s0 < base) return;
-    const int col = (tile * kWave + lane) * N, left = a.width - col;
+    const int col = (tile * kWave + lane) * N;
     const int nc = (s1 - 1) / kLong - chunk + 1;  // chunks that the word covers
     const int per = (nc + kJoinWaves - 1) / kJoinWaves;
     const int c0 = min(wave * per, nc), c1 = min(c0 + per, nc);
@@ -351,19 +371,18 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(EmbedSum a, TG
         for (int u = 0; u < kAhead; ++u) {
             const int at = chunk + min(c + u, c1 - 1);
             const int side = at == chunk && s0 > base ? 1 : 0;  // not the word at its first place
-            const int64_t p = (int64_t)at * 2 + side;
-            load_left<N, float>(a.part + p * a.width + min(col, a.width), c + u < c1 ? max(left, 0) : 0,
-                                x[u]);
+            load_cols<N, float>(a.part + ((int64_t)at * 2 + side) * a.width, col, a.width, x[u]);
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
+            if (c + u < c1)
 #pragma unroll
-            for (int e = 0; e < N; ++e) acc[e] += x[u][e];
+                for (int e = 0; e < N; ++e) acc[e] += x[u][e];
     }
 #pragma unroll
     for (int e = 0; e < N; ++e) sum[wave][lane * N + e] = acc[e];
     __syncthreads();
-    if (wave > 0 || left <= 0) return;
+    if (wave > 0 || col >= a.width) return;
     for (int o = 1; o < kJoinWaves; ++o)
 #pragma unroll
         for (int e = 0; e < N; ++e) acc[e] += sum[o][lane * N + e];
@@ -431,14 +450,15 @@ nsd_status nsd_embed(int32_t ntok, const nsd_embedding *s, const int32_t *ids, c
     NSD_TRY(check_embedding(ntok, s));
     if (ntok == 0) return NSD_OK;
     NSD_REQUIRE(ids && out && (W || s->vocab == 0), "a NULL array");
-    const int tiles = (int)ceil_div(s->width, kWave * values_per_lane(s->wtype, s->otype));
-    const int64_t units = (int64_t)ntok * tiles;
+    const int values = values_per_lane(s->wtype, s->otype), lanes = row_lanes(s->width, values);
+    const int tiles = (int)ceil_div(s->width, kWave * values);
+    const int64_t units = ceil_div(ntok, kWave / lanes) * tiles;
     const int64_t blocks = std::min(ceil_div(units, kEmbedWaves), kMaxEmbedBlocks);
     return by_types(s->wtype, s->otype, [&](auto w, auto o, auto n) -> nsd_status {
         using TW = decltype(w);
         using TO = decltype(o);
         embed_kernel<TW, TO, decltype(n)::value><<<blocks, kEmbedThreads, 0, as_stream(stream)>>>(
-            units, tiles, s->vocab, s->width, s->scale, ids, static_cast<const TW *>(W), s->ldw,
+            ntok, units, tiles, lanes, s->vocab, s->width, s->scale, ids, static_cast<const TW *>(W), s->ldw,
             static_cast<TO *>(out), s->ldo);
         return check_launch("embed_kernel");
     });
@@ -478,7 +498,9 @@ nsd_status nsd_embed_vjp(int32_t ntok, const nsd_embedding *s, const int32_t *id
     a.ntok = ntok;
     a.vocab = s->vocab;
     a.width = s->width;
-    a.tiles = (int)ceil_div(s->width, kWave * values_per_lane(s->otype, s->gtype));
+    const int values = values_per_lane(s->otype, s->gtype);
+    a.tiles = (int)ceil_div(s->width, kWave * values);
+    a.lanes = row_lanes(s->width, values);
     a.nchunks = ntok > kLong ? (int)ceil_div(ntok, kLong) : 0;
     a.accumulate = accumulate != 0;
     a.scale = s->scale;
@@ -488,15 +510,23 @@ nsd_status nsd_embed_vjp(int32_t ntok, const nsd_embedding *s, const int32_t *id
     a.ldw = s->ldw;
     a.ldo = s->ldo;
     a.part = w.part;
-    const int64_t row_units = (int64_t)(accumulate ? ntok : s->vocab) * a.tiles;
-    const int64_t units = row_units + (int64_t)a.nchunks * a.tiles;
+    const int groups = (int)ceil_div(a.tiles, a.tiles > 1 ? 2 : 1);
+    const int64_t row_units = (int64_t)(accumulate ? ntok : s->vocab) * groups;
+    const int64_t units = row_units + (int64_t)a.nchunks * groups;
     const int64_t blocks = std::min(ceil_div(units, kEmbedWaves), kMaxEmbedBlocks);
     return by_types(s->otype, s->gtype, [&](auto r, auto g, auto n) -> nsd_status {
         using TR = decltype(r);
         using TG = decltype(g);
         constexpr int N = decltype(n)::value;
-        embed_sum_kernel<TR, TG, N><<<blocks, kEmbedThreads, 0, st>>>(
-            a, row_units, units, static_cast<const TR *>(dout), static_cast<TG *>(dW));
+        const TR *const rows = static_cast<const TR *>(dout);
+        TG *const to = static_cast<TG *>(dW);
+        auto sum = [&](auto nt, auto wide) {
+            embed_sum_kernel<TR, TG, N, decltype(nt)::value, decltype(wide)::value>
+                <<<blocks, kEmbedThreads, 0, st>>>(a, row_units, units, rows, to);
+        };
+        if (a.tiles > 1) sum(std::integral_constant<int, 2>(), std::true_type());
+        else if (a.width >= N) sum(std::integral_constant<int, 1>(), std::true_type());
+        else sum(std::integral_constant<int, 1>(), std::false_type());
         NSD_TRY(check_launch("embed_sum_kernel"));
         if (a.nchunks == 0) return NSD_OK;
         const int64_t joins = (int64_t)a.nchunks * a.tiles;

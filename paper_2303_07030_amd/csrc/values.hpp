@@ -62,6 +62,48 @@ __device__ __forceinline__ void store_left(T *p, int left, const float (&x)[N]) 
     }
 }
 
+// N columns from `col` on of a row of `width`, where a lane has some: at the row's end it steps
+// back to the last N (the first of which are another lane's: store_cols leaves them), so that
+// every lane moves whole pieces.  Rows of fewer than N columns are read and written one by one.
+template <int N, class T>
+__device__ __forceinline__ void load_cols(const T *row, int col, int width, float (&x)[N]) {
+    if (width >= N) load_values<N, T>(row + min(col, width - N), x);
+    else load_left<N, T>(row + min(col, width), max(width - col, 0), x);
+}
+template <int N, class T>
+__device__ __forceinline__ void store_cols(T *row, int col, int width, const float (&x)[N]) {
+    if (col + N <= width) {
+        store_row_values<N, T>(row + col, x);
+    } else if (width >= N) {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (width - N + e >= col) row[width - N + e] = narrowed<T>(x[e]);
+    } else {
+        store_left<N, T>(row + min(col, width), max(width - col, 0), x);
+    }
+}
+
+// The same as they lie in memory, to be widened where they are used: rows on their way take
+// half the registers.  WIDE: rows have N columns at least.
+template <int N, class T, bool WIDE>
+struct Piece {
+    uint32_t w[N * sizeof(T) / 4];
+    __device__ __forceinline__ void load(const T *row, int col, int width) {
+        if constexpr (WIDE) {
+            __builtin_memcpy(w, row + min(col, width - N), sizeof w);
+        } else {
+            T t[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) t[e] = col + e < width ? row[col + e] : T(0);
+            __builtin_memcpy(w, t, sizeof w);
+        }
+    }
+    __device__ __forceinline__ float value(int e) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
+        else return __uint_as_float(e % 2 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
+    }
+};
+
 inline bool known_dtype(int32_t t) { return t == NSD_F32 || t == NSD_BF16; }
 inline size_t dtype_bytes(int32_t t) { return t == NSD_F32 ? 4 : 2; }
 
