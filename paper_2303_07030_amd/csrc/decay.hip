@@ -283,7 +283,7 @@ struct DecayWs {
         const bool grouped = s->heads != s->kv_heads;
         forth = c.take<float>(states);
         back = dk = dv = sums = nullptr;
-        nvb = (int)ceil_div(s->dv, block_columns(s->dv));
+        nvb = (int)ceil_div(std::max(s->d, s->dv), block_columns(std::max(s->d, s->dv)));
         if (gradient) {
             back = c.take<float>(states);
             dk = c.take<float>(grouped ? (size_t)ntok * s->heads * s->d : 0);
@@ -408,6 +408,17 @@ nsd_status nsd_attn_decay_vjp(int32_t ntok, int32_t nseq, const int32_t *seqptr,
         // S forwards from S0, and R backwards from dS1, to S0's gradient
         NSD_TRY(segment_states(s, w, common, k, v, false, 1.f, w.forth, S0, nullptr, st));
         NSD_TRY(segment_states(s, w, common, q, up, true, s->scale, w.back, dS1, dS0, st));
+        // The gradient of the decay goes with the scan whose states' columns are the wider side:
+        // its state's derivative is held by fewer rows for each wave.
+        auto with_decay = [&](Scan &a, bool here, const Rows &rows, const float *meets,
+                              const float *ends) {
+            if (!ddecay || !here) return kOutput;
+            a.up = rows;
+            a.back = w.cut() ? meets : ends;
+            a.back_by_seq = !w.cut();
+            a.sums = w.sums;
+            return kDerivative;
+        };
         Scan a = common;  // dq: the states transposed
         a.q = up;
         a.k = v;
@@ -419,7 +430,7 @@ nsd_status nsd_attn_decay_vjp(int32_t ntok, int32_t nseq, const int32_t *seqptr,
         a.sk = 1;
         a.sv = s->dv;
         starts(a, w, w.forth, S0);
-        NSD_TRY(launch(kOutput, s, a, st));
+        NSD_TRY(launch(with_decay(a, s->dv < s->d, q, w.back, dS1), s, a, st));
         a = common;  // dk
         a.rev = true;
         a.q = Rows{V, s->ldv, s->dv, grp};
@@ -449,7 +460,7 @@ nsd_status nsd_attn_decay_vjp(int32_t ntok, int32_t nseq, const int32_t *seqptr,
         starts(a, w, w.back, dS1);
         a.end = w.cut() ? nullptr : dS0;
         a.end_by_seq = true;
-        NSD_TRY(launch(kOutput, s, a, st));
+        NSD_TRY(launch(with_decay(a, s->d <= s->dv, v, w.forth, S0), s, a, st));
         if (grp > 1 && ntok > 0) {
             const unsigned blocks = (unsigned)std::min(ntok, 1 << 16);
             auto sum = [&](auto t) {
@@ -462,22 +473,6 @@ nsd_status nsd_attn_decay_vjp(int32_t ntok, int32_t nseq, const int32_t *seqptr,
             if (s->dtype == NSD_F32) sum(float());
             else sum(Bf16());
             NSD_TRY(check_launch("decay_heads_kernel"));
-        }
-        if (ddecay) {
-            a = common;
-            a.q = q;
-            a.k = k;
-            a.v = v;
-            a.up = up;
-            a.s_score = a.s_inter = s->scale;
-            a.s_update = 1.f;
-            a.sk = s->dv;
-            a.sv = 1;
-            starts(a, w, w.forth, S0);
-            a.back = w.cut() ? w.back : dS1;
-            a.back_by_seq = !w.cut();
-            a.sums = w.sums;
-            NSD_TRY(launch(kDerivative, s, a, st));
         }
     }
     if (ddecay == nullptr) return NSD_OK;

@@ -13,10 +13,12 @@
 //   dv: queries K, keys Q, values dO, states R;     backwards
 // (backwards, the state is held with its next decay in it, so that the state of no
 // token is the upstream of the last state: powers i and C - j instead of i + 1 and
-// C - 1 - j).  The gradient of g is the sum of do_t times the derivative of o_t, a
-// scan of S and its derivative T = dS/dg:
-//   dO/dg: weights n w^n,  s w^(i+1) ((i+1) Q S + Q T);   T = w^C (T + C S) + sum
+// C - 1 - j).  The gradient of g is the sum of do_t times the derivative of o_t, or of v_t
+// times that of dv_t, or of q_t times that of dq_t: whichever scan is run, the
+// derivative T of its state goes along,
+//   d/dg: weights n w^n,  s w^(i+1) ((i+1) Q S + Q T);   T = w^C (T + C S) + sum
 //   (C-1-j) w^(C-1-j) k^T v
+// and what the segment's last T adds to what meets it from the other side is added.
 //
 // A block of four or eight waves takes a segment of a sequence, a head and 64 or 128
 // columns of the values, 16 a wave.  A wave's own columns of the state stay in its
@@ -68,7 +70,8 @@ struct Scan {
     bool start_by_seq, end_by_seq;
     int32_t sk, sv;
     int64_t per;
-    // gradient of g: dO, the states that come back to a segment's end, one sum for each block
+    // gradient of g: the rows that the outputs' derivatives meet, the states from the other side
+    // that meet a segment's last one's, one sum for each block
     Rows up;
     const float *back;
     bool back_by_seq;
@@ -353,7 +356,8 @@ struct Stage {
     }
 };
 
-// What a scan does: outputs; the states at the segments' ends alone; the gradient of g.
+// What a scan does: outputs; the states at the segments' ends alone; outputs and the gradient
+// of g.
 enum Kind { kOutput, kState, kDerivative };
 
 // LDS of a block: queries, keys (the scores take their place), keys and values by columns.
@@ -362,28 +366,32 @@ struct Shared {
     static constexpr int C = kChunkOf<T>;
     static constexpr int VB = NW * 16;
     static constexpr int LDK = KD + 16 / sizeof(T);
-    static constexpr int NS = KIND == kDerivative ? 3 : 2;  // parts of scores and states
-    static constexpr int SP = kParts<T, NS>;
+    static constexpr int NS = KIND == kDerivative ? 3 : 2;  // parts of states
+    static constexpr int OP = kParts<T, 2>;                 // of scores; behind them of DERIV's
+    static constexpr int SP = OP + (KIND == kDerivative ? kParts<T, 3> : 0);
     static constexpr int Q = KIND == kState ? 0 : C * LDK;
     static constexpr int KP = KIND == kState ? 0 : LDK > SP * C ? C * LDK : SP * C * C;
     static constexpr int VALUES = Q + KP + KD * C + VB * C;
 };
 
 // Waves of a SIMD, which say how many registers one may have: two blocks of eight waves a CU
-// where the state leaves room for it (a training step's scans 404 and 163 us with one block, 348
-// and 160 with two).
+// where the states leave room for it.  (A training step's scans of 64 by 128 with one block and
+// with two: states and outputs 163 and 160 us; outputs with the gradient of g in bf16 455 and
+// 468, where two spill, in fp32 48 and 40.)
+template <class T>
 constexpr int waves_of(int kd, int nw, Kind kind) {
-    return kd > 128 ? 1 : nw == 4 || (kind == kDerivative && kd > 64) ? 2 : 4;
+    const bool two_states = kind == kDerivative && kd > (sizeof(T) == 2 ? 32 : 64);
+    return kd > 128 ? 1 : nw == 4 || two_states ? 2 : 4;
 }
 
 // KD: width of queries and keys, padded; NW: waves, 16 columns of the values each; blocks: of
 // the segments' heads' columns, nvb for each head.
 template <class T, int KD, int NW, Kind KIND, bool TAIL>
-__global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kernel(Scan a, int32_t nvb) {
+__global__ __launch_bounds__(NW * kWave, waves_of<T>(KD, NW, KIND)) void scan_kernel(Scan a, int32_t nvb) {
     using Sh = Shared<T, KD, NW, KIND>;
     constexpr int C = Sh::C, VB = Sh::VB, LDK = Sh::LDK;
     constexpr int KT = KD / 16, KF = KD / 32, IT = C / 16, JF = C / 32;
-    constexpr int NS = Sh::NS, SP = Sh::SP, VP = kParts<T, 3>;
+    constexpr int NS = Sh::NS, OP = Sh::OP, SP = Sh::SP, VP = kParts<T, 3>;
     constexpr bool DERIV = KIND == kDerivative;
     // Operands of the next products on their way during these: where LDS, not registers, says how
     // many blocks a CU has.
@@ -399,7 +407,7 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
     T *const ldsKt = ldsK + Sh::KP;
     T *const ldsVt = ldsKt + KD * C;
     __shared__ float power[C + 2], power_less[C + 2];
-    __shared__ float weight[2 * C];  // s_score w^n (DERIV: n w^n) at C + n, 0 below C
+    __shared__ float weight[2 * C];  // s_score w^n at C + n, 0 below C
     __shared__ __align__(16) float behind[2 * C];  // s_update w^(C - 1 - j (+ 1)) at j, 0 from C on
     __shared__ int unusual[2];
     __shared__ float wave_sum[NW];
@@ -425,7 +433,7 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
         if (n >= rev && n < C + rev) behind[C - 1 + rev - n] = a.s_update * (float)x;
         if (n < C) {
             behind[C + n] = weight[n] = 0.f;
-            weight[C + n] = a.s_score * (float)x * (DERIV ? (float)n : 1.f);
+            weight[C + n] = a.s_score * (float)x;
         }
     }
     if (threadIdx.x < 2) unusual[threadIdx.x] = 0;
@@ -483,7 +491,7 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
             const T *const byQ = ldsQ + n16 * LDK + (8 * g ^ turned<T>(n16));
             const T *const byK = byQ + (ldsK - ldsQ);
 
-            f32x4v O[IT];
+            f32x4v O[IT], E[IT];  // (E: of DERIV, the outputs' derivatives)
             if constexpr (KIND != kState) {
                 // ---- scores: tile (it, jt) of 16 x 16, jt <= it, shared out among the waves
                 constexpr int TILES = IT * (IT + 1) / 2;
@@ -512,7 +520,13 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
                     const int tile = u * NW + wave, it = it_of(tile), jt = tile - it * (it + 1) / 2;
                     if (tile >= TILES) break;
                     T part[SP][4];
-                    split<T, NS, 4>(p[u], part);
+                    split<T, 2, 4>(p[u], reinterpret_cast<T(&)[OP][4]>(part));
+                    if constexpr (DERIV) {
+                        float y[4];
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) y[r] = p[u][r] * (float)(16 * (it - jt) + apart - r);
+                        split<T, 3, 4>(y, reinterpret_cast<T(&)[kParts<T, 3>][4]>(part[OP]));
+                    }
 #pragma unroll
                     for (int s = 0; s < SP; ++s) {
                         T *const to = ldsP + s * C * C;
@@ -527,7 +541,7 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
                         }
                     }
                 }
-                // ---- from the state (DERIV: (i + 1) times that, and from its derivative)
+                // ---- from the state (E: (i + 1) times that, and from its derivative)
 #pragma unroll
                 for (int it = 0; it < IT; ++it) O[it] = f32x4v{0.f, 0.f, 0.f, 0.f};
                 Frag<T> qf[2][IT];
@@ -535,32 +549,32 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
 #pragma unroll
                     for (int it = 0; it < IT; ++it) qf[f & 1][it] = fragment(byQ + 16 * it * LDK + 32 * f);
                 };
-                auto from_state = [&](const f32x4v (&state)[KT]) {
+                auto from_state = [&](const f32x4v (&state)[KT], f32x4v (&O)[IT]) {
                     if (PIPE) load_q(0);
 #pragma unroll
                     for (int f = 0; f < KF; ++f) {
                         if (!PIPE) load_q(f);
                         else if (f + 1 < KF) load_q(f + 1);
                         hold();
-                        Frag<T> sf[SP];
+                        Frag<T> sf[kParts<T, NS>];
                         float x[8];
 #pragma unroll
                         for (int e = 0; e < 8; ++e) x[e] = state[2 * f + e / 4][e % 4];
                         split<T, NS>(x, sf);
 #pragma unroll
-                        for (int s = 0; s < SP; ++s)
+                        for (int s = 0; s < kParts<T, NS>; ++s)
 #pragma unroll
                             for (int it = 0; it < IT; ++it) mma(O[it], sf[s], qf[f & 1][it]);
                         hold();
                     }
                 };
-                from_state(S);
+                from_state(S, O);
                 if constexpr (DERIV) {
 #pragma unroll
                     for (int it = 0; it < IT; ++it)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) O[it][r] *= (float)(16 * it + n16 + 1);
-                    from_state(D);
+                        for (int r = 0; r < 4; ++r) E[it][r] = O[it][r] * (float)(16 * it + n16 + 1 - rev);
+                    from_state(D, E);
                 }
             }
             // ---- the state behind the chunk
@@ -600,7 +614,10 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
                     const int i = 16 * it + n16;
                     const float w = a.s_inter * power[i + 1 - rev];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) O[it][r] *= w;
+                    for (int r = 0; r < 4; ++r) {
+                        O[it][r] *= w;
+                        if constexpr (DERIV) E[it][r] *= w;
+                    }
                 }
             }
 #pragma unroll
@@ -620,7 +637,7 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
                 split<T, 3>(x, vs);
                 if constexpr (DERIV) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] *= (float)max(len - 1 - (32 * f + 8 * g + e), 0);
+                    for (int e = 0; e < 8; ++e) x[e] *= (float)max(len - 1 + rev - (32 * f + 8 * g + e), 0);
                     split<T, 3>(x, vd);
                 }
 #pragma unroll
@@ -655,7 +672,8 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
                     else if (step + 1 < JF * SP) load_p(step + 1);
                     hold();
 #pragma unroll
-                    for (int it = step / SP * 2; it < IT; ++it) mma(O[it], vf[step / SP], pf[step & 1][it]);
+                    for (int it = step / SP * 2; it < IT; ++it)
+                        mma(step % SP < OP ? O[it] : E[it], vf[step / SP], pf[step & 1][it]);
                     hold();
                 }
             }
@@ -679,8 +697,9 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
                                                  (int64_t)(h / a.up.grp) * a.up.width, it), left, up);
 #pragma unroll
                         for (int r = 0; r < 4; ++r)
-                            dsum = r < left ? __builtin_fmaf(x[r], up[r], dsum) : dsum;
-                    } else if (a.out32) {
+                            dsum = r < left ? __builtin_fmaf(E[it][r], up[r], dsum) : dsum;
+                    }
+                    if (a.out32) {
                         store_left<4, float>(place_of(static_cast<float *>(a.out), a.ldo,
                                                       (int64_t)h * a.v.width, it), left, x);
                     } else {
