@@ -31,7 +31,7 @@ __global__ __launch_bounds__(kJoinThreads) void decay_join_kernel(
     const int64_t e = ((int64_t)(blockIdx.x % nb) * kJoinThreads + threadIdx.x) * VEC;
     if (e >= per) return;
     const int begin = max(seqptr[s], 0), stop = min(seqptr[s + 1], ntok);
-    const int n = max(stop - begin, 0), id0 = seqptr[s] / seg_len + s;
+    const int n = max(stop - begin, 0), id0 = begin / seg_len + s;
     const int nc = n / seg_len + (n % seg_len != 0);
     const int64_t own = ((int64_t)s * H + h) * per + e, step = (int64_t)H * per;
     float *const at = states + ((int64_t)id0 * H + h) * per + e;

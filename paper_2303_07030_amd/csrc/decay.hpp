@@ -87,12 +87,12 @@ struct Segment {
         int lo = 0, hi = a.nseq - 1;
         while (lo < hi) {
             const int mid = (lo + hi + 1) / 2;
-            if (a.seqptr[mid] / a.seg_len + mid <= id) lo = mid;
+            if (max(a.seqptr[mid], 0) / a.seg_len + mid <= id) lo = mid;
             else hi = mid - 1;
         }
         seq = lo;
         const int begin = max(a.seqptr[lo], 0), end = min(a.seqptr[lo + 1], a.ntok);
-        const int c = id - (a.seqptr[lo] / a.seg_len + lo);
+        const int c = id - (begin / a.seg_len + lo);
         const int64_t at = begin + (int64_t)c * a.seg_len;
         on = c == 0 || (c > 0 && at < end);
         first = (int)min(at, (int64_t)a.ntok);

@@ -43,7 +43,8 @@ int words_of_block(int64_t vocab) {
 }
 
 bool by_looking(int64_t ntok, int64_t vocab) {
-    return ceil_div(vocab, words_of_block(vocab)) * ntok <= kMaxLooks && ntok <= (1 << 17);
+    const int64_t blocks = ceil_div(vocab, words_of_block(vocab));
+    return blocks * ntok <= kMaxLooks && ntok <= (1 << 17) && blocks <= UINT32_MAX / kOrderThreads;
 }
 
 // ------------------------------------------------------------------- rows
@@ -215,6 +216,22 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_keys_kernel(int32_t ntok,
                                                                    int32_t *key) {
     const int64_t t = (int64_t)blockIdx.x * kEmbedThreads + threadIdx.x;
     if (t < ntok) key[t] = ids[t] >= 0 && ids[t] < vocab ? ids[t] : vocab;
+}
+
+// The first place of every word in the sorted keys.
+__global__ __launch_bounds__(kEmbedThreads) void embed_starts_kernel(int32_t ntok, int32_t vocab,
+                                                                     const int32_t *__restrict__ key,
+                                                                     int32_t *__restrict__ segptr) {
+    for (int64_t v = (int64_t)blockIdx.x * kEmbedThreads + threadIdx.x; v <= vocab;
+         v += (int64_t)gridDim.x * kEmbedThreads) {
+        int lo = 0, hi = ntok;
+        while (lo < hi) {
+            const int mid = lo + (hi - lo) / 2;
+            if (key[mid] < v) lo = mid + 1;
+            else hi = mid;
+        }
+        segptr[v] = lo;
+    }
 }
 
 // ------------------------------------------------------------------- sums
@@ -481,6 +498,13 @@ nsd_status nsd_embed_vjp(int32_t ntok, const nsd_embedding *s, const int32_t *id
     if (ws == nullptr || ws_bytes < w.bytes)
         return fail(NSD_ERR_WORKSPACE, "workspace %zu bytes at %p, need %zu", ws_bytes, ws, w.bytes);
     NSD_REQUIRE((reinterpret_cast<uintptr_t>(ws) & 255) == 0, "workspace is not 256-byte aligned");
+    const int values = values_per_lane(s->otype, s->gtype);
+    EmbedSum a;
+    a.tiles = (int)ceil_div(s->width, kWave * values);
+    a.nchunks = ntok > kLong ? (int)ceil_div(ntok, kLong) : 0;
+    const int64_t joins = (int64_t)a.nchunks * a.tiles;
+    if (joins > UINT32_MAX / kJoinThreads)
+        return fail(NSD_ERR_TOO_LARGE, "%lld sums of long words", (long long)joins);
     const hipStream_t st = as_stream(stream);
     if (w.key == nullptr) {
         const int per = words_of_block(s->vocab);
@@ -488,20 +512,20 @@ nsd_status nsd_embed_vjp(int32_t ntok, const nsd_embedding *s, const int32_t *id
             ntok, s->vocab, per, ids, w.perm, w.word, w.segptr);
         NSD_TRY(check_launch("embed_order_kernel"));
     } else {
-        embed_keys_kernel<<<ceil_div(ntok, kEmbedThreads), kEmbedThreads, 0, st>>>(ntok, s->vocab, ids,
-                                                                                  w.key);
-        NSD_TRY(check_launch("embed_keys_kernel"));
-        NSD_TRY(radix_sort_pairs(ntok, s->vocab + 1, w.key, nullptr, w.word, w.perm, w.sort, st));
-        NSD_TRY(segptr_from_sorted(ntok, s->vocab, w.word, w.segptr, st));
+        if (ntok > 0) {
+            embed_keys_kernel<<<ceil_div(ntok, kEmbedThreads), kEmbedThreads, 0, st>>>(ntok, s->vocab,
+                                                                                      ids, w.key);
+            NSD_TRY(check_launch("embed_keys_kernel"));
+            NSD_TRY(radix_sort_pairs(ntok, s->vocab + 1, w.key, nullptr, w.word, w.perm, w.sort, st));
+        }
+        const int64_t starts = std::min(ceil_div((int64_t)s->vocab + 1, kEmbedThreads), kMaxEmbedBlocks);
+        embed_starts_kernel<<<starts, kEmbedThreads, 0, st>>>(ntok, s->vocab, w.word, w.segptr);
+        NSD_TRY(check_launch("embed_starts_kernel"));
     }
-    EmbedSum a;
     a.ntok = ntok;
     a.vocab = s->vocab;
     a.width = s->width;
-    const int values = values_per_lane(s->otype, s->gtype);
-    a.tiles = (int)ceil_div(s->width, kWave * values);
     a.lanes = row_lanes(s->width, values);
-    a.nchunks = ntok > kLong ? (int)ceil_div(ntok, kLong) : 0;
     a.accumulate = accumulate != 0;
     a.scale = s->scale;
     a.perm = w.perm;
@@ -529,9 +553,6 @@ nsd_status nsd_embed_vjp(int32_t ntok, const nsd_embedding *s, const int32_t *id
         else sum(std::integral_constant<int, 1>(), std::false_type());
         NSD_TRY(check_launch("embed_sum_kernel"));
         if (a.nchunks == 0) return NSD_OK;
-        const int64_t joins = (int64_t)a.nchunks * a.tiles;
-        if (joins > UINT32_MAX / kJoinThreads)
-            return fail(NSD_ERR_TOO_LARGE, "%lld sums of long words", (long long)joins);
         embed_join_kernel<TG, N><<<joins, kJoinThreads, 0, st>>>(a, static_cast<TG *>(dW));
         return check_launch("embed_join_kernel");
     });

@@ -125,14 +125,15 @@ struct Head {
             b[e] *= r * o.b[e];
         }
     }
-    // turned by the lane's angles, or back
-    __device__ __forceinline__ void turn(const float (&c)[kPairs], const float (&s)[kPairs],
+    // The first n pairs turned by the lane's angles, or back.  (The others are no pairs: an
+    // infinite one times a sine of 0 would take the number beside it away.)
+    __device__ __forceinline__ void turn(const float (&c)[kPairs], const float (&s)[kPairs], int n,
                                          bool back) {
 #pragma unroll
         for (int e = 0; e < kPairs; ++e) {
-            const float sn = back ? -s[e] : s[e], x = a[e];
-            a[e] = x * c[e] - b[e] * sn;
-            b[e] = x * sn + b[e] * c[e];
+            const float sn = back ? -s[e] : s[e], x = a[e], y = b[e];
+            a[e] = e < n ? x * c[e] - y * sn : x;
+            b[e] = e < n ? x * sn + y * c[e] : y;
         }
     }
 };
@@ -253,7 +254,7 @@ __global__ __launch_bounds__(kQkThreads) void qk_rotate_kernel(QkArgs s, int64_t
                         x[i].b[e] = x[i].b[e] * r * (h < s.H ? wq.b[e] : wk.b[e]);
                     }
                 }
-                x[i].turn(angle.c, angle.s, false);
+                x[i].turn(angle.c, angle.s, s.rot / 2 - p0, false);
                 if (on && h < s.H)
                     x[i].store(s, static_cast<T *>(s.Qo) + t * s.ldqo + (int64_t)h * s.d, p0);
                 else if (on && h < heads && krow >= 0)
@@ -309,7 +310,7 @@ __global__ __launch_bounds__(kQkThreads) void qk_rotate_vjp_kernel(QkArgs s, int
 #pragma unroll
                 for (int i = 0; i < kHeadsAhead; ++i) {
                     const int h = h0 + i * SLOTS + slot;
-                    y[i].turn(angle.c, angle.s, true);
+                    y[i].turn(angle.c, angle.s, s.rot / 2 - p0, true);
                     if (s.norm) {
                         const float ss = over_slot<G>(x[i].dot(x[i]));
                         // (a slot without a head: nothing of it, also where eps is 0)

@@ -331,12 +331,34 @@ def test_heads(H, Hk, dtype):
 @pytest.mark.parametrize("d, dv, H, Hk", [(16, 16, 2, 1), (64, 128, 1, 1), (40, 72, 2, 2)])
 @pytest.mark.parametrize("lens", [[1000], [513, 0, 1, 700, 256], [257, 512, 3]])
 def test_sequences_in_segments(lens, d, dv, H, Hk, dtype):
-    """Sequences past the segments' length (256 here)."""
+    """Sequences past the segments' length."""
     c = Case(lens, H, Hk, d, dv, dtype, lead=1)
     whole = nsd.nsd_attn_decay_workspace_size(c.n, c.B, 1, c.desc)
     assert nsd.nsd_attn_decay_workspace_size(c.n, c.B, max(lens), c.desc) > whole
     c.check()
     c.check(start=False)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d, dv", [(24, 70), (70, 24)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_ends_of_sequences_outside_the_rows_are_those_of_the_rows(d, dv, dtype):
+    """What the pointers say beyond the rows is neither read nor written, in segments as well."""
+    c = Case([400, 300], 2, 1, d, dv, dtype)
+    s1, grads = c.forward(), c.backward()
+    want = {i: t.clone() for i, t in c.out.items()}
+    n, ptr = c.n, c.seqptr.clone()
+    c.n = 700  # the rows that calls are told of
+    c.t = {i: t[:700] for i, t in c.t.items()}
+    c.out = {i: t[:700] for i, t in c.out.items()}
+    for t in c.wide_out.values():
+        t[:700] = 3.0
+    c.seqptr[0], c.seqptr[2] = -1_000_000, 2 ** 31 - 1
+    again = [c.forward(400), *c.backward(400)]
+    c.n, c.seqptr = n, ptr
+    assert all(torch.equal(a, b) for a, b in zip(again, [s1, *grads]))
+    assert all(torch.equal(want[i][:700], t) for i, t in c.out.items())
+    assert all(torch.equal(want[i][700:], c.wide_out[i][700:, :want[i].shape[1]]) for i in want)
 
 
 @pytest.mark.gpu

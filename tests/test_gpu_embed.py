@@ -239,6 +239,29 @@ def test_a_table_past_32_bit_offsets():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("ids", [[], [1_099_999_999, 5, 1_099_999_999]])
+def test_more_words_than_a_launch_looks_for(ids):
+    V, n = 1_100_000_000, len(ids)
+    dW = torch.full((V, 1), 2.0, dtype=torch.bfloat16, device="cuda")
+    rows = torch.ones(n, 1, dtype=torch.bfloat16, device="cuda")
+    s = nsd.embed_desc(dW, rows, grad=dW)
+    ws = torch.empty(nsd.nsd_embed_vjp_workspace_size(n, s), dtype=torch.uint8, device="cuda")
+    idd = torch.tensor(ids, dtype=torch.int32, device="cuda")
+    nsd.nsd_embed_vjp(n, s, idd, rows, True, dW, ws)
+    assert torch.all(dW[6:-1] == 2.0)
+    assert dW[5] == 2.0 + ids.count(5) and dW[-1] == 2.0 + ids.count(V - 1)
+    nsd.nsd_embed_vjp(n, s, idd, rows, False, dW, ws)
+    assert torch.count_nonzero(dW) == len(set(ids)) and dW.sum() == n
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("V", [7, 300_000])
+def test_one_word_of_many_in_a_large_batch(V):
+    ids = np.full(140_000, V - 2, np.int32)
+    check(ids, V, 3, 1.0, "f32", "f32", "f32", False)
+
+
+@pytest.mark.gpu
 def test_a_captured_step_follows_the_ids():
     V, w, n = 3000, 200, 6000
     rng = np.random.default_rng(1)

@@ -241,6 +241,33 @@ def test_rows_of_zeros_and_large_values(interleaved):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("d, rot, interleaved", [(32, 16, False), (32, 16, True), (22, 10, False),
+                                                 (22, 10, True), (7, 2, False), (16, 0, False)])
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+def test_what_is_not_rotated_stays_by_itself(d, rot, interleaved, bad):
+    """A number that is not finite behind a head's rotated part is passed on, without a norm,
+    and no number beside it is touched; both ways."""
+    n, H, Hk = 9, 3, 2
+    t = make(n, H, Hk, d, rot, "f32", 1000)
+    s = nsd.qk_desc(H, Hk, d, t["q"], t["k"], t["qo"], t["ko"], rot, interleaved, False)
+    small = (None, None, t["pos"], t["freq"])
+    ins, outs = ("q", "k", "dqo", "dko"), ("qo", "ko", "dq", "dk")
+
+    def run():
+        nsd.nsd_qk_rotate(n, s, t["q"], t["k"], *small, t["qo"], t["ko"])
+        nsd.nsd_qk_rotate_vjp(n, s, t["q"], t["k"], *small, t["dqo"], t["dko"], t["dq"], t["dk"],
+                              None, None, None)
+        return [t[i].clone() for i in outs]
+
+    want = run()
+    for i in ins:
+        t[i][:, d - 1::2 * d] = bad
+    for x, got in zip(want, run()):
+        x[:, d - 1::2 * d] = bad
+        assert torch.equal(got.nan_to_num(7e9), x.nan_to_num(7e9))
+
+
+@pytest.mark.gpu
 def test_weights_with_eps_of_zero():
     """Lanes without a head of their own leave the weights' gradients alone."""
     compare(11, 3, 1, 16, 16, "f32", False, eps=0.0)
