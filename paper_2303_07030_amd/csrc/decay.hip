@@ -246,9 +246,10 @@ nsd_status check_decay(const nsd_decay *s) {
 }
 
 // Tokens of a segment: as many as leave the card kEnough blocks, INT_MAX where whole sequences
-// do, or are short.  (A training step of 5,003 tokens of 6 heads in fp32: segments of 256 tokens
-// 350 us, of 128 305, of 64 203; the kernels of a prompt of 65,536 tokens of 8 heads of 128: 512
-// tokens 321 us, 1,024 365, 256 374.)
+// do, or are short.  (A training step of 5,003 tokens of 6 heads in fp32: segments of at least
+// 256 tokens 306 us, 128 272, 64 181.  A prompt of 65,536 tokens of 8 heads of 128, and a
+// training step of 32,768 tokens of 16 heads of 64 by 128: 512 blocks 373 and 1,325 us, 1,024 325
+// and 1,130, 2,048 353 and 1,157.)
 constexpr int kShortest = 64, kLongest = 8192, kEnough = 1024;
 
 int segment_tokens(int32_t ntok, int32_t max_len, const nsd_decay *s) {
@@ -283,7 +284,8 @@ struct DecayWs {
         const bool grouped = s->heads != s->kv_heads;
         forth = c.take<float>(states);
         back = dk = dv = sums = nullptr;
-        nvb = (int)ceil_div(std::max(s->d, s->dv), block_columns(std::max(s->d, s->dv)));
+        const int wide = std::max(s->d, s->dv);
+        nvb = (int)ceil_div(wide, block_columns(kDerivative, s->dtype == NSD_BF16, wide));
         if (gradient) {
             back = c.take<float>(states);
             dk = c.take<float>(grouped ? (size_t)ntok * s->heads * s->d : 0);

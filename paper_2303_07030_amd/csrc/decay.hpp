@@ -375,30 +375,21 @@ struct Shared {
 };
 
 // Waves of a SIMD, which say how many registers one may have: two blocks of eight waves a CU
-// where the states leave room for it.  (A training step's scans of 64 by 128 with one block and
-// with two: states and outputs 163 and 160 us; outputs with the gradient of g in bf16 455 and
-// 468, where two spill, in fp32 48 and 40.)
-template <class T>
+// where the state leaves room for it (a training step's scan of 64 by 128 163 us with one block
+// and 160 with two, in fp32 with the gradient of g 48 and 40).
 constexpr int waves_of(int kd, int nw, Kind kind) {
-    const bool two_states = kind == kDerivative && kd > (sizeof(T) == 2 ? 32 : 64);
-    return kd > 128 ? 1 : nw == 4 || two_states ? 2 : 4;
+    return kd > 128 ? 1 : nw == 4 || (kind == kDerivative && kd > 64) ? 2 : 4;
 }
 
 // KD: width of queries and keys, padded; NW: waves, 16 columns of the values each; blocks: of
 // the segments' heads' columns, nvb for each head.
 template <class T, int KD, int NW, Kind KIND, bool TAIL>
-__global__ __launch_bounds__(NW * kWave, waves_of<T>(KD, NW, KIND)) void scan_kernel(Scan a, int32_t nvb) {
+__global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kernel(Scan a, int32_t nvb) {
     using Sh = Shared<T, KD, NW, KIND>;
     constexpr int C = Sh::C, VB = Sh::VB, LDK = Sh::LDK;
     constexpr int KT = KD / 16, KF = KD / 32, IT = C / 16, JF = C / 32;
     constexpr int NS = Sh::NS, OP = Sh::OP, SP = Sh::SP, VP = kParts<T, 3>;
     constexpr bool DERIV = KIND == kDerivative;
-    // Operands of the next products on their way during these: where LDS, not registers, says how
-    // many blocks a CU has.
-    constexpr bool PIPE = NW == 4 && KIND != kState;
-    auto hold = [] {
-        if constexpr (PIPE) __builtin_amdgcn_sched_barrier(0);
-    };
     constexpr int GR = KT < IT ? KT : IT;  // rows of the state that a step of their products takes
     __shared__ __align__(16) T lds[Sh::VALUES];
     T *const ldsQ = lds;
@@ -470,7 +461,9 @@ __global__ __launch_bounds__(NW * kWave, waves_of<T>(KD, NW, KIND)) void scan_ke
     int single = 0, turn = 0;  // single: tokens that are still taken one by one
     int pos = 0, len = 0, next = 0, next_len = min(C, seg.n);
     // The next chunk's rows are on their way while one is multiplied where that leaves the card
-    // as many waves; the other blocks of a CU hide them else.
+    // as many waves; the other blocks of a CU hide them else (outputs with a state of 128 by 128:
+    // a prompt 324 us so, 379 with rows ahead; a training step of 64 by 128 1,130 us with rows
+    // ahead, 1,144 without).
     constexpr bool AHEAD = KIND == kState || (KIND == kOutput && KD <= 64);
     auto load = [&](int tid) {
         const int64_t t0 = first + (int64_t)next * dir;
@@ -544,18 +537,12 @@ __global__ __launch_bounds__(NW * kWave, waves_of<T>(KD, NW, KIND)) void scan_ke
                 // ---- from the state (E: (i + 1) times that, and from its derivative)
 #pragma unroll
                 for (int it = 0; it < IT; ++it) O[it] = f32x4v{0.f, 0.f, 0.f, 0.f};
-                Frag<T> qf[2][IT];
-                auto load_q = [&](int f) {
-#pragma unroll
-                    for (int it = 0; it < IT; ++it) qf[f & 1][it] = fragment(byQ + 16 * it * LDK + 32 * f);
-                };
                 auto from_state = [&](const f32x4v (&state)[KT], f32x4v (&O)[IT]) {
-                    if (PIPE) load_q(0);
 #pragma unroll
                     for (int f = 0; f < KF; ++f) {
-                        if (!PIPE) load_q(f);
-                        else if (f + 1 < KF) load_q(f + 1);
-                        hold();
+                        Frag<T> qf[IT];
+#pragma unroll
+                        for (int it = 0; it < IT; ++it) qf[it] = fragment(byQ + 16 * it * LDK + 32 * f);
                         Frag<T> sf[kParts<T, NS>];
                         float x[8];
 #pragma unroll
@@ -564,8 +551,7 @@ __global__ __launch_bounds__(NW * kWave, waves_of<T>(KD, NW, KIND)) void scan_ke
 #pragma unroll
                         for (int s = 0; s < kParts<T, NS>; ++s)
 #pragma unroll
-                            for (int it = 0; it < IT; ++it) mma(O[it], sf[s], qf[f & 1][it]);
-                        hold();
+                            for (int it = 0; it < IT; ++it) mma(O[it], sf[s], qf[it]);
                     }
                 };
                 from_state(S, O);
@@ -578,15 +564,9 @@ __global__ __launch_bounds__(NW * kWave, waves_of<T>(KD, NW, KIND)) void scan_ke
                 }
             }
             // ---- the state behind the chunk
-            Frag<T> vf[JF], kf[2][GR];
-            auto load_k = [&](int step) {
-#pragma unroll
-                for (int i = 0; i < GR; ++i)
-                    kf[step & 1][i] = by_k.at(step % (KT / GR) * GR + i, step / (KT / GR));
-            };
+            Frag<T> vf[JF];
 #pragma unroll
             for (int f = 0; f < JF; ++f) vf[f] = by_v.at(wave, f);
-            if (PIPE) load_k(0);
             const float keep = power[len], less = power_less[len];
             if (keep > 0.5f) {  // a slow decay by what it takes away
 #pragma unroll
@@ -642,40 +622,32 @@ __global__ __launch_bounds__(NW * kWave, waves_of<T>(KD, NW, KIND)) void scan_ke
                 }
 #pragma unroll
                 for (int kg = 0; kg < KT / GR; ++kg) {
-                    const int step = f * (KT / GR) + kg;
-                    if (!PIPE) load_k(step);
-                    else if (step + 1 < JF * (KT / GR)) load_k(step + 1);
-                    hold();
+                    Frag<T> kf[GR];
+#pragma unroll
+                    for (int i = 0; i < GR; ++i) kf[i] = by_k.at(kg * GR + i, f);
 #pragma unroll
                     for (int s = 0; s < VP; ++s)
 #pragma unroll
                         for (int i = 0; i < GR; ++i) {
-                            mma(S[kg * GR + i], kf[step & 1][i], vs[s]);
-                            if constexpr (DERIV) mma(D[kg * GR + i], kf[step & 1][i], vd[s]);
+                            mma(S[kg * GR + i], kf[i], vs[s]);
+                            if constexpr (DERIV) mma(D[kg * GR + i], kf[i], vd[s]);
                         }
-                    hold();
                 }
             }
             // ---- from the chunk's own tokens
             if constexpr (KIND != kState) {
                 __syncthreads();
-                Frag<T> pf[2][IT];
-                auto load_p = [&](int step) {
 #pragma unroll
-                    for (int it = step / SP * 2; it < IT; ++it)
-                        pf[step & 1][it] = by_p.at(step % SP * (C / 16) + it, step / SP);
-                };
-                if (PIPE) load_p(0);
+                for (int f = 0; f < JF; ++f)
 #pragma unroll
-                for (int step = 0; step < JF * SP; ++step) {
-                    if (!PIPE) load_p(step);
-                    else if (step + 1 < JF * SP) load_p(step + 1);
-                    hold();
+                    for (int s = 0; s < SP; ++s) {
+                        Frag<T> pf[IT];
 #pragma unroll
-                    for (int it = step / SP * 2; it < IT; ++it)
-                        mma(step % SP < OP ? O[it] : E[it], vf[step / SP], pf[step & 1][it]);
-                    hold();
-                }
+                        for (int it = 2 * f; it < IT; ++it) pf[it] = by_p.at(s * (C / 16) + it, f);
+#pragma unroll
+                        for (int it = 2 * f; it < IT; ++it)
+                            mma(s < OP ? O[it] : E[it], vf[f], pf[it]);
+                    }
             }
             // ---- outputs: row i by lane % 16, four columns each
             if constexpr (KIND != kState) {
@@ -763,8 +735,13 @@ __global__ __launch_bounds__(NW * kWave, waves_of<T>(KD, NW, KIND)) void scan_ke
     }
 }
 
-// Columns of the values that a block takes.
-inline int block_columns(int width) { return width > 64 ? 128 : 64; }
+// Columns of the values that a block takes.  128 share the scores of 128: a prompt of 65,536
+// tokens of 8 heads of 128 324 us, with 64 columns a block 359.  But two states in parts of
+// bf16 leave a block of eight waves too few registers: a training step's scan of 64 by 128 with
+// the gradient of g 417 us with 64 columns, 449 with 128 (fp32: 46 and 41).
+constexpr int block_columns(Kind kind, bool bf16, int width) {
+    return width > 64 && !(kind == kDerivative && bf16) ? 128 : 64;
+}
 
 nsd_status launch_scan_f32(Kind kind, const Scan &a, hipStream_t st);
 nsd_status launch_scan_bf16(Kind kind, const Scan &a, hipStream_t st);
@@ -783,8 +760,10 @@ nsd_status launch_one(const Scan &a, hipStream_t st) {
 
 template <class T, int KD, Kind KIND>
 nsd_status launch_columns(const Scan &a, hipStream_t st) {
-    return block_columns(a.v.width) == 128 ? launch_one<T, KD, 8, KIND>(a, st)
-                                           : launch_one<T, KD, 4, KIND>(a, st);
+    constexpr bool kBf16 = sizeof(T) == 2;
+    if constexpr (block_columns(KIND, kBf16, kMaxWidth) == 128)
+        if (block_columns(KIND, kBf16, a.v.width) == 128) return launch_one<T, KD, 8, KIND>(a, st);
+    return launch_one<T, KD, 4, KIND>(a, st);
 }
 
 template <class T, Kind KIND>

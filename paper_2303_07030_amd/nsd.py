@@ -776,9 +776,10 @@ def _rows(t, name, n, width, ld, dtype):
     the next: one of another distance would be read, or written, past its end."""
     if not isinstance(t, torch.Tensor):
         return
-    if t.dtype is dtype and t.dim() == 2 and t.stride() == (ld, 1) and t.shape[0] >= n and \
-            t.shape[1] >= width:
-        return
+    if t.dtype is dtype and t.stride() == (ld, 1):  # (each look at a tensor costs 0.1 us)
+        have, wide = t.shape
+        if have >= n and wide >= width:
+            return
     if n > 1 and ld != width:  # rows with something between them
         fits = (t.dim() == 2 and t.shape[0] >= n and t.shape[1] >= width and t.stride(0) == ld
                 and (width == 1 or t.stride(1) == 1))
@@ -944,10 +945,11 @@ def _type_of(dtype: int):
 
 def _row_distance(t, width, name):
     """Values from one row of a matrix of `width` columns to the next."""
-    if t.dim() != 2 or t.shape[1] != width or (width > 1 and t.numel() and t.stride(1) != 1):
-        raise ValueError(f"{name}: {tuple(t.shape)}, strides {t.stride()}, are not rows of "
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 2 or shape[1] != width or (width > 1 and shape[0] and strides[1] != 1):
+        raise ValueError(f"{name}: {tuple(shape)}, strides {strides}, are not rows of "
                          f"{width} values")
-    return t.stride(0) if t.shape[0] > 1 else width
+    return strides[0] if shape[0] > 1 else width
 
 
 def embed_desc(W, out, scale=1.0, grad=None) -> nsd_embedding:
