@@ -31,6 +31,14 @@
 // decayed values) is a sum of two or three of them: two keep 16 bits, far below the
 // rounding of a bf16 result; the states that are carried on, and the gradient of g,
 // are held in 32 bits and take three.  fp32: fp32 products, half the chunk.
+//
+// A prompt of 65,536 tokens of 8 heads of 128 by 128 in bf16: the states 94 us, the outputs 204
+// (2.6 TB/s of the rows' bytes).  Neither bytes nor products bound it alone: the vector units issue in
+// 58% of the cycles (the parts of states and values, rows turned for LDS), the matrix cores are
+// busy in 30%, and two blocks a CU do not lay the one over the other whole; of LDS's cycles 3%
+// are conflicts.  A training step of 32,768 tokens of 16 heads of 64 by 128: states 73 us,
+// outputs 168, dq and dk 170 each, dv with the gradient of g 417 (42% and 17%: two states leave
+// two blocks of four waves a CU).
 #pragma once
 
 #include <type_traits>
@@ -188,7 +196,7 @@ __device__ __forceinline__ int place(int k) {
 // then 4-11, 16-19, 28-31, and so on (found by counting conflicts over row distances), a write
 // of 8 bytes 16 consecutive lanes over half of them.  The 16 bytes of a row that a lane
 // group reads are therefore turned by bits of the row's number, so that neither reads
-// nor writes (Stage's) of bf16 meet: 45% of the cycles of LDS were conflicts before.
+// nor writes (Stage's) of bf16 meet: 3% of the cycles of LDS are conflicts, without it 45%.
 
 // Of rows by token, KD values and 16 bytes apart.
 template <class T>

@@ -14,6 +14,10 @@
 //
 // The gradient's blocks walk tokens with a stride, hold their share of dw in registers
 // and leave one partial each; a second launch adds those up in their order.
+//
+// 16,384 tokens of 32 and 8 heads of 128 in bf16: 72.8 us (4.6 TB/s), the gradient 114 (4.4
+// TB/s) and 7 for the weights'.  8 tokens of 16 and 4 heads of 64 appended: 4.1 us, a launch.
+// 10,007 tokens of 6 and 3 heads of 40, pairs side by side, in fp32: 11.2, 16.6 and 6.5 us.
 #include <algorithm>
 
 #include "values.hpp"
@@ -28,6 +32,8 @@ constexpr int64_t kMaxQkBlocks = UINT32_MAX / kQkThreads;
 constexpr int kMaxHead = 512;
 constexpr int kPairs = 4;           // of a lane
 constexpr int kHeadsAhead = 2;      // heads of a slot in flight
+// Blocks of the gradient: four a CU (16,384 tokens of 40 heads of 128: 512 blocks 162 us, 1,024
+// 107, 2,048 115).
 constexpr int kMaxGradBlocks = 1024;
 
 struct QkArgs {
@@ -447,11 +453,12 @@ Lie lie_of(const nsd_qk *s) {
 }
 
 // Waves for a token: one, but where that leaves the card without work the heads are shared
-// by as many as there are rounds of heads.
+// by as many as there are rounds of heads (8 tokens of 20 heads of 64: 4.2 us, by one wave 4.9;
+// 4,096 of 40 heads of 128: by one 17.2, by two 18.3).
 int head_parts(int32_t ntok, const nsd_qk *s, int heads) {
     const int round = kWave / slot_lanes(s->d) * kHeadsAhead;
     const int rounds = (int)ceil_div(std::max(heads, 1), round);
-    constexpr int64_t kEnough = 8192;
+    constexpr int64_t kEnough = 4096;
     return (int)std::max<int64_t>(1, std::min<int64_t>(rounds, kEnough / std::max(ntok, 1)));
 }
 
