@@ -213,7 +213,22 @@ __device__ __forceinline__ int spread(int row, int j) {
     return row * kChunkOf<T> + ((j / B ^ x) * B | j % B);
 }
 
-// A lane's fragments of such rows: row 16 tile + lane % 16, places 32 f + 8 (lane / 16) on.
+// Place of the score of row i and column j.  SHORT (of bf16): rows of 32 places, the columns from
+// 32 on, which have rows from 32 on alone, behind the others; a quarter less, but two writes meet
+// on a bank.
+template <class T, bool SHORT>
+__device__ __forceinline__ int score_place(int i, int j) {
+    if constexpr (!SHORT) {
+        return spread<T>(i, j);
+    } else {
+        const int row = i + (j & 32), u = row >> 2 & 3;
+        return row * 32 + ((j >> 3 & 3) ^ u ^ (u << 1 & 2)) * 8 + (j & 7);
+    }
+}
+template <class T, bool SHORT>
+constexpr int kScores = SHORT ? 96 * 32 : kChunkOf<T> * kChunkOf<T>;
+
+// A lane's fragments of rows of C places: row 16 tile + lane % 16, places 32 f + 8 (lane / 16) on.
 // Two addresses for all of them, the rest known at compile time (or the same for all lanes).
 template <class T>
 struct Spread {
@@ -232,6 +247,16 @@ struct Spread {
                              __builtin_assume_aligned(p + off + (odd ? other : 0), 16), 16);
         }
         return x;
+    }
+};
+
+// The same of SHORT scores, part after part.
+struct ShortScores {
+    const Bf16 *p;
+    __device__ __forceinline__ ShortScores(const Bf16 *scores, int n16, int g)
+        : p(scores + score_place<Bf16, true>(n16, 8 * g)) {}
+    __device__ __forceinline__ Frag<Bf16> at(int tile, int f) const {
+        return fragment(p + tile / 4 * kScores<Bf16, true> + (16 * (tile % 4) + 32 * f) * 32);
     }
 };
 
@@ -368,7 +393,8 @@ struct Stage {
 // of g.
 enum Kind { kOutput, kState, kDerivative };
 
-// LDS of a block: queries, keys (the scores take their place), keys and values by columns.
+// LDS of a block: queries, keys (the scores take their place; DERIV's parts the queries' as well),
+// keys and values by columns.
 template <class T, int KD, int NW, Kind KIND>
 struct Shared {
     static constexpr int C = kChunkOf<T>;
@@ -378,15 +404,23 @@ struct Shared {
     static constexpr int OP = kParts<T, 2>;                 // of scores; behind them of DERIV's
     static constexpr int SP = OP + (KIND == kDerivative ? kParts<T, 3> : 0);
     static constexpr int Q = KIND == kState ? 0 : C * LDK;
-    static constexpr int KP = KIND == kState ? 0 : LDK > SP * C ? C * LDK : SP * C * C;
-    static constexpr int VALUES = Q + KP + KD * C + VB * C;
+    static constexpr bool SHORT = KIND == kDerivative && sizeof(T) == 2;
+    static constexpr int AT = KIND == kDerivative ? 0 : Q;  // where the scores are put
+    static constexpr int PART = kScores<T, SHORT>;
+    static constexpr int QK = 2 * Q > AT + SP * PART ? 2 * Q : AT + SP * PART;
+    static constexpr int ROWS = KIND == kState ? 0 : QK;
+    static constexpr int VALUES = ROWS + KD * C + VB * C;
 };
 
 // Waves of a SIMD, which say how many registers one may have: two blocks of eight waves a CU
 // where the state leaves room for it (a training step's scan of 64 by 128 163 us with one block
-// and 160 with two, in fp32 with the gradient of g 48 and 40).
+// and 160 with two, in fp32 with the gradient of g 48 and 40), three of four waves with the
+// gradient of g in bf16 (325 us, with two 417).
 constexpr int waves_of(int kd, int nw, Kind kind) {
-    return kd > 128 ? 1 : nw == 4 || (kind == kDerivative && kd > 64) ? 2 : 4;
+    const bool two_states = kind == kDerivative;
+    if (kd > 128) return 1;
+    if (nw == 4) return two_states && kd <= 64 ? 3 : 2;
+    return two_states && kd > 64 ? 2 : 4;
 }
 
 // KD: width of queries and keys, padded; NW: waves, 16 columns of the values each; blocks: of
@@ -402,8 +436,8 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
     __shared__ __align__(16) T lds[Sh::VALUES];
     T *const ldsQ = lds;
     T *const ldsK = ldsQ + Sh::Q;
-    T *const ldsP = ldsK;
-    T *const ldsKt = ldsK + Sh::KP;
+    T *const ldsP = lds + Sh::AT;
+    T *const ldsKt = lds + Sh::ROWS;
     T *const ldsVt = ldsKt + KD * C;
     __shared__ float power[C + 2], power_less[C + 2];
     __shared__ float weight[2 * C];  // s_score w^n at C + n, 0 below C
@@ -488,7 +522,8 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
         if (len > 0) {
             const int n16 = tid % 16, g = tid % kWave / 16;
             // this lane's places in what the products read: all others are a constant from them
-            const Spread<T> by_k(ldsKt, n16, g), by_v(ldsVt, n16, g), by_p(ldsP, n16, g);
+            const Spread<T> by_k(ldsKt, n16, g), by_v(ldsVt, n16, g);
+            const std::conditional_t<Sh::SHORT, ShortScores, Spread<T>> by_p(ldsP, n16, g);
             const T *const byQ = ldsQ + n16 * LDK + (8 * g ^ turned<T>(n16));
             const T *const byK = byQ + (ldsK - ldsQ);
 
@@ -515,36 +550,7 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
 #pragma unroll
                         for (int r = 0; r < 4; ++r) p[u][r] = apart >= r ? p[u][r] : 0.f;
                 }
-                __syncthreads();  // the keys were read: the scores take their place
-#pragma unroll
-                for (int u = 0; u < ROUNDS; ++u) {
-                    const int tile = u * NW + wave, it = it_of(tile), jt = tile - it * (it + 1) / 2;
-                    if (tile >= TILES) break;
-                    T part[SP][4];
-                    split<T, 2, 4>(p[u], reinterpret_cast<T(&)[OP][4]>(part));
-                    if constexpr (DERIV) {
-                        float y[4];
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) y[r] = p[u][r] * (float)(16 * (it - jt) + apart - r);
-                        split<T, 3, 4>(y, reinterpret_cast<T(&)[kParts<T, 3>][4]>(part[OP]));
-                    }
-#pragma unroll
-                    for (int s = 0; s < SP; ++s) {
-                        T *const to = ldsP + s * C * C;
-                        __builtin_memcpy(__builtin_assume_aligned(
-                                             to + spread<T>(16 * it + n16, 16 * jt + 4 * g), 8),
-                                         part[s], 4 * sizeof(T));
-                        if (jt == it && it % 2 == 0) {  // the rest of 32 columns
-                            const T none[4] = {T(0), T(0), T(0), T(0)};
-                            __builtin_memcpy(__builtin_assume_aligned(
-                                                 to + spread<T>(16 * it + n16, 16 * jt + 16 + 4 * g), 8),
-                                             none, sizeof none);
-                        }
-                    }
-                }
-                // ---- from the state (E: (i + 1) times that, and from its derivative)
-#pragma unroll
-                for (int it = 0; it < IT; ++it) O[it] = f32x4v{0.f, 0.f, 0.f, 0.f};
+                // ---- from the state
                 auto from_state = [&](const f32x4v (&state)[KT], f32x4v (&O)[IT]) {
 #pragma unroll
                     for (int f = 0; f < KF; ++f) {
@@ -562,13 +568,47 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
                             for (int it = 0; it < IT; ++it) mma(O[it], sf[s], qf[it]);
                     }
                 };
-                from_state(S, O);
-                if constexpr (DERIV) {
+                if constexpr (DERIV) {  // (i + 1) times that, and from its derivative
+#pragma unroll
+                    for (int it = 0; it < IT; ++it) O[it] = f32x4v{0.f, 0.f, 0.f, 0.f};
+                    from_state(S, O);
 #pragma unroll
                     for (int it = 0; it < IT; ++it)
 #pragma unroll
                         for (int r = 0; r < 4; ++r) E[it][r] = O[it][r] * (float)(16 * it + n16 + 1 - rev);
                     from_state(D, E);
+                }
+                __syncthreads();  // the keys were read: the scores take their place
+#pragma unroll
+                for (int u = 0; u < ROUNDS; ++u) {
+                    const int tile = u * NW + wave, it = it_of(tile), jt = tile - it * (it + 1) / 2;
+                    if (tile >= TILES) break;
+                    T part[SP][4];
+                    split<T, 2, 4>(p[u], reinterpret_cast<T(&)[OP][4]>(part));
+                    if constexpr (DERIV) {
+                        float y[4];
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) y[r] = p[u][r] * (float)(16 * (it - jt) + apart - r);
+                        split<T, 3, 4>(y, reinterpret_cast<T(&)[kParts<T, 3>][4]>(part[OP]));
+                    }
+#pragma unroll
+                    for (int s = 0; s < SP; ++s) {
+                        T *const to = ldsP + s * Sh::PART;
+                        __builtin_memcpy(__builtin_assume_aligned(
+                                             to + score_place<T, Sh::SHORT>(16 * it + n16, 16 * jt + 4 * g), 8),
+                                         part[s], 4 * sizeof(T));
+                        if (jt == it && it % 2 == 0) {  // the rest of 32 columns
+                            const T none[4] = {T(0), T(0), T(0), T(0)};
+                            __builtin_memcpy(__builtin_assume_aligned(
+                                                 to + score_place<T, Sh::SHORT>(16 * it + n16, 16 * jt + 16 + 4 * g), 8),
+                                             none, sizeof none);
+                        }
+                    }
+                }
+                if constexpr (!DERIV) {
+#pragma unroll
+                    for (int it = 0; it < IT; ++it) O[it] = f32x4v{0.f, 0.f, 0.f, 0.f};
+                    from_state(S, O);
                 }
             }
             // ---- the state behind the chunk
@@ -651,7 +691,7 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
                     for (int s = 0; s < SP; ++s) {
                         Frag<T> pf[IT];
 #pragma unroll
-                        for (int it = 2 * f; it < IT; ++it) pf[it] = by_p.at(s * (C / 16) + it, f);
+                        for (int it = 2 * f; it < IT; ++it) pf[it] = by_p.at(s * IT + it, f);
 #pragma unroll
                         for (int it = 2 * f; it < IT; ++it)
                             mma(s < OP ? O[it] : E[it], vf[f], pf[it]);
