@@ -37,8 +37,8 @@
 // 58% of the cycles (the parts of states and values, rows turned for LDS), the matrix cores are
 // busy in 30%, and two blocks a CU do not lay the one over the other whole; of LDS's cycles 3%
 // are conflicts.  A training step of 32,768 tokens of 16 heads of 64 by 128: states 73 us,
-// outputs 168, dq and dk 170 each, dv with the gradient of g 417 (42% and 17%: two states leave
-// two blocks of four waves a CU).
+// outputs 164, dq and dk 170 each, dv with the gradient of g 323 (56% and 23%: two states leave
+// three blocks of four waves a CU).
 #pragma once
 
 #include <type_traits>
@@ -415,7 +415,7 @@ struct Shared {
 // Waves of a SIMD, which say how many registers one may have: two blocks of eight waves a CU
 // where the state leaves room for it (a training step's scan of 64 by 128 163 us with one block
 // and 160 with two, in fp32 with the gradient of g 48 and 40), three of four waves with the
-// gradient of g in bf16 (325 us, with two 417).
+// gradient of g in bf16 (323 us, with two 417).
 constexpr int waves_of(int kd, int nw, Kind kind) {
     const bool two_states = kind == kDerivative;
     if (kd > 128) return 1;
@@ -786,7 +786,7 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
 // Columns of the values that a block takes.  128 share the scores of 128: a prompt of 65,536
 // tokens of 8 heads of 128 324 us, with 64 columns a block 359.  But two states in parts of
 // bf16 leave a block of eight waves too few registers: a training step's scan of 64 by 128 with
-// the gradient of g 417 us with 64 columns, 449 with 128 (fp32: 46 and 41).
+// the gradient of g 323 us with 64 columns, 449 with 128 (fp32: 46 and 41).
 constexpr int block_columns(Kind kind, bool bf16, int width) {
     return width > 64 && !(kind == kDerivative && bf16) ? 128 : 64;
 }
