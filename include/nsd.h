@@ -1140,7 +1140,7 @@ nsd_status nsd_qk_append(int32_t ntok, const nsd_qk *s, const void *Q, const voi
  *
  * nsd_attn_decay       O and, where not NULL, S1 [nseq]: the states after each
  *                      sequence (of an empty one, S0).  S0 [nseq] or NULL (zero).
- *                      S1 may be S0.  max_len (host): sequences are split for up to
+ *                      S1 may be S0; O is none of the rows that are read.  max_len (host): sequences are split for up to
  *                      so many tokens; a longer one is right, and slower.
  * nsd_attn_decay_vjp   gradients of Q, K, V (type and row distances of theirs) and,
  *                      where not NULL, decay [heads] and S0 [nseq], for the upstream
@@ -1150,7 +1150,8 @@ nsd_status nsd_qk_append(int32_t ntok, const nsd_qk *s, const void *Q, const voi
  * nsd_attn_decay_workspace_size  bytes for either call with these sizes.
  * nsd_attn_decay_step  one token for each row, its state in slot[r] of `state`
  *                      [nslots] (slot NULL: in r), updated in place.  Rows that name
- *                      one slot are tokens of it in the rows' order.  A slot outside
+ *                      one slot are tokens of it in the rows' order; O is none of the
+ *                      rows that are read.  A slot outside
  *                      [0, nslots) is padding: its row of O is 0.
  * Async.
  */

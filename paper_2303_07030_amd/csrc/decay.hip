@@ -11,6 +11,7 @@
 // end).
 #include <algorithm>
 #include <climits>
+#include <initializer_list>
 
 #include "decay.hpp"
 
@@ -299,6 +300,17 @@ struct DecayWs {
     bool cut() const { return seg_len != INT_MAX; }
 };
 
+// (Other blocks read the rows that one has written.)
+nsd_status check_apart(std::initializer_list<const void *> written,
+                       std::initializer_list<const void *> read) {
+    for (const void *const *w = written.begin(); w != written.end(); ++w) {
+        for (const void *r : read) NSD_REQUIRE(*w != r, "what is written shares memory with what is read");
+        for (const void *const *o = written.begin(); o != w; ++o)
+            NSD_REQUIRE(*w != *o, "what is written shares memory");
+    }
+    return NSD_OK;
+}
+
 nsd_status launch(Kind kind, const nsd_decay *s, const Scan &a, hipStream_t st) {
     return s->dtype == NSD_F32 ? launch_scan_f32(kind, a, st) : launch_scan_bf16(kind, a, st);
 }
@@ -370,6 +382,7 @@ nsd_status nsd_attn_decay(int32_t ntok, int32_t nseq, const int32_t *seqptr, int
     if (ws == nullptr || ws_bytes < w.bytes)
         return fail(NSD_ERR_WORKSPACE, "workspace %zu bytes at %p, need %zu", ws_bytes, ws, w.bytes);
     NSD_REQUIRE((reinterpret_cast<uintptr_t>(ws) & 255) == 0, "workspace is not 256-byte aligned");
+    if (ntok > 0) NSD_TRY(check_apart({O}, {Q, K, V}));
     const hipStream_t st = as_stream(stream);
     const int grp = s->heads / s->kv_heads;
     const Rows q{Q, s->ldq, s->d, 1}, k{K, s->ldk, s->d, grp}, v{V, s->ldv, s->dv, grp};
@@ -403,6 +416,7 @@ nsd_status nsd_attn_decay_vjp(int32_t ntok, int32_t nseq, const int32_t *seqptr,
     if (ws == nullptr || ws_bytes < w.bytes)
         return fail(NSD_ERR_WORKSPACE, "workspace %zu bytes at %p, need %zu", ws_bytes, ws, w.bytes);
     NSD_REQUIRE((reinterpret_cast<uintptr_t>(ws) & 255) == 0, "workspace is not 256-byte aligned");
+    if (nseq > 0 && ntok > 0) NSD_TRY(check_apart({dQ, dK, dV}, {Q, K, V, dO}));
     const hipStream_t st = as_stream(stream);
     const int grp = s->heads / s->kv_heads;
     if (nseq > 0) {
@@ -493,6 +507,7 @@ nsd_status nsd_attn_decay_step(int32_t nrows, const int32_t *slot, int32_t nslot
     if (nrows == 0) return NSD_OK;
     NSD_REQUIRE(Q && K && V && decay && O && (state || nslots == 0), "a NULL array");
     NSD_REQUIRE(slot || nrows <= nslots, "%d rows over %d states", nrows, nslots);
+    NSD_TRY(check_apart({O}, {Q, K, V}));
     Step a{nrows, nslots, s->heads, s->heads / s->kv_heads, s->d, s->dv, 0, s->scale, slot, Q, K, V,
            s->ldq, s->ldk, s->ldv, s->ldo, decay, state, O};
     const bool four = s->dv % 4 == 0;

@@ -605,6 +605,7 @@ nsd_status nsd_qk_append(int32_t ntok, const nsd_qk *s, const void *Q, const voi
     NSD_REQUIRE(slot, "slots are NULL");
     NSD_REQUIRE((Qo || s->heads == 0) && (Kc || s->kv_heads == 0 || nslots == 0), "Qo or Kc is NULL");
     NSD_REQUIRE(vwidth == 0 || (V && (Vc || nslots == 0)), "V or Vc is NULL");
+    NSD_REQUIRE((Kc != K || s->kv_heads == 0) && (Vc != V || vwidth == 0), "a cache is what is appended");
     NSD_REQUIRE(Qo != Q || s->ldqo == s->ldq || s->heads == 0, "in place with another row distance");
     QkArgs a = qk_args(ntok, s, Q, K, wq, wk, pos, freq);
     a.Qo = Qo;

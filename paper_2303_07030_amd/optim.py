@@ -56,6 +56,8 @@ class GradNorm:
     def measure(self, grad_scale=None, stream=None):
         """The norms of grad_scale (a device fp32 scalar, or None) times the gradients;
         `scale` holds grad_scale as a factor."""
+        if grad_scale is not None:
+            _flat(grad_scale, "grad_scale", self.scale.device, 1, (torch.float32,))
         h = nsd.nsd_clip(self.max_norm, 2 if self.order == 2 else 0,
                          None if grad_scale is None else grad_scale.data_ptr())
         nsd.nsd_grad_norm(self.plan, h, self.norm, self.scale, self.norms, self.ws, stream)
@@ -140,7 +142,8 @@ class AdamW:
         of this step) and lr_dev (device fp32) are read when the step runs: with
         them a captured graph counts its replays.  The count is then the caller's:
         `t`, the steps done, is not advanced, and has to be set before steps
-        without step_dev or a checkpoint of it.  A refused step changes nothing."""
+        without step_dev or a checkpoint of it.  A refused step changes nothing but
+        what `grad_norm` measured."""
         if self.grad_norm is not None:
             self.grad_norm.measure(grad_scale, stream)
             grad_scale = self.grad_norm.scale

@@ -64,7 +64,8 @@ def test_bad_descriptors_are_refused(change, status):
 
 def test_bad_arguments_are_refused():
     s, bad, big = desc(), nsd.NSD_ERR_INVALID_ARG, nsd.NSD_ERR_TOO_LARGE
-    ws = torch.empty(1 << 16, dtype=torch.uint8)
+    ws = torch.empty((1 << 16) + 256, dtype=torch.uint8)
+    ws = ws[-ws.data_ptr() % 256:]
     for many, status in ((calls(s, ntok=-1), bad), (calls(s, nseq=-1), bad),
                          (calls(s, max_len=-1), bad), (calls(s, ntok=2 ** 30 + 1), big),
                          (calls(s, nseq=2 ** 30), big)):
@@ -93,6 +94,14 @@ def test_bad_arguments_are_refused():
         args[place] = 2 * P
         with pytest.raises(nsd.NsdError, match="shares memory"):
             nsd.nsd_attn_decay_vjp(*args)
+    for call in (lambda: nsd.nsd_attn_decay(10, 2, P, 10, s, P, P, P, P, None, P, None, ws),
+                 lambda: nsd.nsd_attn_decay_step(4, P, 9, s, P, 2 * P, 3 * P, P, P, 3 * P),
+                 lambda: nsd.nsd_attn_decay_vjp(10, 2, P, 10, s, P, 2 * P, 3 * P, P, None, 4 * P,
+                                                None, 5 * P, 6 * P, 4 * P, None, None, ws),
+                 lambda: nsd.nsd_attn_decay_vjp(10, 2, P, 10, s, P, 2 * P, 3 * P, P, None, 4 * P,
+                                                None, 5 * P, 6 * P, 5 * P, None, None, ws)):
+        with pytest.raises(nsd.NsdError, match="shares memory"):
+            call()
     for args in ((-1, P, 9), (4, P, -1), (4, None, 3)):
         with pytest.raises(nsd.NsdError) as e:
             nsd.nsd_attn_decay_step(*args, s, P, P, P, P, P, P)

@@ -262,8 +262,8 @@ def test_one_word_of_many_in_a_large_batch(V):
 
 
 @pytest.mark.gpu
-def test_a_captured_step_follows_the_ids():
-    V, w, n = 3000, 200, 6000
+@pytest.mark.parametrize("V, w, n", [(3000, 200, 6000), (200_000, 8, 150_000)])
+def test_a_captured_step_follows_the_ids(V, w, n):
     rng = np.random.default_rng(1)
     W, dout = torch.randn(V, w, device="cuda"), torch.randn(n, w, device="cuda")
     out, dW = torch.empty(n, w, device="cuda"), torch.empty(V, w, device="cuda")

@@ -65,6 +65,7 @@ def test_bad_arguments_are_refused():
                  lambda: nsd.nsd_qk_rotate_vjp(4, desc(norm=0), P, P, P, P, P, P, P, P, P, P, P,
                                                None, None),  # weights without a norm
                  lambda: nsd.nsd_qk_append(4, s, P, P, None, P, P, P, P, None, 9, P, P, None),
+                 lambda: nsd.nsd_qk_append(4, s, P, P, None, P, P, P, P, P, 9, P, P, None),
                  lambda: nsd.nsd_qk_append(4, s, P, P, None, P, P, P, P, P, -1, P, P, None)):
         with pytest.raises(nsd.NsdError) as e:
             call()
