@@ -37,7 +37,7 @@
 // 58% of the cycles (the parts of states and values, rows turned for LDS), the matrix cores are
 // busy in 30%, and two blocks a CU do not lay the one over the other whole; of LDS's cycles 3%
 // are conflicts.  A training step of 32,768 tokens of 16 heads of 64 by 128: states 73 us,
-// outputs 164, dq and dk 170 each, dv with the gradient of g 323 (56% and 23%: two states leave
+// outputs 164, dq and dk 154 each, dv with the gradient of g 323 (56% and 23%: two states leave
 // three blocks of four waves a CU).
 #pragma once
 
@@ -409,17 +409,21 @@ struct Shared {
     static constexpr int PART = kScores<T, SHORT>;
     static constexpr int QK = 2 * Q > AT + SP * PART ? 2 * Q : AT + SP * PART;
     static constexpr int ROWS = KIND == kState ? 0 : QK;
-    static constexpr int VALUES = ROWS + KD * C + VB * C;
+    // Wide keys by columns take the queries' place when those were read: three blocks of four waves
+    // a CU instead of two (a training step's dq and dk, keys of 128, 154 us for 170).
+    static constexpr bool LATE = KIND == kOutput && NW == 4 && KD > 64;
+    static_assert(!LATE || KD * C <= Q, "keys by columns in the queries' place");
+    static constexpr int VALUES = ROWS + (LATE ? 0 : KD * C) + VB * C;
 };
 
 // Waves of a SIMD, which say how many registers one may have: two blocks of eight waves a CU
 // where the state leaves room for it (a training step's scan of 64 by 128 163 us with one block
 // and 160 with two, in fp32 with the gradient of g 48 and 40), three of four waves with the
-// gradient of g in bf16 (323 us, with two 417).
+// gradient of g in bf16 (323 us, with two 417) and where wide keys leave them the LDS.
 constexpr int waves_of(int kd, int nw, Kind kind) {
     const bool two_states = kind == kDerivative;
     if (kd > 128) return 1;
-    if (nw == 4) return two_states && kd <= 64 ? 3 : 2;
+    if (nw == 4) return two_states == (kd <= 64) ? 3 : 2;
     return two_states && kd > 64 ? 2 : 4;
 }
 
@@ -437,8 +441,9 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
     T *const ldsQ = lds;
     T *const ldsK = ldsQ + Sh::Q;
     T *const ldsP = lds + Sh::AT;
-    T *const ldsKt = lds + Sh::ROWS;
-    T *const ldsVt = ldsKt + KD * C;
+    constexpr bool LATE = Sh::LATE;
+    T *const ldsKt = LATE ? lds : lds + Sh::ROWS;
+    T *const ldsVt = lds + Sh::ROWS + (LATE ? 0 : KD * C);
     __shared__ float power[C + 2], power_less[C + 2];
     __shared__ float weight[2 * C];  // s_score w^n at C + n, 0 below C
     __shared__ __align__(16) float behind[2 * C];  // s_update w^(C - 1 - j (+ 1)) at j, 0 from C on
@@ -568,10 +573,12 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
                             for (int it = 0; it < IT; ++it) mma(O[it], sf[s], qf[it]);
                     }
                 };
-                if constexpr (DERIV) {  // (i + 1) times that, and from its derivative
+                if constexpr (DERIV || LATE) {
 #pragma unroll
                     for (int it = 0; it < IT; ++it) O[it] = f32x4v{0.f, 0.f, 0.f, 0.f};
                     from_state(S, O);
+                }
+                if constexpr (DERIV) {  // (i + 1) times that, and from its derivative
 #pragma unroll
                     for (int it = 0; it < IT; ++it)
 #pragma unroll
@@ -579,6 +586,7 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
                     from_state(D, E);
                 }
                 __syncthreads();  // the keys were read: the scores take their place
+                if (LATE) xk.store_transposed(tid, ldsKt);
 #pragma unroll
                 for (int u = 0; u < ROUNDS; ++u) {
                     const int tile = u * NW + wave, it = it_of(tile), jt = tile - it * (it + 1) / 2;
@@ -605,12 +613,13 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
                         }
                     }
                 }
-                if constexpr (!DERIV) {
+                if constexpr (!DERIV && !LATE) {
 #pragma unroll
                     for (int it = 0; it < IT; ++it) O[it] = f32x4v{0.f, 0.f, 0.f, 0.f};
                     from_state(S, O);
                 }
             }
+            if (LATE) __syncthreads();
             // ---- the state behind the chunk
             Frag<T> vf[JF];
 #pragma unroll
@@ -684,7 +693,7 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
             }
             // ---- from the chunk's own tokens
             if constexpr (KIND != kState) {
-                __syncthreads();
+                if (!LATE) __syncthreads();
 #pragma unroll
                 for (int f = 0; f < JF; ++f)
 #pragma unroll
@@ -743,7 +752,7 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
                 xq.store(tid, ldsQ, LDK);
                 xk.store(tid, ldsK, LDK);
             }
-            xk.store_transposed(tid, ldsKt);
+            if (!LATE) xk.store_transposed(tid, ldsKt);
             xv.store_transposed(tid, ldsVt);
             if (KIND != kState && !xv.finite()) unusual[turn] = 1;
             __syncthreads();
