@@ -402,17 +402,18 @@ def test_results_are_the_same_every_time():
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("max_len", [1, 10_000])
 @pytest.mark.parametrize("bad", [math.inf, math.nan])
-def test_numbers_that_are_not_finite_stay_behind_their_token(bad, max_len, dtype):
-    lens, H, d = [200, 400, 90], 2, 32
-    room = (2 * d + 2 * max(lens) + 32) * U
-    mag = definition(Case(lens, H, H, d, d, dtype).arrays(), lens, 0.3, magnitude=True)
+@pytest.mark.parametrize("d, dv", [(32, 32), (40, 100), (100, 40)])
+def test_numbers_that_are_not_finite_stay_behind_their_token(d, dv, bad, max_len, dtype):
+    lens, H = [200, 400, 90], 2
+    room = (d + dv + 2 * max(lens) + 32) * U
+    mag = definition(Case(lens, H, H, d, dv, dtype).arrays(), lens, 0.3, magnitude=True)
     for name in ("v", "k", "q", "do"):
-        c = Case(lens, H, H, d, d, dtype)
+        c = Case(lens, H, H, d, dv, dtype)
         want_s1 = c.forward(max_len)
         want_dg = c.backward(max_len)
         want = {i: t.clone() for i, t in c.out.items()}
         at = 200 + 77
-        c.t[name][at, d + 3] = bad  # of sequence 1, head 1
+        c.t[name][at, c.t[name].shape[1] // H + 3] = bad  # of sequence 1, head 1
         s1 = c.forward(max_len)
         c.backward(max_len)
         for out, later in (("o", True), ("dq", True), ("dk", False), ("dv", False)):
