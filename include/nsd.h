@@ -1130,8 +1130,9 @@ nsd_status nsd_qk_append(int32_t ntok, const nsd_qk *s, const void *Q, const voi
  * [ntok][kv_heads][d], V: [ntok][kv_heads][dv], O: [ntok][heads][dv], all of one
  * nsd_dtype, with ldq, ldk, ldv, ldo values from one row to the next; head h reads
  * key head h / (heads / kv_heads).  d, dv <= 256, distances up to 2^22 values, any
- * alignment.  decay: fp32 [heads], the g_h: at most 0 (-infinity: a token sees itself alone).  States are fp32,
- * [heads][d][dv] for each sequence or slot, whatever the type of the rows.
+ * alignment.  decay: fp32 [heads], the g_h: at most 0 (-infinity: a token sees itself
+ * alone).  States are fp32, [heads][d][dv] for each sequence or slot, whatever the type
+ * of the rows.
  *
  * Sequence s is the rows seqptr[s] to seqptr[s + 1] - 1 (int32 [nseq + 1],
  * non-decreasing, within [0, ntok]); it may be empty.  Rows of no sequence are not
@@ -1140,8 +1141,9 @@ nsd_status nsd_qk_append(int32_t ntok, const nsd_qk *s, const void *Q, const voi
  *
  * nsd_attn_decay       O and, where not NULL, S1 [nseq]: the states after each
  *                      sequence (of an empty one, S0).  S0 [nseq] or NULL (zero).
- *                      S1 may be S0; O is none of the rows that are read.  max_len (host): sequences are split for up to
- *                      so many tokens; a longer one is right, and slower.
+ *                      S1 may be S0; O is none of the rows that are read.
+ *                      max_len (host): sequences are split for up to so many
+ *                      tokens; a longer one is right, and slower.
  * nsd_attn_decay_vjp   gradients of Q, K, V (type and row distances of theirs) and,
  *                      where not NULL, decay [heads] and S0 [nseq], for the upstream
  *                      dO (ldo) and dS1 [nseq] or NULL (zero).  Nothing that is
