@@ -447,7 +447,10 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
     __shared__ float power[C + 2], power_less[C + 2];
     __shared__ float weight[2 * C];  // s_score w^n at C + n, 0 below C
     __shared__ __align__(16) float behind[2 * C];  // s_update w^(C - 1 - j (+ 1)) at j, 0 from C on
-    __shared__ int unusual[2];
+    // A byte for each wave, not 0 where it staged a value that is not finite.  Its wave writes it
+    // for every chunk, so that nothing clears it; between the others' reads of one chunk's and
+    // the next write lies the barrier at the chunk's end.
+    __shared__ __align__(8) uint8_t unusual[NW];
     __shared__ float wave_sum[NW];
 
     const int lane = threadIdx.x % kWave, n16 = lane % 16, g = lane / 16;
@@ -474,7 +477,6 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
             weight[C + n] = a.s_score * (float)x;
         }
     }
-    if (threadIdx.x < 2) unusual[threadIdx.x] = 0;
     // this lane's part of the state: rows 16 kt + 4 g + r, column n16 of the wave's
     f32x4v S[KT], D[KT];  // (D: of DERIV alone)
     auto each_state = [&](const float *from, bool by_seq, auto f) {
@@ -505,7 +507,7 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
     const int64_t first = rev ? (int64_t)seg.first + seg.n - 1 : seg.first;
     const int dir = rev ? -1 : 1;
     float dsum = 0.f;
-    int single = 0, turn = 0;  // single: tokens that are still taken one by one
+    int single = 0;  // tokens that are still taken one by one
     int pos = 0, len = 0, next = 0, next_len = min(C, seg.n);
     // The next chunk's rows are on their way while one is multiplied where that leaves the card
     // as many waves; the other blocks of a CU hide them else (outputs with a state of 128 by 128:
@@ -754,18 +756,23 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
             }
             if (!LATE) xk.store_transposed(tid, ldsKt);
             xv.store_transposed(tid, ldsVt);
-            if (KIND != kState && !xv.finite()) unusual[turn] = 1;
+            if (KIND != kState) {
+                const bool bad = __ballot(!xv.finite()) != 0;
+                if (tid % kWave == 0) unusual[wave] = bad;
+            }
             __syncthreads();
             // A product with a score of 0 keeps an infinite or missing number of a later token
             // out of an earlier one's output no more than a sum would: such chunks go token by
             // token.
-            if (KIND == kState || !unusual[turn] || len == 1) break;
+            if (KIND == kState || len == 1) break;
+            std::conditional_t<NW == 8, uint64_t, uint32_t> any;
+            static_assert(sizeof any == NW, "a byte for each wave");
+            __builtin_memcpy(&any, unusual, NW);
+            if (any == 0) break;
             single = len;
             len = 1;
             __syncthreads();
         }
-        turn ^= 1;
-        if (threadIdx.x == 0) unusual[turn] = 0;  // (written again behind the next barrier)
         if (single > 0) --single;
         next = pos + len;
         next_len = single > 0 ? 1 : min(C, seg.n - next);

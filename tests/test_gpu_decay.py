@@ -439,6 +439,32 @@ def test_numbers_that_are_not_finite_stay_behind_their_token(d, dv, bad, max_len
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d, dv", [(32, 40), (64, 128), (100, 100)])
+@pytest.mark.parametrize("place", [7, 20, 31, 41, 63])
+def test_first_chunks_with_a_number_that_is_not_finite(place, d, dv, dtype):
+    """Many sequences of a chunk or two, each with one in a row that another wave than the
+    first may stage: it reaches no token on its other side, in any of them."""
+    B, H = 40, 4
+    for bad in (math.inf, math.nan):
+        c = Case([64] * B, H, H, d, dv, dtype)
+        for name in ("v", "do"):
+            at = place if name == "v" else 63 - place  # (the scans of dk and dv go backwards)
+            c.t[name][:64 * B].view(B, 64, -1)[:, at] = bad
+        c.forward()
+        c.backward()
+        rows = {i: t[:64 * B].float().view(B, 64, -1) for i, t in c.out.items()}
+        assert torch.isfinite(rows["o"][:, :place]).all()
+        assert not torch.isfinite(rows["o"][:, place]).any()
+        # (dq meets the tokens before, and its own upstream; dk and dv those behind)
+        clean = [t for t in range(place) if t != 63 - place]
+        assert torch.isfinite(rows["dq"][:, clean]).all()
+        clean = [t for t in range(64 - place, 64) if t != place]
+        assert torch.isfinite(rows["dk"][:, clean]).all()
+        assert torch.isfinite(rows["dv"][:, clean]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_states_carry_a_sequence_on(dtype):
     """Two calls, the second from the first's states, are one call; in place, too."""
     c = Case([600], 3, 3, 40, 24, dtype)
