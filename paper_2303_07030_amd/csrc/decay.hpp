@@ -28,9 +28,8 @@
 // through LDS; the next chunk's rows are in flight meanwhile.
 //
 // bf16: products of bf16 rows are exact, and what is not a bf16 number (scores, states,
-// decayed values) is a sum of two or three of them: two keep 16 bits, far below the
-// rounding of a bf16 result; the states that are carried on, and the gradient of g,
-// are held in 32 bits and take three.  fp32: fp32 products, half the chunk.
+// decayed values) is a sum of three of them, 24 bits, as many as a 32-bit float has: the
+// results are those of products in 32 bits.  fp32: fp32 products, half the chunk.
 //
 // A prompt of 65,536 tokens of 8 heads of 128 by 128 in bf16: the states 94 us, the outputs 204
 // (2.6 TB/s of the rows' bytes).  Neither bytes nor products bound it alone: the vector units issue in
@@ -400,20 +399,24 @@ struct Shared {
     static constexpr int C = kChunkOf<T>;
     static constexpr int VB = NW * 16;
     static constexpr int LDK = KD + 16 / sizeof(T);
-    static constexpr int NS = KIND == kDerivative ? 3 : 2;  // parts of states
-    static constexpr int OP = kParts<T, 2>;                 // of scores; behind them of DERIV's
-    static constexpr int SP = OP + (KIND == kDerivative ? kParts<T, 3> : 0);
+    static constexpr int OP = kParts<T, 3>;  // parts of scores; behind them those of DERIV's
+    static constexpr int SP = KIND == kDerivative ? 2 * OP : OP;
     static constexpr int Q = KIND == kState ? 0 : C * LDK;
     static constexpr bool SHORT = KIND == kDerivative && sizeof(T) == 2;
     static constexpr int AT = KIND == kDerivative ? 0 : Q;  // where the scores are put
     static constexpr int PART = kScores<T, SHORT>;
-    static constexpr int QK = 2 * Q > AT + SP * PART ? 2 * Q : AT + SP * PART;
-    static constexpr int ROWS = KIND == kState ? 0 : QK;
+    // Blocks of four waves take their values from LDS before the scores are put there, over keys
+    // and values: three blocks a CU have room for the scores' parts.
+    static constexpr bool OVER = KIND != kState && NW == 4;
+    static constexpr int QKV = 2 * Q + (OVER ? VB * C : 0);
+    static constexpr int ROWS = KIND == kState ? 0 : QKV > AT + SP * PART ? QKV : AT + SP * PART;
     // Wide keys by columns take the queries' place when those were read: three blocks of four waves
     // a CU instead of two (a training step's dq and dk, keys of 128, 154 us for 170).
     static constexpr bool LATE = KIND == kOutput && NW == 4 && KD > 64;
     static_assert(!LATE || KD * C <= Q, "keys by columns in the queries' place");
-    static constexpr int VALUES = ROWS + (LATE ? 0 : KD * C) + VB * C;
+    static constexpr int KT_END = ROWS + (LATE ? 0 : KD * C);
+    static constexpr int V = OVER ? 2 * Q : KT_END;
+    static constexpr int VALUES = OVER ? KT_END : KT_END + VB * C;
 };
 
 // Waves of a SIMD, which say how many registers one may have: two blocks of eight waves a CU
@@ -434,7 +437,7 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
     using Sh = Shared<T, KD, NW, KIND>;
     constexpr int C = Sh::C, VB = Sh::VB, LDK = Sh::LDK;
     constexpr int KT = KD / 16, KF = KD / 32, IT = C / 16, JF = C / 32;
-    constexpr int NS = Sh::NS, OP = Sh::OP, SP = Sh::SP, VP = kParts<T, 3>;
+    constexpr int OP = Sh::OP, SP = Sh::SP, NP = kParts<T, 3>;
     constexpr bool DERIV = KIND == kDerivative;
     constexpr int GR = KT < IT ? KT : IT;  // rows of the state that a step of their products takes
     __shared__ __align__(16) T lds[Sh::VALUES];
@@ -443,7 +446,7 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
     T *const ldsP = lds + Sh::AT;
     constexpr bool LATE = Sh::LATE;
     T *const ldsKt = LATE ? lds : lds + Sh::ROWS;
-    T *const ldsVt = lds + Sh::ROWS + (LATE ? 0 : KD * C);
+    T *const ldsVt = lds + Sh::V;
     __shared__ float power[C + 2], power_less[C + 2];
     __shared__ float weight[2 * C];  // s_score w^n at C + n, 0 below C
     __shared__ __align__(16) float behind[2 * C];  // s_update w^(C - 1 - j (+ 1)) at j, 0 from C on
@@ -534,6 +537,11 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
             const T *const byQ = ldsQ + n16 * LDK + (8 * g ^ turned<T>(n16));
             const T *const byK = byQ + (ldsK - ldsQ);
 
+            Frag<T> vf[JF];  // the wave's columns of the values
+            auto take_values = [&]() {
+#pragma unroll
+                for (int f = 0; f < JF; ++f) vf[f] = by_v.at(wave, f);
+            };
             f32x4v O[IT], E[IT];  // (E: of DERIV, the outputs' derivatives)
             if constexpr (KIND != kState) {
                 // ---- scores: tile (it, jt) of 16 x 16, jt <= it, shared out among the waves
@@ -564,13 +572,13 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
                         Frag<T> qf[IT];
 #pragma unroll
                         for (int it = 0; it < IT; ++it) qf[it] = fragment(byQ + 16 * it * LDK + 32 * f);
-                        Frag<T> sf[kParts<T, NS>];
+                        Frag<T> sf[NP];
                         float x[8];
 #pragma unroll
                         for (int e = 0; e < 8; ++e) x[e] = state[2 * f + e / 4][e % 4];
-                        split<T, NS>(x, sf);
+                        split<T, 3>(x, sf);
 #pragma unroll
-                        for (int s = 0; s < kParts<T, NS>; ++s)
+                        for (int s = 0; s < NP; ++s)
 #pragma unroll
                             for (int it = 0; it < IT; ++it) mma(O[it], sf[s], qf[it]);
                     }
@@ -587,6 +595,7 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
                         for (int r = 0; r < 4; ++r) E[it][r] = O[it][r] * (float)(16 * it + n16 + 1 - rev);
                     from_state(D, E);
                 }
+                if constexpr (Sh::OVER) take_values();
                 __syncthreads();  // the keys were read: the scores take their place
                 if (LATE) xk.store_transposed(tid, ldsKt);
 #pragma unroll
@@ -594,12 +603,12 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
                     const int tile = u * NW + wave, it = it_of(tile), jt = tile - it * (it + 1) / 2;
                     if (tile >= TILES) break;
                     T part[SP][4];
-                    split<T, 2, 4>(p[u], reinterpret_cast<T(&)[OP][4]>(part));
+                    split<T, 3, 4>(p[u], reinterpret_cast<T(&)[OP][4]>(part));
                     if constexpr (DERIV) {
                         float y[4];
 #pragma unroll
                         for (int r = 0; r < 4; ++r) y[r] = p[u][r] * (float)(16 * (it - jt) + apart - r);
-                        split<T, 3, 4>(y, reinterpret_cast<T(&)[kParts<T, 3>][4]>(part[OP]));
+                        split<T, 3, 4>(y, reinterpret_cast<T(&)[OP][4]>(part[OP]));
                     }
 #pragma unroll
                     for (int s = 0; s < SP; ++s) {
@@ -623,9 +632,7 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
             }
             if (LATE) __syncthreads();
             // ---- the state behind the chunk
-            Frag<T> vf[JF];
-#pragma unroll
-            for (int f = 0; f < JF; ++f) vf[f] = by_v.at(wave, f);
+            if constexpr (!Sh::OVER) take_values();
             const float keep = power[len], less = power_less[len];
             if (keep > 0.5f) {  // a slow decay by what it takes away
 #pragma unroll
@@ -661,7 +668,7 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
             }
 #pragma unroll
             for (int f = 0; f < JF; ++f) {
-                Frag<T> vs[VP], vd[VP];
+                Frag<T> vs[NP], vd[NP];
                 T v[8];
                 __builtin_memcpy(v, &vf[f], sizeof v);
                 float x[8];
@@ -685,7 +692,7 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
 #pragma unroll
                     for (int i = 0; i < GR; ++i) kf[i] = by_k.at(kg * GR + i, f);
 #pragma unroll
-                    for (int s = 0; s < VP; ++s)
+                    for (int s = 0; s < NP; ++s)
 #pragma unroll
                         for (int i = 0; i < GR; ++i) {
                             mma(S[kg * GR + i], kf[i], vs[s]);

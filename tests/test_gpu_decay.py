@@ -10,10 +10,10 @@ order is off by n u of them.  A result passes a sum over a head's values (d or d
 over the tokens, and for each chunk of 32 tokens and more two roundings of a decay:
 (d + dv + 2 len + 32) u of the magnitudes.  Where a power or a product is below 2^-126, the
 least normal number, it is off by less than that, whatever multiplies it: 2^-126 of the
-magnitudes without a decay, and of each of the products that a result adds up.  bf16 rows multiply exactly; scores and
-states enter the products of bf16 results as two bf16 numbers each, off by 2^-16; those
-of states and of the decay's gradient as three, off by 2^-24.  A value rounded to its
-type is off by half a step.
+magnitudes without a decay, and of each of the products that a result adds up.  bf16 rows multiply exactly; scores,
+states and decayed values enter the products of bf16 rows as three bf16 numbers each, off
+by 2^-24.  (PARTS leaves scores and states 2^-16, what two numbers would keep; that they keep
+32 bits is tested by itself, exactly.)  A value rounded to its type is off by half a step.
 """
 import math
 
@@ -461,6 +461,53 @@ def test_first_chunks_with_a_number_that_is_not_finite(place, d, dv, dtype):
         clean = [t for t in range(64 - place, 64) if t != place]
         assert torch.isfinite(rows["dk"][:, clean]).all()
         assert torch.isfinite(rows["dv"][:, clean]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("Hk", [1, 2])
+@pytest.mark.parametrize("d, dv", [(16, 16), (64, 128), (128, 40), (100, 100), (256, 256)])
+def test_scores_and_states_keep_32_bits(d, dv, Hk, dtype):
+    """Sums of x = 1 + 2^-9 + 2^-20 and of y = -(1 + 2^-9), as scores or as states: without a
+    decay every product and sum is a multiple of 2^-20 below 4, exact in 32 bits, and what is
+    left is 2^-20.  (As two bf16 numbers x would be y.)"""
+    x, y = [1.0, 2.0 ** -9, 2.0 ** -20], [1.0, 2.0 ** -9, 0.0]
+    ones = [1.0] * 3
+
+    def run(rows, out, want_row, s0=None, ds1=None):
+        c = Case([2], 2, Hk, d, dv, dtype, decays=[0.0, 0.0], scale=1.0)
+        for t in c.t.values():
+            t.zero_()
+        for name, (first, second) in rows.items():
+            heads = Hk if name in ("k", "v") else 2
+            t = c.t[name].view(c.n, heads, -1)
+            for row, value in ((0, first), (1, second)):
+                if isinstance(value, list):
+                    t[row, 0, :3] = torch.tensor(value)
+                else:
+                    t[row, 0] = value
+        for state, value in ((c.s0, s0), (c.ds1, ds1)):
+            state.zero_()
+            if value:
+                state[0, 0] = torch.tensor(value[0])[:, None] if value[1] else torch.tensor(value[0])
+        c.forward()
+        c.backward()
+        want = torch.from_numpy(definition(c.arrays(), [2], 1.0)[out][:2]).to(T[dtype])
+        got = c.out[out][:2].cpu().view(want.shape)
+        assert torch.equal(got, want), (rows, out)  # rounded to its type once
+        assert torch.all(got[want_row, 0].double() == 2.0 ** -20), (rows, out)
+
+    run(dict(q=(ones, ones), k=(x, y), v=(1.0, -1.0)), "o", 1)
+    run(dict(do=(ones, ones), v=(x, y), k=(1.0, -1.0)), "dq", 1)
+    run(dict(v=(ones, ones), do=(x, y), q=(1.0, -1.0)), "dk", 0)
+    run(dict(k=(ones, ones), q=(x, y), do=(1.0, -1.0)), "dv", 0)
+    pair = [1 + 2.0 ** -9 + 2.0 ** -20, -(1 + 2.0 ** -9)]
+    by_key, by_value = (pair + [0.0] * (n - 2) for n in (d, dv))
+    one = ([1.0, 1.0, 0.0], [1.0, 1.0, 0.0])
+    run(dict(q=one), "o", 1, s0=(by_key, True))
+    run(dict(do=one), "dq", 1, s0=(by_value, False))
+    run(dict(v=one), "dk", 0, ds1=(by_value, False))
+    run(dict(k=one), "dv", 0, ds1=(by_key, True))
 
 
 @pytest.mark.gpu
