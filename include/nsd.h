@@ -996,7 +996,7 @@ nsd_status nsd_adamw_step(const nsd_adamw_plan *plan, const nsd_adamw *h, void *
  * with f = *grad_scale (1 where NULL).  Squares and sums are held in 64 bits, so
  * that no gradient of 32 bits overflows or vanishes in them.  A NaN makes the
  * norms that it belongs to and the factor NaN; an infinity makes norms infinite
- * and the factor 0.
+ * and the factor 0 (f where max_norm is infinite).
  *
  * A tensor is a flat array of n < 2^31 - 8192 values, at any address that its
  * type allows.  Tensors may share memory; each counts by itself.
@@ -1023,7 +1023,7 @@ typedef struct nsd_grad_plan {
 } nsd_grad_plan;
 
 typedef struct nsd_clip {
-    double max_norm;         /* > 0; infinity: nothing is clipped */
+    double max_norm;         /* > 0; infinity: nothing is clipped, the factor is f */
     int32_t order;           /* 2, or 0 for the largest magnitude */
     const float *grad_scale; /* device scalar f, or NULL */
 } nsd_clip;

@@ -131,8 +131,9 @@ __global__ __launch_bounds__(kJoinThreads) void grad_join_kernel(
         norms[blockIdx.x - 1] = v;
     } else {
         *norm = v;
-        const double c = max_norm / (v + 1e-6);
-        *scale = (float)(f * (c < 1.0 || c != c ? c : 1.0));
+        // (a norm that is not a number, but no infinite one without a bound, shows in the factor)
+        const double c = v != v ? v : max_norm < HUGE_VAL ? max_norm / (v + 1e-6) : 1.0;
+        *scale = (float)(f * (c > 1.0 ? 1.0 : c));
     }
 }
 
