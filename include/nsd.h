@@ -1141,7 +1141,9 @@ nsd_status nsd_qk_append(int32_t ntok, const nsd_qk *s, const void *Q, const voi
  *
  * nsd_attn_decay       O and, where not NULL, S1 [nseq]: the states after each
  *                      sequence (of an empty one, S0).  S0 [nseq] or NULL (zero).
- *                      S1 may be S0; O is none of the rows that are read.
+ *                      S1 may be S0 itself; nothing else that is written shares
+ *                      memory with what is read (rows between each other's, as of
+ *                      one projection, do not).
  *                      max_len (host): sequences are split for up to so many
  *                      tokens; a longer one is right, and slower.
  * nsd_attn_decay_vjp   gradients of Q, K, V (type and row distances of theirs) and,
@@ -1152,9 +1154,9 @@ nsd_status nsd_qk_append(int32_t ntok, const nsd_qk *s, const void *Q, const voi
  * nsd_attn_decay_workspace_size  bytes for either call with these sizes.
  * nsd_attn_decay_step  one token for each row, its state in slot[r] of `state`
  *                      [nslots] (slot NULL: in r), updated in place.  Rows that name
- *                      one slot are tokens of it in the rows' order; O is none of the
- *                      rows that are read.  A slot outside
- *                      [0, nslots) is padding: its row of O is 0.
+ *                      one slot are tokens of it in the rows' order.  O and the states
+ *                      share no memory with each other or with what is read.  A slot
+ *                      outside [0, nslots) is padding: its row of O is 0.
  * Async.
  */
 typedef struct nsd_decay {

@@ -11,7 +11,6 @@
 // end).
 #include <algorithm>
 #include <climits>
-#include <initializer_list>
 
 #include "decay.hpp"
 
@@ -300,16 +299,21 @@ struct DecayWs {
     bool cut() const { return seg_len != INT_MAX; }
 };
 
-// (Other blocks read the rows that one has written.)
-nsd_status check_apart(std::initializer_list<const void *> written,
-                       std::initializer_list<const void *> read) {
-    for (const void *const *w = written.begin(); w != written.end(); ++w) {
-        for (const void *r : read) NSD_REQUIRE(*w != r, "what is written shares memory with what is read");
-        for (const void *const *o = written.begin(); o != w; ++o)
-            NSD_REQUIRE(*w != *o, "what is written shares memory");
+// A call's arrays.  (Other blocks read what one has written: outputs are apart from them all, but
+// for the states behind the sequences, of which every block writes what it alone has read.)
+struct Areas {
+    int64_t n;  // tokens
+    const nsd_decay *s;
+    int64_t state = 4 * (int64_t)s->heads * s->d * s->dv;
+    Area q(const void *p) const { return row_area(p, n, (int64_t)s->heads * s->d, s->ldq, s->dtype); }
+    Area k(const void *p) const { return row_area(p, n, (int64_t)s->kv_heads * s->d, s->ldk, s->dtype); }
+    Area v(const void *p) const { return row_area(p, n, (int64_t)s->kv_heads * s->dv, s->ldv, s->dtype); }
+    Area o(const void *p) const { return row_area(p, n, (int64_t)s->heads * s->dv, s->ldo, s->dtype); }
+    Area decay(const void *p) const { return flat_area(p, 4 * (int64_t)s->heads); }
+    Area states(const void *p, int64_t count, int same = 0) const {
+        return Area{p, 1, count * state, count * state, same};
     }
-    return NSD_OK;
-}
+};
 
 nsd_status launch(Kind kind, const nsd_decay *s, const Scan &a, hipStream_t st) {
     return s->dtype == NSD_F32 ? launch_scan_f32(kind, a, st) : launch_scan_bf16(kind, a, st);
@@ -382,7 +386,10 @@ nsd_status nsd_attn_decay(int32_t ntok, int32_t nseq, const int32_t *seqptr, int
     if (ws == nullptr || ws_bytes < w.bytes)
         return fail(NSD_ERR_WORKSPACE, "workspace %zu bytes at %p, need %zu", ws_bytes, ws, w.bytes);
     NSD_REQUIRE((reinterpret_cast<uintptr_t>(ws) & 255) == 0, "workspace is not 256-byte aligned");
-    if (ntok > 0) NSD_TRY(check_apart({O}, {Q, K, V}));
+    const Areas of{ntok, s};
+    NSD_TRY(check_apart({of.o(O), of.states(S1, nseq, 1), flat_area(ws, w.bytes)},
+                        {of.q(Q), of.k(K), of.v(V), of.decay(decay), of.states(S0, nseq, 1),
+                         flat_area(seqptr, 4 * ((int64_t)nseq + 1))}));
     const hipStream_t st = as_stream(stream);
     const int grp = s->heads / s->kv_heads;
     const Rows q{Q, s->ldq, s->d, 1}, k{K, s->ldk, s->d, grp}, v{V, s->ldv, s->dv, grp};
@@ -411,12 +418,16 @@ nsd_status nsd_attn_decay_vjp(int32_t ntok, int32_t nseq, const int32_t *seqptr,
     NSD_TRY(check_sizes(ntok, nseq, max_len, s));
     NSD_REQUIRE(nseq == 0 || (seqptr && decay && (ntok == 0 || (Q && K && V && dO && dQ && dK && dV))),
                 "a NULL array");
-    NSD_REQUIRE(dS0 == nullptr || (dS0 != dS1 && dS0 != S0), "dS0 shares memory with what is read");
     const DecayWs w(ws, ntok, nseq, max_len, s, true);
     if (ws == nullptr || ws_bytes < w.bytes)
         return fail(NSD_ERR_WORKSPACE, "workspace %zu bytes at %p, need %zu", ws_bytes, ws, w.bytes);
     NSD_REQUIRE((reinterpret_cast<uintptr_t>(ws) & 255) == 0, "workspace is not 256-byte aligned");
-    if (nseq > 0 && ntok > 0) NSD_TRY(check_apart({dQ, dK, dV}, {Q, K, V, dO}));
+    const Areas of{nseq > 0 ? ntok : 0, s};
+    NSD_TRY(check_apart({of.q(dQ), of.k(dK), of.v(dV), of.decay(ddecay), of.states(dS0, nseq),
+                         flat_area(ws, w.bytes)},
+                        {of.q(Q), of.k(K), of.v(V), of.o(dO), of.decay(nseq > 0 ? decay : nullptr),
+                         of.states(S0, nseq), of.states(dS1, nseq),
+                         flat_area(nseq > 0 ? seqptr : nullptr, 4 * ((int64_t)nseq + 1))}));
     const hipStream_t st = as_stream(stream);
     const int grp = s->heads / s->kv_heads;
     if (nseq > 0) {
@@ -507,7 +518,9 @@ nsd_status nsd_attn_decay_step(int32_t nrows, const int32_t *slot, int32_t nslot
     if (nrows == 0) return NSD_OK;
     NSD_REQUIRE(Q && K && V && decay && O && (state || nslots == 0), "a NULL array");
     NSD_REQUIRE(slot || nrows <= nslots, "%d rows over %d states", nrows, nslots);
-    NSD_TRY(check_apart({O}, {Q, K, V}));
+    const Areas of{nrows, s};
+    NSD_TRY(check_apart({of.o(O), of.states(state, nslots)},
+                        {of.q(Q), of.k(K), of.v(V), of.decay(decay), flat_area(slot, 4 * (int64_t)nrows)}));
     Step a{nrows, nslots, s->heads, s->heads / s->kv_heads, s->d, s->dv, 0, s->scale, slot, Q, K, V,
            s->ldq, s->ldk, s->ldv, s->ldo, decay, state, O};
     const bool four = s->dv % 4 == 0;

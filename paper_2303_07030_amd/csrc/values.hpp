@@ -2,8 +2,10 @@
 // 32 bits in registers.
 #pragma once
 
+#include <initializer_list>
 #include <type_traits>
 
+#include "aliasing.hpp"
 #include "nsd_internal.hpp"
 
 namespace nsd {
@@ -106,5 +108,23 @@ struct Piece {
 
 inline bool known_dtype(int32_t t) { return t == NSD_F32 || t == NSD_BF16; }
 inline size_t dtype_bytes(int32_t t) { return t == NSD_F32 ? 4 : 2; }
+
+// Rows of values of a call's type.
+inline Area row_area(const void *p, int64_t rows, int64_t width, int64_t ld, int32_t dtype, int same = 0) {
+    const int64_t b = (int64_t)dtype_bytes(dtype);
+    return Area{p, rows, width * b, ld * b, same};
+}
+
+// What a call writes is apart from what it reads and from what else it writes.
+inline nsd_status check_apart(std::initializer_list<Area> written, std::initializer_list<Area> read) {
+    for (const Area *w = written.begin(); w != written.end(); ++w) {
+        for (const Area &r : read)
+            NSD_REQUIRE((w->same && w->same == r.same && w->p == r.p && w->ld == r.ld) || !areas_meet(*w, r),
+                        "what is written shares memory with what is read");
+        for (const Area *o = written.begin(); o != w; ++o)
+            NSD_REQUIRE(!areas_meet(*w, *o), "what is written shares memory");
+    }
+    return NSD_OK;
+}
 
 }  // namespace nsd

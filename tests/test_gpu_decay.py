@@ -139,6 +139,48 @@ def test_tensors_of_other_shapes_are_refused():
         nsd.decay_desc(4, 2, 8, 6, q, k, v, o.bfloat16(), 1.0)
 
 
+@pytest.mark.parametrize("call, change", [
+    ("forward", dict(O=("Q", 4))), ("forward", dict(O=("Q", 9 * 32 * 4))),
+    ("forward", dict(O=("V", -24 * 4))), ("forward", dict(O=("decay", 0))),
+    ("forward", dict(O=("S0", 1535))), ("forward", dict(O=("seqptr", 8))),
+    ("forward", dict(O=("ws", 100))), ("forward", dict(S1=("S0", 4))),
+    ("forward", dict(S1=("Q", 0))), ("forward", dict(S1=("O", -8))),
+    ("forward", dict(S1=("decay", 0))), ("forward", dict(S1=("ws", 0))),
+    ("backward", dict(dQ=("Q", 4))), ("backward", dict(dQ=("K", -32 * 4))),
+    ("backward", dict(dK=("dV", 8))), ("backward", dict(dV=("dO", 16))),
+    ("backward", dict(dQ=("dS1", 0))), ("backward", dict(ddecay=("decay", 0))),
+    ("backward", dict(ddecay=("Q", 64))), ("backward", dict(ddecay=("dK", 64))),
+    ("backward", dict(dS0=("S0", 768))), ("backward", dict(dS0=("dS1", 0))),
+    ("backward", dict(dS0=("dO", 4))), ("backward", dict(dS0=("seqptr", 0))),
+    ("backward", dict(dK=("ws", 0))),
+    ("step", dict(O=("Q", 4))), ("step", dict(O=("state", 9 * 768 - 4))),
+    ("step", dict(O=("slot", 0))), ("step", dict(state=("K", 4))),
+    ("step", dict(state=("decay", 0))), ("step", dict(state=("slot", 4)))])
+def test_what_is_written_is_apart(call, change):
+    """At any offset, whatever it is: 10 rows of 128 bytes (Q), 64, 48 and 96, states of 768."""
+    s = desc()
+    hold = torch.empty((1 << 16) + 256, dtype=torch.uint8)
+    ws = hold[-hold.data_ptr() % 256:]
+    names = "seqptr Q K V decay S0 O S1 dO dS1 dQ dK dV ddecay dS0 slot state".split()
+    at = {name: (i + 1) << 24 for i, name in enumerate(names)}
+    at["ws"] = ws.data_ptr()
+    for name, (other, offset) in change.items():
+        at[name] = at[other] + offset
+    p = at.get
+    with pytest.raises(nsd.NsdError, match="shares memory") as e:
+        if call == "forward":
+            nsd.nsd_attn_decay(10, 2, p("seqptr"), 10, s, p("Q"), p("K"), p("V"), p("decay"),
+                               p("S0"), p("O"), p("S1"), ws)
+        elif call == "backward":
+            nsd.nsd_attn_decay_vjp(10, 2, p("seqptr"), 10, s, p("Q"), p("K"), p("V"), p("decay"),
+                                   p("S0"), p("dO"), p("dS1"), p("dQ"), p("dK"), p("dV"),
+                                   p("ddecay"), p("dS0"), ws)
+        else:
+            nsd.nsd_attn_decay_step(10, p("slot"), 9, s, p("Q"), p("K"), p("V"), p("decay"),
+                                    p("state"), p("O"))
+    assert e.value.status == nsd.NSD_ERR_INVALID_ARG
+
+
 # ------------------------------------------------- the definition in 64 bits
 
 def definition(x, lens, scale, magnitude=False):
@@ -508,6 +550,39 @@ def test_scores_and_states_keep_32_bits(d, dv, Hk, dtype):
     run(dict(do=one), "dq", 1, s0=(by_value, False))
     run(dict(v=one), "dk", 0, ds1=(by_value, False))
     run(dict(k=one), "dv", 0, ds1=(by_key, True))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_between_each_others(dtype):
+    """What is read and what is written as columns of one matrix: the same bits."""
+    H, Hk, d, dv = 4, 2, 24, 40
+    c = Case([70, 33], H, Hk, d, dv, dtype)
+    want_s1, want = c.forward(), c.backward()
+    kept = {i: t.clone() for i, t in c.out.items()}
+    widths = dict(q=H * d, k=Hk * d, v=Hk * dv, do=H * dv, dq=H * d, dk=Hk * d, dv=Hk * dv,
+                  o=H * dv)
+    one = torch.zeros(c.n, sum(widths.values()) + 5, dtype=T[dtype], device="cuda")
+    col = 3
+    for name, w in widths.items():
+        part = one[:, col:col + w]
+        col += w
+        if name in c.t:
+            part.copy_(c.t[name])
+            c.t[name] = part
+        else:
+            c.out[name] = part
+    c.desc = nsd.decay_desc(H, Hk, d, dv, c.t["q"], c.t["k"], c.t["v"], c.out["o"], c.scale)
+    s1, grads = c.forward(), c.backward()
+    assert all(torch.equal(a, b) for a, b in zip((s1, *grads), (want_s1, *want)))
+    assert all(torch.equal(t[:103], kept[i][:103]) for i, t in c.out.items())
+    state, again = c.s0.clone(), c.s0.clone()
+    nsd.nsd_attn_decay_step(2, None, 2, c.desc, c.t["q"], c.t["k"], c.t["v"], c.g, state, c.out["o"])
+    rows = {i: c.t[i].contiguous() for i in "qkv"}
+    o = torch.empty(2, H * dv, dtype=T[dtype], device="cuda")
+    s = nsd.decay_desc(H, Hk, d, dv, rows["q"], rows["k"], rows["v"], o, c.scale)
+    nsd.nsd_attn_decay_step(2, None, 2, s, rows["q"], rows["k"], rows["v"], c.g, again, o)
+    assert torch.equal(state, again) and torch.equal(c.out["o"][:2], o)
 
 
 @pytest.mark.gpu
