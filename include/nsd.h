@@ -1095,6 +1095,8 @@ nsd_status nsd_embed_vjp(int32_t ntok, const nsd_embedding *s, const int32_t *id
  *                    caches as they are.  Slots of one call are distinct: of two
  *                    tokens with one slot, either's values may be found there.
  *                    vwidth = 0: no values.
+ * Nothing else that is written shares memory with what is read or written beside it
+ * (rows between each other's, as of one projection, do not).
  * Async.
  */
 typedef struct nsd_qk {

@@ -510,6 +510,17 @@ nsd_status check_heads(const nsd_qk *s, const void *Q, const void *K, const int3
     return NSD_OK;
 }
 
+// A call's arrays; of queries (1) and keys (2) those that a call may take in place have one number.
+struct Areas {
+    int64_t n;  // tokens
+    const nsd_qk *s;
+    Area q(const void *p, int64_t ld) const { return row_area(p, n, (int64_t)s->heads * s->d, ld, s->dtype, 1); }
+    Area k(const void *p, int64_t ld) const { return row_area(p, n, (int64_t)s->kv_heads * s->d, ld, s->dtype, 2); }
+    Area weights(const float *p) const { return flat_area(s->norm ? p : nullptr, 4 * (int64_t)s->d); }
+    Area pos(const int32_t *p) const { return flat_area(s->rot ? p : nullptr, 4 * n); }
+    Area freq(const double *p) const { return flat_area(p, 4 * (int64_t)s->rot); }
+};
+
 }  // namespace
 
 }  // namespace nsd
@@ -527,6 +538,10 @@ nsd_status nsd_qk_rotate(int32_t ntok, const nsd_qk *s, const void *Q, const voi
     NSD_REQUIRE((Qo || s->heads == 0) && (Ko || s->kv_heads == 0), "Qo or Ko is NULL");
     NSD_REQUIRE((Qo != Q || s->ldqo == s->ldq) && (Ko != K || s->ldko == s->ldk || s->kv_heads == 0),
                 "in place with another row distance");
+    const Areas of{ntok, s};
+    NSD_TRY(check_apart({of.q(Qo, s->ldqo), of.k(Ko, s->ldko)},
+                        {of.q(Q, s->ldq), of.k(K, s->ldk), of.weights(wq), of.weights(wk), of.pos(pos),
+                         of.freq(freq)}));
     QkArgs a = qk_args(ntok, s, Q, K, wq, wk, pos, freq);
     a.Qo = Qo;
     a.Ko = Ko;
@@ -567,8 +582,8 @@ nsd_status nsd_qk_rotate_vjp(int32_t ntok, const nsd_qk *s, const void *Q, const
     a.Ko = const_cast<void *>(dKo);
     a.dQ = dQ;
     a.dK = dK;
+    size_t need = 0;
     if (weights) {
-        size_t need;
         NSD_TRY(nsd_qk_rotate_vjp_workspace_size(ntok, s, &need));
         if (ws == nullptr || ws_bytes < need)
             return fail(NSD_ERR_WORKSPACE, "workspace %zu bytes at %p, need %zu", ws_bytes, ws, need);
@@ -576,6 +591,12 @@ nsd_status nsd_qk_rotate_vjp(int32_t ntok, const nsd_qk *s, const void *Q, const
                     "workspace is not 256-byte aligned");
         a.part = static_cast<float *>(ws);
     }
+    const Areas of{any ? ntok : 0, s};
+    NSD_TRY(check_apart({of.q(dQ, s->ldq), of.k(dK, s->ldk), of.weights(dwq), of.weights(dwk),
+                         flat_area(a.part, (int64_t)need)},
+                        {of.q(Q, s->ldq), of.k(K, s->ldk), of.q(dQo, s->ldqo), of.k(dKo, s->ldko),
+                         of.weights(any ? wq : nullptr), of.weights(any ? wk : nullptr), of.pos(pos),
+                         of.freq(any ? freq : nullptr)}));
     int64_t blocks = 0;
     if (any) {
         a.parts = head_parts(ntok, s, std::max(s->heads, s->kv_heads));
@@ -607,6 +628,15 @@ nsd_status nsd_qk_append(int32_t ntok, const nsd_qk *s, const void *Q, const voi
     NSD_REQUIRE(vwidth == 0 || (V && (Vc || nslots == 0)), "V or Vc is NULL");
     NSD_REQUIRE((Kc != K || s->kv_heads == 0) && (Vc != V || vwidth == 0), "a cache is what is appended");
     NSD_REQUIRE(Qo != Q || s->ldqo == s->ldq || s->heads == 0, "in place with another row distance");
+    const Areas of{ntok, s};
+    // (a key that lies in the cache would be overwritten by another token's before it is read)
+    Area kc = of.k(Kc, s->ldko);
+    kc.rows = nslots;
+    kc.same = 0;
+    NSD_TRY(check_apart({of.q(Qo, s->ldqo), kc, row_area(Vc, nslots, vwidth, ldvo, s->dtype)},
+                        {of.q(Q, s->ldq), of.k(K, s->ldk), row_area(V, ntok, vwidth, ldv, s->dtype),
+                         of.weights(wq), of.weights(wk), of.pos(pos), of.freq(freq),
+                         flat_area(slot, 4 * (int64_t)ntok)}));
     QkArgs a = qk_args(ntok, s, Q, K, wq, wk, pos, freq);
     a.Qo = Qo;
     a.Ko = Kc;

@@ -76,6 +76,41 @@ def test_bad_arguments_are_refused():
     nsd.nsd_qk_rotate(0, s, None, None, None, None, None, None, None, None)
 
 
+@pytest.mark.parametrize("call, change", [
+    ("rotate", dict(Qo=("Q", 4))), ("rotate", dict(Qo=("K", 0))), ("rotate", dict(Ko=("Q", 0))),
+    ("rotate", dict(Qo=("K", 0), Ko=("Q", 0))), ("rotate", dict(Ko=("Qo", 3 * 128 + 8))),
+    ("rotate", dict(Ko=("K", -4))), ("rotate", dict(Qo=("wq", 0))), ("rotate", dict(Ko=("pos", 12))),
+    ("rotate", dict(Qo=("freq", 24))),
+    ("vjp", dict(dQ=("dQo", 4))), ("vjp", dict(dQ=("dKo", 0))), ("vjp", dict(dK=("K", 60))),
+    ("vjp", dict(dK=("dQ", 0))), ("vjp", dict(dwq=("wq", 0))), ("vjp", dict(dwq=("dwk", 4))),
+    ("vjp", dict(dwk=("dK", 0))), ("vjp", dict(dQ=("ws", 0))),
+    ("append", dict(Qo=("Q", 4))), ("append", dict(Kc=("K", -128))),
+    ("append", dict(Kc=("V", 0))), ("append", dict(Vc=("V", 4))), ("append", dict(Vc=("Kc", 0))),
+    ("append", dict(Vc=("Q", 0))), ("append", dict(Kc=("slot", 0))), ("append", dict(Qo=("Kc", 8)))])
+def test_what_is_written_is_apart(call, change):
+    """At any offset: 4 rows of 128 bytes (Q) and 64 (K), 9 slots."""
+    s = desc()
+    hold = torch.empty((1 << 20), dtype=torch.uint8)
+    ws = hold[-hold.data_ptr() % 256:]
+    names = ("Q K V wq wk pos freq Qo Ko dQo dKo dQ dK dwq dwk slot Kc Vc").split()
+    at = {name: (i + 1) << 24 for i, name in enumerate(names)}
+    at["ws"] = ws.data_ptr()
+    for name, (other, offset) in change.items():
+        at[name] = (names.index(other) + 1 << 24 if other != "ws" else at["ws"]) + offset
+    small = [at[i] for i in ("wq", "wk", "pos", "freq")]
+    with pytest.raises(nsd.NsdError, match="shares memory") as e:
+        if call == "rotate":
+            nsd.nsd_qk_rotate(4, s, at["Q"], at["K"], *small, at["Qo"], at["Ko"])
+        elif call == "vjp":
+            nsd.nsd_qk_rotate_vjp(4, s, at["Q"], at["K"], *small, at["dQo"], at["dKo"], at["dQ"],
+                                  at["dK"], at["dwq"], at["dwk"], ws)
+        else:  # (values by address: the binding takes their widths from tensors)
+            nsd._check(nsd._lib.nsd_qk_append(4, s, at["Q"], at["K"], at["V"], 6, 6, 8, *small,
+                                              at["slot"], 9, at["Qo"], at["Kc"], at["Vc"], None),
+                       "nsd_qk_append")
+    assert e.value.status == nsd.NSD_ERR_INVALID_ARG
+
+
 def test_tensors_of_other_shapes_are_refused():
     q, k = torch.zeros(4, 32), torch.zeros(4, 16)
     s = nsd.qk_desc(4, 2, 8, q, k, q, k)
@@ -286,6 +321,31 @@ def test_in_place(d):
     gw = torch.empty(2, d, device="cuda")
     nsd.nsd_qk_rotate_vjp(37, s, t["q"], t["k"], *small, dq, dk, dq, dk, gw[0], gw[1], ws)
     assert torch.equal(dq, t["dq"]) and torch.equal(dk, t["dk"])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_columns_of_one_projection(dtype):
+    """Queries and keys in place beside each other in one matrix, and their gradients over the
+    rows themselves or over the upstream: the bits of calls on arrays of their own."""
+    n, H, Hk, d = 21, 4, 2, 24
+    t, s, small = compare(n, H, Hk, d, d, dtype, False)
+    one = torch.cat([t["q"], t["k"], t["k"]], 1)
+    q, k = one[:, :H * d], one[:, H * d:(H + Hk) * d]
+    s = nsd.qk_desc(H, Hk, d, q, k, q, k, d)
+    nsd.nsd_qk_rotate(n, s, q, k, *small, q, k)
+    assert torch.equal(q, t["qo"]) and torch.equal(k, t["ko"])
+    assert torch.equal(one[:, (H + Hk) * d:], t["k"])
+    ws = torch.empty(nsd.nsd_qk_rotate_vjp_workspace_size(n, s), dtype=torch.uint8, device="cuda")
+    gw = torch.empty(2, d, device="cuda")
+    for over in (False, True):
+        rows = torch.cat([t["q"], t["k"]], 1)
+        up = torch.cat([t["dqo"], t["dko"]], 1)
+        x, y = [r.split([H * d, Hk * d], 1) for r in (rows, up)]
+        to = x if over else y
+        s = nsd.qk_desc(H, Hk, d, *x, *y, d)
+        nsd.nsd_qk_rotate_vjp(n, s, *x, *small, *y, *to, gw[0], gw[1], ws)
+        assert torch.equal(to[0], t["dq"]) and torch.equal(to[1], t["dk"])
 
 
 @pytest.mark.gpu
