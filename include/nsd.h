@@ -1052,6 +1052,7 @@ nsd_status nsd_grad_clip(const nsd_grad_plan *plan, const float *scale, void *st
  *                a token; 1: the sums are added to dW, and the other words' rows
  *                are not touched (a head that shares the table wrote its gradient
  *                there).
+ * What is written shares no memory with what is read.
  * Async.
  */
 typedef struct nsd_embedding {

@@ -478,6 +478,8 @@ nsd_status nsd_embed(int32_t ntok, const nsd_embedding *s, const int32_t *ids, c
     NSD_TRY(check_embedding(ntok, s));
     if (ntok == 0) return NSD_OK;
     NSD_REQUIRE(ids && out && (W || s->vocab == 0), "a NULL array");
+    NSD_TRY(check_apart({row_area(out, ntok, s->width, s->ldo, s->otype)},
+                        {row_area(W, s->vocab, s->width, s->ldw, s->wtype), flat_area(ids, 4 * (int64_t)ntok)}));
     const int values = values_per_lane(s->wtype, s->otype), lanes = row_lanes(s->width, values);
     const int tiles = (int)ceil_div(s->width, kWave * values);
     const int64_t units = ceil_div(ntok, kWave / lanes) * tiles;
@@ -509,6 +511,8 @@ nsd_status nsd_embed_vjp(int32_t ntok, const nsd_embedding *s, const int32_t *id
     if (ws == nullptr || ws_bytes < w.bytes)
         return fail(NSD_ERR_WORKSPACE, "workspace %zu bytes at %p, need %zu", ws_bytes, ws, w.bytes);
     NSD_REQUIRE((reinterpret_cast<uintptr_t>(ws) & 255) == 0, "workspace is not 256-byte aligned");
+    NSD_TRY(check_apart({row_area(dW, s->vocab, s->width, s->ldw, s->gtype), flat_area(ws, (int64_t)w.bytes)},
+                        {row_area(dout, ntok, s->width, s->ldo, s->otype), flat_area(ids, 4 * (int64_t)ntok)}));
     const int values = values_per_lane(s->otype, s->gtype);
     EmbedSum a;
     a.tiles = (int)ceil_div(s->width, kWave * values);

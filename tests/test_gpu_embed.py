@@ -56,6 +56,27 @@ def test_bad_arguments_are_refused():
     nsd.nsd_embed_vjp(0, s, None, None, True, None, None)
 
 
+@pytest.mark.parametrize("change", [
+    dict(out=("W", 0)), dict(out=("W", 4)), dict(out=("W", -100)), dict(out=("ids", 0)),
+    dict(dW=("dout", 0)), dict(dW=("dout", 8)), dict(dW=("ids", 12)), dict(dW=("ws", 0)),
+    dict(dout=("ws", 512)), dict(ids=("ws", 0))])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_what_is_written_is_apart(change, accumulate):
+    s = desc()
+    hold = torch.empty((1 << 16) + 256, dtype=torch.uint8)
+    at = dict(W=1 << 24, out=2 << 24, ids=3 << 24, dout=4 << 24, dW=5 << 24)
+    ws = hold[-hold.data_ptr() % 256:]
+    at["ws"] = ws.data_ptr()
+    for name, (other, offset) in change.items():
+        at[name] = at[other] + offset
+    with pytest.raises(nsd.NsdError, match="shares memory") as e:
+        if "out" in change:
+            nsd.nsd_embed(4, s, at["ids"], at["W"], at["out"])
+        else:
+            nsd.nsd_embed_vjp(4, s, at["ids"], at["dout"], accumulate, at["dW"], ws)
+    assert e.value.status == nsd.NSD_ERR_INVALID_ARG
+
+
 def test_tensors_of_other_shapes_are_refused():
     W, out = torch.zeros(10, 8), torch.zeros(4, 8)
     s = nsd.embed_desc(W, out)
