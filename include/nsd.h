@@ -1005,7 +1005,8 @@ nsd_status nsd_adamw_step(const nsd_adamw_plan *plan, const nsd_adamw *h, void *
  * nsd_grad_plan_build  writes the table from host records, whose addresses stay
  *                      in it.  Synchronous.
  * nsd_grad_norm        norm (fp64, one value) and scale (fp32, one value), and,
- *                      when norms is not NULL, norms [ntensors] (fp64).  Async.
+ *                      when norms is not NULL, norms [ntensors] (fp64).  They share
+ *                      no memory with each other or with *grad_scale.  Async.
  * nsd_grad_clip        every gradient times *scale, rounded to its type; nothing
  *                      is written where *scale is 1.  Refused for a plan whose
  *                      tensors share memory.  Async.

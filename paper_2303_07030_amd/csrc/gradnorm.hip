@@ -300,6 +300,11 @@ nsd_status nsd_grad_norm(const nsd_grad_plan *plan, const nsd_clip *h, double *n
     if (ws == nullptr || ws_bytes < need)
         return fail(NSD_ERR_WORKSPACE, "workspace %zu bytes at %p, need %zu", ws_bytes, ws, need);
     NSD_REQUIRE((reinterpret_cast<uintptr_t>(ws) & 255) == 0, "workspace is not 256-byte aligned");
+    // (one block writes the factor while others still read what it is made of)
+    NSD_TRY(check_apart({flat_area(norm, 8), flat_area(scale, 4), flat_area(norms, 8 * (int64_t)plan->ntensors),
+                         flat_area(ws, (int64_t)need)},
+                        {flat_area(h->grad_scale, 4),
+                         flat_area(plan->table, (int64_t)grad_table_bytes(plan->ntensors, plan->nchunks))}));
     Carver c(ws);
     double *part = c.take<double>(plan->nchunks);
     const hipStream_t st = as_stream(stream);

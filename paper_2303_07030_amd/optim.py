@@ -54,8 +54,8 @@ class GradNorm:
                               device=dev)
 
     def measure(self, grad_scale=None, stream=None):
-        """The norms of grad_scale (a device fp32 scalar, or None) times the gradients;
-        `scale` holds grad_scale as a factor."""
+        """The norms of grad_scale (a device fp32 scalar but `scale` itself, or None)
+        times the gradients; `scale` holds grad_scale as a factor."""
         if grad_scale is not None:
             _flat(grad_scale, "grad_scale", self.scale.device, 1, (torch.float32,))
         h = nsd.nsd_clip(self.max_norm, 2 if self.order == 2 else 0,

@@ -56,6 +56,24 @@ def test_bad_calls_are_refused():
         nsd.nsd_grad_clip(plan, torch.zeros(1, dtype=torch.float64))
 
 
+@pytest.mark.parametrize("change", [
+    dict(grad_scale=("scale", 0)), dict(grad_scale=("norm", 4)), dict(grad_scale=("norms", 12)),
+    dict(grad_scale=("ws", 8)), dict(scale=("norm", 0)), dict(norm=("norms", 8)),
+    dict(scale=("ws", 64)), dict(norms=("ws", 0)), dict(norms=("table", 0))])
+def test_what_is_written_is_apart(change):
+    hold = torch.empty((1 << 12) + 256, dtype=torch.uint8)
+    at = {n: (i + 1) << 24 for i, n in enumerate(("norm", "scale", "norms", "grad_scale", "table"))}
+    ws = hold[-hold.data_ptr() % 256:]
+    at["ws"] = ws.data_ptr()
+    for name, (other, offset) in change.items():
+        at[name] = at[other] + offset
+    plan = nsd.nsd_grad_plan(2, 40, 0, at["table"])
+    with pytest.raises(nsd.NsdError, match="shares memory") as e:
+        nsd.nsd_grad_norm(plan, nsd.nsd_clip(1.0, 2, at["grad_scale"]), at["norm"], at["scale"],
+                          at["norms"], ws)
+    assert e.value.status == nsd.NSD_ERR_INVALID_ARG
+
+
 def test_bad_orders_are_refused():
     from paper_2303_07030_amd import optim
     with pytest.raises(ValueError, match="order"):
@@ -167,6 +185,26 @@ def test_empty_lists_and_zero_gradients():
         p.clip()
         assert p.norm.item() == 0.0 and p.scale.item() == 1.0
         assert p.norms.tolist() == [0.0] * len(grads)
+
+
+@pytest.mark.gpu
+def test_a_measures_own_factor_is_not_its_input():
+    """Refused, and nothing changes; another measure's factor is an input like any."""
+    from paper_2303_07030_amd import optim
+    g = torch.full((100,), 2.0, device="cuda")
+    p, other = optim.GradNorm([g], 1.0), optim.GradNorm([g], 5.0)
+    p.measure()
+    old = p.norm.item(), p.scale.item()
+    with pytest.raises(nsd.NsdError, match="shares memory"):
+        p.measure(grad_scale=p.scale)
+    assert (p.norm.item(), p.scale.item()) == old
+    other.measure(grad_scale=p.scale)
+    assert math.isclose(other.norm.item(), 20.0 * old[1], rel_tol=1e-12)
+    w = torch.ones(100, device="cuda")
+    opt = optim.AdamW([w], [g], max_norm=1.0)
+    with pytest.raises(nsd.NsdError, match="shares memory"):
+        opt.step(grad_scale=opt.grad_norm.scale)
+    assert opt.t == 0 and torch.all(w == 1.0)
 
 
 @pytest.mark.gpu
