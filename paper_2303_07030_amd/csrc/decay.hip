@@ -161,7 +161,11 @@ __global__ __launch_bounds__(kStepThreads) void decay_step_kernel(Step a) {
         return;
     }
     float *const S = a.state + ((int64_t)slot * a.H + h) * a.d * a.dv + c;
-    const float w = a.decay[h] == 0.f ? 1.f : (float)exp((double)a.decay[h]);
+    // A slow decay by what it takes away: e^g rounded near 1 would be another decay, the same way
+    // off at every token (g = -1e-6: by 1.3%).
+    const double g = (double)a.decay[h];
+    const bool slow = g != 0.0 && g > -0.6931;  // e^g above 1/2
+    const float w = g == 0.0 ? 1.f : (float)(slow ? expm1(g) : exp(g));
     const bool several = a.slot && a.nrows > 1;
     for (;;) {
         if (threadIdx.x == 0) before = after = INT_MAX;
@@ -201,7 +205,7 @@ __global__ __launch_bounds__(kStepThreads) void decay_step_kernel(Step a) {
                 if (k >= a.d) break;
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
-                    x[u][e] = __builtin_fmaf(ks[k], v[e], w * x[u][e]);
+                    x[u][e] = __builtin_fmaf(ks[k], v[e], __builtin_fmaf(x[u][e], w, slow ? x[u][e] : 0.f));
                     o[e] = __builtin_fmaf(qs[k], x[u][e], o[e]);
                 }
                 __builtin_memcpy(S + (int64_t)k * a.dv, x[u], sizeof x[u]);

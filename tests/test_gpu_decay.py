@@ -669,6 +669,51 @@ def test_rows_that_share_a_slot_are_its_tokens(dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("g", [0.0, -1e-7, -16.5 * 2.0 ** -24, -1e-6, -1e-5, -1e-3, -0.3, -0.69,
+                               -0.7, -5.0])
+def test_a_single_token_takes_the_decay_itself(g):
+    """A state without a new token's part is x + x (e^g - 1), one rounding and that of e^g - 1 (below
+    1/2: x e^g, and that of e^g)."""
+    d = dv = 64
+    s = torch.randn(1, 1, d, dv, generator=torch.Generator().manual_seed(3)).cuda()
+    old = s.double().cpu().numpy()
+    k, q, v = torch.zeros(1, d).cuda(), torch.ones(1, d).cuda(), torch.ones(1, dv).cuda()
+    o = torch.empty(1, dv, device="cuda")
+    decay = torch.full((1,), g, device="cuda")
+    nsd.nsd_attn_decay_step(1, None, 1, nsd.decay_desc(1, 1, d, dv, q, k, v, o, 1.0), q, k, v, decay,
+                            s, o)
+    e = float(decay.item())
+    want = old * math.exp(e)
+    less = min(math.exp(e), 1 - math.exp(e))
+    half_step = np.spacing(np.abs(want).astype(np.float32)).astype(np.float64) / 2
+    got = s.double().cpu().numpy()
+    assert np.all(np.abs(got - want) <= half_step + 2 * U * less * np.abs(old))
+
+
+@pytest.mark.gpu
+def test_slow_decays_do_not_drift():
+    """4,096 tokens one after the other on one state, e^g half a step from a number of 32 bits:
+    rounded to one of them the state would be off by half a step (2^-25) a token, all of it the same
+    way.  Roundings of the state itself go either way: an eighth of 2^-24 a token is left to them
+    (independent, they come to sqrt(2 4096) 2^-24 a value, and 1/64 of that along a state of 64 by
+    64)."""
+    n, d, g = 4096, 64, -16.5 * 2.0 ** -24
+    gen = torch.Generator().manual_seed(4)
+    s = (torch.rand(1, 1, d, d, generator=gen) + 0.5).cuda()
+    k, q, v = (torch.randn(n, d, generator=gen).cuda() * 2.0 ** -5 for _ in range(3))
+    o = torch.empty(n, d, device="cuda")
+    want = s[0, 0].double().cpu().numpy()
+    for kk, vv in zip(k.double().cpu().numpy(), v.double().cpu().numpy()):
+        want = math.exp(g) * want + np.outer(kk, vv)
+    slot = torch.zeros(n, dtype=torch.int32, device="cuda")
+    decay = torch.full((1,), g, device="cuda")
+    nsd.nsd_attn_decay_step(n, slot, 1, nsd.decay_desc(1, 1, d, d, q, k, v, o, 1.0), q, k, v,
+                            decay, s, o)
+    err = s[0, 0].double().cpu().numpy() - want
+    assert abs((err * want).sum()) <= n * U / 8 * (want * want).sum()
+
+
+@pytest.mark.gpu
 def test_steps_go_on_where_a_prompt_ends():
     """A prompt by chunks, then tokens one by one, against one call over all."""
     H, Hk, d, dv, n = 4, 2, 32, 48, 150
