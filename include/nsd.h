@@ -1155,7 +1155,9 @@ nsd_status nsd_qk_append(int32_t ntok, const nsd_qk *s, const void *Q, const voi
  *                      dO (ldo) and dS1 [nseq] or NULL (zero).  Nothing that is
  *                      written shares memory with what is read.  Gradients of a key
  *                      head add up its query heads'.
- * nsd_attn_decay_workspace_size  bytes for either call with these sizes.
+ * nsd_attn_decay_workspace_size  bytes for the call (gradient = 1: for either) with
+ *                      these sizes, and with smaller ones: fewer tokens or sequences, a
+ *                      shorter max_len.
  * nsd_attn_decay_step  one token for each row, its state in slot[r] of `state`
  *                      [nslots] (slot NULL: in r), updated in place.  Rows that name
  *                      one slot are tokens of it in the rows' order.  O and the states

@@ -265,6 +265,19 @@ int segment_tokens(int32_t ntok, int32_t max_len, const nsd_decay *s) {
     return max_len <= len ? INT_MAX : len;
 }
 
+// The most segments that a batch of up to `ntok` tokens is cut into, less one for each sequence; -1
+// if none is cut.  (Fewer tokens may have more segments, as theirs are shorter.)
+int64_t most_segments(int32_t ntok, int32_t max_len, const nsd_decay *s) {
+    const int64_t enough = ceil_div(kEnough, ceil_div(std::max(s->d, s->dv), 128) * s->heads);
+    int64_t most = -1;
+    for (int64_t len = kShortest; len <= kLongest && len < max_len; len *= 2) {
+        // the most tokens whose segments are of this length
+        const int64_t n = len == kLongest ? ntok : std::min<int64_t>(ntok, 2 * len * enough - 1);
+        if (len == kShortest || n / len >= enough) most = std::max(most, n / len);
+    }
+    return most;
+}
+
 nsd_status check_sizes(int32_t ntok, int32_t nseq, int32_t max_len, const nsd_decay *s) {
     NSD_TRY(check_decay(s));
     NSD_REQUIRE(ntok >= 0 && nseq >= 0 && max_len >= 0, "a negative size");
@@ -277,16 +290,19 @@ nsd_status check_sizes(int32_t ntok, int32_t nseq, int32_t max_len, const nsd_de
     return NSD_OK;
 }
 
+// The workspace of a call; `room`: of any that is no larger (of the same heads).
 struct DecayWs {
     float *forth, *back, *dk, *dv, *sums;
     int32_t seg_len, nseg, nvb;
     size_t bytes;
-    DecayWs(void *ws, int32_t ntok, int32_t nseq, int32_t max_len, const nsd_decay *s, bool gradient) {
+    DecayWs(void *ws, int32_t ntok, int32_t nseq, int32_t max_len, const nsd_decay *s, bool gradient,
+            bool room = false) {
         Carver c(ws);
         seg_len = segment_tokens(ntok, max_len, s);
         nseg = ntok / seg_len + nseq;
-        const bool cut = seg_len != INT_MAX;
-        const size_t states = cut ? (size_t)nseg * s->heads * s->d * s->dv : 0;
+        const int64_t cuts = room ? most_segments(ntok, max_len, s) : cut() ? ntok / seg_len : -1;
+        const int64_t segments = std::max<int64_t>(cuts, 0) + nseq;
+        const size_t states = cuts >= 0 ? (size_t)segments * s->heads * s->d * s->dv : 0;
         const bool grouped = s->heads != s->kv_heads;
         forth = c.take<float>(states);
         back = dk = dv = sums = nullptr;
@@ -296,7 +312,7 @@ struct DecayWs {
             back = c.take<float>(states);
             dk = c.take<float>(grouped ? (size_t)ntok * s->heads * s->d : 0);
             dv = c.take<float>(grouped ? (size_t)ntok * s->heads * s->dv : 0);
-            sums = c.take<float>((size_t)nseg * s->heads * nvb);
+            sums = c.take<float>((size_t)segments * s->heads * nvb);
         }
         bytes = std::max<size_t>(c.bytes(), 256);
     }
@@ -375,7 +391,7 @@ nsd_status nsd_attn_decay_workspace_size(int32_t ntok, int32_t nseq, int32_t max
                                          const nsd_decay *s, int32_t gradient, size_t *bytes) {
     NSD_REQUIRE(bytes != nullptr, "bytes is NULL");
     NSD_TRY(check_sizes(ntok, nseq, max_len, s));
-    *bytes = DecayWs(nullptr, ntok, nseq, max_len, s, gradient != 0).bytes;
+    *bytes = DecayWs(nullptr, ntok, nseq, max_len, s, gradient != 0, true).bytes;
     return NSD_OK;
 }
 

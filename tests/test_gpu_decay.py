@@ -116,6 +116,31 @@ def test_bad_arguments_are_refused():
     nsd.nsd_attn_decay_step(0, None, 0, s, None, None, None, None, None, None)
 
 
+@pytest.mark.parametrize("heads, d, dv", [(8, 128, 128), (16, 64, 128), (1, 16, 16), (6, 40, 72),
+                                          (3, 200, 33), (4096, 1, 1), (1024, 8, 8)])
+@pytest.mark.parametrize("gradient", [False, True])
+def test_a_workspace_serves_smaller_batches(heads, d, dv, gradient):
+    """Around the sizes at which the segments' length changes (a power of two tokens times 1,024
+    blocks over the heads' columns)."""
+    s = desc(heads=heads, kv_heads=1, d=d, dv=dv, ldq=heads * d, ldk=d, ldv=dv, ldo=heads * dv)
+
+    def size(ntok, nseq, max_len):
+        return nsd.nsd_attn_decay_workspace_size(ntok, nseq, max_len, s, gradient)
+
+    cols = heads * (2 if max(d, dv) > 128 else 1)
+    steps = {2 ** p * -(-1024 // cols) for p in range(6, 15)} | {2 ** p for p in range(5, 18)}
+    tokens = sorted({max(n + i, 0) for n in steps for i in (-1, 0, 1)} | {32_767, 65_535, 10 ** 6})
+    lens = sorted({n + i for n in (2 ** p for p in range(5, 15)) for i in (0, 1)} | {10 ** 6})
+    for max_len in lens:
+        sizes = [size(n, 3, max_len) for n in tokens]
+        assert sizes == sorted(sizes)
+    for n in tokens:
+        sizes = [size(n, 3, m) for m in lens]
+        assert sizes == sorted(sizes)
+        sizes = [size(n, b, 10 ** 6) for b in (0, 1, 2, 50, 1000)]
+        assert sizes == sorted(sizes)
+
+
 def test_tensors_of_other_shapes_are_refused():
     q, k, v, o = (torch.zeros(5, w) for w in (32, 16, 12, 24))
     s = nsd.decay_desc(4, 2, 8, 6, q, k, v, o, 1.0)
@@ -410,6 +435,29 @@ def test_ends_of_sequences_outside_the_rows_are_those_of_the_rows(d, dv, dtype):
     assert all(torch.equal(a, b) for a, b in zip(again, [s1, *grads]))
     assert all(torch.equal(want[i][:700], t) for i, t in c.out.items())
     assert all(torch.equal(want[i][700:], c.wide_out[i][700:, :want[i].shape[1]]) for i in want)
+
+
+@pytest.mark.gpu
+def test_shorter_batches_in_a_longer_ones_workspace():
+    """16,384 tokens of 8 heads are cut into half as many segments as 16,383: the same bits as in a
+    workspace of their own, and nothing written past what the size query said."""
+    c = Case([16_384], 8, 8, 16, 16, "bf16")
+    most = nsd.nsd_attn_decay_workspace_size(16_384, 1, 16_384, c.desc, True)
+    ws = torch.empty(most + 1024, dtype=torch.uint8, device="cuda")
+    for n in (16_384, 16_383, 8_191, 4_000, 65):
+        c.n, c.seqptr = n, torch.tensor([0, n], dtype=torch.int32, device="cuda")
+        outs = []
+        for own in (False, True):
+            dg, s1, ds0 = torch.empty(8, device="cuda"), *torch.empty_like(c.s0.expand(2, *c.s0.shape))
+            o, dq, dk, dv = (torch.zeros_like(c.out[i]) for i in ("o", "dq", "dk", "dv"))
+            ws.fill_(0x7F)
+            w = [c.ws(n, False), c.ws(n, True)] if own else [ws[:most]] * 2
+            args = (n, 1, c.seqptr, n, c.desc, c.t["q"], c.t["k"], c.t["v"], c.g, c.s0)
+            nsd.nsd_attn_decay(*args, o, s1, w[0])
+            nsd.nsd_attn_decay_vjp(*args, c.t["do"], c.ds1, dq, dk, dv, dg, ds0, w[1])
+            outs.append([o, dq, dk, dv, dg, s1, ds0])
+        assert all(torch.equal(a, b) for a, b in zip(*outs)), n
+        assert torch.all(ws[most:] == 0x7F)
 
 
 @pytest.mark.gpu
