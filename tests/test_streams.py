@@ -38,6 +38,29 @@ def owners(monkeypatch):
     return owner
 
 
+@pytest.mark.parametrize("raw", [True, False])
+def test_the_current_stream(monkeypatch, raw):
+    """A GPU that comes up after a first call is seen, and a torch without a function for the
+    handle alone serves as well."""
+    there = [False]
+    monkeypatch.setattr(nsd, "_has_gpu", False)
+    monkeypatch.setattr(torch.cuda, "is_available", lambda: there[0])
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: types.SimpleNamespace(cuda_stream=0x55))
+    monkeypatch.setattr(nsd, "_raw_stream", (lambda device: 0x40 + device) if raw else None)
+    assert nsd._stream(None) is None and nsd._stream(7) == 7
+    there[0] = True
+    assert nsd._stream(None) == (0x43 if raw else 0x55)
+
+
+@pytest.mark.gpu
+def test_the_current_stream_by_its_handle():
+    """Either way, on the default stream and on another."""
+    for s in (torch.cuda.default_stream(), torch.cuda.Stream()):
+        with torch.cuda.stream(s):
+            assert nsd._stream(None) == torch.cuda.current_stream().cuda_stream == s.cuda_stream
+
+
 @pytest.mark.parametrize("stream, owner", [(None, None), (0, ("external", 0)),
                                            (0x77, ("external", 0x77)), ("side", "side")])
 def test_staging_of_values_in_csc_order_belongs_to_the_call(owners, monkeypatch, stream, owner):
