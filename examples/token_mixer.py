@@ -28,8 +28,8 @@ from paper_2303_07030_amd import nsd, optim  # noqa: E402
 
 
 class TokenMixer:
-    """Weights, buffers and one step over batches of up to `tokens` tokens in `sequences`
-    sequences."""
+    """Weights, buffers and one step over batches of up to `tokens` tokens, all of them in one
+    of up to `sequences` packed sequences."""
 
     def __init__(self, vocab, tokens, sequences, width=128, heads=4, kv_heads=2, d=32, dv=32,
                  out=32, dtype=torch.bfloat16, lr=1e-2, max_norm=1.0, seed=0, device="cuda"):
@@ -73,36 +73,39 @@ class TokenMixer:
             nsd.nsd_attn_decay_workspace_size(tokens, sequences, tokens, self.attn, True))]
 
     def forward(self, ids, seqptr, pos):
-        n = self.n
-        nsd.nsd_embed(n, self.embedding, ids, self.table, self.x)
-        torch.mm(self.x, self.wq, out=self.q)
-        torch.mm(self.x, self.wk, out=self.k)
-        torch.mm(self.x, self.wv, out=self.v)
-        nsd.nsd_qk_rotate(n, self.turn, self.q, self.k, self.nq, self.nk, pos, self.freq, self.qr,
-                          self.kr)
-        nsd.nsd_attn_decay(n, self.seqs, seqptr, n, self.attn, self.qr, self.kr, self.v,
-                           self.decay, None, self.o, None, self.ws[2])
-        return self.o @ self.wo
+        n, seqs = ids.numel(), seqptr.numel() - 1
+        if n > self.n or seqs > self.seqs:
+            raise ValueError(f"{n} tokens in {seqs} sequences, room for {self.n} in {self.seqs}")
+        x, q, k, v, o = (t[:n] for t in (self.x, self.q, self.k, self.v, self.o))
+        nsd.nsd_embed(n, self.embedding, ids, self.table, x)
+        torch.mm(x, self.wq, out=q)
+        torch.mm(x, self.wk, out=k)
+        torch.mm(x, self.wv, out=v)
+        nsd.nsd_qk_rotate(n, self.turn, q, k, self.nq, self.nk, pos, self.freq, self.qr, self.kr)
+        nsd.nsd_attn_decay(n, seqs, seqptr, n, self.attn, self.qr, self.kr, v, self.decay, None,
+                           o, None, self.ws[2])
+        return o @ self.wo
 
     def backward(self, ids, seqptr, pos, y, target):
         """The loss; leaves every parameter's gradient in `grads`."""
-        n = self.n
+        n, seqs = ids.numel(), seqptr.numel() - 1
+        x, o, dx, do, dqr, dkr, dvv = (t[:n] for t in (self.x, self.o, self.dx, self.do, self.dqr,
+                                                       self.dkr, self.dvv))
         gtable, gwq, gwk, gwv, gwo, gnq, gnk, gdecay = self.grads
         diff = y.float() - target
         dy = (diff / n).to(self.dtype)
-        torch.mm(self.o.t(), dy, out=gwo)
-        torch.mm(dy, self.wo.t(), out=self.do)
-        nsd.nsd_attn_decay_vjp(n, self.seqs, seqptr, n, self.attn, self.qr, self.kr, self.v,
-                               self.decay, None, self.do, None, self.dqr, self.dkr, self.dvv,
-                               gdecay, None, self.ws[2])
+        torch.mm(o.t(), dy, out=gwo)
+        torch.mm(dy, self.wo.t(), out=do)
+        nsd.nsd_attn_decay_vjp(n, seqs, seqptr, n, self.attn, self.qr, self.kr, self.v, self.decay,
+                               None, do, None, dqr, dkr, dvv, gdecay, None, self.ws[2])
         # (the rotated rows' gradients become those of the projections' outputs in place)
         nsd.nsd_qk_rotate_vjp(n, self.turn, self.q, self.k, self.nq, self.nk, pos, self.freq,
-                              self.dqr, self.dkr, self.dqr, self.dkr, gnq, gnk, self.ws[1])
-        for w, dproj in ((gwq, self.dqr), (gwk, self.dkr), (gwv, self.dvv)):
-            torch.mm(self.x.t(), dproj, out=w)
-        torch.mm(self.dqr, self.wq.t(), out=self.dx)
-        self.dx.addmm_(self.dkr, self.wk.t()).addmm_(self.dvv, self.wv.t())
-        nsd.nsd_embed_vjp(n, self.embedding, ids, self.dx, False, gtable, self.ws[0])
+                              dqr, dkr, dqr, dkr, gnq, gnk, self.ws[1])
+        for w, dproj in ((gwq, dqr), (gwk, dkr), (gwv, dvv)):
+            torch.mm(x.t(), dproj, out=w)
+        torch.mm(dqr, self.wq.t(), out=dx)
+        dx.addmm_(dkr, self.wk.t()).addmm_(dvv, self.wv.t())
+        nsd.nsd_embed_vjp(n, self.embedding, ids, dx, False, gtable, self.ws[0])
         return 0.5 * (diff * diff).sum() / n
 
     def step(self, ids, seqptr, pos, target):

@@ -127,6 +127,28 @@ def test_the_step_takes_clipped_gradients(example):
     assert abs(p.scale.item() - 1e-3 / (norm + 1e-6)) <= 2.0 ** -22 * p.scale.item()
 
 
+def test_a_shorter_batch(example):
+    """Fewer tokens and sequences than there is room for: the gradients of a model that has
+    room for them alone (sums of the dense products may have another order); more are refused."""
+    import torch
+    net, ids, seqptr, pos, target = make(example, torch.float32)
+    room = example.TokenMixer(30, 20_000, 9, width=24, heads=4, kv_heads=2, d=8, dv=8, out=6,
+                              dtype=torch.float32)
+    for t in (room.x, room.q, room.k, room.v, room.o, room.do, room.dqr, room.dkr, room.dvv):
+        t.fill_(float("nan"))
+    losses = []
+    for m in (net, room):
+        y = m.forward(ids, seqptr, pos)
+        losses.append(m.backward(ids, seqptr, pos, y, target).item())
+    assert abs(losses[0] - losses[1]) <= TOL * losses[0]
+    for a, b in zip(net.grads, room.grads):
+        close(b, a.double().cpu(), tuple(a.shape))
+    more = torch.zeros(71, dtype=torch.int32, device="cuda")
+    for args in ((more, seqptr, more), (ids, torch.zeros(6, dtype=torch.int32, device="cuda"), pos)):
+        with pytest.raises(ValueError, match="room for 70 in 4"):
+            net.forward(*args)
+
+
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 def test_training_runs(example, dtype):
     import torch
