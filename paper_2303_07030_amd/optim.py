@@ -14,6 +14,7 @@ import math
 import torch
 
 from . import nsd
+from .operand import _allocate_on
 
 
 def _flat(t, what, device, n=None, dtypes=None):
@@ -44,14 +45,17 @@ class GradNorm:
             _flat(g, f"gradient {i}", dev, dtypes=(torch.float32, torch.bfloat16))
         records = [nsd.nsd_grad_tensor(g.numel(), g.data_ptr(), nsd.dtype_of(g))
                    for g in self.grads]
-        table = torch.empty(nsd.nsd_grad_plan_size(records), dtype=torch.uint8, device=dev)
-        self.plan = nsd.nsd_grad_plan_build(records, table, stream)
         self.max_norm, self.order = max_norm, order
-        self.norm = torch.zeros(1, dtype=torch.float64, device=dev)
-        self.norms = torch.zeros(len(records), dtype=torch.float64, device=dev)
-        self.scale = torch.ones(1, device=dev)
-        self.ws = torch.empty(nsd.nsd_grad_norm_workspace_size(self.plan), dtype=torch.uint8,
-                              device=dev)
+        with _allocate_on(stream, dev):
+            # (filled before the plan is built, which waits for its stream: a measure on any
+            # stream comes later)
+            self.norm = torch.zeros(1, dtype=torch.float64, device=dev)
+            self.norms = torch.zeros(len(records), dtype=torch.float64, device=dev)
+            self.scale = torch.ones(1, device=dev)
+            table = torch.empty(nsd.nsd_grad_plan_size(records), dtype=torch.uint8, device=dev)
+            self.plan = nsd.nsd_grad_plan_build(records, table, stream)
+            self.ws = torch.empty(nsd.nsd_grad_norm_workspace_size(self.plan), dtype=torch.uint8,
+                                  device=dev)
 
     def measure(self, grad_scale=None, stream=None):
         """The norms of grad_scale (a device fp32 scalar but `scale` itself, or None)

@@ -221,6 +221,26 @@ def test_gradients_of_several_tensors():
 
 
 @pytest.mark.gpu
+def test_a_measure_on_another_stream():
+    """What the measure leaves is not overwritten by the first values, which a busy current
+    stream would come to later."""
+    from paper_2303_07030_amd import optim
+    g = torch.full((1000,), 2.0, device="cuda")
+    side = torch.cuda.Stream()
+    a, b = torch.randn(2, 4096, 4096, device="cuda")
+    torch.cuda.synchronize()
+    for built, stream in ((side, side), (side.cuda_stream, side.cuda_stream), (None, side)):
+        for _ in range(40):
+            torch.mm(a, b)
+        p = optim.GradNorm([g], 1.0, stream=built)
+        p.measure(stream=stream)
+        torch.cuda.synchronize()
+        assert math.isclose(p.norm.item(), math.sqrt(4000.0), rel_tol=1e-12)
+        assert math.isclose(p.norms.item(), math.sqrt(4000.0), rel_tol=1e-12)
+        assert math.isclose(p.scale.item(), 1.0 / math.sqrt(4000.0), rel_tol=1e-6)
+
+
+@pytest.mark.gpu
 def test_a_captured_measure_and_clip_follow_the_gradients():
     from paper_2303_07030_amd import optim
     grads = grads_of(torch.bfloat16, seed=2)
