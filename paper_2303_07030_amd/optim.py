@@ -134,6 +134,8 @@ class AdamW:
                 nsd.dtype_of(self.grads[i]), decay[i]))
         table = torch.empty(nsd.nsd_adamw_plan_size(self.records), dtype=torch.uint8,
                             device=self.params[0].device if count else "cuda")
+        if stream is not None and count:  # the states' first values were filled on the current one
+            torch.cuda.current_stream(dev).synchronize()
         self.plan = nsd.nsd_adamw_plan_build(self.records, state_bits, table, stream)
         self.grad_norm = None if max_norm is None else GradNorm(self.grads, max_norm,
                                                                 stream=stream)

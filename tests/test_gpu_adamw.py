@@ -458,3 +458,26 @@ def test_a_refused_step_changes_nothing():
     for o in opts:
         o.step()
     assert opts[0].t == opts[1].t == 4
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_step_on_another_stream_than_the_construction(dtype):
+    """States and copies are there for a step on the stream that was named, however busy the
+    current one is."""
+    from paper_2303_07030_amd import optim
+    g = torch.Generator(device="cuda").manual_seed(3)
+    w = torch.randn(5000, device="cuda", generator=g).to(dtype)
+    grad = torch.randn(5000, device="cuda", generator=g)
+    a, b = torch.randn(2, 4096, 4096, device="cuda")
+    side, weights, opts = torch.cuda.Stream(), [w.clone(), w.clone()], []
+    torch.cuda.synchronize()
+    for stream, x in zip((None, side), weights):
+        for _ in range(40):
+            torch.mm(a, b)
+        opts.append(optim.AdamW([x], [grad], masters=True, stream=stream, max_norm=1.0))
+        opts[-1].step(stream=stream)
+        opts[-1].step(stream=stream)
+        torch.cuda.synchronize()
+    assert torch.equal(*weights) and not torch.equal(weights[0], w)
+    assert torch.equal(opts[0].m[0], opts[1].m[0]) and torch.equal(opts[0].v[0], opts[1].v[0])
