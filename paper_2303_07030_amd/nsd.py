@@ -1059,7 +1059,7 @@ def nsd_qk_rotate_vjp(ntok, s: nsd_qk, Q, K, wq, wk, pos, freq, dQo, dKo, dQ, dK
 def nsd_qk_append(ntok, s: nsd_qk, Q, K, V, wq, wk, pos, freq, slot, nslots, Qo, Kc, Vc,
                   stream=None):
     """V [ntok, any width] and Vc [nslots, the same]: their row distances are taken
-    (None: no values)."""
+    (V None: no values)."""
     T = _type_of(s.dtype)
     _qk_rows(ntok, s, ((Q, "Q", s.heads, s.ldq), (K, "K", s.kv_heads, s.ldk),
                        (Qo, "Qo", s.heads, s.ldqo)), T)
@@ -1069,7 +1069,8 @@ def nsd_qk_append(ntok, s: nsd_qk, Q, K, V, wq, wk, pos, freq, slot, nslots, Qo,
     vwidth, ldv, ldvo = 0, 0, 0
     if V is not None:
         vwidth = V.shape[-1]
-        ldv, ldvo = _row_distance(V, vwidth, "V"), _row_distance(Vc, vwidth, "Vc")
+        ldv = _row_distance(V, vwidth, "V")
+        ldvo = vwidth if Vc is None else _row_distance(Vc, vwidth, "Vc")
         _rows(V, "V", ntok, vwidth, ldv, T)
         _rows(Vc, "Vc", nslots, vwidth, ldvo, T)
     _check(_lib.nsd_qk_append(ntok, C.byref(s), _p(Q), _p(K), _p(V), vwidth, ldv, ldvo, _p(wq),

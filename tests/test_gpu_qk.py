@@ -186,6 +186,27 @@ def test_the_gradient_is_that_of_the_definition():
                 assert abs((side[0] - side[1]) / (2 * h) - grad[i]) <= 1e-7
 
 
+def test_values_without_a_cache_are_refused():
+    q, k, v = torch.zeros(4, 32), torch.zeros(4, 16), torch.zeros(4, 6)
+    w, pos, freq = torch.zeros(8), torch.zeros(4, dtype=torch.int32), torch.zeros(4).double()
+    cache = torch.zeros(9, 16)
+    s = nsd.qk_desc(4, 2, 8, q, k, q, cache)
+    with pytest.raises(nsd.NsdError, match="V or Vc is NULL"):
+        nsd.nsd_qk_append(4, s, q, k, v, w, w, pos, freq, pos, 9, q, cache, None)
+
+
+@pytest.mark.gpu
+def test_a_cache_of_no_slots():
+    """Every slot is outside it: the queries alone are written, and no cache need be there."""
+    t = make(5, 4, 2, 8, 8, "f32", 50)
+    v, want = torch.zeros(5, 6, device="cuda"), torch.empty_like(t["qo"])
+    s = nsd.qk_desc(4, 2, 8, t["q"], t["k"], t["qo"], t["ko"])
+    small = (t["wq"], t["wk"], t["pos"], t["freq"])
+    nsd.nsd_qk_rotate(5, s, t["q"], t["k"], *small, want, t["ko"])
+    nsd.nsd_qk_append(5, s, t["q"], t["k"], v, *small, t["pos"], 0, t["qo"], None, None)
+    assert torch.equal(t["qo"], want)
+
+
 # ------------------------------------------------------------- on the GPU
 
 def make(n, H, Hk, d, rot, dtype, far, seed=0, gap=0):
