@@ -246,7 +246,7 @@ __global__ __launch_bounds__(kEmbedThreads) void embed_starts_kernel(int32_t nto
 // ------------------------------------------------------------------- sums
 
 struct EmbedSum {
-    int32_t ntok, vocab, width, tiles, lanes, nchunks;
+    int32_t vocab, width, tiles, lanes, nchunks;
     bool accumulate;
     float scale;
     const int32_t *perm, *word, *segptr;
@@ -537,7 +537,6 @@ nsd_status nsd_embed_vjp(int32_t ntok, const nsd_embedding *s, const int32_t *id
         embed_starts_kernel<<<starts, kEmbedThreads, 0, st>>>(ntok, s->vocab, w.word, w.segptr);
         NSD_TRY(check_launch("embed_starts_kernel"));
     }
-    a.ntok = ntok;
     a.vocab = s->vocab;
     a.width = s->width;
     a.lanes = row_lanes(s->width, values);

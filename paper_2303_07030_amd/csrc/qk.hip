@@ -124,13 +124,6 @@ struct Head {
         }
         return t;
     }
-    __device__ __forceinline__ void times(const Head &o, float r) {
-#pragma unroll
-        for (int e = 0; e < kPairs; ++e) {
-            a[e] *= r * o.a[e];
-            b[e] *= r * o.b[e];
-        }
-    }
     // The first n pairs turned by the lane's angles, or back.  (The others are no pairs: an
     // infinite one times a sine of 0 would take the number beside it away.)
     __device__ __forceinline__ void turn(const float (&c)[kPairs], const float (&s)[kPairs], int n,
