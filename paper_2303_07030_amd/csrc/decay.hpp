@@ -512,11 +512,12 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
     float dsum = 0.f;
     int single = 0;  // tokens that are still taken one by one
     int pos = 0, len = 0, next = 0, next_len = min(C, seg.n);
-    // The next chunk's rows are on their way while one is multiplied where that leaves the card
-    // as many waves; the other blocks of a CU hide them else (outputs with a state of 128 by 128:
-    // a prompt 324 us so, 379 with rows ahead; a training step of 64 by 128 1,130 us with rows
-    // ahead, 1,144 without).
-    constexpr bool AHEAD = KIND == kState || (KIND == kOutput && KD <= 64);
+    // States alone leave registers for the next chunk's rows, on their way while one is multiplied
+    // (128 by 128, a prompt: 94 us, 102 without).  Other scans have the other blocks of a CU to
+    // hide them: with outputs' rows ahead as well a prompt took 384 us in place of 334, a
+    // training step 1,050 in place of 1,013, and keys of up to 64 gained nothing by them (1,019 and
+    // 1,013; 8,192 tokens of 8 heads of 64 by 128 in fp32, forwards: 103 and 91).
+    constexpr bool AHEAD = KIND == kState;
     auto load = [&](int tid) {
         const int64_t t0 = first + (int64_t)next * dir;
         if (KIND != kState) xq.load(tid, a.q, h, 0, t0, a.rev, next_len);
