@@ -5,7 +5,7 @@
 // card: the states of every segment by itself (a scan without outputs), a join that
 // carries each sequence's state through its segments,
 //   start_{c+1} = w^n start_c + state_c
-// (HBM-bound: a prompt of 128 segments of 8 heads of 128 by 128 23 us, 5.8 TB/s),
+// (HBM-bound: a prompt of 128 segments of 8 heads of 128 by 128 24 us, 5.5 TB/s),
 // and the scan of every segment from its start.  The join leaves at a segment's place in the
 // workspace the state that the segment starts from (backwards: the one that comes back to its
 // end).
@@ -140,7 +140,7 @@ struct Step {
 
 // A row's head and some columns of its state: read, decayed, added to, written, multiplied.  HBM-
 // bound: the state is 8 bytes a value, the row nothing beside it.  64 rows of 16 heads of 64 by
-// 128: 12.2 us (5.5 TB/s).
+// 128: 13.4 us (5.0 TB/s).
 template <class T, int VEC>
 __global__ __launch_bounds__(kStepThreads) void decay_step_kernel(Step a) {
     __shared__ float qs[kMaxWidth], ks[kMaxWidth];
@@ -253,9 +253,10 @@ nsd_status check_decay(const nsd_decay *s) {
 
 // Tokens of a segment: as many as leave the card kEnough blocks, INT_MAX where whole sequences
 // do, or are short.  (A training step of 5,003 tokens of 6 heads in fp32: segments of at least
-// 256 tokens 306 us, 128 272, 64 181.  A prompt of 65,536 tokens of 8 heads of 128, and a
-// training step of 32,768 tokens of 16 heads of 64 by 128: 512 blocks 373 and 1,325 us, 1,024 325
-// and 1,130, 2,048 353 and 1,157.)
+// 256 tokens 315 us, 128 275, 64 182; 4,096 tokens of 8 heads of 64 in bf16, forwards, where 64
+// tokens are one chunk: 34, 30 and 35; of 16 heads over 4 of 128: 74, 75 and 85.  A prompt of
+// 65,536 tokens of 8 heads of 128, and a training step of 32,768 tokens of 16 heads of 64 by 128:
+// 512 blocks 393 and 1,154 us, 1,024 334 and 1,019, 2,048 361 and 1,041.)
 constexpr int kShortest = 64, kLongest = 8192, kEnough = 1024;
 
 int segment_tokens(int32_t ntok, int32_t max_len, const nsd_decay *s) {
@@ -545,8 +546,8 @@ nsd_status nsd_attn_decay_step(int32_t nrows, const int32_t *slot, int32_t nslot
            s->ldq, s->ldk, s->ldv, s->ldo, decay, state, O};
     const bool four = s->dv % 4 == 0;
     // Lanes over a state's row: 128 columns a block, fewer where that leaves too few blocks (4
-    // rows of 16 heads of 64 by 128: 4.9 us, with 128 columns 5.6; 16 rows: 6.0 with 64 columns,
-    // 5.6 with 128).
+    // rows of 16 heads of 64 by 128: 5.1 us, with 128 columns 5.5; 16 rows: 6.1 with 64 columns,
+    // 5.7 with 128).
     int cols = 128;
     while (cols > 32 && (int64_t)nrows * s->heads * ceil_div(s->dv, cols) < 256) cols /= 2;
     while (cols / 2 >= s->dv && cols > 32) cols /= 2;

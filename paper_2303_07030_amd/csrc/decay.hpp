@@ -31,12 +31,12 @@
 // decayed values) is a sum of three of them, 24 bits, as many as a 32-bit float has: the
 // results are those of products in 32 bits.  fp32: fp32 products, half the chunk.
 //
-// A prompt of 65,536 tokens of 8 heads of 128 by 128 in bf16: the states 94 us, the outputs 204
-// (2.6 TB/s of the rows' bytes).  Neither bytes nor products bound it alone: the vector units issue in
-// 58% of the cycles (the parts of states and values, rows turned for LDS), the matrix cores are
-// busy in 30%, and two blocks a CU do not lay the one over the other whole; of LDS's cycles 3%
-// are conflicts.  A training step of 32,768 tokens of 16 heads of 64 by 128: states 73 us,
-// outputs 164, dq and dk 154 each, dv with the gradient of g 323 (56% and 23%: two states leave
+// A prompt of 65,536 tokens of 8 heads of 128 by 128 in bf16: the states 90 us, the outputs 220
+// (2.4 TB/s of the rows' bytes).  Neither bytes nor products bound it alone: the vector units issue in
+// 59% of the cycles (the parts of states and values, rows turned for LDS), the matrix cores are
+// busy in 32%, and two blocks a CU do not lay the one over the other whole; of LDS's cycles 4%
+// are conflicts.  A training step of 32,768 tokens of 16 heads of 64 by 128: states 68 us,
+// outputs 172, dq and dk 146 each, dv with the gradient of g 295 (57% and 24%: two states leave
 // three blocks of four waves a CU).
 #pragma once
 
@@ -195,7 +195,8 @@ __device__ __forceinline__ int place(int k) {
 // then 4-11, 16-19, 28-31, and so on (found by counting conflicts over row distances), a write
 // of 8 bytes 16 consecutive lanes over half of them.  The 16 bytes of a row that a lane
 // group reads are therefore turned by bits of the row's number, so that neither reads
-// nor writes (Stage's) of bf16 meet: 3% of the cycles of LDS are conflicts, without it 45%.
+// nor writes (Stage's) of bf16 meet: of the cycles of LDS none are conflicts in scans of states,
+// 4 to 7% in those of outputs and 13% where the scores are SHORT (45% without it, in outputs).
 
 // Of rows by token, KD values and 16 bytes apart.
 template <class T>
@@ -411,7 +412,7 @@ struct Shared {
     static constexpr int QKV = 2 * Q + (OVER ? VB * C : 0);
     static constexpr int ROWS = KIND == kState ? 0 : QKV > AT + SP * PART ? QKV : AT + SP * PART;
     // Wide keys by columns take the queries' place when those were read: three blocks of four waves
-    // a CU instead of two (a training step's dq and dk, keys of 128, 154 us for 170).
+    // a CU instead of two (a training step, whose dq and dk have keys of 128, 1,019 us for 1,065).
     static constexpr bool LATE = KIND == kOutput && NW == 4 && KD > 64;
     static_assert(!LATE || KD * C <= Q, "keys by columns in the queries' place");
     static constexpr int KT_END = ROWS + (LATE ? 0 : KD * C);
@@ -420,9 +421,9 @@ struct Shared {
 };
 
 // Waves of a SIMD, which say how many registers one may have: two blocks of eight waves a CU
-// where the state leaves room for it (a training step's scan of 64 by 128 163 us with one block
-// and 160 with two, in fp32 with the gradient of g 48 and 40), three of four waves with the
-// gradient of g in bf16 (323 us, with two 417) and where wide keys leave them the LDS.
+// where the state leaves room for it (a prompt 334 us, with one block 398; a training step 1,019
+// and 1,050, one of 5,003 tokens in fp32 182 and 195), three of four waves with the gradient of g
+// in bf16 (the step 1,019 us, with two 1,105) and where wide keys leave them the LDS.
 constexpr int waves_of(int kd, int nw, Kind kind) {
     const bool two_states = kind == kDerivative;
     if (kd > 128) return 1;
@@ -808,9 +809,12 @@ __global__ __launch_bounds__(NW * kWave, waves_of(KD, NW, KIND)) void scan_kerne
 }
 
 // Columns of the values that a block takes.  128 share the scores of 128: a prompt of 65,536
-// tokens of 8 heads of 128 324 us, with 64 columns a block 359.  But two states in parts of
-// bf16 leave a block of eight waves too few registers: a training step's scan of 64 by 128 with
-// the gradient of g 323 us with 64 columns, 449 with 128 (fp32: 46 and 41).
+// tokens of 8 heads of 128 334 us, with 64 columns a block 342, 8,192 tokens of heads of 256 159
+// and 220, a training step of 5,003 tokens in fp32 182 and 192.  But two states in parts of bf16
+// leave a block of eight waves too few registers: a training step of 32,768 tokens of 64 by 128
+// 1,019 us with 64 columns for the scan with the gradient of g, 1,149 with 128 (the gradient of four
+// sequences of 8,192 tokens of 128 by 128: 1,422 and 1,474; heads of 256, whose block has a CU
+// for itself, go the other way, 871 and 773).
 constexpr int block_columns(Kind kind, bool bf16, int width) {
     return width > 64 && !(kind == kDerivative && bf16) ? 128 : 64;
 }

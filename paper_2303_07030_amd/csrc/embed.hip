@@ -17,8 +17,9 @@
 // words there; their sums of long words are joined in order by a second launch.
 //
 // 32,768 tokens of 50,000 words of 1,024 columns in bf16, words as frequent as in text: rows
-// 23.5 us (5.7 TB/s), the order 15, sums 48.6 (3.5 TB/s of tokens' rows and table), joins 4.8.
-// 16 tokens: 3.2 us, a launch.  10,007 tokens of 5,003 words of 333 columns in fp32: 7.8, 8.2,
+// 28 us (4.8 TB/s), the order 15, sums 60 (2.8 TB/s of tokens' rows and table), joins 4.9 (on
+// inputs of their own for each call; on the same ones, from the caches, rows 23.5 and sums 49).
+// 16 tokens: 2.9 us, a launch.  10,007 tokens of 5,003 words of 333 columns in fp32: 8.1, 7.6,
 // 17 and 4.1 us.
 #include <algorithm>
 

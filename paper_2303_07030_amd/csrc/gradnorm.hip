@@ -10,8 +10,8 @@
 // sum has one order.  Squares in 64 bits cost two instructions a value at half
 // and quarter rate, far below what a value's bytes take.
 //
-// 200 million values of 24 tensors in bf16: 84.7 us (4.7 TB/s) and 6.2 for the join; scaled in
-// place 169 (4.7 TB/s).  300 tensors of 2 million values in fp32: 3.8 and 2.8 us, launches.
+// 200 million values of 24 tensors in bf16: 94 us (4.3 TB/s) and 6.1 for the join; scaled in
+// place 169 (4.7 TB/s).  300 tensors of 2 million values in fp32: 4.8 and 2.7 us, launches.
 #include <algorithm>
 #include <cmath>
 #include <cstdlib>

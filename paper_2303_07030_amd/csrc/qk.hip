@@ -15,9 +15,9 @@
 // The gradient's blocks walk tokens with a stride, hold their share of dw in registers
 // and leave one partial each; a second launch adds those up in their order.
 //
-// 16,384 tokens of 32 and 8 heads of 128 in bf16: 72.8 us (4.6 TB/s), the gradient 114 (4.4
-// TB/s) and 7 for the weights'.  8 tokens of 16 and 4 heads of 64 appended: 4.1 us, a launch.
-// 10,007 tokens of 6 and 3 heads of 40, pairs side by side, in fp32: 11.2, 16.6 and 6.5 us.
+// 16,384 tokens of 32 and 8 heads of 128 in bf16: 65 us (5.1 TB/s), the gradient 113 (4.5
+// TB/s) and 7 for the weights'.  8 tokens of 16 and 4 heads of 64 appended: 4.0 us, a launch.
+// 10,007 tokens of 6 and 3 heads of 40, pairs side by side, in fp32: 10.2, 14.8 and 6.0 us.
 #include <algorithm>
 
 #include "values.hpp"
