@@ -448,7 +448,7 @@ def test_shorter_batches_in_a_longer_ones_workspace():
         c.n, c.seqptr = n, torch.tensor([0, n], dtype=torch.int32, device="cuda")
         outs = []
         for own in (False, True):
-            dg, s1, ds0 = torch.empty(8, device="cuda"), *torch.empty_like(c.s0.expand(2, *c.s0.shape))
+            dg, s1, ds0 = (torch.empty_like(t) for t in (c.g, c.s0, c.s0))
             o, dq, dk, dv = (torch.zeros_like(c.out[i]) for i in ("o", "dq", "dk", "dv"))
             ws.fill_(0x7F)
             w = [c.ws(n, False), c.ws(n, True)] if own else [ws[:most]] * 2
@@ -578,8 +578,9 @@ def test_scores_and_states_keep_32_bits(d, dv, Hk, dtype):
                     t[row, 0] = value
         for state, value in ((c.s0, s0), (c.ds1, ds1)):
             state.zero_()
-            if value:
-                state[0, 0] = torch.tensor(value[0])[:, None] if value[1] else torch.tensor(value[0])
+            if value:  # of each row of the state, or of each column
+                row = torch.tensor(value[0])
+                state[0, 0] = row[:, None] if value[1] else row
         c.forward()
         c.backward()
         want = torch.from_numpy(definition(c.arrays(), [2], 1.0)[out][:2]).to(T[dtype])
