@@ -1089,7 +1089,8 @@ nsd_status nsd_embed_vjp(int32_t ntok, const nsd_embedding *s, const int32_t *id
  *                    distances).
  * nsd_qk_rotate_vjp  the upstream dQo (ldqo) and dKo (ldko) give dQ (ldq), dK (ldk)
  *                    and, where not NULL, dwq and dwk (fp32 [d], sums over all
- *                    tokens and heads).  dQ may be dQo itself (ldq = ldqo), dK dKo.
+ *                    tokens and heads).  dQ may be dQo itself (ldq = ldqo) or Q, dK
+ *                    dKo or K.
  * nsd_qk_append      the serving form: token t's key and value go to row slot[t]
  *                    of the caches Kc (ldko) and Vc (ldvo; rows of vwidth values
  *                    copied from V's, ldv), as nsd_attn_diff_decode and others read
